@@ -175,6 +175,70 @@ int rlhf_op_lm_head_logprob(int act_half, const void* A, const void* W_head, con
 int rlhf_op_head_dot(int act_dtype, int w_dtype, const void* xn, const void* w, int rows, int d, float* out,
                      const int32_t* out_dst, void* stream);
 
+/* ---- the Actor's update, as the training stage takes it up from the stage's results: the loss on the logits of a
+ * forward pass with its gradient, the embedding lookup with its gradient, and the norm and clipping of all
+ * gradients.  All of them can be captured into a graph; a scratch buffer belongs to one call at a time (calls
+ * ordered on one stream may share it, graphs that may run at the same time may not). */
+
+/* Clipped policy loss with a KL term towards the Reference, on logits, forward and gradient in one pass.  Row r of logits
+ * [rows, vocab] (logit_dtype RLHF_FP32, RLHF_BF16 or 2 = IEEE half; row stride ld elements) is what predicts
+ * y = tokens[r].  With l = log_softmax(logits[r])[y], A = adv[r], w = weight[r] (1 where weight == NULL),
+ *   rho = exp(l - lp_old[r]),   policy_r = -min(rho * A, clamp(rho, 1 - clip_low, 1 + clip_high) * A),
+ *   x = lp_ref[r] - l,          kl_r = exp(x) - x - 1    (0 where lp_ref == NULL, which needs kl_coef == 0),
+ * the loss is the sum over the rows of w * (policy_r + kl_coef * kl_r): weights 1/n give the mean over n tokens.
+ *   stats[4] = loss, sum of w * policy_r, sum of w * kl_r, sum of w over the rows whose gradient the clamp cut off
+ *   lp[r]    = l
+ *   dlogits[r] = grad_scale * d loss / d logits[r], in logit_dtype, row stride ld_grad; NULL: no gradient is taken.  It may be
+ *              the logits themselves (same ld), else the two must not overlap.
+ * Everything is float until the gradient is rounded once.  The rows are summed in a fixed order.
+ * A row with weight 0 or a negative token is left out: its logits and its other inputs, whatever they hold, are not used,
+ * lp[r] = 0, its gradient is zero.  Logits of -inf have probability 0.  A row whose result is not a number (all
+ * logits -inf, a logit of +inf, NaN, a token of vocab or more) makes lp[r], its gradient and stats NaN.
+ * Columns of dlogits behind vocab are left as they are.  clip_low in [0, 1], clip_high >= 0, kl_coef >= 0.
+ * scratch: rlhf_op_policy_loss_scratch_floats(rows, vocab) floats. */
+int64_t rlhf_op_policy_loss_scratch_floats(int rows, int vocab);
+int rlhf_op_policy_loss(int logit_dtype, const void* logits, int64_t ld, const int32_t* tokens, const float* lp_old,
+                        const float* lp_ref, const float* adv, const float* weight, float clip_low, float clip_high,
+                        float kl_coef, float grad_scale, float* lp, float* stats, void* dlogits, int64_t ld_grad,
+                        float* scratch, int rows, int vocab, void* stream);
+
+/* Embedding lookup with scaling: out[r] = scale * table[tokens[r]], table [vocab, d] and out [rows, d] each in its own
+ * type (RLHF_FP32, RLHF_BF16, 2 = IEEE half) and row stride; any d.  One rounding, to out's type.  A negative token gives
+ * a row of zeros (padding), one of vocab or more a row of NaN. */
+int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, int64_t ld_table, const int32_t* tokens, float scale,
+                  void* out, int64_t ld_out, int rows, int d, int vocab, void* stream);
+
+/* Its gradient: dtable[v] = scale * (sum of dout[r] over the rows r with tokens[r] == v), every row of dtable written
+ * (zeros where no row has the token); with accumulate != 0 that sum is added to dtable[v] instead and rows of other
+ * tokens are left as they are.  The rows of a token are summed in float, in an order that depends on the tokens alone:
+ * the same call gives the same bits.  Rows with tokens outside [0, vocab) count for nothing.  Types and strides as
+ * above, dout in dout_dtype, dtable in table_dtype.  dout and dtable must not overlap.
+ * scratch: rlhf_op_embed_grad_scratch_bytes(rows, d, vocab) bytes, 16-byte aligned. */
+int64_t rlhf_op_embed_grad_scratch_bytes(int rows, int d, int vocab);
+int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* dout, int64_t ld_dout, const int32_t* tokens, float scale,
+                       int accumulate, void* dtable, int64_t ld_table, void* scratch, int rows, int d, int vocab,
+                       void* stream);
+
+/* The gradients of a model: n_tensors entries in HOST memory, read before a call returns.  src: n elements of dtype
+ * (RLHF_FP32, RLHF_BF16, 2 = IEEE half), contiguous.  dst: where the clipped gradient goes, in the same type: src itself,
+ * or memory that overlaps no other entry's; NULL where only the norm is taken. */
+typedef struct rlhf_tensor {
+    const void* src;
+    void* dst;
+    int64_t n;
+    int32_t dtype;
+} rlhf_tensor;
+
+/* norm[0] (device float) = the square root of the sum of the squares of all elements.  Sums are held in double: no square overflows or
+ * vanishes.  scratch: rlhf_op_grad_norm_scratch_doubles(tensors, n_tensors) doubles. */
+int64_t rlhf_op_grad_norm_scratch_doubles(const rlhf_tensor* tensors, int n_tensors);
+int rlhf_op_grad_norm(const rlhf_tensor* tensors, int n_tensors, float* norm, double* scratch, void* stream);
+
+/* dst = src * f with f = max_norm / norm[0] where norm[0] is finite and above max_norm, else 1: the gradients of a step
+ * whose norm is not finite pass unchanged, for the caller to drop.  Between the two calls norm may be combined with that of other
+ * ranks.  max_norm > 0. */
+int rlhf_op_clip_grads(const rlhf_tensor* tensors, int n_tensors, const float* norm, float max_norm, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

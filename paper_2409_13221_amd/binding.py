@@ -81,6 +81,10 @@ class rlhf_snapshot(C.Structure):
                 + [(n, C.c_int32) for n in ("cap_samples", "cap_max_pages", "cap_pool_pages")])
 
 
+class rlhf_tensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
 class rlhf_kernel_profile(C.Structure):
     _fields_ = [("launches", C.c_int64), ("sampled", C.c_int64), ("sampled_ms", C.c_double),
                 ("sampled_bytes", C.c_double), ("sampled_flops", C.c_double), ("total_bytes", C.c_double),
@@ -146,6 +150,19 @@ def lib() -> C.CDLL:
         L.rlhf_op_gemm_tall_tile.restype = C.c_int
         L.rlhf_op_bf16_to_half.argtypes = [vp, vp, i64, vp]
         L.rlhf_op_bf16_to_half.restype = C.c_int
+        L.rlhf_op_policy_loss_scratch_floats.argtypes = [C.c_int] * 2
+        L.rlhf_op_policy_loss.argtypes = [C.c_int, vp, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i64, vp,
+                                          C.c_int, C.c_int, vp]
+        L.rlhf_op_embed.argtypes = [C.c_int, C.c_int, vp, i64, vp, f32, vp, i64, C.c_int, C.c_int, C.c_int, vp]
+        L.rlhf_op_embed_grad_scratch_bytes.argtypes = [C.c_int] * 3
+        L.rlhf_op_embed_grad.argtypes = [C.c_int, C.c_int, vp, i64, vp, f32, C.c_int, vp, i64, vp, C.c_int, C.c_int, C.c_int, vp]
+        L.rlhf_op_grad_norm_scratch_doubles.argtypes = [vp, C.c_int]
+        L.rlhf_op_grad_norm.argtypes = [vp, C.c_int, vp, vp, vp]
+        L.rlhf_op_clip_grads.argtypes = [vp, C.c_int, vp, f32, vp]
+        for name in ("rlhf_op_policy_loss_scratch_floats", "rlhf_op_embed_grad_scratch_bytes", "rlhf_op_grad_norm_scratch_doubles"):
+            getattr(L, name).restype = i64
+        for name in ("rlhf_op_policy_loss", "rlhf_op_embed", "rlhf_op_embed_grad", "rlhf_op_grad_norm", "rlhf_op_clip_grads"):
+            getattr(L, name).restype = C.c_int
         for name in ("rlhf_op_rmsnorm", "rlhf_op_rope_kv", "rlhf_op_swiglu", "rlhf_op_pick", "rlhf_op_gather_lp",
                      "rlhf_op_head_dot"):
             getattr(L, name).restype = C.c_int
@@ -568,3 +585,132 @@ def rlhf_op_gemm_tall_tile(bid: int, tiles_m: int, tiles_n: int):
     if rc < 0:
         raise RlhfError(rc, "rlhf_op_gemm_tall_tile")
     return (tm.value, tn.value) if rc == 1 else None
+
+
+# ------------------------------------------------------------------------- the Actor's update
+
+def _on_device(*tensors) -> None:
+    """Kernels are launched on the current device's current stream: every tensor has to be there."""
+    import torch
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("all tensors must be in device memory")
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{dev}")
+
+
+def _vector(t, n: int, dtype, what: str):
+    """t as a contiguous vector of n entries, or None."""
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} entries")
+    return t
+
+
+def _matrix(t, rows: int, cols: int, what: str) -> int:
+    """Row stride of a [rows, cols] matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be [{rows}, {cols}] with contiguous rows")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"rows of {what} overlap")
+    return ld
+
+
+def rlhf_op_policy_loss(logits, tokens, lp_old, adv, lp, stats, dlogits=None, lp_ref=None, weight=None, clip_low: float = 0.2,
+                        clip_high: float = 0.2, kl_coef: float = 0.0, grad_scale: float = 1.0, scratch=None) -> None:
+    """Clipped policy loss with a KL term on logits [rows, vocab] (float32, bfloat16, float16): writes lp [rows], stats [4] = (loss,
+    policy part, KL, clipped weight) and, unless None, dlogits like logits (or logits itself).  tokens int32 [rows], negative = row
+    left out; lp_old, adv, lp_ref, weight float32 [rows].  scratch: float32, rlhf_op_policy_loss_scratch_floats entries."""
+    import torch
+    f32, (rows, vocab) = torch.float32, logits.shape
+    _on_device(logits, tokens, lp_old, adv, lp, stats, dlogits, lp_ref, weight, scratch)
+    ld, ld_grad = _matrix(logits, rows, vocab, "logits"), vocab
+    if dlogits is not None:
+        if dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits must have the type of logits")
+        ld_grad = _matrix(dlogits, rows, vocab, "dlogits")
+    _vector(tokens, rows, torch.int32, "tokens")
+    for t, what in ((lp_old, "lp_old"), (adv, "adv"), (lp, "lp"), (lp_ref, "lp_ref"), (weight, "weight")):
+        _vector(t, rows, f32, what)
+    _vector(stats, 4, f32, "stats")
+    need = lib().rlhf_op_policy_loss_scratch_floats(rows, vocab)
+    if scratch is None:
+        scratch = torch.empty(need, device=logits.device)
+    elif scratch.dtype != f32 or scratch.numel() < need or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous float32 tensor of {need} entries")
+    _op_check(lib().rlhf_op_policy_loss(_act_code(logits), logits.data_ptr(), ld, tokens.data_ptr(), lp_old.data_ptr(),
+                                        _ptr(lp_ref), adv.data_ptr(), _ptr(weight), clip_low, clip_high, kl_coef, grad_scale,
+                                        lp.data_ptr(), stats.data_ptr(), _ptr(dlogits), ld_grad, scratch.data_ptr(), rows, vocab,
+                                        _stream_ptr()), "rlhf_op_policy_loss")
+
+
+def rlhf_op_embed(table, tokens, out, scale: float = 1.0) -> None:
+    """out[r] = scale * table[tokens[r]]; table [vocab, d] and out [rows, d] float32, bfloat16 or float16, tokens int32 [rows]."""
+    import torch
+    (vocab, d), rows = table.shape, tokens.numel()
+    _on_device(table, tokens, out)
+    _vector(tokens, rows, torch.int32, "tokens")
+    _op_check(lib().rlhf_op_embed(_act_code(table), _act_code(out), table.data_ptr(), _matrix(table, vocab, d, "table"), tokens.data_ptr(),
+                                  scale, out.data_ptr(), _matrix(out, rows, d, "out"), rows, d, vocab, _stream_ptr()), "rlhf_op_embed")
+
+
+def rlhf_op_embed_grad(dout, tokens, dtable, scale: float = 1.0, accumulate: bool = False, scratch=None) -> None:
+    """dtable[v] = scale * sum of dout[r] over the rows with tokens[r] == v, added to dtable[v] with accumulate; dout [rows, d], dtable
+    [vocab, d].  scratch: uint8, rlhf_op_embed_grad_scratch_bytes entries."""
+    import torch
+    (vocab, d), rows = dtable.shape, tokens.numel()
+    _on_device(dout, tokens, dtable, scratch)
+    _vector(tokens, rows, torch.int32, "tokens")
+    need = lib().rlhf_op_embed_grad_scratch_bytes(rows, d, vocab)
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=dtable.device)
+    elif scratch.dtype != torch.uint8 or scratch.numel() < need or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous uint8 tensor of {need} entries")
+    _op_check(lib().rlhf_op_embed_grad(_act_code(dout), _act_code(dtable), dout.data_ptr(), _matrix(dout, rows, d, "dout"), tokens.data_ptr(),
+                                       scale, int(accumulate), dtable.data_ptr(), _matrix(dtable, vocab, d, "dtable"), scratch.data_ptr(),
+                                       rows, d, vocab, _stream_ptr()), "rlhf_op_embed_grad")
+
+
+class rlhf_tensor_list:
+    """The gradients of a model for rlhf_op_grad_norm and rlhf_op_clip_grads: contiguous tensors, and where each goes when it is
+    clipped (None: in place).  Holds on to the tensors, whose memory must stay where it is."""
+
+    def __init__(self, src, dst=None):
+        self.src = list(src)
+        self.dst = self.src if dst is None else list(dst)
+        if len(self.src) != len(self.dst):
+            raise ValueError("as many destinations as sources are needed")
+        for s, d in zip(self.src, self.dst):
+            if s.dtype != d.dtype or s.shape != d.shape or not s.is_contiguous() or not d.is_contiguous() or s.device != d.device:
+                raise ValueError("sources and destinations must be contiguous and alike in shape, type and device")
+            if s.device != self.src[0].device or not s.is_cuda:
+                raise ValueError("all tensors must be in the memory of one device")
+        self.n = len(self.src)
+        self.array = (rlhf_tensor * max(self.n, 1))(*(rlhf_tensor(s.data_ptr(), d.data_ptr(), s.numel(), _act_code(s))
+                                                       for s, d in zip(self.src, self.dst)))
+        self.scratch_doubles = lib().rlhf_op_grad_norm_scratch_doubles(self.array, self.n)
+
+
+def rlhf_op_grad_norm(tensors: rlhf_tensor_list, norm, scratch=None) -> None:
+    """norm float32 [1] = 2-norm over all tensors of the list.  scratch: float64, tensors.scratch_doubles entries."""
+    import torch
+    _on_device(norm, scratch, *tensors.src[:1])
+    _vector(norm, 1, torch.float32, "norm")
+    if scratch is None:
+        scratch = torch.empty(tensors.scratch_doubles, dtype=torch.float64, device=norm.device)
+    elif scratch.dtype != torch.float64 or scratch.numel() < tensors.scratch_doubles or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous float64 tensor of {tensors.scratch_doubles} entries")
+    _op_check(lib().rlhf_op_grad_norm(tensors.array, tensors.n, norm.data_ptr(), scratch.data_ptr(), _stream_ptr()), "rlhf_op_grad_norm")
+
+
+def rlhf_op_clip_grads(tensors: rlhf_tensor_list, norm, max_norm: float) -> None:
+    """Scales every tensor of the list by max_norm / norm where norm is finite and above max_norm."""
+    import torch
+    _on_device(norm, *tensors.src[:1])
+    _vector(norm, 1, torch.float32, "norm")
+    _op_check(lib().rlhf_op_clip_grads(tensors.array, tensors.n, norm.data_ptr(), max_norm, _stream_ptr()), "rlhf_op_clip_grads")

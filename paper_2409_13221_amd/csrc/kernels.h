@@ -232,6 +232,36 @@ hipError_t launch_gae(hipStream_t st, const float* lp_actor, const float* lp_ref
                       const float* reward, const PackRow* rows, int n, int stride, float gamma, float kl_coef,
                       const GaePowers& pw, float* adv, float* ret);
 
+// ---- the Actor's update (include/rlhf_ops.h states what each computes)
+struct PolicyArgs {
+    const void* logits;         // [rows, vocab], row stride ld
+    size_t ld;
+    const int* tokens;          // [rows]
+    const float* weight;        // [rows] or NULL
+    const float* lp_old;        // [rows]
+    const float* lp_ref;        // [rows] or NULL
+    const float* adv;           // [rows]
+    void* grad;                 // [rows, vocab], row stride ld_grad; or NULL
+    size_t ld_grad;
+    float* lp;                  // [rows]
+    float* terms;               // [3][rows]: w * policy, w * kl, w * cut
+    int rows, vocab;
+    float lo, hi, kl_coef, grad_scale;      // lo, hi: bounds of the ratio
+};
+size_t policy_scratch_floats(int rows, int vocab);
+hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, float* stats);
+
+hipError_t launch_embed_rows(hipStream_t st, int tdt, int odt, const void* table, size_t ld_table, const int* tokens, float scale,
+                             void* out, size_t ld_out, int rows, int d, int vocab);
+size_t embed_grad_scratch_bytes(int rows, int d, int vocab);
+hipError_t launch_embed_grad(hipStream_t st, int gdt, int tdt, const void* dout, size_t ld_dout, const int* tokens, float scale,
+                             bool accumulate, void* dtable, size_t ld_table, void* scratch, int rows, int d, int vocab);
+
+struct GradTensor { const void* src; void* dst; size_t n; int dtype; };
+size_t grad_norm_scratch_doubles(const GradTensor* t, int n);
+hipError_t launch_grad_norm(hipStream_t st, const GradTensor* t, int n, float* norm, double* scratch);
+hipError_t launch_clip_grads(hipStream_t st, const GradTensor* t, int n, const float* norm, float max_norm);
+
 // ---- attention
 // Decode: one query row per active sample against its paged K/V.  q [rows, Hq*hd]; out the same.
 // row_sample[r] selects the page-table row; ctx_len[r] keys are visible.  part_* hold split

@@ -3,7 +3,10 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <mutex>
+#include <new>
+#include <vector>
 
 #include "../../include/rlhf.h"
 #include "kernels.h"
@@ -269,6 +272,117 @@ extern "C" int rlhf_op_lm_head_logprob(int act_half, const void* A, const void* 
 extern "C" int rlhf_op_bf16_to_half(const void* src, void* dst, int64_t n, void* stream) {
     if (!src || !dst || n < 0 || n % 2) return RLHF_EINVAL;
     return status_of(launch_bf16_to_half((hipStream_t)stream, src, dst, (size_t)n));
+}
+
+// ---- the Actor's update
+
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + nb && y < x + na;
+}
+static size_t elem_bytes(int dt) { return dt == kF32 ? 4 : 2; }
+// bytes from the first to behind the last element of a matrix
+static size_t span(int rows, int cols, int64_t ld, int dt) {
+    return rows > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem_bytes(dt) : 0;
+}
+static bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+extern "C" int64_t rlhf_op_policy_loss_scratch_floats(int rows, int vocab) {
+    return rows > 0 && vocab > 0 ? (int64_t)policy_scratch_floats(rows, vocab) : 0;
+}
+
+extern "C" int rlhf_op_policy_loss(int logit_dtype, const void* logits, int64_t ld, const int32_t* tokens,
+                                   const float* lp_old, const float* lp_ref, const float* adv, const float* weight,
+                                   float clip_low, float clip_high, float kl_coef, float grad_scale, float* lp, float* stats,
+                                   void* dlogits, int64_t ld_grad, float* scratch, int rows, int vocab, void* stream) {
+    const int dt = act_of(logit_dtype);
+    if (dt < 0 || rows < 0 || vocab < 1 || ld < vocab || !stats || (dlogits && ld_grad < vocab)) return RLHF_EINVAL;
+    if (rows > 0 && (!logits || !tokens || !lp_old || !adv || !lp || !scratch)) return RLHF_EINVAL;
+    // written so that a NaN is refused
+    if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f) || !(kl_coef >= 0.f && kl_coef < INFINITY) ||
+        !(grad_scale > -INFINITY && grad_scale < INFINITY) || (!lp_ref && kl_coef != 0.f))
+        return RLHF_EINVAL;
+    if (!aligned(logits, elem_bytes(dt)) || !aligned(dlogits, elem_bytes(dt))) return RLHF_EINVAL;
+    if (dlogits && !(dlogits == logits && ld_grad == ld) &&
+        overlap(logits, span(rows, vocab, ld, dt), dlogits, span(rows, vocab, ld_grad, dt)))
+        return RLHF_EINVAL;
+    PolicyArgs a;
+    a.logits = logits; a.ld = (size_t)ld; a.tokens = tokens;
+    a.weight = weight; a.lp_old = lp_old; a.lp_ref = lp_ref; a.adv = adv;
+    a.grad = dlogits; a.ld_grad = (size_t)ld_grad; a.lp = lp; a.terms = scratch;
+    a.rows = rows; a.vocab = vocab;
+    a.lo = 1.f - clip_low; a.hi = 1.f + clip_high; a.kl_coef = kl_coef; a.grad_scale = grad_scale;
+    return status_of(launch_policy_loss((hipStream_t)stream, dt, a, stats));
+}
+
+extern "C" int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, int64_t ld_table, const int32_t* tokens,
+                             float scale, void* out, int64_t ld_out, int rows, int d, int vocab, void* stream) {
+    const int tdt = act_of(table_dtype), odt = act_of(out_dtype);
+    if (tdt < 0 || odt < 0 || rows < 0 || d < 1 || vocab < 1 || ld_table < d || ld_out < d) return RLHF_EINVAL;
+    if (rows == 0) return RLHF_OK;
+    if (!table || !tokens || !out || !aligned(table, elem_bytes(tdt)) || !aligned(out, elem_bytes(odt)) ||
+        overlap(table, span(vocab, d, ld_table, tdt), out, span(rows, d, ld_out, odt)))
+        return RLHF_EINVAL;
+    return status_of(launch_embed_rows((hipStream_t)stream, tdt, odt, table, (size_t)ld_table, tokens, scale, out,
+                                       (size_t)ld_out, rows, d, vocab));
+}
+
+extern "C" int64_t rlhf_op_embed_grad_scratch_bytes(int rows, int d, int vocab) {
+    return rows > 0 && d > 0 && vocab > 0 ? (int64_t)embed_grad_scratch_bytes(rows, d, vocab) : 0;
+}
+
+extern "C" int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* dout, int64_t ld_dout, const int32_t* tokens,
+                                  float scale, int accumulate, void* dtable, int64_t ld_table, void* scratch, int rows,
+                                  int d, int vocab, void* stream) {
+    const int gdt = act_of(dout_dtype), tdt = act_of(table_dtype);
+    if (gdt < 0 || tdt < 0 || rows < 0 || d < 1 || vocab < 1 || ld_dout < d || ld_table < d || !dtable ||
+        !aligned(dtable, elem_bytes(tdt)))
+        return RLHF_EINVAL;
+    if (rows > 0 && (!dout || !tokens || !scratch || !aligned(dout, elem_bytes(gdt)) || !aligned(scratch, 16) ||
+                     overlap(dout, span(rows, d, ld_dout, gdt), dtable, span(vocab, d, ld_table, tdt))))
+        return RLHF_EINVAL;
+    return status_of(launch_embed_grad((hipStream_t)stream, gdt, tdt, dout, (size_t)ld_dout, tokens, scale, accumulate != 0,
+                                       dtable, (size_t)ld_table, scratch, rows, d, vocab));
+}
+
+// The caller's list in the launchers' form; empty tensors are dropped.  false: an entry that cannot be used.
+static bool grad_tensors(const rlhf_tensor* t, int n, bool write, std::vector<GradTensor>* out) {
+    if (n < 0 || (n > 0 && !t)) return false;
+    out->reserve((size_t)n);
+    for (int i = 0; i < n; ++i) {
+        const int dt = act_of(t[i].dtype);
+        if (dt < 0 || t[i].n < 0) return false;
+        if (t[i].n == 0) continue;
+        const size_t bytes = (size_t)t[i].n * elem_bytes(dt);
+        if (!t[i].src || !aligned(t[i].src, elem_bytes(dt)) || (write && !t[i].dst) || !aligned(t[i].dst, elem_bytes(dt)))
+            return false;
+        if (write && t[i].dst != t[i].src && overlap(t[i].src, bytes, t[i].dst, bytes)) return false;
+        out->push_back(GradTensor{t[i].src, t[i].dst, (size_t)t[i].n, dt});
+    }
+    return true;
+}
+
+extern "C" int64_t rlhf_op_grad_norm_scratch_doubles(const rlhf_tensor* tensors, int n_tensors) try {
+    std::vector<GradTensor> v;
+    return grad_tensors(tensors, n_tensors, false, &v) ? (int64_t)grad_norm_scratch_doubles(v.data(), (int)v.size()) : 0;
+} catch (const std::bad_alloc&) {
+    return 0;
+}
+
+extern "C" int rlhf_op_grad_norm(const rlhf_tensor* tensors, int n_tensors, float* norm, double* scratch, void* stream) try {
+    std::vector<GradTensor> v;
+    if (!norm || !grad_tensors(tensors, n_tensors, false, &v) || (!v.empty() && (!scratch || !aligned(scratch, 8)))) return RLHF_EINVAL;
+    return status_of(launch_grad_norm((hipStream_t)stream, v.data(), (int)v.size(), norm, scratch));
+} catch (const std::bad_alloc&) {
+    return RLHF_ENOMEM;
+}
+
+extern "C" int rlhf_op_clip_grads(const rlhf_tensor* tensors, int n_tensors, const float* norm, float max_norm, void* stream) try {
+    std::vector<GradTensor> v;
+    if (!norm || !(max_norm > 0.f) || !grad_tensors(tensors, n_tensors, true, &v)) return RLHF_EINVAL;
+    return status_of(launch_clip_grads((hipStream_t)stream, v.data(), (int)v.size(), norm, max_norm));
+} catch (const std::bad_alloc&) {
+    return RLHF_ENOMEM;
 }
 
 extern "C" int rlhf_op_gemm_tall_grid(int tiles_m, int tiles_n) {

@@ -1,0 +1,632 @@
+"""The operators of the Actor's update (policy loss on logits, embedding and its gradient, gradient norm and clipping)
+against their float64 forms in oracle/update.py.
+
+Tolerances.  E = 2^-24 is the half step of float, U that of the output type.  A log-probability l = z_y - m - log s has a
+sum s of V positive terms: a term is off by (its exponent + 4) E, by at most ln V E on the average over the softmax, the sum of
+at most V / 256 terms a thread and 16 joins by as many E, and log, differences and l itself by a few |l| E.  The rest follows by
+the derivatives of the formulas; see _policy_check."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import update as U
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+TDT = {"fp32": torch.float32, "bf16": torch.bfloat16, "half": torch.float16}
+HALF_STEP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "half": 2.0 ** -11}
+TINY = {"fp32": 1e-38, "bf16": 1e-38, "half": 2.0 ** -25}       # half a step of the subnormal numbers
+
+
+def _R():
+    import paper_2409_13221_amd as R
+    return R
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------ policy loss
+
+def _policy_case(seed, rows, vocab, dtype, masked=0.2, moved=0.2, pad=0):
+    """Device inputs; logits have `pad` columns behind vocab, filled with NaN."""
+    r = np.random.default_rng(seed)
+    z = torch.full((rows, vocab + pad), float("nan"), dtype=TDT[dtype])
+    z[:, :vocab] = torch.from_numpy((r.normal(size=(rows, vocab)) * 2).astype(np.float32)).to(TDT[dtype])
+    y = r.integers(0, vocab, rows)
+    l = U.log_softmax(_np(z[:, :vocab]))[np.arange(rows), y]
+    w = r.uniform(0.1, 1.0, rows) * (r.uniform(size=rows) >= masked)
+    f = lambda a: torch.from_numpy(np.asarray(a, np.float32)).cuda()
+    return dict(logits=z.cuda()[:, :vocab], tokens=torch.from_numpy(y.astype(np.int32)).cuda(), lp_old=f(l - moved * r.normal(size=rows)),
+                adv=f(r.normal(size=rows)), lp_ref=f(l + 0.4 * r.normal(size=rows)), weight=f(w))
+
+
+def _policy_run(c, grad=True, inplace=False, **kw):
+    R = _R()
+    z = c["logits"]
+    rows = z.shape[0]
+    lp, stats = torch.full((rows,), 77.0, device="cuda"), torch.full((4,), 77.0, device="cuda")
+    d = None
+    if grad:
+        d = z if inplace else torch.full(z.shape, 77.0, device="cuda", dtype=z.dtype)
+    R.rlhf_op_policy_loss(z, c["tokens"], c["lp_old"], c["adv"], lp, stats, dlogits=d, lp_ref=c.get("lp_ref"), weight=c.get("weight"), **kw)
+    torch.cuda.synchronize()
+    return lp, stats, d
+
+
+def _policy_check(c, got, dtype, kl_coef=0.0, grad_scale=1.0, logits=None, **kw):
+    z = _np(c["logits"]) if logits is None else logits
+    y, old, adv = c["tokens"].cpu().numpy(), _np(c["lp_old"]), _np(c["adv"])
+    ref = None if c.get("lp_ref") is None else _np(c["lp_ref"])
+    w = np.ones(len(y)) if c.get("weight") is None else _np(c["weight"])
+    lp, stats, grad = U.policy_loss(z, y, old, adv, lp_ref=ref, weight=w, kl_coef=kl_coef, grad_scale=grad_scale, **kw)
+    V = z.shape[1]
+    keep = (w != 0) & (y >= 0)
+    tol = E * (V / 256 + 64 + 4 * np.abs(lp))
+    assert (np.abs(_np(got[0]) - lp) <= tol * keep).all(), np.abs(_np(got[0]) - lp).max()
+    rho = np.exp(lp - old) * keep
+    t_rho = tol + E * (8 + np.abs(lp - old))                       # relative
+    x = (ref - lp) * keep if ref is not None else np.zeros(len(y))
+    ex = np.exp(x)
+    t_pol = np.abs(w * adv) * rho * t_rho + 4 * E * np.abs(w * adv) * rho
+    t_kl = w * (np.abs(ex - 1) * (tol + E * np.abs(x)) + 8 * E * (np.abs(ex - 1) + np.abs(x)))
+    t_stats = np.array([t_pol.sum() + kl_coef * t_kl.sum(), t_pol.sum(), t_kl.sum(), 0.0]) + 2 * E * np.abs(stats) + E * (w * keep).sum() * 1e-3
+    assert (np.abs(_np(got[1]) - stats) <= t_stats).all(), (_np(got[1]), stats, t_stats)
+    if got[2] is None:
+        return
+    m = np.where(np.isfinite(z), z, -np.inf).max(1, keepdims=True)
+    with np.errstate(invalid="ignore"):
+        p = np.exp(U.log_softmax(z))
+        dist = np.where(p > 0, m - z, 0.0)
+    p = np.where(keep[:, None], p, 0.0)
+    slope = np.abs(adv) * rho + kl_coef * np.abs(ex - 1)
+    t_slope = np.abs(adv) * rho * (t_rho + 8 * E) + kl_coef * (ex * (tol + 8 * E))
+    onehot = np.arange(V) == y[:, None]
+    t = np.abs(w * grad_scale)[:, None] * (t_slope[:, None] * np.abs(onehot - p) + slope[:, None] * (p * (dist + V / 256 + 48) + 2 * onehot) * E)
+    t = np.where(keep[:, None], t, 0.0) + HALF_STEP[dtype] * (np.abs(grad) + t) * 1.01 + TINY[dtype] * keep[:, None]
+    off = np.abs(_np(got[2]) - grad)
+    assert (off <= t).all(), (off.max(), np.argwhere(off > t)[:5])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("rows,vocab,pad", [(1, 1, 0), (3, 2, 0), (5, 7, 1), (2, 64, 0), (9, 255, 0), (300, 256, 8), (17, 1023, 0), (8, 4096, 0),
+                                            (4, 4097, 3), (33, 8200, 0), (64, 32000, 0), (300, 5003, 0), (3, 32001, 0), (7, 65537, 2),
+                                            (2, 131072, 0), (3, 131075, 0), (1, 300001, 0)])
+def test_policy_loss(dtype, rows, vocab, pad):
+    c = _policy_case(rows * 7 + vocab, rows, vocab, dtype, pad=pad)
+    kw = dict(kl_coef=0.1, grad_scale=1024.0 if dtype == "half" else 1.0)
+    _policy_check(c, _policy_run(c, **kw), dtype, **kw)
+
+
+@pytest.mark.parametrize("rows,vocab", [(3, 100), (40, 32000), (2, 140001)])
+@pytest.mark.parametrize("dtype", ["fp32", "half"])
+def test_policy_loss_without_gradient_and_options(dtype, rows, vocab):
+    c = _policy_case(rows + vocab, rows, vocab, dtype)
+    _policy_check(c, _policy_run(c, grad=False, kl_coef=0.3), dtype, kl_coef=0.3)
+    kw = dict(clip_low=0.1, clip_high=0.3, grad_scale=100.0)
+    _policy_check(c, _policy_run(c, **kw), dtype, **kw)                       # the KL is measured, and not in the loss
+    del c["lp_ref"], c["weight"]
+    _policy_check(c, _policy_run(c, **kw), dtype, **kw)
+    kw = dict(clip_low=1.0, clip_high=float("inf"), grad_scale=100.0)         # nothing is ever cut
+    got = _policy_run(c, **kw)
+    _policy_check(c, got, dtype, **kw)
+    assert float(got[1][3]) == 0.0
+
+
+@pytest.mark.parametrize("rows,vocab,pad", [(5, 200, 3), (3, 32000, 0), (300, 5000, 5), (2, 140003, 1)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_policy_loss_in_place_and_guard_columns(dtype, rows, vocab, pad):
+    """The gradient may overwrite the logits; columns behind vocab stay, in either form; both give the same bits."""
+    c = _policy_case(3, rows, vocab, dtype, pad=pad)
+    z = _np(c["logits"])
+    base = c["logits"]._base if pad else c["logits"]
+    out = torch.full((rows, vocab + pad), 5.0, device="cuda", dtype=TDT[dtype])
+    lp, stats, _ = _policy_run(c, grad=False, kl_coef=0.1)
+    R = _R()
+    R.rlhf_op_policy_loss(c["logits"], c["tokens"], c["lp_old"], c["adv"], lp, stats, dlogits=out[:, :vocab], lp_ref=c["lp_ref"],
+                          weight=c["weight"], kl_coef=0.1)
+    got = _policy_run(c, inplace=True, kl_coef=0.1)
+    _policy_check(c, got, dtype, kl_coef=0.1, logits=z)
+    assert torch.equal(got[2], out[:, :vocab]) and torch.equal(got[0], lp) and torch.equal(got[1], stats)
+    if pad:
+        assert (out[:, vocab:] == 5.0).all() and base[:, vocab:].isnan().all()
+
+
+@pytest.mark.parametrize("vocab", [33, 32000, 140001])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_policy_loss_left_out_rows(dtype, vocab):
+    """Rows of weight 0 or a negative token count for nothing, whatever the rest of them holds."""
+    c = _policy_case(5, 12, vocab, dtype, masked=0.0)
+    c["weight"][[1, 4]] = 0.0
+    c["tokens"][7] = -1
+    c["tokens"][4] = vocab + 5
+    want = _policy_run(c, kl_coef=0.1)
+    for r in (1, 4, 7):
+        c["logits"][r] = float("nan") if r != 4 else float("-inf")
+        c["lp_old"][r], c["adv"][r], c["lp_ref"][r] = float("nan"), float("inf"), float("-inf")
+    got = _policy_run(c, kl_coef=0.1)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert not got[2][[1, 4, 7]].any() and not got[0][[1, 4, 7]].any()
+    assert torch.isfinite(got[1]).all()
+    c["weight"].zero_()
+    got = _policy_run(c, kl_coef=0.1)
+    assert not any(t.any() for t in got)
+
+
+@pytest.mark.parametrize("vocab", [40, 32000, 140001])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_policy_loss_masked_and_extreme_logits(dtype, vocab):
+    """-inf and the type's lowest value in logits: probability 0, gradient 0; one column left alone: log-prob 0."""
+    c = _policy_case(6, 6, vocab, dtype, masked=0.0)
+    z, y = c["logits"], c["tokens"].long()
+    low = torch.finfo(z.dtype).min
+    kept = torch.zeros(z.shape, dtype=torch.bool, device="cuda")
+    kept[torch.arange(6), y] = True
+    kept[:, ::3] = True
+    z[0][~kept[0]] = float("-inf")
+    z[1][~kept[1]] = low
+    only = torch.zeros_like(kept[2])
+    only[y[2]] = True
+    z[2][~only] = float("-inf")
+    z[3][~only] = low
+    z[3, y[3]] = torch.finfo(z.dtype).max
+    z[4].fill_(low)                                      # a uniform row, at the very edge of the type
+    zz = _np(z)
+    l = U.log_softmax(zz)[np.arange(6), y.cpu().numpy()]
+    c["lp_old"] = torch.from_numpy((l + 0.1).astype(np.float32)).cuda()
+    c["lp_ref"] = torch.from_numpy((l - 0.2).astype(np.float32)).cuda()
+    got = _policy_run(c, kl_coef=0.1)
+    _policy_check(c, got, dtype, kl_coef=0.1)
+    assert not got[2][0][~kept[0]].any() and not got[2][1][~kept[1]].any() and not got[2][2].any() and not got[2][3].any()
+
+
+@pytest.mark.parametrize("vocab", [40, 32000, 140001])
+def test_policy_loss_rows_that_are_no_number(vocab):
+    """A bad row shows in its own log-prob and gradient and in the sums, and nowhere else."""
+    c = _policy_case(7, 8, vocab, "fp32", masked=0.0)
+    want = _policy_run(c)
+    c["logits"][1] = float("-inf")
+    c["logits"][2, vocab // 2] = float("inf")
+    c["logits"][3, vocab - 1] = float("nan")
+    c["tokens"][4] = vocab
+    got = _policy_run(c)
+    bad = [1, 2, 3, 4]
+    assert got[0][bad].isnan().all() and got[1][:3].isnan().all()
+    assert all(got[2][r].isnan().any() for r in bad)
+    good = [0, 5, 6, 7]
+    assert torch.equal(got[0][good], want[0][good]) and torch.equal(got[2][good], want[2][good])
+
+
+def test_policy_loss_token_out_of_reach_and_huge_ratios():
+    c = _policy_case(8, 4, 50, "fp32", masked=0.0)
+    del c["lp_ref"]
+    c["logits"][0, int(c["tokens"][0])] = float("-inf")         # the token's probability is 0: ratio 0
+    c["adv"][:] = torch.tensor([1.0, 0.0, 1.0, -1.0], device="cuda")
+    c["lp_old"][1:] -= 500.0                                    # ratio beyond float
+    lp, stats, d = _policy_run(c)
+    assert lp[0] == float("-inf") and torch.isfinite(lp[1:]).all()
+    assert not d[0].any() and not d[1].any() and not d[2].any()   # cut or without advantage
+    assert d[3].abs().max() == float("inf") and stats[0] == float("inf")
+    c["weight"][3] = 0.0
+    lp, stats, d = _policy_run(c)
+    want = -float(c["weight"][2]) * 1.2
+    assert abs(float(stats[0]) - want) <= 4 * E * abs(want)
+
+
+@pytest.mark.parametrize("vocab", [50, 140001])
+def test_policy_loss_of_no_rows(vocab):
+    z = torch.empty(0, vocab, device="cuda")
+    f, i = torch.empty(0, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    stats = torch.full((4,), 7.0, device="cuda")
+    _R().rlhf_op_policy_loss(z, i, f, f, f, stats, dlogits=torch.empty_like(z))
+    torch.cuda.synchronize()
+    assert not stats.any()
+
+
+def test_policy_loss_against_differences():
+    """Central differences of the kernel's own loss.  The loss is a sum of 6 rows of size at most 3, off by a few hundred E: with a
+    step of 2^-6 that is 2e-3 E-steps below 1e-4; the third derivative of a row is at most 6 w |A| rho, times h^2 / 6 = 4e-5."""
+    c = _policy_case(9, 6, 12, "fp32", masked=0.0, moved=0.02)
+    kw = dict(kl_coef=0.1, clip_low=0.5, clip_high=0.5)
+    _, _, d = _policy_run(c, **kw)
+    h = 2.0 ** -6
+    for r in range(6):
+        for v in range(12):
+            s = []
+            for sign in (1, -1):
+                e = dict(c, logits=c["logits"].clone())
+                e["logits"][r, v] += sign * h
+                s.append(float(_policy_run(e, grad=False, **kw)[1][0]))
+            assert abs((s[0] - s[1]) / (2 * h) - float(d[r, v])) < 1e-3
+
+
+def test_policy_loss_offsets_beyond_32_bits():
+    """Rows 2.5 * 10^9 bytes apart, and gradients likewise."""
+    ld = 1_250_000_003
+    c = _policy_case(10, 3, 5000, "bf16", masked=0.0)
+    base = torch.empty(2 * ld + 5000, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(2 * ld + 5000, dtype=torch.bfloat16, device="cuda")
+    far, d = base.as_strided((3, 5000), (ld, 1)), out.as_strided((3, 5000), (ld, 1))
+    far.copy_(c["logits"])
+    want = _policy_run(c, kl_coef=0.1)
+    lp, stats = torch.empty(3, device="cuda"), torch.empty(4, device="cuda")
+    _R().rlhf_op_policy_loss(far, c["tokens"], c["lp_old"], c["adv"], lp, stats, dlogits=d, lp_ref=c["lp_ref"], weight=c["weight"], kl_coef=0.1)
+    torch.cuda.synchronize()
+    assert torch.equal(d, want[2]) and torch.equal(lp, want[0]) and torch.equal(stats, want[1])
+
+
+# ------------------------------------------------------------------------------- embedding and gradient
+
+def _tokens(r, rows, vocab, kind):
+    if kind == "one":
+        t = np.full(rows, vocab // 2)
+    elif kind == "tail":
+        t = np.exp(r.uniform(size=rows) * np.log(vocab + 1)).astype(np.int64) - 1
+    elif kind == "each":
+        t = r.permutation(max(rows, vocab))[:rows] % vocab
+    elif kind == "padded":
+        t = np.where(r.uniform(size=rows) < 0.5, -1, r.integers(0, vocab, rows))
+    else:
+        t = r.integers(0, vocab, rows)
+    return np.clip(t, -1, vocab - 1).astype(np.int32)
+
+
+@pytest.mark.parametrize("tdt", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("odt", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("rows,d,vocab,pad,scale", [(1, 1, 1, 0, 1.0), (3, 5, 10, 0, 2.5), (7, 64, 100, 3, 1.0), (130, 257, 50, 0, 0.3),
+                                                    (65, 768, 300, 8, 27.7), (5, 8192, 20, 0, 1.0), (2, 20001, 7, 1, 3.0)])
+def test_embed(tdt, odt, rows, d, vocab, pad, scale):
+    r = np.random.default_rng(rows + d)
+    table = torch.from_numpy(r.normal(size=(vocab, d + pad)).astype(np.float32)).to(TDT[tdt]).cuda()[:, :d]
+    tok = _tokens(r, rows, vocab, "padded" if rows > 5 else "any")
+    out = torch.full((rows, d + pad), 9.0, dtype=TDT[odt], device="cuda")
+    _R().rlhf_op_embed(table, torch.from_numpy(tok).cuda(), out[:, :d], scale=scale)
+    torch.cuda.synchronize()
+    want = U.embed(_np(table), tok, np.float64(np.float32(scale)))
+    off = np.abs(_np(out[:, :d]) - want)
+    assert (off <= (E + HALF_STEP[odt] * 1.01) * np.abs(want) + TINY[odt]).all()      # one product, one rounding
+    assert (out[:, d:] == 9.0).all()
+
+
+def test_embed_token_beyond_the_vocabulary_and_no_rows():
+    R = _R()
+    table = torch.ones(4, 10, device="cuda")
+    out = torch.zeros(3, 10, device="cuda")
+    R.rlhf_op_embed(table, torch.tensor([4, -1, 3], dtype=torch.int32, device="cuda"), out)
+    torch.cuda.synchronize()
+    assert out[0].isnan().all() and not out[1].any() and (out[2] == 1).all()
+    R.rlhf_op_embed(table, torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, 10, device="cuda"))
+    torch.cuda.synchronize()
+
+
+def _egrad_check(got, dout, tok, vocab, scale, odt, start=None):
+    scale = np.float64(np.float32(scale))
+    want = U.embed_grad(dout, tok, vocab, scale, start=start)
+    size = U.embed_grad(np.abs(dout), tok, vocab, abs(scale), start=None if start is None else np.abs(start))
+    n = np.bincount(tok[(tok >= 0) & (tok < vocab)], minlength=vocab)[:, None]
+    # n additions, the product and the addition to the start, each off by E of at most the sum of the sizes; one rounding
+    tol = (n + 3) * E * size
+    tol += HALF_STEP[odt] * (np.abs(want) + tol) * 1.01 + TINY[odt]
+    off = np.abs(got - want)
+    assert (off <= tol).all(), (off.max(), np.argwhere(off > tol)[:4])
+    none = (n[:, 0] == 0)
+    np.testing.assert_array_equal(got[none], 0.0 if start is None else start[none])
+
+
+@pytest.mark.parametrize("gdt,tdt", [("fp32", "fp32"), ("bf16", "fp32"), ("bf16", "bf16"), ("half", "half"), ("fp32", "bf16"), ("half", "fp32")])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("rows,d,vocab,kind", [
+    (1, 1, 1, "any"), (2, 3, 5, "one"), (5, 64, 7, "any"), (64, 33, 11, "tail"), (61, 768, 400, "tail"), (257, 100, 1, "one"), (300, 257, 37, "padded"),
+    (1000, 72, 2000, "each"), (1025, 40, 999, "tail"), (2049, 520, 300, "tail"), (3000, 24, 50000, "any"), (5000, 130, 60, "one"), (9000, 19, 700, "tail"),
+    (17000, 16, 257, "tail"), (70000, 9, 1000, "padded"), (70001, 8, 3, "one")])
+def test_embed_grad(gdt, tdt, accumulate, rows, d, vocab, kind):
+    R = _R()
+    r = np.random.default_rng(rows + d + vocab)
+    tok = _tokens(r, rows, vocab, kind)
+    dout = torch.from_numpy(r.normal(size=(rows, d)).astype(np.float32)).to(TDT[gdt]).cuda()
+    start = torch.from_numpy(r.normal(size=(vocab, d)).astype(np.float32)).to(TDT[tdt]).cuda() if accumulate else \
+        torch.full((vocab, d), float("nan"), dtype=TDT[tdt], device="cuda")
+    tk, got = torch.from_numpy(tok).cuda(), start.clone()
+    R.rlhf_op_embed_grad(dout, tk, got, scale=0.7, accumulate=accumulate)
+    again = start.clone()
+    R.rlhf_op_embed_grad(dout, tk, again, scale=0.7, accumulate=accumulate)
+    torch.cuda.synchronize()
+    _egrad_check(_np(got), _np(dout), tok, vocab, 0.7, tdt, _np(start) if accumulate else None)
+    assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("rows,d", [(50, 36), (6000, 70), (20000, 5)])
+def test_embed_grad_strides_bad_tokens_and_guards(rows, d):
+    """Padded rows of both matrices, tokens beyond the vocabulary, columns behind d left as they were."""
+    R = _R()
+    r = np.random.default_rng(rows)
+    vocab = 90
+    tok = r.integers(-2, vocab + 3, rows).astype(np.int32)
+    dout = torch.from_numpy(r.normal(size=(rows, d + 3)).astype(np.float32)).cuda()
+    base = torch.full((vocab, d + 5), 4.0, device="cuda")
+    R.rlhf_op_embed_grad(dout[:, 1:d + 1], torch.from_numpy(tok).cuda(), base[:, 2:d + 2], scale=-2.0)
+    torch.cuda.synchronize()
+    _egrad_check(_np(base[:, 2:d + 2]), _np(dout[:, 1:d + 1]), tok, vocab, -2.0, "fp32")
+    assert (base[:, :2] == 4.0).all() and (base[:, d + 2:] == 4.0).all()
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_grad_of_no_rows(accumulate):
+    got = torch.full((6, 10), 3.0, device="cuda")
+    _R().rlhf_op_embed_grad(torch.empty(0, 10, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), got, accumulate=accumulate)
+    torch.cuda.synchronize()
+    assert (got == (3.0 if accumulate else 0.0)).all()
+
+
+@pytest.mark.parametrize("rows", [3, 3000])
+def test_embedding_offsets_beyond_32_bits(rows):
+    """A table whose rows lie 1.5 * 10^9 bytes apart."""
+    R = _R()
+    ld, d, vocab = 375_000_001, 300, 4
+    r = np.random.default_rng(4)
+    base = torch.empty((vocab - 1) * ld + d, device="cuda")
+    table = base.as_strided((vocab, d), (ld, 1))
+    table.copy_(torch.from_numpy(r.normal(size=(vocab, d)).astype(np.float32)))
+    tok = r.integers(0, vocab, rows).astype(np.int32)
+    tok[0] = vocab - 1
+    out, tk = torch.empty(rows, d, device="cuda"), torch.from_numpy(tok).cuda()
+    R.rlhf_op_embed(table, tk, out)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(_np(out), _np(table)[tok])
+    R.rlhf_op_embed_grad(out, tk, table)
+    torch.cuda.synchronize()
+    _egrad_check(_np(table), _np(out), tok, vocab, 1.0, "fp32")
+
+
+# -------------------------------------------------------------------------------- gradient norm, clipping
+
+def _grads(seed, shapes, dtypes, offset=0):
+    r = np.random.default_rng(seed)
+    out = []
+    for i, s in enumerate(shapes):
+        n = int(np.prod(s))
+        t = torch.from_numpy(r.normal(size=n + offset).astype(np.float32)).to(TDT[dtypes[i % len(dtypes)]]).cuda()
+        out.append(t[offset:].view(s))
+    return out
+
+
+def _clip_check(src, dst, norm, max_norm, before):
+    want = U.grad_norm(before)
+    assert abs(float(norm) - want) <= E * want * 1.001
+    f = U.clip_factor(want, max_norm)
+    for t, b in zip(dst, before):
+        u = {torch.float32: E, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[t.dtype]
+        tiny = 2.0 ** -25 if t.dtype == torch.float16 else 1e-38
+        if f == 1.0:
+            np.testing.assert_array_equal(_np(t), b)
+        else:                                                    # the norm, the quotient, the product: E each; one rounding
+            assert (np.abs(_np(t) - f * b) <= (3 * E + u * 1.01) * np.abs(f * b) + tiny).all()
+
+
+SHAPE_SETS = {"one": [(1,)], "small": [(3,), (17, 5), (1,), (64,), (255,), (1, 1)], "empty": [(0,), (5, 0), (7,), (0,)],
+              "odd": [(4097,), (33, 1001), (8191, 3), (65537,)], "large": [(3000001,), (1000, 1000), (7,)],
+              "many": [((i * 37) % 911 + 1,) for i in range(700)]}
+
+
+@pytest.mark.parametrize("dtypes", [("fp32",), ("bf16",), ("half", "fp32", "bf16")])
+@pytest.mark.parametrize("shapes", sorted(SHAPE_SETS))
+@pytest.mark.parametrize("inplace,offset,max_norm", [(True, 0, 0.7), (False, 1, 0.7), (False, 0, 1e9), (True, 3, 1e9)])
+def test_norm_and_clipping(dtypes, shapes, inplace, offset, max_norm):
+    R = _R()
+    src = _grads(len(shapes), SHAPE_SETS[shapes], dtypes, offset)
+    before = [_np(t) for t in src]
+    dst = src if inplace else [torch.full_like(t, 5.0) for t in src]
+    lst = R.rlhf_tensor_list(src, None if inplace else dst)
+    norm = torch.full((1,), 77.0, device="cuda")
+    R.rlhf_op_grad_norm(lst, norm)
+    R.rlhf_op_clip_grads(lst, norm, max_norm)
+    again = torch.zeros(1, device="cuda")
+    if not inplace:
+        R.rlhf_op_grad_norm(lst, again)
+        torch.cuda.synchronize()
+        assert torch.equal(norm, again)
+        for t, b in zip(src, before):
+            np.testing.assert_array_equal(_np(t), b)
+    torch.cuda.synchronize()
+    _clip_check(src, dst, norm, max_norm, before)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e30])
+def test_norm_where_squares_leave_float(size):
+    R = _R()
+    t = [torch.full((1000,), size, device="cuda"), torch.full((3, 3), -size, device="cuda")]
+    norm = torch.zeros(1, device="cuda")
+    lst = R.rlhf_tensor_list(t)
+    R.rlhf_op_grad_norm(lst, norm)
+    R.rlhf_op_clip_grads(lst, norm, 1.0)
+    torch.cuda.synchronize()
+    want = U.grad_norm([np.full(1009, np.float32(size))])
+    assert abs(float(norm) - want) <= 1.001 * E * want
+    if size > 1:
+        assert abs(U.grad_norm([_np(x) for x in t]) - 1.0) <= 4 * E
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("inplace", [True, False])
+def test_gradients_that_are_not_finite_pass_unchanged(bad, inplace):
+    R = _R()
+    t = _grads(1, [(5000,), (64, 3)], ("fp32",))
+    t[0][4321] = bad
+    before = [x.clone() for x in t]
+    dst = t if inplace else [torch.zeros_like(x) for x in t]
+    lst, norm = R.rlhf_tensor_list(t, dst), torch.zeros(1, device="cuda")
+    R.rlhf_op_grad_norm(lst, norm)
+    R.rlhf_op_clip_grads(lst, norm, 0.1)
+    torch.cuda.synchronize()
+    assert not torch.isfinite(norm).any()
+    for a, b in zip(dst, before):
+        np.testing.assert_array_equal(a.cpu().numpy(), b.cpu().numpy())
+
+
+def test_norm_of_nothing_and_zeros():
+    R = _R()
+    norm = torch.full((1,), 7.0, device="cuda")
+    R.rlhf_op_grad_norm(R.rlhf_tensor_list([]), norm)
+    torch.cuda.synchronize()
+    assert float(norm) == 0.0
+    z = torch.zeros(100, device="cuda")
+    lst = R.rlhf_tensor_list([z])
+    norm.fill_(7.0)
+    R.rlhf_op_grad_norm(lst, norm)
+    R.rlhf_op_clip_grads(lst, norm, 1.0)
+    torch.cuda.synchronize()
+    assert float(norm) == 0.0 and not z.any()
+
+
+def test_norm_combined_between_the_calls():
+    """The norm that clipping goes by is the caller's: here as of two ranks with the same gradients."""
+    R = _R()
+    t = _grads(2, [(1000,), (37, 11)], ("fp32",))
+    before = [_np(x) for x in t]
+    lst, norm = R.rlhf_tensor_list(t), torch.zeros(1, device="cuda")
+    R.rlhf_op_grad_norm(lst, norm)
+    norm.mul_(2.0 ** 0.5)
+    R.rlhf_op_clip_grads(lst, norm, 1.0)
+    torch.cuda.synchronize()
+    f = 1.0 / (U.grad_norm(before) * 2.0 ** 0.5)
+    for x, b in zip(t, before):
+        assert (np.abs(_np(x) - f * b) <= 6 * E * np.abs(f * b)).all()
+
+
+# -------------------------------------------------------------------------------------- all of them together
+
+class _Update:
+    """A one-matrix model from embedding to loss: h = s T[token], logits = h W^T, and its gradients by the library's
+    operators (the two products between them by torch)."""
+
+    def __init__(self, seed, rows, d, vocab):
+        r = np.random.default_rng(seed)
+        f = lambda a: torch.from_numpy(np.asarray(a, np.float32)).cuda()
+        self.scale, self.max_norm = 3.0, 0.05
+        self.T, self.W = f(r.normal(size=(vocab, d)) * 0.3), f(r.normal(size=(vocab, d)) * 0.3)
+        self.tok = torch.from_numpy(_tokens(r, rows, vocab, "tail")).cuda()
+        self.nxt = torch.from_numpy(r.integers(0, vocab, rows).astype(np.int32)).cuda()
+        self.nxt[3] = -1
+        lp = U.log_softmax(U.embed(_np(self.T), self.tok.cpu().numpy(), self.scale) @ _np(self.W).T)
+        l = lp[np.arange(rows), self.nxt.cpu().numpy()]
+        self.old, self.ref = f(l + 0.05 * r.normal(size=rows)), f(l + 0.2 * r.normal(size=rows))
+        self.adv, self.w = f(r.normal(size=rows)), f(np.full(rows, 1.0 / rows))
+        e = lambda *s: torch.empty(*s, device="cuda")
+        self.h, self.z, self.dz = e(rows, d), e(1, rows, vocab), e(rows, vocab)
+        self.dT, self.dW, self.lp, self.stats, self.norm = e(vocab, d), e(vocab, d), e(rows), e(4), e(1)
+        R = _R()
+        self.list = R.rlhf_tensor_list([self.dT, self.dW])
+        # a scratch of its own for each step: nothing is shared with another update
+        self.s1 = e(R.lib().rlhf_op_policy_loss_scratch_floats(rows, vocab))
+        self.s2 = torch.empty(R.lib().rlhf_op_embed_grad_scratch_bytes(rows, d, vocab), dtype=torch.uint8, device="cuda")
+        self.s3 = torch.empty(self.list.scratch_doubles, dtype=torch.float64, device="cuda")
+
+    def step(self):
+        R = _R()
+        R.rlhf_op_embed(self.T, self.tok, self.h, scale=self.scale)
+        R.rlhf_op_gemm(self.h, self.W, self.z, 1)
+        R.rlhf_op_policy_loss(self.z[0], self.nxt, self.old, self.adv, self.lp, self.stats, dlogits=self.dz, lp_ref=self.ref,
+                              weight=self.w, kl_coef=0.1, scratch=self.s1)
+        torch.mm(self.dz.t(), self.h, out=self.dW)
+        R.rlhf_op_embed_grad(torch.mm(self.dz, self.W), self.tok, self.dT, scale=self.scale, scratch=self.s2)
+        R.rlhf_op_grad_norm(self.list, self.norm, scratch=self.s3)
+        R.rlhf_op_clip_grads(self.list, self.norm, self.max_norm)
+
+    def outputs(self):
+        return [t.clone() for t in (self.lp, self.stats, self.dT, self.dW, self.norm)]
+
+    def reference(self):
+        T, W = _np(self.T), _np(self.W)
+        tok = self.tok.cpu().numpy()
+        h = U.embed(T, tok, self.scale)
+        lp, stats, dz = U.policy_loss(h @ W.T, self.nxt.cpu().numpy(), _np(self.old), _np(self.adv), lp_ref=_np(self.ref),
+                                      weight=_np(self.w), kl_coef=float(np.float32(0.1)))
+        dT, dW = U.embed_grad(dz @ W, tok, len(T), self.scale), dz.T @ h
+        norm = U.grad_norm([dT, dW])
+        f = U.clip_factor(norm, self.max_norm)
+        return [lp, stats, dT * f, dW * f, np.array([norm])]
+
+
+def _update_check(got, want):
+    # float products of up to 512 terms, logits up to about 20: a log-prob is off by 20 * 512 E at the very most, everything after
+    # it in proportion; in the 2-norm, a tenth of that
+    for g, w in zip(got, want):
+        assert np.linalg.norm(_np(g) - w) <= 1e3 * E * np.linalg.norm(w) + 1e-12, (np.linalg.norm(_np(g) - w), np.linalg.norm(w))
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(40, 64, 500), (300, 256, 4096), (2500, 48, 700)])
+def test_update_of_a_small_model(rows, d, vocab):
+    u = _Update(rows, rows, d, vocab)
+    u.step()
+    torch.cuda.synchronize()
+    assert float(u.norm) > u.max_norm
+    _update_check(u.outputs(), u.reference())
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(40, 64, 500), (2500, 48, 700)])
+def test_update_in_a_graph_and_on_another_stream(rows, d, vocab):
+    """Captured and replayed several times with new inputs and eager work in between; two graphs; a stream of its own."""
+    a, b = _Update(1, rows, d, vocab), _Update(2, rows, d, vocab)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        a.step(), b.step()
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    _update_check(a.outputs(), a.reference())
+    graphs = []
+    for u in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            u.step()
+        graphs.append(g)
+    for k in range(4):
+        for u in (a, b):
+            u.adv.mul_(-1.1)
+            u.tok.copy_(u.tok.roll(7 * k + 1))
+        want = []
+        for u in (a, b):
+            u.step()
+            want.append(u.outputs())
+            for t in (u.lp, u.stats, u.dT, u.dW, u.norm, u.dz):
+                t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for u, w in zip((a, b), want):
+            for x, y in zip(u.outputs(), w):
+                assert torch.equal(x, y)
+    _update_check(a.outputs(), a.reference())
+
+
+def test_loss_of_a_finished_stage():
+    """The stage's own results as the loss takes them up: log-probs, Reference and advantages of every generated token against
+    logits that give the same log-probs.  The Actor has not moved: ratio 1, nothing clipped, the KL that of the stage."""
+    from tests import stage_harness as H
+    from workload import CONFIGS
+    cfg = CONFIGS["tiny"]
+    inp = H.make_inputs(cfg, n=6)
+    with H.GpuStage(cfg, inp) as g:
+        g.submit()
+        g.R.rlhf_run_stage(g.ctx, False, 0, 8192, 0b1110)
+        res = g.results()
+        n = int(res["gen_len"].sum())
+        adv, _ = g.R.rlhf_compute_gae(g.ctx, 0.99, 0.95, 0.1, n)
+    dev = lambda a, dt=torch.float32: torch.tensor(np.asarray(a), dtype=dt).cuda()
+    V, tok = cfg.model.vocab, dev(res["tokens"], torch.int32)
+    lp = res["lp_actor"].astype(np.float64)
+    # a row whose other columns share what the token leaves: its log-softmax at the token is the stage's log-prob
+    z = np.repeat(np.log(-np.expm1(lp) / (V - 1))[:, None], V, 1)
+    z[np.arange(n), res["tokens"]] = lp
+    c = dict(logits=dev(z), tokens=tok, lp_old=dev(lp), adv=dev(adv), lp_ref=dev(res["lp_ref"]), weight=dev(np.full(n, 1.0 / n)))
+    got = _policy_run(c, kl_coef=0.1)
+    _policy_check(c, got, "fp32", kl_coef=0.1)
+    assert float(got[1][3]) == 0.0
+    x = res["lp_ref"].astype(np.float64) - lp
+    tol = E * (V / 256 + 64 + 8 * np.abs(lp).max())               # of a log-prob, as in _policy_check, and of the logits' rounding
+    assert abs(float(got[1][1]) + adv.astype(np.float64).mean()) <= 2 * tol * np.abs(adv).mean()
+    assert abs(float(got[1][2]) - (np.expm1(x) - x).mean()) <= 2 * tol * np.abs(np.expm1(x)).mean() + 1e-7
