@@ -200,6 +200,19 @@ def test_policy_loss_rows_that_are_no_number(vocab):
     assert torch.equal(got[0][good], want[0][good]) and torch.equal(got[2][good], want[2][good])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 40, 63, 5003, 32001, 140001])
+def test_policy_loss_writes_nothing_for_tokens_beyond_the_vocabulary(dtype, vocab):
+    rows = 4
+    c = _policy_case(11, rows, vocab, dtype, masked=0.0)
+    c["tokens"][:] = torch.tensor([vocab, vocab + 1, vocab + 7, 2 ** 31 - 1], dtype=torch.int32)
+    out = torch.full((rows, vocab + 9), 5.0, device="cuda", dtype=TDT[dtype])
+    lp, stats = torch.zeros(rows, device="cuda"), torch.zeros(4, device="cuda")
+    _R().rlhf_op_policy_loss(c["logits"], c["tokens"], c["lp_old"], c["adv"], lp, stats, dlogits=out[:, :vocab], weight=c["weight"])
+    torch.cuda.synchronize()
+    assert lp.isnan().all() and out[:, :vocab].isnan().all() and (out[:, vocab:] == 5.0).all()
+
+
 def test_policy_loss_token_out_of_reach_and_huge_ratios():
     c = _policy_case(8, 4, 50, "fp32", masked=0.0)
     del c["lp_ref"]
