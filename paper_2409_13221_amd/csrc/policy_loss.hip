@@ -23,34 +23,92 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, int r, float w,
     return o;
 }
 
-// A row in registers: IT vectors of 16 bytes a thread, THREADS threads, read once, all loads in flight together.  Each wave takes
-// its own maximum and sum of exponentials, one exchange joins them; the exponentials stay in the registers of the logits, so
-// that the gradient is one product away.
+// Two floats as two packed 16-bit elements, and back; rounded to nearest, a NaN stays one.
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<bf16_t>(float lo, float hi) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, pair{(__bf16)lo, (__bf16)hi});
+}
+template <> __device__ __forceinline__ uint32_t pack2<f16_t>(float lo, float hi) {
+    typedef f16_t pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, pair{(f16_t)lo, (f16_t)hi});
+}
+template <typename T> __device__ __forceinline__ float unpack(uint32_t w, int hi);
+template <> __device__ __forceinline__ float unpack<bf16_t>(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xFFFF0000u : w << 16); }
+template <> __device__ __forceinline__ float unpack<f16_t>(uint32_t w, int hi) {
+    typedef f16_t pair __attribute__((ext_vector_type(2)));
+    return (float)__builtin_bit_cast(pair, w)[hi];
+}
+
+// 16 bytes of a row, at any alignment of the element's, packed as they came.
 template <typename T> struct Vec {
     static constexpr int N = 16 / sizeof(T);
-    // N elements at p, any alignment
-    static __device__ __forceinline__ void load(const T* p, float* o) {
-        T v[N];
-        __builtin_memcpy(v, p, 16);
+    uint32_t w[4];
+    // Logits are read once and gradients written once: evict-first in the L2 (8192 x 32000 bf16 201 -> 181 us).
+    typedef uint32_t Quad __attribute__((ext_vector_type(4), aligned(2), may_alias));
+    template <bool ONCE = true> __device__ __forceinline__ void load(const T* p) {
+        const Quad q = ONCE ? __builtin_nontemporal_load((const Quad*)p) : *(const Quad*)p;
 #pragma unroll
-        for (int e = 0; e < N; ++e) o[e] = to_f32<T>(v[e]);
+        for (int k = 0; k < 4; ++k) w[k] = q[k];
     }
-    static __device__ __forceinline__ void store(T* p, const float* x) {
-        T v[N];
+    __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store(Quad{w[0], w[1], w[2], w[3]}, (Quad*)p); }
+    __device__ __forceinline__ void get(float (&x)[N]) const {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = from_f32<T>(x[e]);
-        __builtin_memcpy(p, v, 16);
+        for (int e = 0; e < N; ++e) x[e] = unpack<T>(w[e / 2], e & 1);
+    }
+    __device__ __forceinline__ void set(const float (&x)[N]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = pack2<T>(x[2 * k], x[2 * k + 1]);
+    }
+    __device__ __forceinline__ void fill(float v) {
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = v;
+        set(x);
+    }
+    // What get() gave before is not kept for get() after it: the packed form is the one that stays in registers.
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[k]));
+    }
+};
+template <> __device__ __forceinline__ void Vec<float>::get(float (&x)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
+}
+template <> __device__ __forceinline__ void Vec<float>::set(const float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(x[e]);
+}
+
+// Running maximum m and sum s of exp(z - m) of a thread's logits; m = -inf, s = 0 to begin with.
+struct Running {
+    float m = -INFINITY, s = 0.f;
+    template <int N> __device__ __forceinline__ void add(const float (&x)[N]) {
+        float mx = m;
+#pragma unroll
+        for (int e = 0; e < N; ++e) mx = fmaxf(mx, x[e]);
+        const float ref = mx == -INFINITY ? 0.f : mx;          // exp(-inf - 0) is 0, exp(-inf + inf) would be NaN
+        float t = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) t += __expf(x[e] - ref);
+        s = s * __expf(m - ref) + t;
+        m = mx;
     }
 };
 
 // What joins the waves of a row (up to 16): maximum and sum of exp(z - maximum).  Every 16 lanes hold all waves' pairs.
 template <int WAVES>
-__device__ __forceinline__ void join_waves(float m, float s, float (*red)[2], float& M, float& S) {
+__device__ __forceinline__ void join_row(const Running& run, float (*red)[2], float& M, float& S) {
     const int lane = threadIdx.x & 63;
-    if (lane == 0) { red[threadIdx.x >> 6][0] = m; red[threadIdx.x >> 6][1] = s; }
-    __syncthreads();
-    m = red[lane % WAVES][0];
-    s = red[lane % WAVES][1];
+    float m = wave_max(run.m);
+    float s = wave_sum(run.s * __expf(run.m - (m == -INFINITY ? 0.f : m)));
+    if (WAVES > 1) {
+        if (lane == 0) { red[threadIdx.x >> 6][0] = m; red[threadIdx.x >> 6][1] = s; }
+        __syncthreads();
+        m = red[lane % WAVES][0];
+        s = red[lane % WAVES][1];
+    }
     M = m;
 #pragma unroll
     for (int o = 1; o < WAVES; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, kWave));
@@ -71,79 +129,98 @@ __device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, fl
     out[1] = -o.slope * a.grad_scale / S;
 }
 
-template <typename T>
-__device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, int threads) {
-    if (threadIdx.x < 3) a.terms[(size_t)threadIdx.x * a.rows + r] = 0.f;
-    if (threadIdx.x == 0) a.lp[r] = 0.f;
-    if (!g) return;
-    constexpr int N = Vec<T>::N;
-    const float zero[N] = {};
-    for (int i = threadIdx.x * N; i < a.vocab; i += threads * N) {
-        if (i + N <= a.vocab) Vec<T>::store(g + i, zero);
-        else for (int e = i; e < a.vocab; ++e) g[e] = from_f32<T>(0.f);
-    }
+// The vectors of a row start where what is written of it, or else what is read, reaches a 16-byte boundary; the few columns
+// before and behind them go to a thread each.
+template <typename T> __device__ __forceinline__ int columns_before(const T* row, int vocab) {
+    return min((int)((0 - (uintptr_t)row) % 16 / sizeof(T)), vocab);
 }
 
-template <typename T, int IT, int THREADS, int WAVES_PER_SIMD>
-__global__ __launch_bounds__(THREADS, WAVES_PER_SIMD) void k_policy_row(PolicyArgs a) {
+template <typename T>
+__device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, int t, int threads) {
+    if (t < 3) a.terms[(size_t)t * a.rows + r] = 0.f;
+    if (t == 0) a.lp[r] = 0.f;
+    if (!g) return;
+    constexpr int N = Vec<T>::N;
+    Vec<T> zero;
+    zero.fill(0.f);
+    const int head = columns_before<T>(g, a.vocab), whole = (a.vocab - head) / N * N, odd = t < head ? t : t + whole;
+    for (int i = t * N; i < whole; i += threads * N) zero.store(g + head + i);
+    if (odd < a.vocab) g[odd] = from_f32<T>(0.f);
+}
+
+// A row in registers: IT vectors of 16 bytes a thread, requested all at once.  Each is taken into the thread's running maximum and
+// sum as it arrives, so that the exponentials hide behind the loads; the gradient takes them anew from the logits, which
+// costs less than room for them in 32 bits would (a 16-bit row of 32000 is 16 registers of 1024 threads).
+// ROWS rows of THREADS threads each in a workgroup; more than one only where a row is one wave's.
+template <typename T, int IT, int THREADS, int ROWS, int WAVES_PER_SIMD>
+__global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(PolicyArgs a) {
+    static_assert(ROWS == 1 || THREADS == kWave, "rows of more than a wave meet at barriers");
     constexpr int N = Vec<T>::N;
     __shared__ float red[THREADS / 64][2];
     __shared__ float s_row[2];
-    const int r = blockIdx.x, t = threadIdx.x, V = a.vocab;
+    const int r = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / THREADS : 0), t = threadIdx.x % THREADS, V = a.vocab;
+    if (ROWS > 1 && r >= a.rows) return;
     const T* z = (const T*)a.logits + (size_t)r * a.ld;
     T* g = a.grad ? (T*)a.grad + (size_t)r * a.ld_grad : nullptr;
     const int y = a.tokens[r];
     const float w = a.weight ? a.weight[r] : 1.f;
-    if (y < 0 || w == 0.f) return left_out_row<T>(a, r, g, THREADS);
-    const unsigned whole = V / N * N, last = whole + t;    // columns in vectors; the few behind them, one a thread
-    float x[IT][N], xl = -INFINITY;
+    if (y < 0 || w == 0.f) return left_out_row<T>(a, r, g, t, THREADS);
+    const int head = columns_before<T>(g ? g : z, V);
+    const unsigned whole = (V - head) / N * N;
+    const int odd = t < head ? t : t + (int)whole;
+    z += head;
+    if (g) g += head;
+    Vec<T> x[IT];
+    float xl[1] = {-INFINITY};
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         const unsigned i = (it * THREADS + t) * N;
-        if (i < whole) Vec<T>::load(z + i, x[it]);
-        else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[it][e] = -INFINITY;
-        }
+        if (i < whole) x[it].load(z + i);
+        else x[it].fill(-INFINITY);
     }
-    if (last < (unsigned)V) xl = to_f32<T>(z[last]);
-    const float zy = to_f32<T>(z[min(y, V - 1)]);
-    float m = xl;
+    if (odd < V) xl[0] = to_f32<T>(z[odd - head]);
+    const float zy = to_f32<T>(z[min(y, V - 1) - head]);
+    Running run;
 #pragma unroll
-    for (int it = 0; it < IT; ++it)
-#pragma unroll
-        for (int e = 0; e < N; ++e) m = fmaxf(m, x[it][e]);
-    m = wave_max(m);
-    const float mm = m == -INFINITY ? 0.f : m;             // exp(-inf - 0) is 0, exp(-inf + inf) would be NaN
-    float s = 0.f;
-#pragma unroll
-    for (int it = 0; it < IT; ++it)
-#pragma unroll
-        for (int e = 0; e < N; ++e) { x[it][e] = __expf(x[it][e] - mm); s += x[it][e]; }
-    xl = __expf(xl - mm);
-    s += xl;
-    float M, S;
-    join_waves<THREADS / 64>(m, wave_sum(s), red, M, S);
-    if (t == 0) finish_row(a, r, y, w, zy, M, S, s_row);
-    if (!g) return;
-    __syncthreads();
-    const float f = s_row[1] * __expf(mm - M);
+    for (int it = 0; it < IT; ++it) {
+        float f[N];
+        x[it].get(f);
+        run.add(f);
+        x[it].forget();
+    }
+    run.add(xl);
+    float M, S, row[2];
+    join_row<THREADS / 64>(run, red, M, S);
+    if (ROWS > 1) {
+        finish_row(a, r, y, w, zy, M, S, row);
+        if (!g) return;
+    } else {
+        if (t == 0) finish_row(a, r, y, w, zy, M, S, s_row);
+        if (!g) return;
+        __syncthreads();
+        row[0] = s_row[0];
+        row[1] = s_row[1];
+    }
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         const unsigned i = (it * THREADS + t) * N;
+        float f[N];
+        x[it].get(f);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[it][e] *= f;
-        if (i < whole) Vec<T>::store(g + i, x[it]);
+        for (int e = 0; e < N; ++e) f[e] = row[1] * __expf(f[e] - M);
+        x[it].set(f);
+        if (i < whole) x[it].store(g + i);
     }
-    if (last < (unsigned)V) g[last] = from_f32<T>(xl * f);
+    if (odd < V) g[odd - head] = from_f32<T>(row[1] * __expf(xl[0] - M));
     // the token's own column, by the thread that has just written it
-    if (y < V && ((unsigned)y >= whole ? (unsigned)y == last : (y / N) % THREADS == t)) g[y] = from_f32<T>(s_row[0]);
+    const unsigned in = y - head;
+    if (y < V && (in < whole ? in / N % THREADS == (unsigned)t : y == odd)) g[(int)in] = from_f32<T>(row[0]);
 }
 
 // Rows that no workgroup's registers hold: read once for the statistics, and again, out of the caches, for the gradient.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, IT = 4;
     __shared__ float red[16][2];
     __shared__ float s_row[2];
     const int r = blockIdx.x, t = threadIdx.x, V = a.vocab;
@@ -151,82 +228,110 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
     T* g = a.grad ? (T*)a.grad + (size_t)r * a.ld_grad : nullptr;
     const int y = a.tokens[r];
     const float w = a.weight ? a.weight[r] : 1.f;
-    if (y < 0 || w == 0.f) return left_out_row<T>(a, r, g, 1024);
+    if (y < 0 || w == 0.f) return left_out_row<T>(a, r, g, t, 1024);
     const float zy = to_f32<T>(z[min(y, V - 1)]);
-    float m = -INFINITY, s = 0.f;
-    for (int i = t * N; i < V; i += 1024 * N) {
-        float x[N];
-        if (i + N <= V) Vec<T>::load(z + i, x);
-        else
-            for (int e = 0; e < N; ++e) x[e] = i + e < V ? to_f32<T>(z[i + e]) : -INFINITY;
-        float mx = m;
+    const int head = columns_before<T>(g ? g : z, V), whole = (V - head) / N * N, odd = t < head ? t : t + whole;
+    const float xl[1] = {odd < V ? to_f32<T>(z[odd]) : -INFINITY};
+    z += head;
+    if (g) g += head;
+    Running run;
+    for (int i0 = 0; i0 < whole; i0 += IT * 1024 * N) {
+        Vec<T> x[IT];
 #pragma unroll
-        for (int e = 0; e < N; ++e) mx = fmaxf(mx, x[e]);
-        const float mm = mx == -INFINITY ? 0.f : mx;
-        s *= m == -INFINITY ? 0.f : __expf(m - mm);
+        for (int it = 0; it < IT; ++it) {
+            const int i = i0 + (it * 1024 + t) * N;
+            if (i < whole) x[it].template load<false>(z + i);
+            else x[it].fill(-INFINITY);
+        }
 #pragma unroll
-        for (int e = 0; e < N; ++e) s += __expf(x[e] - mm);
-        m = mx;
+        for (int it = 0; it < IT; ++it) {
+            float f[N];
+            x[it].get(f);
+            run.add(f);
+        }
     }
-    const float mw = wave_max(m);
-    s = wave_sum(m == -INFINITY ? s : s * __expf(m - mw));       // s holds NaN where a logit did
+    run.add(xl);
     float M, S;
-    join_waves<16>(mw, s, red, M, S);
+    join_row<16>(run, red, M, S);
     if (t == 0) finish_row(a, r, y, w, zy, M, S, s_row);
     if (!g) return;
     __syncthreads();
     const float f = s_row[1];
-    for (int i = t * N; i < V; i += 1024 * N) {
-        float x[N];
-        if (i + N <= V) {
-            Vec<T>::load(z + i, x);
+    for (int i0 = 0; i0 < whole; i0 += IT * 1024 * N) {
+        Vec<T> x[IT];
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = f * __expf(x[e] - M);
-            Vec<T>::store(g + i, x);
-        } else {
-            for (int e = i; e < V; ++e) g[e] = from_f32<T>(f * __expf(to_f32<T>(z[e]) - M));
+        for (int it = 0; it < IT; ++it) {
+            const int i = i0 + (it * 1024 + t) * N;
+            if (i < whole) x[it].load(z + i);
         }
-        if (y >= i && y < min(i + N, V)) g[y] = from_f32<T>(s_row[0]);     // behind the thread's own store to the same place
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int i = i0 + (it * 1024 + t) * N;
+            if (i >= whole) break;
+            float d[N];
+            x[it].get(d);
+#pragma unroll
+            for (int e = 0; e < N; ++e) d[e] = f * __expf(d[e] - M);
+            x[it].set(d);
+            x[it].store(g + i);
+        }
     }
+    if (odd < V) g[odd - head] = from_f32<T>(f * __expf(xl[0] - M));
+    const unsigned in = y - head;
+    if (y < V && (in < (unsigned)whole ? in / N % 1024 == (unsigned)t : y == odd)) g[(int)in] = from_f32<T>(s_row[0]);
 }
 
-// The loss and its parts: every row's terms, summed in a fixed order.
-__global__ __launch_bounds__(256) void k_policy_stats(const float* __restrict__ terms, int rows, float kl_coef, float* __restrict__ stats) {
-    __shared__ double red[3][4];
+// Sums of the rows' terms in a fixed order: `rows` rows a workgroup, to out[3][workgroups], or for one workgroup to stats.
+__global__ __launch_bounds__(1024) void k_policy_stats(const float* __restrict__ terms, int n, int rows, float kl_coef,
+                                                       float* __restrict__ out, float* __restrict__ stats) {
+    __shared__ double red[3][16];
+    const unsigned t = threadIdx.x, lo = blockIdx.x * (unsigned)rows, hi = min((unsigned)n, lo + (unsigned)rows);
     double s[3] = {0., 0., 0.};
-    for (int i = threadIdx.x; i < rows; i += 256)
-        for (int k = 0; k < 3; ++k) s[k] += terms[(size_t)k * rows + i];
+    for (unsigned i = lo + t; i < hi; i += 1024)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) s[k] += terms[(size_t)k * n + i];
+#pragma unroll
     for (int k = 0; k < 3; ++k) {
         for (int o = 32; o > 0; o >>= 1) s[k] += __shfl_xor(s[k], o, kWave);
-        if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = s[k];
+        if ((t & 63) == 0) red[k][t >> 6] = s[k];
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int k = 0; k < 3; ++k) s[k] = (red[k][0] + red[k][1]) + (red[k][2] + red[k][3]);
-        stats[0] = (float)(s[0] + (kl_coef != 0.f ? kl_coef * s[1] : 0.));
-        stats[1] = (float)s[0];
-        stats[2] = (float)s[1];
-        stats[3] = (float)s[2];
-    }
+    if (t >= 3) return;
+    double v = 0.;
+    for (int i = 0; i < 16; ++i) v += red[t][i];
+    if (!stats) { out[t * gridDim.x + blockIdx.x] = (float)v; return; }
+    stats[1 + t] = (float)v;
+    const double kl = __shfl(v, 1, kWave);
+    if (t == 0) stats[0] = (float)(v + (kl_coef != 0.f ? kl_coef * kl : 0.));
 }
 
-size_t policy_scratch_floats(int rows, int vocab) { return (size_t)3 * rows; }
+// More rows than this are summed in two steps.
+constexpr int kStatsRows = 8192;
+static int stats_blocks(int rows) { return rows > kStatsRows ? (rows + kStatsRows - 1) / kStatsRows : 0; }
+size_t policy_scratch_floats(int rows, int vocab) { return 3 * ((size_t)rows + stats_blocks(rows)); }
 
 template <typename T>
 static void policy_rows(hipStream_t st, const PolicyArgs& a) {
     constexpr int N = Vec<T>::N;
-#define RLHF_POLICY(PER_THREAD, THREADS, WAVES) \
-    if (a.vocab <= PER_THREAD * THREADS) return k_policy_row<T, PER_THREAD / N, THREADS, WAVES><<<a.rows, THREADS, 0, st>>>(a)
-    RLHF_POLICY(16, 256, 8);
-    RLHF_POLICY(32, 256, 8);
-    RLHF_POLICY(32, 1024, 8);
-    RLHF_POLICY(64, 1024, 4);
-    RLHF_POLICY(96, 1024, 4);
+#define RLHF_POLICY(IT, THREADS, ROWS, WAVES) \
+    if (a.vocab < (IT * THREADS + 1) * N)     \
+        return k_policy_row<T, IT, THREADS, ROWS, WAVES><<<(a.rows + ROWS - 1) / ROWS, THREADS * ROWS, 0, st>>>(a)
+    RLHF_POLICY(2, 64, 4, 8);
+    RLHF_POLICY(4, 64, 4, 8);
+    RLHF_POLICY(8, 64, 4, 8);
+    RLHF_POLICY(4, 256, 1, 8);
+    RLHF_POLICY(4, 512, 1, 8);
+    RLHF_POLICY(8, 512, 1, 8);
+    RLHF_POLICY(8, 1024, 1, 8);
+    RLHF_POLICY(13, 1024, 1, 4);
+    RLHF_POLICY(16, 1024, 1, 4);
+    RLHF_POLICY(22, 1024, 1, 4);
 #undef RLHF_POLICY
     k_policy_long_row<T><<<a.rows, 1024, 0, st>>>(a);
 }
 
 hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, float* stats) {
+    if (a.vocab > 1 << 30) return hipErrorInvalidValue;          // column numbers are ints
     if (a.rows > 0) {
         if (dtype == kBF16) policy_rows<bf16_t>(st, a);
         else if (dtype == kF16) policy_rows<f16_t>(st, a);
@@ -234,7 +339,10 @@ hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, fl
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    k_policy_stats<<<1, 256, 0, st>>>(a.terms, a.rows, a.kl_coef, stats);
+    const int blocks = stats_blocks(a.rows);
+    float* part = a.terms + (size_t)3 * a.rows;
+    if (blocks > 0) k_policy_stats<<<blocks, 1024, 0, st>>>(a.terms, a.rows, kStatsRows, a.kl_coef, part, nullptr);
+    k_policy_stats<<<1, 1024, 0, st>>>(blocks > 0 ? part : a.terms, blocks > 0 ? blocks : a.rows, INT32_MAX, a.kl_coef, nullptr, stats);
     return hipGetLastError();
 }
 
