@@ -2,6 +2,7 @@
 // One workgroup per row: maximum, sum of exponentials, the row's scalars, then the gradient.
 #include "common.h"
 #include "kernels.h"
+#include "vec.h"
 
 namespace rlhf {
 
@@ -21,64 +22,6 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, int r, float w,
         if (a.kl_coef != 0.f) o.slope -= a.kl_coef * em * w;
     }
     return o;
-}
-
-// Two floats as two packed 16-bit elements, and back; rounded to nearest, a NaN stays one.
-template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t pack2<bf16_t>(float lo, float hi) {
-    typedef __bf16 pair __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, pair{(__bf16)lo, (__bf16)hi});
-}
-template <> __device__ __forceinline__ uint32_t pack2<f16_t>(float lo, float hi) {
-    typedef f16_t pair __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, pair{(f16_t)lo, (f16_t)hi});
-}
-template <typename T> __device__ __forceinline__ float unpack(uint32_t w, int hi);
-template <> __device__ __forceinline__ float unpack<bf16_t>(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xFFFF0000u : w << 16); }
-template <> __device__ __forceinline__ float unpack<f16_t>(uint32_t w, int hi) {
-    typedef f16_t pair __attribute__((ext_vector_type(2)));
-    return (float)__builtin_bit_cast(pair, w)[hi];
-}
-
-// 16 bytes of a row, at any alignment of the element's, packed as they came.
-template <typename T> struct Vec {
-    static constexpr int N = 16 / sizeof(T);
-    uint32_t w[4];
-    // Logits are read once and gradients written once: evict-first in the L2 (8192 x 32000 bf16 201 -> 181 us).
-    typedef uint32_t Quad __attribute__((ext_vector_type(4), aligned(2), may_alias));
-    template <bool ONCE = true> __device__ __forceinline__ void load(const T* p) {
-        const Quad q = ONCE ? __builtin_nontemporal_load((const Quad*)p) : *(const Quad*)p;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = q[k];
-    }
-    __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store(Quad{w[0], w[1], w[2], w[3]}, (Quad*)p); }
-    __device__ __forceinline__ void get(float (&x)[N]) const {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = unpack<T>(w[e / 2], e & 1);
-    }
-    __device__ __forceinline__ void set(const float (&x)[N]) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = pack2<T>(x[2 * k], x[2 * k + 1]);
-    }
-    __device__ __forceinline__ void fill(float v) {
-        float x[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = v;
-        set(x);
-    }
-    // What get() gave before is not kept for get() after it: the packed form is the one that stays in registers.
-    __device__ __forceinline__ void forget() {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[k]));
-    }
-};
-template <> __device__ __forceinline__ void Vec<float>::get(float (&x)[4]) const {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
-}
-template <> __device__ __forceinline__ void Vec<float>::set(const float (&x)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(x[e]);
 }
 
 // Running maximum m and sum s of exp(z - m) of a thread's logits; m = -inf, s = 0 to begin with.
@@ -144,7 +87,7 @@ __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, i
     Vec<T> zero;
     zero.fill(0.f);
     const int head = columns_before<T>(g, a.vocab), whole = (a.vocab - head) / N * N, odd = t < head ? t : t + whole;
-    for (int i = t * N; i < whole; i += threads * N) zero.store(g + head + i);
+    for (int i = t * N; i < whole; i += threads * N) zero.template store<true>(g + head + i);
     if (odd < a.vocab) g[odd] = from_f32<T>(0.f);
 }
 
@@ -175,7 +118,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         const unsigned i = (it * THREADS + t) * N;
-        if (i < whole) x[it].load(z + i);
+        if (i < whole) x[it].template load<true>(z + i);
         else x[it].fill(-INFINITY);
     }
     if (odd < V) xl[0] = to_f32<T>(z[odd - head]);
@@ -209,7 +152,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = row[1] * __expf(f[e] - M);
         x[it].set(f);
-        if (i < whole) x[it].store(g + i);
+        if (i < whole) x[it].template store<true>(g + i);
     }
     if (odd < V) g[odd - head] = from_f32<T>(row[1] * __expf(xl[0] - M));
     // the token's own column, by the thread that has just written it
@@ -262,7 +205,7 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             const int i = i0 + (it * 1024 + t) * N;
-            if (i < whole) x[it].load(z + i);
+            if (i < whole) x[it].template load<true>(z + i);
         }
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
@@ -273,7 +216,7 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
 #pragma unroll
             for (int e = 0; e < N; ++e) d[e] = f * __expf(d[e] - M);
             x[it].set(d);
-            x[it].store(g + i);
+            x[it].template store<true>(g + i);
         }
     }
     if (odd < V) g[odd - head] = from_f32<T>(f * __expf(xl[0] - M));
