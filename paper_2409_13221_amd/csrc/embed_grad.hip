@@ -5,58 +5,78 @@
 
 namespace rlhf {
 
-// How threads lie over rows of d columns: a thread has eight columns of a row at a time, `wide` threads (a power of two, at most
-// 256) lie side by side and 256 / wide rows share a workgroup; grid.y covers what is wider than 2048 columns.
-struct RowShape { int wide_log2, slices; };
-static RowShape row_shape(int d) {
-    const int pieces = (d + 7 + 7) / 8;                  // a row that starts off a boundary has one more
+// How threads lie over rows of d columns.  A thread has H pieces of C columns of a row, 16 bytes of the wider type each; `wide` threads (a
+// power of two, 8 to 256) lie side by side, their first pieces next to each other, then their second ones, so that the lanes of a
+// wave write whole lines; 256 / wide rows share a workgroup, and grid.y covers what is wider than one.
+template <typename A, typename B> struct Shape {
+    static constexpr int C = sizeof(A) == 2 && sizeof(B) == 2 ? 8 : 4, H = 8 / C;
+};
+struct Grid { int wide_log2, slices; };
+static Grid grid_of(int d, int C, int H) {
+    const int pieces = (d + 2 * C - 2) / C;              // a row that starts off a boundary has one more
     int lg = 3;
-    while (lg < 8 && (1 << lg) < pieces) ++lg;
-    return RowShape{lg, (pieces + (1 << lg) - 1) >> lg};
+    while (lg < 8 && (H << lg) < pieces) ++lg;
+    return Grid{lg, (pieces + (H << lg) - 1) / (H << lg)};
 }
 // Row and column numbers are ints.
-static bool sizes_fit(int rows, int d, int vocab, const RowShape& s) { return rows <= 1 << 30 && d <= 1 << 30 && vocab <= 1 << 30 && s.slices <= 65535; }
+static bool sizes_fit(int rows, int d, int vocab) { return rows <= 1 << 30 && vocab <= 1 << 30 && d <= 1 << 22; }
 
-// Columns [lo, hi) of piece c of a row at p: pieces meet where p + column reaches a 16-byte boundary.
-template <typename T> __device__ __forceinline__ void piece_columns(const T* p, int c, int d, int& lo, int& hi) {
-    const int shift = (int)((uintptr_t)p % 16 / sizeof(T));
-    hi = min(d, c * 8 - shift + 8);
-    lo = max(0, c * 8 - shift);
+// Columns [lo[h], hi[h]) of this thread's pieces of a row at p: pieces meet where the row reaches a boundary of C elements.
+template <int C, int H, typename T> __device__ __forceinline__ void my_columns(const T* p, int wide_log2, int d, int (&lo)[H], int (&hi)[H]) {
+    const int shift = (int)((uintptr_t)p % (C * sizeof(T)) / sizeof(T));
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const int piece = ((blockIdx.y * H + h) << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1));
+        hi[h] = min(d, piece * C - shift + C);
+        lo[h] = max(0, piece * C - shift);
+    }
 }
 
-// The same columns of another row: eight at once, or the few there are.
-template <bool ONCE, typename T> __device__ __forceinline__ void load_piece(const T* row, int lo, int hi, float (&x)[8]) {
-    if (hi - lo == 8) return load8_any<ONCE, T>(row + lo, x);
+// Columns [lo, hi) of a row as they lie in memory: C at once, or the few there are.
+template <typename T, int C> struct Piece {
+    Vec<T, C> v;
+    template <bool ONCE> __device__ __forceinline__ void load(const T* row, int lo, int hi) {
+        if (hi - lo == C) return v.template load<ONCE>(row + lo);
+        float x[C];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = lo + e < hi ? to_f32<T>(row[lo + e]) : 0.f;
-}
-template <bool ONCE, typename T> __device__ __forceinline__ void store_piece(T* row, int lo, int hi, const float (&x)[8]) {
-    if (hi - lo == 8) return store8_any<ONCE, T>(row + lo, x);
+        for (int e = 0; e < C; ++e) x[e] = lo + e < hi ? to_f32<T>(row[lo + e]) : 0.f;
+        v.set(x);
+    }
+    template <bool ONCE> __device__ __forceinline__ void store(T* row, int lo, int hi) const {
+        if (hi - lo == C) return v.template store<ONCE>(row + lo);
+        float x[C];
+        v.get(x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (lo + e < hi) row[lo + e] = from_f32<T>(x[e]);
-}
+        for (int e = 0; e < C; ++e)
+            if (lo + e < hi) row[lo + e] = from_f32<T>(x[e]);
+    }
+};
 
 template <typename T, typename O>
 __global__ __launch_bounds__(256) void k_embed_rows(const T* __restrict__ table, size_t ld_table, const int* __restrict__ tokens,
                                                     O* __restrict__ out, size_t ld_out, float scale, int rows, int d, int vocab, int wide_log2) {
+    constexpr int C = Shape<T, O>::C, H = Shape<T, O>::H;
     const int r = blockIdx.x * (256 >> wide_log2) + (threadIdx.x >> wide_log2);
     if (r >= rows) return;
     const int v = tokens[r];
+    const bool known = (unsigned)v < (unsigned)vocab;
     O* o = out + (size_t)r * ld_out;
-    int lo, hi;
-    piece_columns(o, (blockIdx.y << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1)), d, lo, hi);
-    if (lo >= hi) return;
-    float x[8];
-    if ((unsigned)v < (unsigned)vocab) {
-        load_piece<false>(table + (size_t)v * ld_table, lo, hi, x);
+    int lo[H], hi[H];
+    my_columns<C, H>(o, wide_log2, d, lo, hi);
+    Piece<T, C> in[H];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= scale;
-    } else {
+    for (int h = 0; h < H; ++h)
+        if (known) in[h].template load<false>(table + (size_t)v * ld_table, lo[h], hi[h]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = v < 0 ? 0.f : NAN;
+    for (int h = 0; h < H; ++h) {
+        float x[C];
+        in[h].v.get(x);
+#pragma unroll
+        for (int e = 0; e < C; ++e) x[e] = known ? x[e] * scale : v < 0 ? 0.f : NAN;
+        Piece<O, C> res;
+        res.v.set(x);
+        res.template store<false>(o, lo[h], hi[h]);
     }
-    store_piece<false>(o, lo, hi, x);
 }
 
 // ---- gradient: rows grouped by token, then every token's rows summed in ascending order.
@@ -71,7 +91,9 @@ static Buckets buckets_of(int vocab) {
     while (((int64_t)vocab + (1ll << lg) - 1) >> lg > kMaxSubs) ++lg;
     return Buckets{lg, (int)(((int64_t)vocab + (1ll << lg) - 1) >> lg)};
 }
-struct Run { int start, count; };       // a token's rows: order[start .. start + count)
+// A place of the grouped order: which row it holds, and the run of its token, the places [start, start + count).
+struct Place { int row, token, start, count; };
+struct Run { int start, count; };
 
 constexpr int kAhead = 8;               // tokens a lane has in flight
 __device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, int (&v)[kAhead]) {
@@ -79,18 +101,18 @@ __device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, i
     for (int j = 0; j < kAhead; ++j) v[j] = i + j * 64 < end ? tokens[i + j * 64] : -1;
 }
 
-__global__ __launch_bounds__(1024) void k_group_tokens(const int* __restrict__ tokens, int n, int vocab, Buckets b, int* __restrict__ order,
-                                                       Run* __restrict__ runs, int* __restrict__ total) {
-    extern __shared__ int next[];       // [16 waves][subs]
+__device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int n, int vocab, const Buckets& b, int mine, Place* __restrict__ places,
+                                             Run* __restrict__ runs, int* __restrict__ total) {
+    extern __shared__ int next[];       // [16 waves][subs] next free place, then [subs] of Run
     __shared__ int s_part[16], s_before[16];
-    const int t = threadIdx.x, w = t >> 6, lane = t & 63, mine = blockIdx.x, mask = (1 << b.log2) - 1;
+    Run* s_run = (Run*)(next + 16 * b.subs);
+    const int t = threadIdx.x, w = t >> 6, lane = t & 63, mask = (1 << b.log2) - 1;
     for (int i = t; i < 16 * b.subs; i += 1024) next[i] = 0;
     __syncthreads();
     const int share = ((n + 1023) >> 10) << 6;                     // rows of a wave
     const int first = min(n, w * share), end = min(n, first + share);
-    int before = 0;
+    int before = 0, v[kAhead];
     for (int i0 = first; i0 < end; i0 += 64 * kAhead) {
-        int v[kAhead];
         load_tokens(tokens, i0 + lane, end, v);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
@@ -117,7 +139,7 @@ __global__ __launch_bounds__(1024) void k_group_tokens(const int* __restrict__ t
     for (int i = 0; i < w; ++i) sum += s_part[i];
     int start = base + sum - count;
     if (t < b.subs) {
-        runs[(size_t)mine * b.subs + t] = Run{start, count};
+        s_run[t] = runs[(size_t)mine * b.subs + t] = Run{start, count};
         for (int i = 0; i < 16; ++i) {
             const int c = next[i * b.subs + t];
             next[i * b.subs + t] = start;
@@ -127,8 +149,7 @@ __global__ __launch_bounds__(1024) void k_group_tokens(const int* __restrict__ t
     if (mine == mask && t == 1023) *total = base + sum;
     __syncthreads();
     for (int i0 = first; i0 < end; i0 += 64 * kAhead) {
-        int v[kAhead];
-        load_tokens(tokens, i0 + lane, end, v);
+        if (share > 64 * kAhead) load_tokens(tokens, i0 + lane, end, v);     // else they are still there
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int sub = v[j] >> b.log2;
@@ -140,100 +161,203 @@ __global__ __launch_bounds__(1024) void k_group_tokens(const int* __restrict__ t
                 int at = 0;
                 if (lane == leader) at = atomicAdd(&next[w * b.subs + sub], __popcll(all));
                 at = __shfl(at, leader, kWave);
-                if (same) order[at + __popcll(all & ((1ull << lane) - 1))] = i0 + j * 64 + lane;
+                if (same)
+                    places[at + __popcll(all & ((1ull << lane) - 1))] = Place{i0 + j * 64 + lane, v[j], s_run[sub].start, s_run[sub].count};
                 left = left && !same;
             }
         }
     }
 }
 
-// Rows [p, end) of the order, summed into x in that order; four rows in flight.
-template <typename G>
-__device__ __forceinline__ void sum_rows(const G* __restrict__ dout, size_t ld, const int* __restrict__ order, int p, int end, int lo, int hi,
-                                         float (&x)[8]) {
-    for (; p + 4 <= end; p += 4) {
-        float y[4][8];
+// The grouping, and beside it (workgroups behind the buckets) zeros for the whole table unless sums are added to what it holds: the
+// rows that tokens have are written a second time, but zeros need nothing looked up and go out at the rate of a fill
+// (32000 x 4096 float: 97 us where each row asks first whether a token has it, 76 so, and the grouping hides behind it).
+constexpr int kZeroRows = 8;            // rows of the table a thread clears
+template <typename T>
+__global__ __launch_bounds__(1024) void k_group_and_clear(const int* __restrict__ tokens, int n, int vocab, Buckets b, Place* __restrict__ places,
+                                                          Run* __restrict__ runs, int* __restrict__ total, T* __restrict__ dtable, size_t ld,
+                                                          int d, int wide_log2, int slices) {
+    const int buckets = n > 0 ? 1 << b.log2 : 0;
+    if ((int)blockIdx.x < buckets) return group_tokens(tokens, n, vocab, b, blockIdx.x, places, runs, total);
+    constexpr int C = 16 / sizeof(T);
+    const unsigned block = blockIdx.x - buckets, slice = block % slices, per = 1024 >> wide_log2;
+    const int r0 = (block / slices) * (per * kZeroRows) + (threadIdx.x >> wide_log2), piece = (slice << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1));
+    Piece<T, C> zero;
+    zero.v.fill(0.f);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load_piece<true>(dout + (size_t)order[p + k] * ld, lo, hi, y[k]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += y[k][e];
-    }
-    for (; p < end; ++p) {
-        float y[8];
-        load_piece<true>(dout + (size_t)order[p] * ld, lo, hi, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += y[e];
+    for (int k = 0; k < kZeroRows; ++k) {
+        const int r = r0 + k * per;
+        if (r >= vocab) return;
+        T* o = dtable + (size_t)r * ld;
+        const int shift = (int)((uintptr_t)o % 16 / sizeof(T));
+        zero.template store<true>(o, max(0, piece * C - shift), min(d, piece * C - shift + C));
     }
 }
 
-__device__ __forceinline__ Run run_of(const Run* runs, const Buckets& b, int v) {
-    return runs[(size_t)(v & ((1 << b.log2) - 1)) * b.subs + (v >> b.log2)];
-}
-
-// A frequent token's run is cut into pieces of `chunk` places of the order, summed by workgroups of their own; a run of at most
-// two chunks is not.
-template <typename G>
-__global__ __launch_bounds__(256) void k_run_chunks(const G* __restrict__ dout, size_t ld, const int* __restrict__ tokens,
-                                                    const int* __restrict__ order, const int* __restrict__ total, const Run* __restrict__ runs,
-                                                    Buckets b, float* __restrict__ part, size_t ld_part, int chunk, int d, int wide_log2) {
-    const int k = blockIdx.x * (256 >> wide_log2) + (threadIdx.x >> wide_log2);
-    const int64_t p = (int64_t)k * chunk;
-    if (p + chunk > *total) return;
-    const int v = tokens[order[p]];
-    const Run run = run_of(runs, b, v);
-    if (run.count <= 2 * chunk || p + chunk > (int64_t)run.start + run.count) return;
-    const int lo = ((blockIdx.y << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1))) * 8, hi = min(d, lo + 8);
-    if (lo >= hi) return;
-    float x[8] = {};
-    sum_rows(dout, ld, order, (int)p, (int)p + chunk, lo, hi, x);
-    store_piece<false>(part + (size_t)k * ld_part, lo, hi, x);
-}
-
-// Rows of the table: all of them, or (accumulate) those whose token's first place in the order is the thread's.
-template <typename G, typename T>
-__global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, size_t ld, const int* __restrict__ tokens,
-                                                    const int* __restrict__ order, const int* __restrict__ total, const Run* __restrict__ runs,
-                                                    Buckets b, const float* __restrict__ part, size_t ld_part, int chunk, T* __restrict__ dtable,
-                                                    size_t ld_table, float scale, int accumulate, int n, int d, int vocab, int wide_log2) {
-    const int i = blockIdx.x * (256 >> wide_log2) + (threadIdx.x >> wide_log2);
-    int v = i;
-    if (accumulate) {
-        if (i >= *total) return;
-        v = tokens[order[i]];
-    }
-    if (v >= vocab) return;
-    const Run run = n > 0 ? run_of(runs, b, v) : Run{0, 0};
-    if (accumulate && run.start != i) return;
-    T* o = dtable + (size_t)v * ld_table;
-    int lo, hi;
-    piece_columns(o, (blockIdx.y << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1)), d, lo, hi);
-    if (lo >= hi) return;
-    float x[8] = {};
-    const int end = run.start + run.count;
-    if (run.count <= 2 * chunk) {
-        sum_rows(dout, ld, order, run.start, end, lo, hi, x);
-    } else {                                            // the rows before the first whole chunk, the chunks, the rest
-        const int c0 = (run.start + chunk - 1) / chunk, c1 = end / chunk;
-        sum_rows(dout, ld, order, run.start, c0 * chunk, lo, hi, x);
-        for (int c = c0; c < c1; ++c) {
-            float y[8];
-            load_piece<false>(part + (size_t)c * ld_part, lo, hi, y);
+// x += rows index(0) .. index(count - 1) of m in that order, FLIGHT rows in flight, as they lie in memory.  The indices come a group
+// of lanes at a time, so that no row waits for its own: `width` lanes (a power of two) of a wave share the rows, and all of
+// them have to be here, those without columns (lo >= hi) too.
+template <int FLIGHT, int C, int H, typename G, typename Index>
+__device__ __forceinline__ void sum_rows(const G* __restrict__ m, size_t ld, int count, int width, Index index, const int (&lo)[H], const int (&hi)[H],
+                                         float (&x)[H][C]) {
+    const int lane = threadIdx.x & 63, mine = lane & (width - 1), base = lane - mine;
+    for (int p0 = 0; p0 < count; p0 += width) {
+        const int many = min(width, count - p0), r = index(p0 + min(mine, many - 1));
+        for (int p = 0; p < many; p += FLIGHT) {
+            Piece<G, C> y[FLIGHT][H];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += y[e];
+            for (int k = 0; k < FLIGHT; ++k) {
+                const int row = __shfl(r, base + min(p + k, many - 1), kWave);
+                if (p + k < many)
+#pragma unroll
+                    for (int h = 0; h < H; ++h) y[k][h].template load<true>(m + (size_t)row * ld, lo[h], hi[h]);
+            }
+#pragma unroll
+            for (int k = 0; k < FLIGHT; ++k)
+                if (p + k < many)
+#pragma unroll
+                    for (int h = 0; h < H; ++h) {
+                        float f[C];
+                        y[k][h].v.get(f);
+#pragma unroll
+                        for (int e = 0; e < C; ++e) x[h][e] += f[e];
+                    }
         }
-        sum_rows(dout, ld, order, c1 * chunk, end, lo, hi, x);
     }
+}
+
+// The order is cut into chunks.  A run of more places than a chunk has is long: workgroups of their own sum what each chunk holds of
+// it (of at most two long runs: one that began before the chunk, one that begins in it), and k_long_runs joins the sums.
+constexpr int kFlight = 8;
+constexpr int kJoinWaves = 16, kJoinBuckets = 4;
+struct Chunks {
+    float* part;            // [chunks][2][ld]
+    size_t ld;
+    int size, count;        // count: 0 where no run can be long
+};
+
+struct GradArgs {
+    const Place* places;    // [*total]
+    const int* total;
+    const Run* runs;
+    Buckets b;
+    Chunks c;
+    size_t ld_dout, ld_table;
+    float scale;
+    int d, wide_log2;
+};
+
+template <int C, int H, typename G>
+__device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const GradArgs& a, int k) {
+    const int total = *a.total, from = k * a.c.size, to = min(total, from + a.c.size);
+    if (from >= to) return;
+    int lo[H], hi[H];
+    my_columns<C, H>((const G*)nullptr, a.wide_log2, a.d, lo, hi);
+    const Place ends[2] = {a.places[from], a.places[to - 1]};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= scale;
-    if (accumulate) {
-        float y[8];
-        load_piece<false>(o, lo, hi, y);
+    for (int s = 0; s < 2; ++s) {
+        const Place& run = ends[s];
+        if (run.count <= a.c.size || s != (run.start > from)) continue;       // slot 1: it begins behind the chunk's first place
+        const int p = max(from, run.start), end = min(to, run.start + run.count);
+        float x[H][C] = {};
+        sum_rows<kFlight, C, H>(dout, a.ld_dout, end - p, min(64, 1 << a.wide_log2), [&](int i) { return a.places[p + i].row; }, lo, hi, x);
+        float* part = a.c.part + ((size_t)k * 2 + s) * a.c.ld;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += y[e];
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int e = 0; e < C; e += 4) {
+                Piece<float, 4> o;
+                o.v.set({x[h][e], x[h][e + 1], x[h][e + 2], x[h][e + 3]});
+                if (lo[h] + e < hi[h]) o.template store<false>(part, lo[h] + e, min(hi[h], lo[h] + e + 4));
+            }
     }
-    store_piece<false>(o, lo, hi, x);
+}
+
+// Everything but the joining of long runs.  Workgroups in front: chunks of long runs.  The others: the places of the order, of which
+// those where a run begins have something to do.
+template <typename G, typename T, bool ACCUMULATE>
+__global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, T* __restrict__ dtable, GradArgs a) {
+    constexpr int C = Shape<G, T>::C, H = Shape<G, T>::H;
+    const int per = 256 >> a.wide_log2, chunk_groups = (a.c.count + per - 1) / per;
+    int i = threadIdx.x >> a.wide_log2;
+    if ((int)blockIdx.x < chunk_groups) {
+        i += blockIdx.x * per;
+        if (i < a.c.count) sum_chunk<C, H>(dout, a, i);
+        return;
+    }
+    i += (blockIdx.x - chunk_groups) * per;
+    if (i >= *a.total) return;
+    const Place run = a.places[i];
+    if (run.start != i || (a.c.count > 0 && run.count > a.c.size)) return;
+    T* o = dtable + (size_t)run.token * a.ld_table;
+    int lo[H], hi[H];
+    my_columns<C, H>(o, a.wide_log2, a.d, lo, hi);
+    Piece<T, C> old[H];
+    if (ACCUMULATE)
+#pragma unroll
+        for (int h = 0; h < H; ++h) old[h].template load<false>(o, lo[h], hi[h]);
+    float x[H][C] = {};
+    sum_rows<kFlight, C, H>(dout, a.ld_dout, run.count, min(64, 1 << a.wide_log2), [&](int j) { return a.places[i + j].row; }, lo, hi, x);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        float f[C];
+        if (ACCUMULATE) old[h].v.get(f);
+#pragma unroll
+        for (int e = 0; e < C; ++e) x[h][e] = ACCUMULATE ? f[e] + a.scale * x[h][e] : a.scale * x[h][e];
+        old[h].v.set(x[h]);
+        old[h].template store<false>(o, lo[h], hi[h]);
+    }
+}
+
+// Joins the chunks of long runs.  A workgroup looks through the runs of kJoinBuckets buckets, far apart like frequent tokens are
+// near, and has 256 columns of the long ones; each wave takes every 16th chunk, and the waves meet in LDS.
+template <typename T, bool ACCUMULATE>
+__global__ __launch_bounds__(64 * kJoinWaves) void k_long_runs(T* __restrict__ dtable, GradArgs a) {
+    __shared__ float part[kJoinWaves - 1][4][64];
+    __shared__ int s_token[kJoinBuckets * kMaxSubs], s_n;
+    __shared__ Run s_run[kJoinBuckets * kMaxSubs];
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int lo[1] = {(int)(blockIdx.y * 64 + lane) * 4}, hi[1] = {min(a.d, lo[0] + 4)};
+    const int apart = (1 << a.b.log2) / kJoinBuckets;
+    if (threadIdx.x == 0) s_n = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kJoinBuckets * a.b.subs; i += 64 * kJoinWaves) {
+        const int k = i / a.b.subs, sub = i - k * a.b.subs, bucket = blockIdx.x + k * apart;
+        const Run run = a.runs[(size_t)bucket * a.b.subs + sub];
+        if (run.count <= a.c.size) continue;
+        const int at = atomicAdd(&s_n, 1);
+        s_token[at] = sub << a.b.log2 | bucket;
+        s_run[at] = run;
+    }
+    __syncthreads();
+    for (int j = 0; j < s_n; ++j) {                  // in any order: each is a row of its own
+        const Run run = s_run[j];
+        const int first = run.start / a.c.size, chunks = (run.start + run.count - 1) / a.c.size - first + 1, slot = run.start > first * a.c.size;
+        float x[1][4] = {};
+        sum_rows<kFlight, 4, 1>(a.c.part, a.c.ld, (chunks - w + kJoinWaves - 1) / kJoinWaves, 64,
+                                [&](int i) { const int c = w + kJoinWaves * i; return (first + c) * 2 + (c == 0 ? slot : 0); }, lo, hi, x);
+        if (w > 0)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[w - 1][e][lane] = x[0][e];
+        __syncthreads();
+        if (w == 0) {
+            for (int i = 0; i < min(chunks, kJoinWaves) - 1; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[0][e] += part[i][e][lane];
+            T* o = dtable + (size_t)s_token[j] * a.ld_table;
+            Piece<T, 4> res;
+            float f[4] = {};
+            if (ACCUMULATE) {
+                res.template load<false>(o, lo[0], hi[0]);
+                res.v.get(f);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] += a.scale * x[0][e];
+            res.v.set(f);
+            res.template store<false>(o, lo[0], hi[0]);
+        }
+        __syncthreads();
+    }
 }
 
 #define RLHF_TYPES2(A, B, CALL)                                                        \
@@ -247,68 +371,89 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
     else if (B == kF16) { using Y = f16_t; CALL; }                                     \
     else { using Y = float; CALL; }
 
+template <typename T, typename O>
+static void embed_rows(hipStream_t st, const T* table, size_t ld_table, const int* tokens, float scale, O* out, size_t ld_out, int rows, int d,
+                       int vocab) {
+    const Grid g = grid_of(d, Shape<T, O>::C, Shape<T, O>::H);
+    const int per = 256 >> g.wide_log2;
+    k_embed_rows<T, O><<<dim3((rows + per - 1) / per, g.slices), 256, 0, st>>>(table, ld_table, tokens, out, ld_out, scale, rows, d, vocab,
+                                                                              g.wide_log2);
+}
+
 hipError_t launch_embed_rows(hipStream_t st, int tdt, int odt, const void* table, size_t ld_table, const int* tokens, float scale,
                              void* out, size_t ld_out, int rows, int d, int vocab) {
     if (rows <= 0) return hipSuccess;
-    const RowShape s = row_shape(d);
-    if (!sizes_fit(rows, d, vocab, s)) return hipErrorInvalidValue;
-    const int per = 256 >> s.wide_log2;
-    const dim3 grid((rows + per - 1) / per, s.slices);
-    RLHF_TYPES2(tdt, odt, (k_embed_rows<X, Y><<<grid, 256, 0, st>>>((const X*)table, ld_table, tokens, (Y*)out, ld_out, scale, rows, d, vocab,
-                                                                    s.wide_log2)));
+    if (!sizes_fit(rows, d, vocab)) return hipErrorInvalidValue;
+    RLHF_TYPES2(tdt, odt, (embed_rows(st, (const X*)table, ld_table, tokens, scale, (Y*)out, ld_out, rows, d, vocab)));
     return hipGetLastError();
 }
 
-// Places of the order a chunk has: a long run is then about as many chunks as a chunk has rows.
-static int run_chunk(int n) {
-    int c = 64;
-    while ((int64_t)c * c < n / 2) c *= 2;
+// Places of the order a chunk has: summing a chunk and joining the chunks of the longest run then take about as long.
+static int chunk_size(int n) {
+    int c = 32;
+    while ((int64_t)c * c * 64 < n) c *= 2;
     return c;
 }
-struct GradScratch { size_t runs, order, total, part, bytes; };
+struct GradScratch { size_t runs, places, total, part, bytes; };
 static GradScratch grad_scratch(int rows, int d, int vocab) {
     const auto up = [](size_t x) { return (x + 15) / 16 * 16; };
     const Buckets b = buckets_of(vocab);
-    const int chunk = run_chunk(rows);
+    const int size = chunk_size(rows);
     GradScratch s;
     s.runs = 0;
-    s.order = up(((size_t)b.subs << b.log2) * sizeof(Run));
-    s.total = s.order + up((size_t)rows * sizeof(int));
+    s.places = up(((size_t)b.subs << b.log2) * sizeof(Run));
+    s.total = s.places + (size_t)rows * sizeof(Place);
     s.part = s.total + 16;
-    s.bytes = s.part + (rows > 2 * chunk ? (size_t)(rows / chunk) * up((size_t)d * sizeof(float)) : 0);
+    s.bytes = s.part + (rows > size ? (size_t)((rows + size - 1) / size) * 2 * up((size_t)d * sizeof(float)) : 0);
     return s;
 }
 size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return grad_scratch(rows, d, vocab).bytes; }
 
+template <typename G, typename T, bool ACCUMULATE>
+static hipError_t table_grad(hipStream_t st, const G* dout, T* dtable, GradArgs a, int rows) {
+    const Grid g = grid_of(a.d, Shape<G, T>::C, Shape<G, T>::H);
+    a.wide_log2 = g.wide_log2;
+    const int per = 256 >> g.wide_log2;
+    k_table_grad<G, T, ACCUMULATE><<<dim3((a.c.count + per - 1) / per + (rows + per - 1) / per, g.slices), 256, 0, st>>>(dout, dtable, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.c.count == 0) return e;
+    k_long_runs<T, ACCUMULATE><<<dim3((1 << a.b.log2) / kJoinBuckets, (a.d + 255) / 256), 64 * kJoinWaves, 0, st>>>(dtable, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t group_and_clear(hipStream_t st, const int* tokens, int rows, int vocab, const Buckets& b, Place* places, Run* runs, int* total, T* dtable,
+                                  size_t ld, int d, bool clear) {
+    Grid g = grid_of(d, 16 / sizeof(T), 1);
+    const int64_t per = (int64_t)(1024 >> g.wide_log2) * kZeroRows;
+    const int64_t blocks = (rows > 0 ? 1 << b.log2 : 0) + (clear ? (vocab + per - 1) / per * g.slices : 0);
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    k_group_and_clear<T><<<(unsigned)blocks, 1024, b.subs * (16 * sizeof(int) + sizeof(Run)), st>>>(tokens, rows, vocab, b, places, runs, total, dtable,
+                                                                                                   ld, d, g.wide_log2, g.slices);
+    return hipGetLastError();
+}
+
 hipError_t launch_embed_grad(hipStream_t st, int gdt, int tdt, const void* dout, size_t ld_dout, const int* tokens, float scale,
                              bool accumulate, void* dtable, size_t ld_table, void* scratch, int rows, int d, int vocab) {
     if (accumulate && rows <= 0) return hipSuccess;
-    const RowShape s = row_shape(d);
-    if (!sizes_fit(rows, d, vocab, s)) return hipErrorInvalidValue;
-    const int per = 256 >> s.wide_log2, chunk = run_chunk(rows);
+    if (!sizes_fit(rows, d, vocab)) return hipErrorInvalidValue;
     const GradScratch g = grad_scratch(rows, d, vocab);
-    const Buckets b = buckets_of(vocab);
-    Run* runs = (Run*)((char*)scratch + g.runs);
-    int* order = (int*)((char*)scratch + g.order);
+    Place* places = (Place*)((char*)scratch + g.places);
     int* total = (int*)((char*)scratch + g.total);
-    float* part = (float*)((char*)scratch + g.part);
-    const size_t ld_part = ((size_t)d + 3) / 4 * 4;
-    hipError_t e = hipSuccess;
-    if (rows > 0) {
-        k_group_tokens<<<1 << b.log2, 1024, 16 * b.subs * sizeof(int), st>>>(tokens, rows, vocab, b, order, runs, total);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        if (rows > 2 * chunk) {
-            const dim3 grid((rows / chunk + per - 1) / per, s.slices);
-            if (gdt == kBF16) k_run_chunks<bf16_t><<<grid, 256, 0, st>>>((const bf16_t*)dout, ld_dout, tokens, order, total, runs, b, part, ld_part, chunk, d, s.wide_log2);
-            else if (gdt == kF16) k_run_chunks<f16_t><<<grid, 256, 0, st>>>((const f16_t*)dout, ld_dout, tokens, order, total, runs, b, part, ld_part, chunk, d, s.wide_log2);
-            else k_run_chunks<float><<<grid, 256, 0, st>>>((const float*)dout, ld_dout, tokens, order, total, runs, b, part, ld_part, chunk, d, s.wide_log2);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-    }
-    const dim3 grid(((accumulate ? rows : vocab) + per - 1) / per, s.slices);
-    RLHF_TYPES2(gdt, tdt, (k_table_grad<X, Y><<<grid, 256, 0, st>>>((const X*)dout, ld_dout, tokens, order, total, runs, b, part, ld_part, chunk,
-                                                                    (Y*)dtable, ld_table, scale, accumulate, rows, d, vocab, s.wide_log2)));
-    return hipGetLastError();
+    Run* runs = (Run*)((char*)scratch + g.runs);
+    GradArgs a;
+    a.places = places; a.total = total; a.runs = runs;
+    a.b = buckets_of(vocab);
+    a.c = Chunks{(float*)((char*)scratch + g.part), ((size_t)d + 3) / 4 * 4, chunk_size(rows), 0};
+    if (rows > a.c.size) a.c.count = (rows + a.c.size - 1) / a.c.size;
+    a.ld_dout = ld_dout; a.ld_table = ld_table; a.scale = scale; a.d = d;
+    hipError_t e = tdt == kBF16  ? group_and_clear(st, tokens, rows, vocab, a.b, places, runs, total, (bf16_t*)dtable, ld_table, d, !accumulate)
+                   : tdt == kF16 ? group_and_clear(st, tokens, rows, vocab, a.b, places, runs, total, (f16_t*)dtable, ld_table, d, !accumulate)
+                                 : group_and_clear(st, tokens, rows, vocab, a.b, places, runs, total, (float*)dtable, ld_table, d, !accumulate);
+    if (e != hipSuccess || rows <= 0) return e;
+    RLHF_TYPES2(gdt, tdt, (e = accumulate ? table_grad<X, Y, true>(st, (const X*)dout, (Y*)dtable, a, rows)
+                                          : table_grad<X, Y, false>(st, (const X*)dout, (Y*)dtable, a, rows)));
+    return e;
 }
 
 }  // namespace rlhf

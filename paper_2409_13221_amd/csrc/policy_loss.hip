@@ -83,7 +83,7 @@ __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, i
     if (t < 3) a.terms[(size_t)t * a.rows + r] = 0.f;
     if (t == 0) a.lp[r] = 0.f;
     if (!g) return;
-    constexpr int N = Vec<T>::N;
+    constexpr int N = 16 / sizeof(T);
     Vec<T> zero;
     zero.fill(0.f);
     const int head = columns_before<T>(g, a.vocab), whole = (a.vocab - head) / N * N, odd = t < head ? t : t + whole;
@@ -98,7 +98,7 @@ __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, i
 template <typename T, int IT, int THREADS, int ROWS, int WAVES_PER_SIMD>
 __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(PolicyArgs a) {
     static_assert(ROWS == 1 || THREADS == kWave, "rows of more than a wave meet at barriers");
-    constexpr int N = Vec<T>::N;
+    constexpr int N = 16 / sizeof(T);
     __shared__ float red[THREADS / 64][2];
     __shared__ float s_row[2];
     const int r = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / THREADS : 0), t = threadIdx.x % THREADS, V = a.vocab;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
 // Rows that no workgroup's registers hold: read once for the statistics, and again, out of the caches, for the gradient.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
-    constexpr int N = Vec<T>::N, IT = 4;
+    constexpr int N = 16 / sizeof(T), IT = 4;
     __shared__ float red[16][2];
     __shared__ float s_row[2];
     const int r = blockIdx.x, t = threadIdx.x, V = a.vocab;
@@ -255,7 +255,7 @@ size_t policy_scratch_floats(int rows, int vocab) { return 3 * ((size_t)rows + s
 
 template <typename T>
 static void policy_rows(hipStream_t st, const PolicyArgs& a) {
-    constexpr int N = Vec<T>::N;
+    constexpr int N = 16 / sizeof(T);
 #define RLHF_POLICY(IT, THREADS, ROWS, WAVES) \
     if (a.vocab < (IT * THREADS + 1) * N)     \
         return k_policy_row<T, IT, THREADS, ROWS, WAVES><<<(a.rows + ROWS - 1) / ROWS, THREADS * ROWS, 0, st>>>(a)

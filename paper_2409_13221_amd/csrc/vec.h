@@ -1,4 +1,4 @@
-// 16 bytes of a row at a time, at any alignment of its elements.
+// A few elements of a row at a time, at any alignment.
 #pragma once
 #include "common.h"
 
@@ -21,29 +21,43 @@ template <> __device__ __forceinline__ float unpack<f16_t>(uint32_t w, int hi) {
     return (float)__builtin_bit_cast(pair, w)[hi];
 }
 
-// 16 bytes of a row, at any alignment of the element's, packed as they came.
-template <typename T> struct Vec {
-    static constexpr int N = 16 / sizeof(T);
-    uint32_t w[4];
-    typedef uint32_t Quad __attribute__((ext_vector_type(4), aligned(2), may_alias));
-    // ONCE: what nobody reads again soon, evict-first in the L2 (policy loss of 8192 x 32000 bf16 201 -> 181 us).
+// N elements of a row, 8 or 16 bytes, at any alignment of the element's, packed as they came.
+template <typename T, int N = 16 / sizeof(T)> struct Vec {
+    static constexpr int WORDS = N * sizeof(T) / 4;
+    static_assert(N % 2 == 0 && (WORDS == 2 || WORDS == 4), "8 or 16 bytes");
+    uint32_t w[WORDS];
+    typedef uint32_t Words __attribute__((ext_vector_type(WORDS), aligned(2), may_alias));
+    // ONCE: what nobody reads again soon, evict-first in the L2 (policy loss of 8192 x 32000 bf16 201 -> 181 us).  A store of
+    // that kind has to fill its lines together with its neighbours (lanes 32 bytes apart: 80 -> 230 us for 524 MB).
     template <bool ONCE> __device__ __forceinline__ void load(const T* p) {
-        const Quad q = ONCE ? __builtin_nontemporal_load((const Quad*)p) : *(const Quad*)p;
+        const Words q = ONCE ? __builtin_nontemporal_load((const Words*)p) : *(const Words*)p;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = q[k];
+        for (int k = 0; k < WORDS; ++k) w[k] = q[k];
     }
     template <bool ONCE> __device__ __forceinline__ void store(T* p) const {
-        const Quad q{w[0], w[1], w[2], w[3]};
-        if (ONCE) __builtin_nontemporal_store(q, (Quad*)p);
-        else *(Quad*)p = q;
+        Words q;
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) q[k] = w[k];
+        if (ONCE) __builtin_nontemporal_store(q, (Words*)p);
+        else *(Words*)p = q;
     }
     __device__ __forceinline__ void get(float (&x)[N]) const {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = unpack<T>(w[e / 2], e & 1);
+            for (int e = 0; e < N; ++e) x[e] = __uint_as_float(w[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = unpack<T>(w[e / 2], e & 1);
+        }
     }
     __device__ __forceinline__ void set(const float (&x)[N]) {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = pack2<T>(x[2 * k], x[2 * k + 1]);
+            for (int e = 0; e < N; ++e) w[e] = __float_as_uint(x[e]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) w[k] = pack2<T>(x[2 * k], x[2 * k + 1]);
+        }
     }
     __device__ __forceinline__ void fill(float v) {
         float x[N];
@@ -54,43 +68,8 @@ template <typename T> struct Vec {
     // What get() gave before is not kept for get() after it: the packed form is the one that stays in registers.
     __device__ __forceinline__ void forget() {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[k]));
+        for (int k = 0; k < WORDS; ++k) asm volatile("" : "+v"(w[k]));
     }
 };
-template <> __device__ __forceinline__ void Vec<float>::get(float (&x)[4]) const {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
-}
-template <> __device__ __forceinline__ void Vec<float>::set(const float (&x)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(x[e]);
-}
-
-// Eight elements at p, at any alignment, as floats.
-template <bool ONCE, typename T> __device__ __forceinline__ void load8_any(const T* p, float (&x)[8]) {
-    constexpr int N = Vec<T>::N;
-    Vec<T> v[8 / N];
-#pragma unroll
-    for (int k = 0; k < 8 / N; ++k) v[k].template load<ONCE>(p + k * N);
-#pragma unroll
-    for (int k = 0; k < 8 / N; ++k) {
-        float y[N];
-        v[k].get(y);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[k * N + e] = y[e];
-    }
-}
-template <bool ONCE, typename T> __device__ __forceinline__ void store8_any(T* p, const float (&x)[8]) {
-    constexpr int N = Vec<T>::N;
-#pragma unroll
-    for (int k = 0; k < 8 / N; ++k) {
-        float y[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[k * N + e];
-        Vec<T> v;
-        v.set(y);
-        v.template store<ONCE>(p + k * N);
-    }
-}
 
 }  // namespace rlhf
