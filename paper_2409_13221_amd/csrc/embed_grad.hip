@@ -101,6 +101,16 @@ __device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, i
     for (int j = 0; j < kAhead; ++j) v[j] = i + j * 64 < end ? tokens[i + j * 64] : -1;
 }
 
+// use(token, whether it is this lane's, the lanes that have it) for each token among those of the lanes with `has`.
+template <typename Use> __device__ __forceinline__ void each_token(bool has, int token, Use use) {
+    for (uint64_t m = __ballot(has); m; m = __ballot(has)) {
+        const int t = __builtin_amdgcn_readlane(token, __ffsll((unsigned long long)m) - 1);
+        const bool same = has && token == t;
+        use(t, same, __ballot(same));
+        has = has && !same;
+    }
+}
+
 __device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int n, int vocab, const Buckets& b, int mine, Place* __restrict__ places,
                                              Run* __restrict__ runs, int* __restrict__ total) {
     extern __shared__ int next[];       // [16 waves][subs] next free place, then [subs] of Run
@@ -116,10 +126,12 @@ __device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int
         load_tokens(tokens, i0 + lane, end, v);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if ((unsigned)v[j] >= (unsigned)vocab) continue;
+            const bool valid = (unsigned)v[j] < (unsigned)vocab;
             const int k = v[j] & mask;
-            if (k < mine) ++before;
-            if (k == mine) atomicAdd(&next[w * b.subs + (v[j] >> b.log2)], 1);
+            if (valid && k < mine) ++before;
+            each_token(valid && k == mine, v[j], [&](int token, bool, uint64_t rows) {
+                if (lane == 0) atomicAdd(&next[w * b.subs + (token >> b.log2)], __popcll(rows));
+            });
         }
     }
     for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, kWave);
@@ -148,24 +160,21 @@ __device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int
     }
     if (mine == mask && t == 1023) *total = base + sum;
     __syncthreads();
+    int last = -1, at = 0;                                         // a token in a row of rows: its place is at hand
     for (int i0 = first; i0 < end; i0 += 64 * kAhead) {
         if (share > 64 * kAhead) load_tokens(tokens, i0 + lane, end, v);     // else they are still there
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int sub = v[j] >> b.log2;
-            bool left = (unsigned)v[j] < (unsigned)vocab && (v[j] & mask) == mine;
-            for (uint64_t m = __ballot(left); m; m = __ballot(left)) {     // one token of the 64 rows at a time
-                const int leader = __ffsll((unsigned long long)m) - 1;
-                const bool same = left && sub == __shfl(sub, leader, kWave);
-                const uint64_t all = __ballot(same);
-                int at = 0;
-                if (lane == leader) at = atomicAdd(&next[w * b.subs + sub], __popcll(all));
-                at = __shfl(at, leader, kWave);
-                if (same)
-                    places[at + __popcll(all & ((1ull << lane) - 1))] = Place{i0 + j * 64 + lane, v[j], s_run[sub].start, s_run[sub].count};
-                left = left && !same;
-            }
-        }
+        for (int j = 0; j < kAhead; ++j)
+            each_token((unsigned)v[j] < (unsigned)vocab && (v[j] & mask) == mine, v[j], [&](int token, bool same, uint64_t rows) {
+                const int sub = token >> b.log2;
+                if (token != last) {
+                    if (last >= 0 && lane == 0) next[w * b.subs + (last >> b.log2)] = at;
+                    at = next[w * b.subs + sub];
+                    last = token;
+                }
+                if (same) places[at + __popcll(rows & ((1ull << lane) - 1))] = Place{i0 + j * 64 + lane, token, s_run[sub].start, s_run[sub].count};
+                at += __popcll(rows);
+            });
     }
 }
 
@@ -229,7 +238,6 @@ __device__ __forceinline__ void sum_rows(const G* __restrict__ m, size_t ld, int
 // The order is cut into chunks.  A run of more places than a chunk has is long: workgroups of their own sum what each chunk holds of
 // it (of at most two long runs: one that began before the chunk, one that begins in it), and k_long_runs joins the sums.
 constexpr int kFlight = 8;
-constexpr int kJoinWaves = 16, kJoinBuckets = 4;
 struct Chunks {
     float* part;            // [chunks][2][ld]
     size_t ld;
@@ -310,18 +318,20 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
 }
 
 // Joins the chunks of long runs.  A workgroup looks through the runs of kJoinBuckets buckets, far apart like frequent tokens are
-// near, and has 256 columns of the long ones; each wave takes every 16th chunk, and the waves meet in LDS.
-template <typename T, bool ACCUMULATE>
-__global__ __launch_bounds__(64 * kJoinWaves) void k_long_runs(T* __restrict__ dtable, GradArgs a) {
-    __shared__ float part[kJoinWaves - 1][4][64];
+// near, and has 4 * LANES columns of the long ones; LANES lanes take every (1024 / LANES)-th chunk, and all meet in LDS.  What bounds
+// it is how fast one compute unit reads (about 30 GB/s from memory): narrow columns where there are few.
+constexpr int kJoinBuckets = 4;
+template <typename T, bool ACCUMULATE, int LANES>
+__global__ __launch_bounds__(1024) void k_long_runs(T* __restrict__ dtable, GradArgs a) {
+    constexpr int WORKERS = 1024 / LANES;
+    __shared__ float part[4][1024];
     __shared__ int s_token[kJoinBuckets * kMaxSubs], s_n;
     __shared__ Run s_run[kJoinBuckets * kMaxSubs];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int lo[1] = {(int)(blockIdx.y * 64 + lane) * 4}, hi[1] = {min(a.d, lo[0] + 4)};
+    const int t = threadIdx.x, w = t / LANES, lo[1] = {(int)(blockIdx.y * LANES + t % LANES) * 4}, hi[1] = {min(a.d, lo[0] + 4)};
     const int apart = (1 << a.b.log2) / kJoinBuckets;
-    if (threadIdx.x == 0) s_n = 0;
+    if (t == 0) s_n = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < kJoinBuckets * a.b.subs; i += 64 * kJoinWaves) {
+    for (int i = t; i < kJoinBuckets * a.b.subs; i += 1024) {
         const int k = i / a.b.subs, sub = i - k * a.b.subs, bucket = blockIdx.x + k * apart;
         const Run run = a.runs[(size_t)bucket * a.b.subs + sub];
         if (run.count <= a.c.size) continue;
@@ -334,16 +344,15 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_long_runs(T* __restrict__ d
         const Run run = s_run[j];
         const int first = run.start / a.c.size, chunks = (run.start + run.count - 1) / a.c.size - first + 1, slot = run.start > first * a.c.size;
         float x[1][4] = {};
-        sum_rows<kFlight, 4, 1>(a.c.part, a.c.ld, (chunks - w + kJoinWaves - 1) / kJoinWaves, 64,
-                                [&](int i) { const int c = w + kJoinWaves * i; return (first + c) * 2 + (c == 0 ? slot : 0); }, lo, hi, x);
-        if (w > 0)
+        sum_rows<kFlight, 4, 1>(a.c.part, a.c.ld, max(0, (chunks - w + WORKERS - 1) / WORKERS), LANES,
+                                [&](int i) { const int c = w + WORKERS * i; return (first + c) * 2 + (c == 0 ? slot : 0); }, lo, hi, x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[w - 1][e][lane] = x[0][e];
+        for (int e = 0; e < 4; ++e) part[e][t] = x[0][e];
         __syncthreads();
-        if (w == 0) {
-            for (int i = 0; i < min(chunks, kJoinWaves) - 1; ++i)
+        if (t < LANES) {
+            for (int i = 1; i < min(chunks, WORKERS); ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[0][e] += part[i][e][lane];
+                for (int e = 0; e < 4; ++e) x[0][e] += part[e][i * LANES + t];
             T* o = dtable + (size_t)s_token[j] * a.ld_table;
             Piece<T, 4> res;
             float f[4] = {};
@@ -417,7 +426,9 @@ static hipError_t table_grad(hipStream_t st, const G* dout, T* dtable, GradArgs 
     k_table_grad<G, T, ACCUMULATE><<<dim3((a.c.count + per - 1) / per + (rows + per - 1) / per, g.slices), 256, 0, st>>>(dout, dtable, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.c.count == 0) return e;
-    k_long_runs<T, ACCUMULATE><<<dim3((1 << a.b.log2) / kJoinBuckets, (a.d + 255) / 256), 64 * kJoinWaves, 0, st>>>(dtable, a);
+    const int groups = (1 << a.b.log2) / kJoinBuckets;
+    if (a.d <= 1024) k_long_runs<T, ACCUMULATE, 16><<<dim3(groups, (a.d + 63) / 64), 1024, 0, st>>>(dtable, a);
+    else k_long_runs<T, ACCUMULATE, 64><<<dim3(groups, (a.d + 255) / 256), 1024, 0, st>>>(dtable, a);
     return hipGetLastError();
 }
 
