@@ -12,8 +12,10 @@ template <typename A, typename B> struct Shape {
     static constexpr int C = sizeof(A) == 2 && sizeof(B) == 2 ? 8 : 4, H = 8 / C;
 };
 struct Grid { int wide_log2, slices; };
-static Grid grid_of(int d, int C, int H) {
-    const int pieces = (d + 2 * C - 2) / C;              // a row that starts off a boundary has one more
+// p, ld: what the pieces go by (my_columns); rows that start off a boundary may have a piece more.
+template <typename T> static Grid grid_of(const T* p, size_t ld, int d, int C, int H) {
+    const bool on_boundary = (uintptr_t)p % (C * sizeof(T)) == 0 && ld % C == 0;
+    const int pieces = (d + (on_boundary ? C - 1 : 2 * C - 2)) / C;
     int lg = 3;
     while (lg < 8 && (H << lg) < pieces) ++lg;
     return Grid{lg, (pieces + (H << lg) - 1) / (H << lg)};
@@ -22,11 +24,11 @@ static Grid grid_of(int d, int C, int H) {
 static bool sizes_fit(int rows, int d, int vocab) { return rows <= 1 << 30 && vocab <= 1 << 30 && d <= 1 << 22; }
 
 // Columns [lo[h], hi[h]) of this thread's pieces of a row at p: pieces meet where the row reaches a boundary of C elements.
-template <int C, int H, typename T> __device__ __forceinline__ void my_columns(const T* p, int wide_log2, int d, int (&lo)[H], int (&hi)[H]) {
+template <int C, int H, typename T> __device__ __forceinline__ void my_columns(const T* p, int slice, int wide_log2, int d, int (&lo)[H], int (&hi)[H]) {
     const int shift = (int)((uintptr_t)p % (C * sizeof(T)) / sizeof(T));
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-        const int piece = ((blockIdx.y * H + h) << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1));
+        const int piece = ((slice * H + h) << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1));
         hi[h] = min(d, piece * C - shift + C);
         lo[h] = max(0, piece * C - shift);
     }
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(256) void k_embed_rows(const T* __restrict__ table,
     const bool known = (unsigned)v < (unsigned)vocab;
     O* o = out + (size_t)r * ld_out;
     int lo[H], hi[H];
-    my_columns<C, H>(o, wide_log2, d, lo, hi);
+    my_columns<C, H>(o, blockIdx.y, wide_log2, d, lo, hi);
     Piece<T, C> in[H];
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -178,29 +180,49 @@ __device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int
     }
 }
 
-// The grouping, and beside it (workgroups behind the buckets) zeros for the whole table unless sums are added to what it holds: the
-// rows that tokens have are written a second time, but zeros need nothing looked up and go out at the rate of a fill
-// (32000 x 4096 float: 97 us where each row asks first whether a token has it, 76 so, and the grouping hides behind it).
-constexpr int kZeroRows = 8;            // rows of the table a thread clears
-template <typename T>
-__global__ __launch_bounds__(1024) void k_group_and_clear(const int* __restrict__ tokens, int n, int vocab, Buckets b, Place* __restrict__ places,
-                                                          Run* __restrict__ runs, int* __restrict__ total, T* __restrict__ dtable, size_t ld,
-                                                          int d, int wide_log2, int slices) {
-    const int buckets = n > 0 ? 1 << b.log2 : 0;
-    if ((int)blockIdx.x < buckets) return group_tokens(tokens, n, vocab, b, blockIdx.x, places, runs, total);
+__device__ __forceinline__ Run run_of(const Run* runs, const Buckets& b, int v) {
+    return runs[(size_t)(v & ((1 << b.log2) - 1)) * b.subs + (v >> b.log2)];
+}
+
+// Zeros for the rows [from, to) of the table that have no token (runs == NULL: for all), by workgroups of THREADS threads,
+// kZeroRows rows a thread.  `wide` threads lie over a row, a slice of it if it is wider.
+struct Clear { int from, to, wide_log2, slices; };
+constexpr int kZeroRows = 8;
+template <int THREADS, typename T>
+__device__ __forceinline__ void clear_rows(T* __restrict__ dtable, size_t ld, int d, const Clear& c, unsigned block, const Run* runs, const Buckets& b) {
     constexpr int C = 16 / sizeof(T);
-    const unsigned block = blockIdx.x - buckets, slice = block % slices, per = 1024 >> wide_log2;
-    const int r0 = (block / slices) * (per * kZeroRows) + (threadIdx.x >> wide_log2), piece = (slice << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1));
+    const int per = THREADS >> c.wide_log2, slice = block % c.slices;
+    const int r0 = c.from + (int)(block / c.slices) * (per * kZeroRows) + (threadIdx.x >> c.wide_log2);
+    const int piece = (slice << c.wide_log2) + (threadIdx.x & ((1 << c.wide_log2) - 1));
+    bool empty[kZeroRows];
+#pragma unroll
+    for (int k = 0; k < kZeroRows; ++k) {
+        const int r = r0 + k * per;
+        empty[k] = r < c.to && (!runs || run_of(runs, b, r).count == 0);
+    }
     Piece<T, C> zero;
     zero.v.fill(0.f);
 #pragma unroll
     for (int k = 0; k < kZeroRows; ++k) {
-        const int r = r0 + k * per;
-        if (r >= vocab) return;
-        T* o = dtable + (size_t)r * ld;
+        if (!empty[k]) continue;
+        T* o = dtable + (size_t)(r0 + k * per) * ld;
         const int shift = (int)((uintptr_t)o % 16 / sizeof(T));
         zero.template store<true>(o, max(0, piece * C - shift), min(d, piece * C - shift + C));
     }
+}
+template <int THREADS> static int64_t clear_blocks(const Clear& c) {
+    const int64_t per = (int64_t)(THREADS >> c.wide_log2) * kZeroRows;
+    return (c.to - c.from + per - 1) / per * c.slices;
+}
+
+// The grouping, and beside it (workgroups behind the buckets) zeros for as many rows of the table as go out in its time.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_group_and_clear(const int* __restrict__ tokens, int n, int vocab, Buckets b, Place* __restrict__ places,
+                                                          Run* __restrict__ runs, int* __restrict__ total, T* __restrict__ dtable, size_t ld,
+                                                          int d, Clear clear) {
+    const int buckets = n > 0 ? 1 << b.log2 : 0;
+    if ((int)blockIdx.x < buckets) group_tokens(tokens, n, vocab, b, blockIdx.x, places, runs, total);
+    else clear_rows<1024>(dtable, ld, d, clear, blockIdx.x - buckets, nullptr, b);
 }
 
 // x += rows index(0) .. index(count - 1) of m in that order, FLIGHT rows in flight, as they lie in memory.  The indices come a group
@@ -252,15 +274,17 @@ struct GradArgs {
     Chunks c;
     size_t ld_dout, ld_table;
     float scale;
-    int d, wide_log2;
+    int d, wide_log2, slices;
+    Clear clear;
+    unsigned table_blocks, clear_blocks;
 };
 
 template <int C, int H, typename G>
-__device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const GradArgs& a, int k) {
+__device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const GradArgs& a, int k, int slice) {
     const int total = *a.total, from = k * a.c.size, to = min(total, from + a.c.size);
     if (from >= to) return;
     int lo[H], hi[H];
-    my_columns<C, H>((const G*)nullptr, a.wide_log2, a.d, lo, hi);
+    my_columns<C, H>((const G*)nullptr, slice, a.wide_log2, a.d, lo, hi);
     const Place ends[2] = {a.places[from], a.places[to - 1]};
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -281,25 +305,41 @@ __device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const Grad
     }
 }
 
-// Everything but the joining of long runs.  Workgroups in front: chunks of long runs.  The others: the places of the order, of which
-// those where a run begins have something to do.
+// Everything but the joining of long runs.  Workgroups in front: chunks of long runs.  Behind them: the places of the order, of
+// which those where a run begins have something to do.  In between, evenly: zeros for rows without a token, which keep the
+// memory busy while the sums wait for their rows (8192 rows of 4096 into 32000 x 4096 float: one after the other
+// 90 + 36 us).
 template <typename G, typename T, bool ACCUMULATE>
 __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, T* __restrict__ dtable, GradArgs a) {
     constexpr int C = Shape<G, T>::C, H = Shape<G, T>::H;
-    const int per = 256 >> a.wide_log2, chunk_groups = (a.c.count + per - 1) / per;
-    int i = threadIdx.x >> a.wide_log2;
-    if ((int)blockIdx.x < chunk_groups) {
-        i += blockIdx.x * per;
-        if (i < a.c.count) sum_chunk<C, H>(dout, a, i);
+    unsigned block = blockIdx.x;
+    if (!ACCUMULATE && a.clear_blocks > 0) {
+        const uint64_t all = a.table_blocks + a.clear_blocks;
+        const unsigned before = (unsigned)((uint64_t)block * a.clear_blocks / all);
+        if ((uint64_t)(block + 1ull) * a.clear_blocks / all > before) return clear_rows<256>(dtable, a.ld_table, a.d, a.clear, before, a.runs, a.b);
+        block -= before;
+    }
+    const int per = 256 >> a.wide_log2, chunk_groups = (a.c.count + per - 1) / per, slice = block % a.slices;
+    int place = block / a.slices;
+    if (place < chunk_groups) {
+        const int k = place * per + (threadIdx.x >> a.wide_log2);
+        if (k < a.c.count) sum_chunk<C, H>(dout, a, k, slice);
         return;
     }
-    i += (blockIdx.x - chunk_groups) * per;
+    place -= chunk_groups;
+    // workgroups go to the 8 XCDs in turn: the eight of a turn are exchanged by the other digits of their number, else runs of
+    // 8 places would all begin on one XCD
+    unsigned digits = place >> 3;
+    digits ^= digits >> 3;
+    digits ^= digits >> 6;
+    digits ^= digits >> 12;
+    const int i = (place ^ (digits & 7)) * per + (threadIdx.x >> a.wide_log2);
     if (i >= *a.total) return;
     const Place run = a.places[i];
     if (run.start != i || (a.c.count > 0 && run.count > a.c.size)) return;
     T* o = dtable + (size_t)run.token * a.ld_table;
     int lo[H], hi[H];
-    my_columns<C, H>(o, a.wide_log2, a.d, lo, hi);
+    my_columns<C, H>(o, slice, a.wide_log2, a.d, lo, hi);
     Piece<T, C> old[H];
     if (ACCUMULATE)
 #pragma unroll
@@ -383,7 +423,7 @@ __global__ __launch_bounds__(1024) void k_long_runs(T* __restrict__ dtable, Grad
 template <typename T, typename O>
 static void embed_rows(hipStream_t st, const T* table, size_t ld_table, const int* tokens, float scale, O* out, size_t ld_out, int rows, int d,
                        int vocab) {
-    const Grid g = grid_of(d, Shape<T, O>::C, Shape<T, O>::H);
+    const Grid g = grid_of(out, ld_out, d, Shape<T, O>::C, Shape<T, O>::H);
     const int per = 256 >> g.wide_log2;
     k_embed_rows<T, O><<<dim3((rows + per - 1) / per, g.slices), 256, 0, st>>>(table, ld_table, tokens, out, ld_out, scale, rows, d, vocab,
                                                                               g.wide_log2);
@@ -418,29 +458,38 @@ static GradScratch grad_scratch(int rows, int d, int vocab) {
 }
 size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return grad_scratch(rows, d, vocab).bytes; }
 
+// Rows of the table that are cleared beside the grouping: 32 MB, what goes out in the 6 us that 8192 tokens take.
+static int rows_cleared_first(size_t row_bytes, int rows, int vocab) {
+    const size_t first = (32u << 20) / row_bytes;
+    return rows > 0 && first < (size_t)vocab ? (int)first : vocab;
+}
+
 template <typename G, typename T, bool ACCUMULATE>
-static hipError_t table_grad(hipStream_t st, const G* dout, T* dtable, GradArgs a, int rows) {
-    const Grid g = grid_of(a.d, Shape<G, T>::C, Shape<G, T>::H);
+static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int* tokens, GradArgs a, Place* places, Run* runs, int* total, int rows,
+                             int vocab) {
+    const Grid z = grid_of(dtable, a.ld_table, a.d, 16 / sizeof(T), 1);
+    const int first = ACCUMULATE ? 0 : rows_cleared_first(a.d * sizeof(T), rows, vocab);
+    const Clear beside{0, first, z.wide_log2, z.slices};
+    a.clear = Clear{first, ACCUMULATE ? first : vocab, z.wide_log2, z.slices};
+    const int64_t group_blocks = (rows > 0 ? 1 << a.b.log2 : 0) + clear_blocks<1024>(beside), clear = clear_blocks<256>(a.clear);
+    const Grid g = grid_of(dtable, a.ld_table, a.d, Shape<G, T>::C, Shape<G, T>::H);
     a.wide_log2 = g.wide_log2;
-    const int per = 256 >> g.wide_log2;
-    k_table_grad<G, T, ACCUMULATE><<<dim3((a.c.count + per - 1) / per + (rows + per - 1) / per, g.slices), 256, 0, st>>>(dout, dtable, a);
-    const hipError_t e = hipGetLastError();
+    a.slices = g.slices;
+    const int64_t per = 256 >> g.wide_log2;
+    const int64_t table = ((a.c.count + per - 1) / per + (rows + 8 * per - 1) / (8 * per) * 8) * g.slices;
+    if (group_blocks > INT32_MAX || table + clear > INT32_MAX) return hipErrorInvalidValue;
+    k_group_and_clear<T><<<(unsigned)group_blocks, 1024, a.b.subs * (16 * sizeof(int) + sizeof(Run)), st>>>(tokens, rows, vocab, a.b, places, runs, total,
+                                                                                                         dtable, a.ld_table, a.d, beside);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || rows <= 0) return e;
+    a.table_blocks = (unsigned)table;
+    a.clear_blocks = (unsigned)clear;
+    k_table_grad<G, T, ACCUMULATE><<<(unsigned)(table + clear), 256, 0, st>>>(dout, dtable, a);
+    e = hipGetLastError();
     if (e != hipSuccess || a.c.count == 0) return e;
     const int groups = (1 << a.b.log2) / kJoinBuckets;
     if (a.d <= 1024) k_long_runs<T, ACCUMULATE, 16><<<dim3(groups, (a.d + 63) / 64), 1024, 0, st>>>(dtable, a);
     else k_long_runs<T, ACCUMULATE, 64><<<dim3(groups, (a.d + 255) / 256), 1024, 0, st>>>(dtable, a);
-    return hipGetLastError();
-}
-
-template <typename T>
-static hipError_t group_and_clear(hipStream_t st, const int* tokens, int rows, int vocab, const Buckets& b, Place* places, Run* runs, int* total, T* dtable,
-                                  size_t ld, int d, bool clear) {
-    Grid g = grid_of(d, 16 / sizeof(T), 1);
-    const int64_t per = (int64_t)(1024 >> g.wide_log2) * kZeroRows;
-    const int64_t blocks = (rows > 0 ? 1 << b.log2 : 0) + (clear ? (vocab + per - 1) / per * g.slices : 0);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    k_group_and_clear<T><<<(unsigned)blocks, 1024, b.subs * (16 * sizeof(int) + sizeof(Run)), st>>>(tokens, rows, vocab, b, places, runs, total, dtable,
-                                                                                                   ld, d, g.wide_log2, g.slices);
     return hipGetLastError();
 }
 
@@ -458,12 +507,9 @@ hipError_t launch_embed_grad(hipStream_t st, int gdt, int tdt, const void* dout,
     a.c = Chunks{(float*)((char*)scratch + g.part), ((size_t)d + 3) / 4 * 4, chunk_size(rows), 0};
     if (rows > a.c.size) a.c.count = (rows + a.c.size - 1) / a.c.size;
     a.ld_dout = ld_dout; a.ld_table = ld_table; a.scale = scale; a.d = d;
-    hipError_t e = tdt == kBF16  ? group_and_clear(st, tokens, rows, vocab, a.b, places, runs, total, (bf16_t*)dtable, ld_table, d, !accumulate)
-                   : tdt == kF16 ? group_and_clear(st, tokens, rows, vocab, a.b, places, runs, total, (f16_t*)dtable, ld_table, d, !accumulate)
-                                 : group_and_clear(st, tokens, rows, vocab, a.b, places, runs, total, (float*)dtable, ld_table, d, !accumulate);
-    if (e != hipSuccess || rows <= 0) return e;
-    RLHF_TYPES2(gdt, tdt, (e = accumulate ? table_grad<X, Y, true>(st, (const X*)dout, (Y*)dtable, a, rows)
-                                          : table_grad<X, Y, false>(st, (const X*)dout, (Y*)dtable, a, rows)));
+    hipError_t e = hipSuccess;
+    RLHF_TYPES2(gdt, tdt, (e = accumulate ? embed_grad<X, Y, true>(st, (const X*)dout, (Y*)dtable, tokens, a, places, runs, total, rows, vocab)
+                                          : embed_grad<X, Y, false>(st, (const X*)dout, (Y*)dtable, tokens, a, places, runs, total, rows, vocab)));
     return e;
 }
 
