@@ -82,26 +82,20 @@ __global__ __launch_bounds__(256) void k_embed_rows(const T* __restrict__ table,
 }
 
 // ---- gradient: rows grouped by token, then every token's rows summed in ascending order.
-// The vocabulary is dealt to 2^log2 buckets by its low bits (frequent tokens have neighbouring ids), `subs` tokens each.  A
-// workgroup per bucket looks through all tokens twice: the first time it counts its own, per wave (a wave has one contiguous share
-// of the rows), and how many lie in earlier buckets; the second time each wave puts its rows behind those of the waves before
-// it.  No sort passes over memory, no atomics whose order could show: 256 workgroups read the tokens out of the L2.
-struct Buckets { int log2, subs; };
+// The vocabulary is dealt to 2^log2 buckets by its low bits (frequent tokens have neighbouring ids), `subs` tokens each, and the
+// rows to `parts` parts, 256 workgroups together unless the vocabulary is large.  A workgroup for each bucket and part reads all tokens out of the L2, counts its bucket's and how many lie
+// in earlier buckets, and puts the rows of its part into their places: a row's place follows from the counts alone, so there
+// are no sort passes over memory and no atomics whose order could show.
+struct Buckets { int log2, subs, parts; };
 constexpr int kMaxSubs = 512;
 static Buckets buckets_of(int vocab) {
-    int lg = 8;
+    int lg = 6;
     while (((int64_t)vocab + (1ll << lg) - 1) >> lg > kMaxSubs) ++lg;
-    return Buckets{lg, (int)(((int64_t)vocab + (1ll << lg) - 1) >> lg)};
+    return Buckets{lg, (int)(((int64_t)vocab + (1ll << lg) - 1) >> lg), lg < 8 ? 256 >> lg : 1};
 }
 // A place of the grouped order: which row it holds, and the run of its token, the places [start, start + count).
 struct Place { int row, token, start, count; };
 struct Run { int start, count; };
-
-constexpr int kAhead = 8;               // tokens a lane has in flight
-__device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, int (&v)[kAhead]) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) v[j] = i + j * 64 < end ? tokens[i + j * 64] : -1;
-}
 
 // use(token, whether it is this lane's, the lanes that have it) for each token among those of the lanes with `has`.
 template <typename Use> __device__ __forceinline__ void each_token(bool has, int token, Use use) {
@@ -113,36 +107,55 @@ template <typename Use> __device__ __forceinline__ void each_token(bool has, int
     }
 }
 
-__device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int n, int vocab, const Buckets& b, int mine, Place* __restrict__ places,
-                                             Run* __restrict__ runs, int* __restrict__ total) {
-    extern __shared__ int next[];       // [16 waves][subs] next free place, then [subs] of Run
+constexpr int kAhead = 8;               // tokens a lane has in flight
+__device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, int (&v)[kAhead]) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) v[j] = i + j * 64 < end ? tokens[i + j * 64] : -1;
+}
+
+// LDS, in ints: next [16][subs], the count and later the next place of a wave's rows of a token; run [subs], start and count;
+// early [subs], rows of earlier parts.
+static size_t group_lds_bytes(const Buckets& b) { return (size_t)b.subs * 19 * sizeof(int); }
+
+__device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int n, int vocab, const Buckets& b, int mine, int part,
+                                             Place* __restrict__ places, Run* __restrict__ runs, int* __restrict__ total) {
+    extern __shared__ int next[];
     __shared__ int s_part[16], s_before[16];
     Run* s_run = (Run*)(next + 16 * b.subs);
+    int* early = next + 18 * b.subs;
     const int t = threadIdx.x, w = t >> 6, lane = t & 63, mask = (1 << b.log2) - 1;
-    for (int i = t; i < 16 * b.subs; i += 1024) next[i] = 0;
+    for (int i = t; i < 19 * b.subs; i += 1024) next[i] = 0;
     __syncthreads();
-    const int share = ((n + 1023) >> 10) << 6;                     // rows of a wave
-    const int first = min(n, w * share), end = min(n, first + share);
-    int before = 0, v[kAhead];
+    // rows of a part, a sixteenth of it for each wave to place; and of a wave to count
+    const int piece = (n + b.parts * 1024 - 1) / (b.parts * 1024) * 64, from = min(n, part * 16 * piece), to = min(n, from + 16 * piece);
+    const int share = ((n + 1023) >> 10) << 6, first = min(n, w * share), end = min(n, first + share);
+    int before = 0;
     for (int i0 = first; i0 < end; i0 += 64 * kAhead) {
+        int v[kAhead];
         load_tokens(tokens, i0 + lane, end, v);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const bool valid = (unsigned)v[j] < (unsigned)vocab;
-            const int k = v[j] & mask;
-            if (valid && k < mine) ++before;
-            each_token(valid && k == mine, v[j], [&](int token, bool, uint64_t rows) {
-                if (lane == 0) atomicAdd(&next[w * b.subs + (token >> b.log2)], __popcll(rows));
-            });
+            const int key = (unsigned)v[j] < (unsigned)vocab ? v[j] & mask : INT32_MAX;
+            before += key < mine;
+            const uint64_t hits = __ballot(key == mine);
+            if (hits == 0) continue;
+            // 64 rows lie in one wave's piece.  One token's are counted at once (equal addresses are served one by one, and padding
+            // fills waves), the others' lane by lane.
+            const int i = i0 + j * 64, lead = __ffsll((unsigned long long)hits) - 1;
+            int* const also = i < from ? early : i < to ? next + (i - from) / piece * b.subs : nullptr;
+            const bool same = key == mine && v[j] == __builtin_amdgcn_readlane(v[j], lead);
+            const int many = __popcll(__ballot(same)), sub = v[j] >> b.log2;
+            if (key != mine || (same && lane != lead)) continue;
+            atomicAdd(&s_run[sub].count, same ? many : 1);
+            if (also) atomicAdd(&also[sub], same ? many : 1);
         }
     }
     for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, kWave);
     if (lane == 0) s_before[w] = before;
     __syncthreads();
-    int base = 0, count = 0;
+    int base = 0;
     for (int i = 0; i < 16; ++i) base += s_before[i];
-    if (t < b.subs)
-        for (int i = 0; i < 16; ++i) count += next[i * b.subs + t];
+    const int count = t < b.subs ? s_run[t].count : 0;
     int sum = count;                                               // inclusive over the tokens of the bucket
     for (int o = 1; o < 64; o <<= 1) {
         const int x = __shfl_up(sum, o, kWave);
@@ -151,20 +164,24 @@ __device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int
     if (lane == 63) s_part[w] = sum;
     __syncthreads();
     for (int i = 0; i < w; ++i) sum += s_part[i];
-    int start = base + sum - count;
     if (t < b.subs) {
-        s_run[t] = runs[(size_t)mine * b.subs + t] = Run{start, count};
+        int at = base + sum - count;
+        s_run[t].start = at;
+        if (part == 0) runs[(size_t)mine * b.subs + t] = Run{at, count};
+        at += early[t];
         for (int i = 0; i < 16; ++i) {
             const int c = next[i * b.subs + t];
-            next[i * b.subs + t] = start;
-            start += c;
+            next[i * b.subs + t] = at;
+            at += c;
         }
     }
-    if (mine == mask && t == 1023) *total = base + sum;
+    if (mine == mask && part == 0 && t == 1023) *total = base + sum;
     __syncthreads();
+    const int mine0 = min(to, from + w * piece), mine1 = min(to, mine0 + piece);
     int last = -1, at = 0;                                         // a token in a row of rows: its place is at hand
-    for (int i0 = first; i0 < end; i0 += 64 * kAhead) {
-        if (share > 64 * kAhead) load_tokens(tokens, i0 + lane, end, v);     // else they are still there
+    for (int i0 = mine0; i0 < mine1; i0 += 64 * kAhead) {
+        int v[kAhead];
+        load_tokens(tokens, i0 + lane, mine1, v);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
             each_token((unsigned)v[j] < (unsigned)vocab && (v[j] & mask) == mine, v[j], [&](int token, bool same, uint64_t rows) {
@@ -220,9 +237,9 @@ template <typename T>
 __global__ __launch_bounds__(1024) void k_group_and_clear(const int* __restrict__ tokens, int n, int vocab, Buckets b, Place* __restrict__ places,
                                                           Run* __restrict__ runs, int* __restrict__ total, T* __restrict__ dtable, size_t ld,
                                                           int d, Clear clear) {
-    const int buckets = n > 0 ? 1 << b.log2 : 0;
-    if ((int)blockIdx.x < buckets) group_tokens(tokens, n, vocab, b, blockIdx.x, places, runs, total);
-    else clear_rows<1024>(dtable, ld, d, clear, blockIdx.x - buckets, nullptr, b);
+    const int groups = n > 0 ? b.parts << b.log2 : 0;
+    if ((int)blockIdx.x < groups) group_tokens(tokens, n, vocab, b, blockIdx.x / b.parts, blockIdx.x % b.parts, places, runs, total);
+    else clear_rows<1024>(dtable, ld, d, clear, blockIdx.x - groups, nullptr, b);
 }
 
 // x += rows index(0) .. index(count - 1) of m in that order, FLIGHT rows in flight, as they lie in memory.  The indices come a group
@@ -277,6 +294,7 @@ struct GradArgs {
     int d, wide_log2, slices;
     Clear clear;
     unsigned table_blocks, clear_blocks;
+    int window;             // places of the order that share threads
 };
 
 template <int C, int H, typename G>
@@ -305,8 +323,8 @@ __device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const Grad
     }
 }
 
-// Everything but the joining of long runs.  Workgroups in front: chunks of long runs.  Behind them: the places of the order, of
-// which those where a run begins have something to do.  In between, evenly: zeros for rows without a token, which keep the
+// Everything but the joining of long runs.  Workgroups in front: chunks of long runs.  Behind them: a window of places of the order
+// each, and the short runs that begin there.  In between, evenly: zeros for rows without a token, which keep the
 // memory busy while the sums wait for their rows (8192 rows of 4096 into 32000 x 4096 float: one after the other
 // 90 + 36 us).
 template <typename G, typename T, bool ACCUMULATE>
@@ -328,56 +346,98 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
     }
     place -= chunk_groups;
     // workgroups go to the 8 XCDs in turn: the eight of a turn are exchanged by the other digits of their number, else runs of
-    // 8 places would all begin on one XCD
+    // 64 places would all begin on one XCD
     unsigned digits = place >> 3;
     digits ^= digits >> 3;
     digits ^= digits >> 6;
     digits ^= digits >> 12;
-    const int i = (place ^ (digits & 7)) * per + (threadIdx.x >> a.wide_log2);
-    if (i >= *a.total) return;
-    const Place run = a.places[i];
-    if (run.start != i || (a.c.count > 0 && run.count > a.c.size)) return;
-    T* o = dtable + (size_t)run.token * a.ld_table;
+    const int p0 = ((place ^ (digits & 7)) * per + (threadIdx.x >> a.wide_log2)) * a.window;
+    const int total = *a.total;
+    if (p0 >= total) return;
+    // the window's places, one a lane of the group; from the first where a run begins to the end of the last short run that does
+    const int lane = threadIdx.x & 63, width = min(64, 1 << a.wide_log2), mine = lane & (width - 1), base = lane - mine;
+    const Place w = a.places[min(p0 + min(mine, a.window - 1), total - 1)];
+    const uint64_t begins = __ballot(mine < a.window && w.start == p0 + mine) >> base & (~0ull >> (64 - width));
+    if (begins == 0) return;
+    int at = p0 + __ffsll((unsigned long long)begins) - 1;
+    const int last = 63 - __clzll((long long)begins), many = __shfl(w.count, base + last, kWave);
+    const int end = p0 + last + (a.c.count > 0 && many > a.c.size ? 0 : many);
     int lo[H], hi[H];
-    my_columns<C, H>(o, slice, a.wide_log2, a.d, lo, hi);
+    my_columns<C, H>((const T*)nullptr, slice, a.wide_log2, a.d, lo, hi);
+    // rows in the order of their places, kBatch in flight; a run is stored where the next begins
+    constexpr int kBatch = ACCUMULATE ? 4 : 8;
+    float x[H][C];
     Piece<T, C> old[H];
-    if (ACCUMULATE)
+    T* o = nullptr;
+    const auto flush = [&]() {
+        if (!o) return;
 #pragma unroll
-        for (int h = 0; h < H; ++h) old[h].template load<false>(o, lo[h], hi[h]);
-    float x[H][C] = {};
-    sum_rows<kFlight, C, H>(dout, a.ld_dout, run.count, min(64, 1 << a.wide_log2), [&](int j) { return a.places[i + j].row; }, lo, hi, x);
+        for (int h = 0; h < H; ++h) {
+            float f[C];
+            if (ACCUMULATE) old[h].v.get(f);
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-        float f[C];
-        if (ACCUMULATE) old[h].v.get(f);
+            for (int e = 0; e < C; ++e) f[e] = ACCUMULATE ? f[e] + a.scale * x[h][e] : a.scale * x[h][e];
+            Piece<T, C> res;
+            res.v.set(f);
+            res.template store<false>(o, lo[h], hi[h]);
+        }
+    };
+    for (; at < end; at += kBatch) {
+        const Place q = a.places[min(at + min(mine, kBatch - 1), end - 1)];
+        Piece<G, C> row[kBatch][H];
+        Piece<T, C> had[kBatch][H];
+        int token[kBatch];
 #pragma unroll
-        for (int e = 0; e < C; ++e) x[h][e] = ACCUMULATE ? f[e] + a.scale * x[h][e] : a.scale * x[h][e];
-        old[h].v.set(x[h]);
-        old[h].template store<false>(o, lo[h], hi[h]);
+        for (int k = 0; k < kBatch; ++k) {
+            const int r = __shfl(q.row, base + k, kWave), start = __shfl(q.start, base + k, kWave);
+            token[k] = __shfl(q.token, base + k, kWave);
+            if (start != at + k) token[k] = -1;             // the run goes on
+            if (at + k < end)
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    row[k][h].template load<true>(dout + (size_t)r * a.ld_dout, lo[h], hi[h]);
+                    if (ACCUMULATE && token[k] >= 0) had[k][h].template load<false>(dtable + (size_t)token[k] * a.ld_table, lo[h], hi[h]);
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (at + k >= end) break;
+            if (token[k] >= 0) {
+                flush();
+                o = dtable + (size_t)token[k] * a.ld_table;
+            }
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                float f[C];
+                row[k][h].v.get(f);
+                if (ACCUMULATE && token[k] >= 0) old[h] = had[k][h];
+#pragma unroll
+                for (int e = 0; e < C; ++e) x[h][e] = token[k] >= 0 ? f[e] : x[h][e] + f[e];
+            }
+        }
     }
+    flush();
 }
 
-// Joins the chunks of long runs.  A workgroup looks through the runs of kJoinBuckets buckets, far apart like frequent tokens are
-// near, and has 4 * LANES columns of the long ones; LANES lanes take every (1024 / LANES)-th chunk, and all meet in LDS.  What bounds
-// it is how fast one compute unit reads (about 30 GB/s from memory): narrow columns where there are few.
-constexpr int kJoinBuckets = 4;
+// Joins the chunks of long runs.  A workgroup looks through the runs of a bucket and has 4 * LANES columns of the long ones; LANES lanes
+// take every (1024 / LANES)-th chunk, and all meet in LDS.  What bounds it is how fast one compute unit reads (about 30 GB/s
+// from memory): narrow columns where there are few.
 template <typename T, bool ACCUMULATE, int LANES>
 __global__ __launch_bounds__(1024) void k_long_runs(T* __restrict__ dtable, GradArgs a) {
     constexpr int WORKERS = 1024 / LANES;
     __shared__ float part[4][1024];
-    __shared__ int s_token[kJoinBuckets * kMaxSubs], s_n;
-    __shared__ Run s_run[kJoinBuckets * kMaxSubs];
+    __shared__ int s_token[kMaxSubs], s_n;
+    __shared__ Run s_run[kMaxSubs];
     const int t = threadIdx.x, w = t / LANES, lo[1] = {(int)(blockIdx.y * LANES + t % LANES) * 4}, hi[1] = {min(a.d, lo[0] + 4)};
-    const int apart = (1 << a.b.log2) / kJoinBuckets;
     if (t == 0) s_n = 0;
     __syncthreads();
-    for (int i = t; i < kJoinBuckets * a.b.subs; i += 1024) {
-        const int k = i / a.b.subs, sub = i - k * a.b.subs, bucket = blockIdx.x + k * apart;
-        const Run run = a.runs[(size_t)bucket * a.b.subs + sub];
-        if (run.count <= a.c.size) continue;
-        const int at = atomicAdd(&s_n, 1);
-        s_token[at] = sub << a.b.log2 | bucket;
-        s_run[at] = run;
+    if (t < a.b.subs) {
+        const Run run = a.runs[(size_t)blockIdx.x * a.b.subs + t];
+        if (run.count > a.c.size) {
+            const int at = atomicAdd(&s_n, 1);
+            s_token[at] = t << a.b.log2 | blockIdx.x;
+            s_run[at] = run;
+        }
     }
     __syncthreads();
     for (int j = 0; j < s_n; ++j) {                  // in any order: each is a row of its own
@@ -406,6 +466,52 @@ __global__ __launch_bounds__(1024) void k_long_runs(T* __restrict__ dtable, Grad
             res.template store<false>(o, lo[0], hi[0]);
         }
         __syncthreads();
+    }
+}
+
+// Up to kFewRows rows: no grouping ahead.  A thread group a row; that of a token's first row finds the others and sums them.
+constexpr int kFewRows = 256;
+template <typename G, typename T, bool ACCUMULATE>
+__global__ __launch_bounds__(256) void k_few_rows_grad(const G* __restrict__ dout, size_t ld_dout, const int* __restrict__ tokens, T* __restrict__ dtable,
+                                                       size_t ld_table, float scale, int n, int d, int vocab, int wide_log2) {
+    constexpr int C = Shape<G, T>::C, H = Shape<G, T>::H;
+    __shared__ int s_tok[kFewRows];
+    __shared__ uint8_t s_rows[4][8][kFewRows];          // of a wave's groups (8 at most)
+    const int t = threadIdx.x;
+    s_tok[t] = t < n ? tokens[t] : -1;
+    __syncthreads();
+    const int i = blockIdx.x * (256 >> wide_log2) + (t >> wide_log2);
+    const int lane = t & 63, width = min(64, 1 << wide_log2), mine = lane & (width - 1), base = lane - mine;
+    const int v = i < n ? s_tok[i] : -1;
+    if ((unsigned)v >= (unsigned)vocab) return;
+    uint8_t* rows = s_rows[t >> 6][base / width];
+    int count = 0;
+    for (int j0 = 0; j0 < n; j0 += width) {
+        const bool same = j0 + mine < n && s_tok[j0 + mine] == v;
+        const uint64_t all = __ballot(same) >> base & (~0ull >> (64 - width));
+        if (count == 0 && all && j0 + __ffsll((unsigned long long)all) - 1 < i) return;      // an earlier row's
+        if (same) rows[count + __popcll(all & ((1ull << mine) - 1))] = (uint8_t)(j0 + mine);
+        count += __popcll(all);
+    }
+    // the list is the wave's own; its lanes run together, but what one has written another may read only behind this
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    T* o = dtable + (size_t)v * ld_table;
+    int lo[H], hi[H];
+    my_columns<C, H>(o, blockIdx.y, wide_log2, d, lo, hi);
+    Piece<T, C> old[H];
+    if (ACCUMULATE)
+#pragma unroll
+        for (int h = 0; h < H; ++h) old[h].template load<false>(o, lo[h], hi[h]);
+    float x[H][C] = {};
+    sum_rows<kFlight, C, H>(dout, ld_dout, count, width, [&](int j) { return (int)rows[j]; }, lo, hi, x);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        float f[C];
+        if (ACCUMULATE) old[h].v.get(f);
+#pragma unroll
+        for (int e = 0; e < C; ++e) f[e] = ACCUMULATE ? f[e] + scale * x[h][e] : scale * x[h][e];
+        old[h].v.set(f);
+        old[h].template store<false>(o, lo[h], hi[h]);
     }
 }
 
@@ -469,17 +575,35 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
                              int vocab) {
     const Grid z = grid_of(dtable, a.ld_table, a.d, 16 / sizeof(T), 1);
     const int first = ACCUMULATE ? 0 : rows_cleared_first(a.d * sizeof(T), rows, vocab);
+    if (rows > 0 && rows <= kFewRows) {
+        if (!ACCUMULATE) {
+            const Clear whole{0, vocab, z.wide_log2, z.slices};
+            if (clear_blocks<1024>(whole) > INT32_MAX) return hipErrorInvalidValue;
+            k_group_and_clear<T><<<(unsigned)clear_blocks<1024>(whole), 1024, 0, st>>>(tokens, 0, vocab, a.b, places, runs, total, dtable, a.ld_table, a.d,
+                                                                                      whole);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        const Grid g = grid_of(dtable, a.ld_table, a.d, Shape<G, T>::C, Shape<G, T>::H);
+        const int per = 256 >> g.wide_log2;
+        k_few_rows_grad<G, T, ACCUMULATE><<<dim3((rows + per - 1) / per, g.slices), 256, 0, st>>>(dout, a.ld_dout, tokens, dtable, a.ld_table, a.scale, rows,
+                                                                                                a.d, vocab, g.wide_log2);
+        return hipGetLastError();
+    }
     const Clear beside{0, first, z.wide_log2, z.slices};
     a.clear = Clear{first, ACCUMULATE ? first : vocab, z.wide_log2, z.slices};
-    const int64_t group_blocks = (rows > 0 ? 1 << a.b.log2 : 0) + clear_blocks<1024>(beside), clear = clear_blocks<256>(a.clear);
+    const int64_t group_blocks = (rows > 0 ? (int64_t)a.b.parts << a.b.log2 : 0) + clear_blocks<1024>(beside), clear = clear_blocks<256>(a.clear);
     const Grid g = grid_of(dtable, a.ld_table, a.d, Shape<G, T>::C, Shape<G, T>::H);
     a.wide_log2 = g.wide_log2;
     a.slices = g.slices;
     const int64_t per = 256 >> g.wide_log2;
-    const int64_t table = ((a.c.count + per - 1) / per + (rows + 8 * per - 1) / (8 * per) * 8) * g.slices;
+    // up to eight places (a place where no run begins costs little then), fewer where they would not fill the chip
+    a.window = rows >= 8192 ? 8 : rows >= 1024 ? rows / 1024 : 1;
+    const int64_t windows = (rows + a.window * per - 1) / (a.window * per);
+    const int64_t table = ((a.c.count + per - 1) / per + (windows + 7) / 8 * 8) * g.slices;
     if (group_blocks > INT32_MAX || table + clear > INT32_MAX) return hipErrorInvalidValue;
-    k_group_and_clear<T><<<(unsigned)group_blocks, 1024, a.b.subs * (16 * sizeof(int) + sizeof(Run)), st>>>(tokens, rows, vocab, a.b, places, runs, total,
-                                                                                                         dtable, a.ld_table, a.d, beside);
+    k_group_and_clear<T><<<(unsigned)group_blocks, 1024, group_lds_bytes(a.b), st>>>(tokens, rows, vocab, a.b, places, runs, total, dtable, a.ld_table,
+                                                                                    a.d, beside);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || rows <= 0) return e;
     a.table_blocks = (unsigned)table;
@@ -487,7 +611,7 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
     k_table_grad<G, T, ACCUMULATE><<<(unsigned)(table + clear), 256, 0, st>>>(dout, dtable, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.c.count == 0) return e;
-    const int groups = (1 << a.b.log2) / kJoinBuckets;
+    const int groups = 1 << a.b.log2;
     if (a.d <= 1024) k_long_runs<T, ACCUMULATE, 16><<<dim3(groups, (a.d + 63) / 64), 1024, 0, st>>>(dtable, a);
     else k_long_runs<T, ACCUMULATE, 64><<<dim3(groups, (a.d + 255) / 256), 1024, 0, st>>>(dtable, a);
     return hipGetLastError();
