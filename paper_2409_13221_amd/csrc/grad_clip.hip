@@ -1,14 +1,48 @@
-// Global 2-norm of many gradients, and their scaling by it.
+// Global 2-norm of many gradients, and their scaling by it.  Both are a stream over memory; what matters beside is that a model of
+// hundreds of small tensors is not hundreds of launches.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
+#include "vec.h"
 
 namespace rlhf {
 
-constexpr int kNormBlocks = 256;
+// Tensors travel as kernel arguments, kPackTensors to a launch: nothing has to be copied to the device first, and a captured graph
+// holds all it needs.  Each is cut into chunks of vectors of 16 bytes, a workgroup a chunk.
+constexpr int kPackTensors = 64;
+struct PackTensor { const void* src; void* dst; size_t n; int first, dtype; };      // first: the tensor's first chunk
+struct Pack {
+    PackTensor t[kPackTensors];
+    int tensors, chunks, vectors;        // vectors: of a chunk
+};
+
+// Chunk c of the pack: its tensor, and the vectors [from, to) of it.  `head` elements come before the first vector, which begins where p
+// reaches a 16-byte boundary; they and the few behind the last vector go to the tensor's first chunk, a thread each (odd < n).
+struct Work { int i; size_t from, to, odd; int head; };
+template <typename T, bool DST> __device__ __forceinline__ Work work_of(const Pack& pk, int i, int c) {
+    constexpr int N = 16 / sizeof(T);
+    const PackTensor& t = pk.t[i];
+    const uintptr_t p = (uintptr_t)(DST ? t.dst : t.src);
+    const int head = (int)min((size_t)((0 - p) % 16 / sizeof(T)), t.n);
+    const size_t all = (t.n - head) / N, from = (size_t)(c - t.first) * pk.vectors, whole = all * N;
+    Work w{i, from, min(all, from + pk.vectors), t.n, head};
+    if (c == t.first) w.odd = (int)threadIdx.x < head ? threadIdx.x : threadIdx.x + whole;
+    return w;
+}
+__device__ __forceinline__ int tensor_of(const Pack& pk, int c) {
+    int lo = 0, hi = pk.tensors;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (pk.t[mid].first <= c) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
 
 __device__ __forceinline__ double block_sum_double(double v, double* red) {
+#pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     double t = 0.;
@@ -16,64 +50,152 @@ __device__ __forceinline__ double block_sum_double(double v, double* red) {
     return t;
 }
 
+// Squares are summed in double: a float's square fits, whatever the float, and the two instructions an element are hidden behind
+// the loads.
+constexpr int kUnroll = 4;
 template <typename T>
-__global__ __launch_bounds__(256) void k_sum_squares(const T* __restrict__ x, size_t n, double* __restrict__ part) {
-    __shared__ double red[4];
+__device__ __forceinline__ double sum_squares(const Pack& pk, int i, int c) {
+    constexpr int N = 16 / sizeof(T);
+    const Work w = work_of<T, false>(pk, i, c);
+    const T* x = (const T*)pk.t[i].src;
     double s = 0.;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
-        const double v = to_f32<T>(x[i]);
-        s += v * v;
+    if (w.odd < pk.t[i].n) {
+        const double v = to_f32<T>(x[w.odd]);
+        s = v * v;
     }
-    s = block_sum_double(s, red);
-    if (threadIdx.x == 0) part[blockIdx.x] = s;
+    x += w.head;
+    for (size_t k0 = w.from + threadIdx.x; k0 < w.to; k0 += 256 * kUnroll) {
+        Vec<T> v[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (k0 + u * 256 < w.to) v[u].template load<false>(x + (k0 + u * 256) * N);
+            else v[u].fill(0.f);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            float f[N];
+            v[u].get(f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) s += (double)f[e] * (double)f[e];
+        }
+    }
+    return s;
 }
 
-__global__ __launch_bounds__(256) void k_norm_finish(const double* __restrict__ part, int n, float* __restrict__ norm) {
+__global__ __launch_bounds__(256) void k_sum_squares(Pack pk, double* __restrict__ part) {
     __shared__ double red[4];
+    const int c = blockIdx.x, i = tensor_of(pk, c), dt = pk.t[i].dtype;
+    double s = dt == kBF16 ? sum_squares<bf16_t>(pk, i, c) : dt == kF16 ? sum_squares<f16_t>(pk, i, c) : sum_squares<float>(pk, i, c);
+    s = block_sum_double(s, red);
+    if (threadIdx.x == 0) part[c] = s;
+}
+
+__global__ __launch_bounds__(1024) void k_norm_finish(const double* __restrict__ part, int n, float* __restrict__ norm) {
+    __shared__ double red[16];
     double s = 0.;
-    for (int i = threadIdx.x; i < n; i += 256) s += part[i];
+    for (int i = threadIdx.x; i < n; i += 1024) s += part[i];
     s = block_sum_double(s, red);
     if (threadIdx.x == 0) norm[0] = (float)sqrt(s);
 }
 
-__device__ __forceinline__ float clip_factor(float norm, float max_norm) {
-    return norm > max_norm && norm < INFINITY ? max_norm / norm : 1.f;
-}
-
 template <typename T>
-__global__ __launch_bounds__(256) void k_scale(const T* x, T* y, size_t n, const float* __restrict__ norm, float max_norm) {
-    const float f = clip_factor(norm[0], max_norm);
-    if (f == 1.f) {
-        if (x != y) for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) y[i] = x[i];
-        return;
+__device__ __forceinline__ void scale_chunk(const Pack& pk, int i, int c, float f) {
+    constexpr int N = 16 / sizeof(T);
+    const Work w = work_of<T, true>(pk, i, c);
+    const T* x = (const T*)pk.t[i].src;
+    T* y = (T*)pk.t[i].dst;
+    if (w.odd < pk.t[i].n) y[w.odd] = from_f32<T>(f * to_f32<T>(x[w.odd]));
+    x += w.head;
+    y += w.head;
+    for (size_t k0 = w.from + threadIdx.x; k0 < w.to; k0 += 256 * kUnroll) {
+        Vec<T> v[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (k0 + u * 256 < w.to) v[u].template load<true>(x + (k0 + u * 256) * N);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (k0 + u * 256 >= w.to) break;
+            float a[N];
+            v[u].get(a);
+#pragma unroll
+            for (int e = 0; e < N; ++e) a[e] *= f;
+            v[u].set(a);
+            v[u].template store<true>(y + (k0 + u * 256) * N);
+        }
     }
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) y[i] = from_f32<T>(f * to_f32<T>(x[i]));
 }
 
-size_t grad_norm_scratch_doubles(const GradTensor* t, int n) { return (size_t)n * kNormBlocks; }
+// From the last chunk to the first: what the norm read last is still in the memory-side cache.
+__global__ __launch_bounds__(256) void k_clip(Pack pk, const float* __restrict__ norm, float max_norm) {
+    const int c = pk.chunks - 1 - blockIdx.x, i = tensor_of(pk, c), dt = pk.t[i].dtype;
+    const float g = norm[0], f = g > max_norm && g < INFINITY ? max_norm / g : 1.f;
+    if (f == 1.f && pk.t[i].src == pk.t[i].dst) return;
+    if (dt == kBF16) scale_chunk<bf16_t>(pk, i, c, f);
+    else if (dt == kF16) scale_chunk<f16_t>(pk, i, c, f);
+    else scale_chunk<float>(pk, i, c, f);
+}
+
+// Vectors of a chunk: 64 KB, more where that would be over 8192 chunks or so.
+static size_t vectors_of(const GradTensor* t, int n) {
+    size_t bytes = 0;
+    for (int i = 0; i < n; ++i) bytes += t[i].n * (t[i].dtype == kF32 ? 4 : 2);
+    return std::max<size_t>(4096, (bytes / 16 / 8192 + 1023) / 1024 * 1024);
+}
+static size_t chunks_of(const GradTensor& t, size_t vectors) {
+    const size_t all = t.n * (t.dtype == kF32 ? 4 : 2) / 16;
+    return std::max<size_t>(1, (all + vectors - 1) / vectors);
+}
+
+size_t grad_norm_scratch_doubles(const GradTensor* t, int n) {
+    size_t c = 0;
+    for (int i = 0; i < n; ++i) c += chunks_of(t[i], vectors_of(t, n));
+    return c;
+}
+
+// launch(pack, chunks before it) for every pack of the list, from the front or from the back.
+template <typename Launch>
+static hipError_t each_pack(const GradTensor* t, int n, bool backwards, Launch launch) {
+    const size_t vectors = vectors_of(t, n);
+    const int packs = (n + kPackTensors - 1) / kPackTensors;
+    if (vectors > INT32_MAX) return hipErrorInvalidValue;
+    size_t before = 0;
+    for (int k = 0; k < packs; ++k) {
+        const int at = (backwards ? packs - 1 - k : k) * kPackTensors;
+        Pack pk;
+        pk.tensors = std::min(kPackTensors, n - at);
+        pk.vectors = (int)vectors;
+        size_t chunks = 0;
+        for (int i = 0; i < pk.tensors; ++i) {
+            const GradTensor& g = t[at + i];
+            pk.t[i] = PackTensor{g.src, g.dst, g.n, (int)chunks, g.dtype};
+            chunks += chunks_of(g, vectors);
+        }
+        if (chunks > INT32_MAX) return hipErrorInvalidValue;
+        pk.chunks = (int)chunks;
+        const hipError_t e = launch(pk, before);
+        if (e != hipSuccess) return e;
+        before += chunks;
+    }
+    return hipSuccess;
+}
 
 hipError_t launch_grad_norm(hipStream_t st, const GradTensor* t, int n, float* norm, double* scratch) {
-    for (int i = 0; i < n; ++i) {
-        double* p = scratch + (size_t)i * kNormBlocks;
-        if (t[i].dtype == kBF16) k_sum_squares<bf16_t><<<kNormBlocks, 256, 0, st>>>((const bf16_t*)t[i].src, t[i].n, p);
-        else if (t[i].dtype == kF16) k_sum_squares<f16_t><<<kNormBlocks, 256, 0, st>>>((const f16_t*)t[i].src, t[i].n, p);
-        else k_sum_squares<float><<<kNormBlocks, 256, 0, st>>>((const float*)t[i].src, t[i].n, p);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    k_norm_finish<<<1, 256, 0, st>>>(scratch, n * kNormBlocks, norm);
+    size_t all = 0;
+    hipError_t e = each_pack(t, n, false, [&](const Pack& pk, size_t before) {
+        k_sum_squares<<<pk.chunks, 256, 0, st>>>(pk, scratch + before);
+        all = before + pk.chunks;
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    if (all > INT32_MAX) return hipErrorInvalidValue;
+    k_norm_finish<<<1, 1024, 0, st>>>(scratch, (int)all, norm);
     return hipGetLastError();
 }
 
 hipError_t launch_clip_grads(hipStream_t st, const GradTensor* t, int n, const float* norm, float max_norm) {
-    for (int i = 0; i < n; ++i) {
-        if (t[i].dtype == kBF16) k_scale<bf16_t><<<1024, 256, 0, st>>>((const bf16_t*)t[i].src, (bf16_t*)t[i].dst, t[i].n, norm, max_norm);
-        else if (t[i].dtype == kF16) k_scale<f16_t><<<1024, 256, 0, st>>>((const f16_t*)t[i].src, (f16_t*)t[i].dst, t[i].n, norm, max_norm);
-        else k_scale<float><<<1024, 256, 0, st>>>((const float*)t[i].src, (float*)t[i].dst, t[i].n, norm, max_norm);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    return each_pack(t, n, true, [&](const Pack& pk, size_t) {
+        k_clip<<<pk.chunks, 256, 0, st>>>(pk, norm, max_norm);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace rlhf
