@@ -10,8 +10,12 @@ namespace rlhf {
 
 // Tensors travel as kernel arguments, kPackTensors to a launch: nothing has to be copied to the device first, and a captured graph
 // holds all it needs.  Each is cut into chunks of vectors of 16 bytes, a workgroup a chunk.
-constexpr int kPackTensors = 64;
-struct PackTensor { const void* src; void* dst; size_t n; int first, dtype; };      // first: the tensor's first chunk
+constexpr int kPackTensors = 128;
+struct PackTensor {
+    const void* src;
+    void* dst;
+    uint64_t n : 40, first : 22, dtype : 2;        // elements, the tensor's first chunk, type: 24 bytes in all, 3 KB a launch
+};
 struct Pack {
     PackTensor t[kPackTensors];
     int tensors, chunks, vectors;        // vectors: of a chunk
@@ -24,17 +28,17 @@ template <typename T, bool DST> __device__ __forceinline__ Work work_of(const Pa
     constexpr int N = 16 / sizeof(T);
     const PackTensor& t = pk.t[i];
     const uintptr_t p = (uintptr_t)(DST ? t.dst : t.src);
-    const int head = (int)min((size_t)((0 - p) % 16 / sizeof(T)), t.n);
-    const size_t all = (t.n - head) / N, from = (size_t)(c - t.first) * pk.vectors, whole = all * N;
+    const int head = (int)min((size_t)((0 - p) % 16 / sizeof(T)), (size_t)t.n);
+    const size_t all = (t.n - head) / N, from = (size_t)(c - (int)t.first) * pk.vectors, whole = all * N;
     Work w{i, from, min(all, from + pk.vectors), t.n, head};
-    if (c == t.first) w.odd = (int)threadIdx.x < head ? threadIdx.x : threadIdx.x + whole;
+    if (c == (int)t.first) w.odd = (int)threadIdx.x < head ? threadIdx.x : threadIdx.x + whole;
     return w;
 }
 __device__ __forceinline__ int tensor_of(const Pack& pk, int c) {
     int lo = 0, hi = pk.tensors;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (pk.t[mid].first <= c) lo = mid;
+        if ((int)pk.t[mid].first <= c) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -134,11 +138,13 @@ __global__ __launch_bounds__(256) void k_clip(Pack pk, const float* __restrict__
     else scale_chunk<float>(pk, i, c, f);
 }
 
-// Vectors of a chunk: 64 KB, more where that would be over 8192 chunks or so.
+// Vectors of a chunk: 16 KB, one round trip of a workgroup's threads, up to 32 MB; then up to 64 KB; more where that would be over
+// 16384 chunks.
 static size_t vectors_of(const GradTensor* t, int n) {
-    size_t bytes = 0;
-    for (int i = 0; i < n; ++i) bytes += t[i].n * (t[i].dtype == kF32 ? 4 : 2);
-    return std::max<size_t>(4096, (bytes / 16 / 8192 + 1023) / 1024 * 1024);
+    size_t all = 0;
+    for (int i = 0; i < n; ++i) all += t[i].n * (t[i].dtype == kF32 ? 4 : 2) / 16;
+    const auto up = [](size_t x) { return std::max<size_t>(1, (x + 1023) / 1024) * 1024; };
+    return std::max(std::min<size_t>(4096, up(all / 2048)), up(all / 16384));
 }
 static size_t chunks_of(const GradTensor& t, size_t vectors) {
     const size_t all = t.n * (t.dtype == kF32 ? 4 : 2) / 16;
@@ -156,7 +162,7 @@ template <typename Launch>
 static hipError_t each_pack(const GradTensor* t, int n, bool backwards, Launch launch) {
     const size_t vectors = vectors_of(t, n);
     const int packs = (n + kPackTensors - 1) / kPackTensors;
-    if (vectors > INT32_MAX) return hipErrorInvalidValue;
+    if (vectors > 1 << 30) return hipErrorInvalidValue;
     size_t before = 0;
     for (int k = 0; k < packs; ++k) {
         const int at = (backwards ? packs - 1 - k : k) * kPackTensors;
@@ -166,10 +172,10 @@ static hipError_t each_pack(const GradTensor* t, int n, bool backwards, Launch l
         size_t chunks = 0;
         for (int i = 0; i < pk.tensors; ++i) {
             const GradTensor& g = t[at + i];
-            pk.t[i] = PackTensor{g.src, g.dst, g.n, (int)chunks, g.dtype};
+            if (g.n >> 40 || chunks >> 22) return hipErrorInvalidValue;
+            pk.t[i] = PackTensor{g.src, g.dst, g.n, chunks, (uint64_t)g.dtype};
             chunks += chunks_of(g, vectors);
         }
-        if (chunks > INT32_MAX) return hipErrorInvalidValue;
         pk.chunks = (int)chunks;
         const hipError_t e = launch(pk, before);
         if (e != hipSuccess) return e;

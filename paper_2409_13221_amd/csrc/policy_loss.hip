@@ -224,28 +224,33 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
     if (y < V && (in < (unsigned)whole ? in / N % 1024 == (unsigned)t : y == odd)) g[(int)in] = from_f32<T>(s_row[0]);
 }
 
-// Sums of the rows' terms in a fixed order: `rows` rows a workgroup, to out[3][workgroups], or for one workgroup to stats.
-__global__ __launch_bounds__(1024) void k_policy_stats(const float* __restrict__ terms, int n, int rows, float kl_coef,
-                                                       float* __restrict__ out, float* __restrict__ stats) {
-    __shared__ double red[3][16];
-    const unsigned t = threadIdx.x, lo = blockIdx.x * (unsigned)rows, hi = min((unsigned)n, lo + (unsigned)rows);
+// Sums of the rows' terms in a fixed order: `rows` rows a workgroup, to out[3][workgroups], or for one workgroup to stats.  The threads'
+// sums meet in LDS, where a wave each takes one of the three: a third of the lane exchanges one after the other.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_policy_stats(const float* __restrict__ terms, int n, int rows, float kl_coef,
+                                                          float* __restrict__ out, float* __restrict__ stats) {
+    __shared__ double part[3][THREADS], sum[3];
+    const unsigned t = threadIdx.x, w = t >> 6, lane = t & 63, lo = blockIdx.x * (unsigned)rows, hi = min((unsigned)n, lo + (unsigned)rows);
     double s[3] = {0., 0., 0.};
-    for (unsigned i = lo + t; i < hi; i += 1024)
+    for (unsigned i = lo + t; i < hi; i += THREADS)
 #pragma unroll
         for (int k = 0; k < 3; ++k) s[k] += terms[(size_t)k * n + i];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        for (int o = 32; o > 0; o >>= 1) s[k] += __shfl_xor(s[k], o, kWave);
-        if ((t & 63) == 0) red[k][t >> 6] = s[k];
+    for (int k = 0; k < 3; ++k) part[k][t] = s[k];
+    __syncthreads();
+    if (w < 3) {
+        double v = 0.;
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) v += part[w][i * 64 + lane];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+        if (lane == 0) sum[w] = v;
     }
     __syncthreads();
     if (t >= 3) return;
-    double v = 0.;
-    for (int i = 0; i < 16; ++i) v += red[t][i];
-    if (!stats) { out[t * gridDim.x + blockIdx.x] = (float)v; return; }
-    stats[1 + t] = (float)v;
-    const double kl = __shfl(v, 1, kWave);
-    if (t == 0) stats[0] = (float)(v + (kl_coef != 0.f ? kl_coef * kl : 0.));
+    if (!stats) { out[t * gridDim.x + blockIdx.x] = (float)sum[t]; return; }
+    stats[1 + t] = (float)sum[t];
+    if (t == 0) stats[0] = (float)(sum[0] + (kl_coef != 0.f ? kl_coef * sum[1] : 0.));
 }
 
 // More rows than this are summed in two steps.
@@ -284,8 +289,11 @@ hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, fl
     }
     const int blocks = stats_blocks(a.rows);
     float* part = a.terms + (size_t)3 * a.rows;
-    if (blocks > 0) k_policy_stats<<<blocks, 1024, 0, st>>>(a.terms, a.rows, kStatsRows, a.kl_coef, part, nullptr);
-    k_policy_stats<<<1, 1024, 0, st>>>(blocks > 0 ? part : a.terms, blocks > 0 ? blocks : a.rows, INT32_MAX, a.kl_coef, nullptr, stats);
+    if (blocks > 0) k_policy_stats<1024><<<blocks, 1024, 0, st>>>(a.terms, a.rows, kStatsRows, a.kl_coef, part, nullptr);
+    const float* terms = blocks > 0 ? part : a.terms;
+    const int n = blocks > 0 ? blocks : a.rows;
+    if (n <= 1024) k_policy_stats<256><<<1, 256, 0, st>>>(terms, n, n, a.kl_coef, nullptr, stats);
+    else k_policy_stats<1024><<<1, 1024, 0, st>>>(terms, n, n, a.kl_coef, nullptr, stats);
     return hipGetLastError();
 }
 
