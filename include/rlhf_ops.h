@@ -213,7 +213,7 @@ int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, int64_t ld_
  * tokens are left as they are.  The rows of a token are summed in float, in an order that depends on the tokens alone:
  * the same call gives the same bits.  Rows with tokens outside [0, vocab) count for nothing.  Types and strides as
  * above, dout in dout_dtype, dtable in table_dtype.  dout and dtable must not overlap.
- * scratch: rlhf_op_embed_grad_scratch_bytes(rows, d, vocab) bytes, 16-byte aligned. */
+ * scratch: rlhf_op_embed_grad_scratch_bytes(rows, d, vocab) bytes, 16-byte aligned (none for few rows: NULL will do). */
 int64_t rlhf_op_embed_grad_scratch_bytes(int rows, int d, int vocab);
 int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* dout, int64_t ld_dout, const int32_t* tokens, float scale,
                        int accumulate, void* dtable, int64_t ld_table, void* scratch, int rows, int d, int vocab,

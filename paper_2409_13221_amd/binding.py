@@ -669,11 +669,11 @@ def rlhf_op_embed_grad(dout, tokens, dtable, scale: float = 1.0, accumulate: boo
     _vector(tokens, rows, torch.int32, "tokens")
     need = lib().rlhf_op_embed_grad_scratch_bytes(rows, d, vocab)
     if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=dtable.device)
+        scratch = torch.empty(need, dtype=torch.uint8, device=dtable.device) if need else None
     elif scratch.dtype != torch.uint8 or scratch.numel() < need or not scratch.is_contiguous():
         raise ValueError(f"scratch must be a contiguous uint8 tensor of {need} entries")
     _op_check(lib().rlhf_op_embed_grad(_act_code(dout), _act_code(dtable), dout.data_ptr(), _matrix(dout, rows, d, "dout"), tokens.data_ptr(),
-                                       scale, int(accumulate), dtable.data_ptr(), _matrix(dtable, vocab, d, "dtable"), scratch.data_ptr(),
+                                       scale, int(accumulate), dtable.data_ptr(), _matrix(dtable, vocab, d, "dtable"), _ptr(scratch),
                                        rows, d, vocab, _stream_ptr()), "rlhf_op_embed_grad")
 
 

@@ -107,10 +107,10 @@ template <typename Use> __device__ __forceinline__ void each_token(bool has, int
     }
 }
 
-constexpr int kAhead = 8;               // tokens a lane has in flight
-__device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, int (&v)[kAhead]) {
+constexpr int kAhead = 16, kPlace = 8;  // tokens a lane has in flight while they are counted, and while their rows are placed
+template <int AHEAD> __device__ __forceinline__ void load_tokens(const int* tokens, int i, int end, int (&v)[AHEAD]) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) v[j] = i + j * 64 < end ? tokens[i + j * 64] : -1;
+    for (int j = 0; j < AHEAD; ++j) v[j] = i + j * 64 < end ? tokens[i + j * 64] : -1;
 }
 
 // LDS, in ints: next [16][subs], the count and later the next place of a wave's rows of a token; run [subs], start and count;
@@ -179,11 +179,11 @@ __device__ __forceinline__ void group_tokens(const int* __restrict__ tokens, int
     __syncthreads();
     const int mine0 = min(to, from + w * piece), mine1 = min(to, mine0 + piece);
     int last = -1, at = 0;                                         // a token in a row of rows: its place is at hand
-    for (int i0 = mine0; i0 < mine1; i0 += 64 * kAhead) {
-        int v[kAhead];
+    for (int i0 = mine0; i0 < mine1; i0 += 64 * kPlace) {
+        int v[kPlace];
         load_tokens(tokens, i0 + lane, mine1, v);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
+        for (int j = 0; j < kPlace; ++j)
             each_token((unsigned)v[j] < (unsigned)vocab && (v[j] & mask) == mine, v[j], [&](int token, bool same, uint64_t rows) {
                 const int sub = token >> b.log2;
                 if (token != last) {
@@ -291,7 +291,7 @@ struct GradArgs {
     Chunks c;
     size_t ld_dout, ld_table;
     float scale;
-    int d, wide_log2, slices;
+    int rows, d, wide_log2, slices;
     Clear clear;
     unsigned table_blocks, clear_blocks;
     int window;             // places of the order that share threads
@@ -299,11 +299,14 @@ struct GradArgs {
 
 template <int C, int H, typename G>
 __device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const GradArgs& a, int k, int slice) {
-    const int total = *a.total, from = k * a.c.size, to = min(total, from + a.c.size);
+    // The chunk's ends are read together with the number of places, which only the last chunk waits for.
+    const int from = k * a.c.size, guess = min(a.rows, from + a.c.size);
+    const Place head = a.places[from], tail = a.places[guess - 1];
+    const int total = *a.total, to = min(total, guess);
     if (from >= to) return;
     int lo[H], hi[H];
     my_columns<C, H>((const G*)nullptr, slice, a.wide_log2, a.d, lo, hi);
-    const Place ends[2] = {a.places[from], a.places[to - 1]};
+    const Place ends[2] = {head, to == guess ? tail : a.places[to - 1]};
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const Place& run = ends[s];
@@ -352,12 +355,13 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
     digits ^= digits >> 6;
     digits ^= digits >> 12;
     const int p0 = ((place ^ (digits & 7)) * per + (threadIdx.x >> a.wide_log2)) * a.window;
+    if (p0 >= a.rows) return;
+    // the window's places and the next ones, one a lane of the group, read together with the number of places
+    const int lane = threadIdx.x & 63, width = min(64, 1 << a.wide_log2), mine = lane & (width - 1), base = lane - mine, seen = min(width, 16);
+    const Place w = a.places[min(p0 + min(mine, seen - 1), a.rows - 1)];
     const int total = *a.total;
-    if (p0 >= total) return;
-    // the window's places, one a lane of the group; from the first where a run begins to the end of the last short run that does
-    const int lane = threadIdx.x & 63, width = min(64, 1 << a.wide_log2), mine = lane & (width - 1), base = lane - mine;
-    const Place w = a.places[min(p0 + min(mine, a.window - 1), total - 1)];
-    const uint64_t begins = __ballot(mine < a.window && w.start == p0 + mine) >> base & (~0ull >> (64 - width));
+    // from the first place of the window where a run begins to the end of the last short run that does
+    const uint64_t begins = __ballot(mine < a.window && p0 + mine < total && w.start == p0 + mine) >> base & (~0ull >> (64 - width));
     if (begins == 0) return;
     int at = p0 + __ffsll((unsigned long long)begins) - 1;
     const int last = 63 - __clzll((long long)begins), many = __shfl(w.count, base + last, kWave);
@@ -382,8 +386,16 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
             res.template store<false>(o, lo[h], hi[h]);
         }
     };
+    // the places of the first batch are there already; those of the others come while the rows of the one before do
+    const auto batch = [&](int p) { return a.places[min(p + min(mine, kBatch - 1), max(end, 1) - 1)]; };
+    Place q;
+    if (at - p0 + kBatch <= seen) {
+        const int from = base + at - p0 + min(mine, kBatch - 1);
+        q = Place{__shfl(w.row, from, kWave), __shfl(w.token, from, kWave), __shfl(w.start, from, kWave), 0};
+    } else {
+        q = batch(at);
+    }
     for (; at < end; at += kBatch) {
-        const Place q = a.places[min(at + min(mine, kBatch - 1), end - 1)];
         Piece<G, C> row[kBatch][H];
         Piece<T, C> had[kBatch][H];
         int token[kBatch];
@@ -399,6 +411,7 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
                     if (ACCUMULATE && token[k] >= 0) had[k][h].template load<false>(dtable + (size_t)token[k] * a.ld_table, lo[h], hi[h]);
                 }
         }
+        if (at + kBatch < end) q = batch(at + kBatch);
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             if (at + k >= end) break;
@@ -420,12 +433,14 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
 }
 
 // Joins the chunks of long runs.  A workgroup looks through the runs of a bucket and has 4 * LANES columns of the long ones; LANES lanes
-// take every (1024 / LANES)-th chunk, and all meet in LDS.  What bounds it is how fast one compute unit reads (about 30 GB/s
+// take every (kJoinThreads / LANES)-th chunk, and all meet in LDS.  What bounds it is how fast one compute unit reads (about 30 GB/s
 // from memory): narrow columns where there are few.
+constexpr int kJoinThreads = 1024;
 template <typename T, bool ACCUMULATE, int LANES>
-__global__ __launch_bounds__(1024) void k_long_runs(T* __restrict__ dtable, GradArgs a) {
-    constexpr int WORKERS = 1024 / LANES;
-    __shared__ float part[4][1024];
+__global__ __launch_bounds__(kJoinThreads) void k_long_runs(T* __restrict__ dtable, GradArgs a) {
+    static_assert(kJoinThreads >= kMaxSubs, "a thread a token of the bucket");
+    constexpr int WORKERS = kJoinThreads / LANES;
+    __shared__ float part[4][kJoinThreads];
     __shared__ int s_token[kMaxSubs], s_n;
     __shared__ Run s_run[kMaxSubs];
     const int t = threadIdx.x, w = t / LANES, lo[1] = {(int)(blockIdx.y * LANES + t % LANES) * 4}, hi[1] = {min(a.d, lo[0] + 4)};
@@ -562,7 +577,7 @@ static GradScratch grad_scratch(int rows, int d, int vocab) {
     s.bytes = s.part + (rows > size ? (size_t)((rows + size - 1) / size) * 2 * up((size_t)d * sizeof(float)) : 0);
     return s;
 }
-size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return grad_scratch(rows, d, vocab).bytes; }
+size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return rows <= kFewRows ? 0 : grad_scratch(rows, d, vocab).bytes; }
 
 // Rows of the table that are cleared beside the grouping: 32 MB, what goes out in the 6 us that 8192 tokens take.
 static int rows_cleared_first(size_t row_bytes, int rows, int vocab) {
@@ -612,8 +627,8 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
     e = hipGetLastError();
     if (e != hipSuccess || a.c.count == 0) return e;
     const int groups = 1 << a.b.log2;
-    if (a.d <= 1024) k_long_runs<T, ACCUMULATE, 16><<<dim3(groups, (a.d + 63) / 64), 1024, 0, st>>>(dtable, a);
-    else k_long_runs<T, ACCUMULATE, 64><<<dim3(groups, (a.d + 255) / 256), 1024, 0, st>>>(dtable, a);
+    if (a.d <= 1024) k_long_runs<T, ACCUMULATE, 16><<<dim3(groups, (a.d + 63) / 64), kJoinThreads, 0, st>>>(dtable, a);
+    else k_long_runs<T, ACCUMULATE, 64><<<dim3(groups, (a.d + 255) / 256), kJoinThreads, 0, st>>>(dtable, a);
     return hipGetLastError();
 }
 
@@ -630,7 +645,7 @@ hipError_t launch_embed_grad(hipStream_t st, int gdt, int tdt, const void* dout,
     a.b = buckets_of(vocab);
     a.c = Chunks{(float*)((char*)scratch + g.part), ((size_t)d + 3) / 4 * 4, chunk_size(rows), 0};
     if (rows > a.c.size) a.c.count = (rows + a.c.size - 1) / a.c.size;
-    a.ld_dout = ld_dout; a.ld_table = ld_table; a.scale = scale; a.d = d;
+    a.ld_dout = ld_dout; a.ld_table = ld_table; a.scale = scale; a.rows = rows; a.d = d;
     hipError_t e = hipSuccess;
     RLHF_TYPES2(gdt, tdt, (e = accumulate ? embed_grad<X, Y, true>(st, (const X*)dout, (Y*)dtable, tokens, a, places, runs, total, rows, vocab)
                                           : embed_grad<X, Y, false>(st, (const X*)dout, (Y*)dtable, tokens, a, places, runs, total, rows, vocab)));

@@ -338,7 +338,7 @@ extern "C" int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* d
     if (gdt < 0 || tdt < 0 || rows < 0 || d < 1 || vocab < 1 || ld_dout < d || ld_table < d || !dtable ||
         !aligned(dtable, elem_bytes(tdt)))
         return RLHF_EINVAL;
-    if (rows > 0 && (!dout || !tokens || !scratch || !aligned(dout, elem_bytes(gdt)) || !aligned(scratch, 16) ||
+    if (rows > 0 && (!dout || !tokens || (!scratch && embed_grad_scratch_bytes(rows, d, vocab) > 0) || !aligned(dout, elem_bytes(gdt)) || !aligned(scratch, 16) ||
                      overlap(dout, span(rows, d, ld_dout, gdt), dtable, span(vocab, d, ld_table, tdt))))
         return RLHF_EINVAL;
     return status_of(launch_embed_grad((hipStream_t)stream, gdt, tdt, dout, (size_t)ld_dout, tokens, scale, accumulate != 0,
