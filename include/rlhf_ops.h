@@ -194,7 +194,8 @@ int rlhf_op_head_dot(int act_dtype, int w_dtype, const void* xn, const void* w, 
  * A row with weight 0 or a negative token is left out: its logits and its other inputs, whatever they hold, are not used,
  * lp[r] = 0, its gradient is zero.  Logits of -inf have probability 0.  A row whose result is not a number (all
  * logits -inf, a logit of +inf, NaN, a token of vocab or more) makes lp[r], its gradient and stats NaN.
- * Columns of dlogits behind vocab are left as they are.  clip_low in [0, 1], clip_high >= 0, kl_coef >= 0.
+ * Columns of dlogits behind vocab are left as they are.  clip_low in [0, 1], clip_high >= 0, kl_coef >= 0.  rows and vocab at most
+ * 2^30.
  * scratch: rlhf_op_policy_loss_scratch_floats(rows, vocab) floats. */
 int64_t rlhf_op_policy_loss_scratch_floats(int rows, int vocab);
 int rlhf_op_policy_loss(int logit_dtype, const void* logits, int64_t ld, const int32_t* tokens, const float* lp_old,
@@ -203,7 +204,7 @@ int rlhf_op_policy_loss(int logit_dtype, const void* logits, int64_t ld, const i
                         float* scratch, int rows, int vocab, void* stream);
 
 /* Embedding lookup with scaling: out[r] = scale * table[tokens[r]], table [vocab, d] and out [rows, d] each in its own
- * type (RLHF_FP32, RLHF_BF16, 2 = IEEE half) and row stride; any d.  One rounding, to out's type.  A negative token gives
+ * type (RLHF_FP32, RLHF_BF16, 2 = IEEE half) and row stride; d at most 2^22, rows and vocab 2^30.  One rounding, to out's type.  A negative token gives
  * a row of zeros (padding), one of vocab or more a row of NaN. */
 int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, int64_t ld_table, const int32_t* tokens, float scale,
                   void* out, int64_t ld_out, int rows, int d, int vocab, void* stream);

