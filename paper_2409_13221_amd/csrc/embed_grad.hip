@@ -53,7 +53,7 @@ template <typename T, int C> struct Piece {
         v.get(x);
 #pragma unroll
         for (int e = 0; e < C; ++e)
-            if (lo + e < hi) row[lo + e] = from_f32<T>(x[e]);
+            if (lo + e < hi) row[lo + e] = round_to<T>(x[e]);
     }
 };
 

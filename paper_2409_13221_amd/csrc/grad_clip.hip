@@ -108,7 +108,7 @@ __device__ __forceinline__ void scale_chunk(const Pack& pk, int i, int c, float 
     const Work w = work_of<T, true>(pk, i, c);
     const T* x = (const T*)pk.t[i].src;
     T* y = (T*)pk.t[i].dst;
-    if (w.odd < pk.t[i].n) y[w.odd] = from_f32<T>(f * to_f32<T>(x[w.odd]));
+    if (w.odd < pk.t[i].n) y[w.odd] = round_to<T>(f * to_f32<T>(x[w.odd]));
     x += w.head;
     y += w.head;
     for (size_t k0 = w.from + threadIdx.x; k0 < w.to; k0 += 256 * kUnroll) {

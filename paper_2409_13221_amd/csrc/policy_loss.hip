@@ -21,7 +21,7 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, int r, float w,
     RowLoss o{-(cut ? c : u) * w, 0.f, cut ? w : 0.f, cut ? 0.f : -u * w};
     if (a.lp_ref) {
         const float x = a.lp_ref[r] - l, em = expm1f(x);
-        o.kl = (em - x) * w;
+        o.kl = (x == INFINITY ? x : em - x) * w;               // a token of probability 0
         if (a.kl_coef != 0.f) o.slope -= a.kl_coef * em * w;
     }
     return o;
@@ -91,7 +91,7 @@ __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, i
     zero.fill(0.f);
     const int head = columns_before<T>(g, a.vocab), whole = (a.vocab - head) / N * N, odd = t < head ? t : t + whole;
     for (int i = t * N; i < whole; i += threads * N) zero.template store<true>(g + head + i);
-    if (odd < a.vocab) g[odd] = from_f32<T>(0.f);
+    if (odd < a.vocab) g[odd] = round_to<T>(0.f);
 }
 
 // A row in registers: IT vectors of 16 bytes a thread, requested all at once.  Each is taken into the thread's running maximum and
@@ -159,10 +159,10 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
         x[it].set(f);
         if (i < whole) x[it].template store<true>(g + i);
     }
-    if (odd < V) g[odd - head] = from_f32<T>(row[1] * __expf(xl[0] - M));
+    if (odd < V) g[odd - head] = round_to<T>(row[1] * __expf(xl[0] - M));
     // the token's own column, by the thread that has just written it
     const unsigned in = y - head;
-    if (y < V && (in < whole ? in / N % THREADS == (unsigned)t : y == odd)) g[(int)in] = from_f32<T>(row[0]);
+    if (y < V && (in < whole ? in / N % THREADS == (unsigned)t : y == odd)) g[(int)in] = round_to<T>(row[0]);
 }
 
 // Rows that no workgroup's registers hold (beyond 90000 floats, 180000 of 16 bits): read once for the statistics, and again, out of
@@ -225,9 +225,9 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
             x[it].template store<true>(g + i);
         }
     }
-    if (odd < V) g[odd - head] = from_f32<T>(f * __expf(xl[0] - M));
+    if (odd < V) g[odd - head] = round_to<T>(f * __expf(xl[0] - M));
     const unsigned in = y - head;
-    if (y < V && (in < (unsigned)whole ? in / N % 1024 == (unsigned)t : y == odd)) g[(int)in] = from_f32<T>(s_row[0]);
+    if (y < V && (in < (unsigned)whole ? in / N % 1024 == (unsigned)t : y == odd)) g[(int)in] = round_to<T>(s_row[0]);
 }
 
 // Sums of the rows' terms in a fixed order: `rows` rows a workgroup, to out[3][workgroups], or for one workgroup to stats.  The threads'

@@ -14,6 +14,10 @@ template <> __device__ __forceinline__ uint32_t pack2<f16_t>(float lo, float hi)
     typedef f16_t pair __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, pair{(f16_t)lo, (f16_t)hi});
 }
+// One float to T, rounded to nearest; a NaN stays one whatever its payload (f32_to_bf16 carries some of them over into -0).
+template <typename T> __device__ __forceinline__ T round_to(float x) { return from_f32<T>(x); }
+template <> __device__ __forceinline__ bf16_t round_to<bf16_t>(float x) { return __builtin_bit_cast(bf16_t, (__bf16)x); }
+
 template <typename T> __device__ __forceinline__ float unpack(uint32_t w, int hi);
 template <> __device__ __forceinline__ float unpack<bf16_t>(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xFFFF0000u : w << 16); }
 template <> __device__ __forceinline__ float unpack<f16_t>(uint32_t w, int hi) {

@@ -245,6 +245,33 @@ def test_policy_loss_token_out_of_reach_and_huge_ratios():
     assert abs(float(stats[0]) - want) <= 4 * E * abs(want)
 
 
+def test_policy_loss_kl_of_a_token_out_of_reach():
+    c = _policy_case(12, 3, 50, "fp32", masked=0.0)
+    c["logits"][1, int(c["tokens"][1])] = float("-inf")
+    _, stats, d = _policy_run(c)                                # measured, not in the loss
+    assert stats[2] == float("inf") and torch.isfinite(stats[:2]).all() and torch.isfinite(d).all()
+    _, stats, d = _policy_run(c, kl_coef=0.1)
+    assert stats[0] == float("inf") and torch.isfinite(d[[0, 2]]).all()
+
+
+@pytest.mark.parametrize("odt", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("tdt", ["fp32", "half"])
+@pytest.mark.parametrize("d", [3, 64, 301])
+def test_a_nan_stays_one_whatever_its_payload(tdt, odt, d):
+    R = _R()
+    bits = torch.full((4, d), -1, dtype=torch.int32 if tdt == "fp32" else torch.int16, device="cuda")
+    bits[1] = 2 ** 31 - 1 if tdt == "fp32" else 2 ** 15 - 1
+    nan = bits.view(TDT[tdt])
+    tok = torch.arange(4, dtype=torch.int32, device="cuda")
+    out = torch.zeros(4, d, dtype=TDT[odt], device="cuda")
+    R.rlhf_op_embed(nan, tok, out)
+    few, many = torch.zeros(4, d, dtype=TDT[odt], device="cuda"), torch.zeros(4, d, dtype=TDT[odt], device="cuda")
+    R.rlhf_op_embed_grad(nan, tok, few)
+    R.rlhf_op_embed_grad(nan.repeat(75, 1), tok.repeat(75), many)
+    torch.cuda.synchronize()
+    assert out.isnan().all() and few.isnan().all() and many.isnan().all()
+
+
 @pytest.mark.parametrize("vocab", [50, 140001])
 def test_policy_loss_of_no_rows(vocab):
     z = torch.empty(0, vocab, device="cuda")
