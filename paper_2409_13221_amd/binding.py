@@ -597,12 +597,14 @@ def _on_device(*tensors) -> None:
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        at = t.get_device()              # -1: host memory
+        if at == dev:
+            continue
+        if at < 0:
             raise ValueError("all tensors must be in device memory")
-        if dev is None:
-            dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{dev}")
+        if at != torch.cuda.current_device():
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+        dev = at
 
 
 def _vector(t, n: int, dtype, what: str):
@@ -636,18 +638,20 @@ def rlhf_op_policy_loss(logits, tokens, lp_old, adv, lp, stats, dlogits=None, lp
             raise ValueError("dlogits must have the type of logits")
         ld_grad = _matrix(dlogits, rows, vocab, "dlogits")
     _vector(tokens, rows, torch.int32, "tokens")
-    for t, what in ((lp_old, "lp_old"), (adv, "adv"), (lp, "lp"), (lp_ref, "lp_ref"), (weight, "weight")):
-        _vector(t, rows, f32, what)
+    for t in (lp_old, adv, lp, lp_ref, weight):
+        if t is not None and (t.dtype != f32 or t.numel() != rows or not t.is_contiguous()):
+            raise ValueError(f"lp_old, adv, lp, lp_ref and weight must be contiguous float32 tensors of {rows} entries")
     _vector(stats, 4, f32, "stats")
-    need = lib().rlhf_op_policy_loss_scratch_floats(rows, vocab)
+    L = lib()
+    need = L.rlhf_op_policy_loss_scratch_floats(rows, vocab)
     if scratch is None:
         scratch = torch.empty(need, device=logits.device)
     elif scratch.dtype != f32 or scratch.numel() < need or not scratch.is_contiguous():
         raise ValueError(f"scratch must be a contiguous float32 tensor of {need} entries")
-    _op_check(lib().rlhf_op_policy_loss(_act_code(logits), logits.data_ptr(), ld, tokens.data_ptr(), lp_old.data_ptr(),
-                                        _ptr(lp_ref), adv.data_ptr(), _ptr(weight), clip_low, clip_high, kl_coef, grad_scale,
-                                        lp.data_ptr(), stats.data_ptr(), _ptr(dlogits), ld_grad, scratch.data_ptr(), rows, vocab,
-                                        _stream_ptr()), "rlhf_op_policy_loss")
+    _op_check(L.rlhf_op_policy_loss(_act_code(logits), logits.data_ptr(), ld, tokens.data_ptr(), lp_old.data_ptr(),
+                                    _ptr(lp_ref), adv.data_ptr(), _ptr(weight), clip_low, clip_high, kl_coef, grad_scale,
+                                    lp.data_ptr(), stats.data_ptr(), _ptr(dlogits), ld_grad, scratch.data_ptr(), rows, vocab,
+                                    _stream_ptr()), "rlhf_op_policy_loss")
 
 
 def rlhf_op_embed(table, tokens, out, scale: float = 1.0) -> None:
