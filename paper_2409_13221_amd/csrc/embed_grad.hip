@@ -26,34 +26,40 @@ template <typename T> static Grid grid_of(const T* p, size_t ld, int d, int C, i
 // Row and column numbers are ints.
 static bool sizes_fit(int rows, int d, int vocab) { return rows <= 1 << 30 && vocab <= 1 << 30 && d <= 1 << 22; }
 
-// Columns [lo[h], hi[h]) of this thread's pieces of a row at p: pieces meet where the row reaches a boundary of C elements.
-template <int C, int H, typename T> __device__ __forceinline__ void my_columns(const T* p, int slice, int wide_log2, int d, int (&lo)[H], int (&hi)[H]) {
+// A piece is the columns [lo, hi) of a row, C or, at the row's ends, fewer.  It is read as the C columns from `at` on, which are
+// inside the row wherever that has C columns: a short piece reads some of its neighbour's, since loads one by one would
+// have to be waited for before the next row's are sent (700 rows of 100: 20 us instead of 7).
+struct Cols { int at, lo, hi; };
+template <int C> __device__ __forceinline__ Cols cols_of(int lo, int hi, int d) { return Cols{min(lo, max(0, d - C)), lo, hi}; }
+
+// This thread's pieces of a row at p: pieces meet where the row reaches a boundary of C elements.
+template <int C, int H, typename T> __device__ __forceinline__ void my_columns(const T* p, int slice, int wide_log2, int d, Cols (&cols)[H]) {
     const int shift = (int)((uintptr_t)p % (C * sizeof(T)) / sizeof(T));
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         const int piece = ((slice * H + h) << wide_log2) + (threadIdx.x & ((1 << wide_log2) - 1));
-        hi[h] = min(d, piece * C - shift + C);
-        lo[h] = max(0, piece * C - shift);
+        cols[h] = cols_of<C>(max(0, piece * C - shift), min(d, piece * C - shift + C), d);
     }
 }
 
-// Columns [lo, hi) of a row as they lie in memory: C at once, or the few there are.
+// A piece as it lies in memory, of a row of d columns.
 template <typename T, int C> struct Piece {
     Vec<T, C> v;
-    template <bool ONCE> __device__ __forceinline__ void load(const T* row, int lo, int hi) {
-        if (hi - lo == C) return v.template load<ONCE>(row + lo);
-        float x[C];
+    template <bool ONCE> __device__ __forceinline__ void load(const T* row, const Cols& c, int d) {
+        if (c.lo >= c.hi) return;
+        if (c.at + C <= d) return v.template load<ONCE>(row + c.at);
+        float x[C];                     // rows of fewer than C columns
 #pragma unroll
-        for (int e = 0; e < C; ++e) x[e] = lo + e < hi ? to_f32<T>(row[lo + e]) : 0.f;
+        for (int e = 0; e < C; ++e) x[e] = c.at + e < d ? to_f32<T>(row[c.at + e]) : 0.f;
         v.set(x);
     }
-    template <bool ONCE> __device__ __forceinline__ void store(T* row, int lo, int hi) const {
-        if (hi - lo == C) return v.template store<ONCE>(row + lo);
+    template <bool ONCE> __device__ __forceinline__ void store(T* row, const Cols& c) const {
+        if (c.hi - c.lo == C) return v.template store<ONCE>(row + c.lo);
         float x[C];
         v.get(x);
 #pragma unroll
         for (int e = 0; e < C; ++e)
-            if (lo + e < hi) row[lo + e] = round_to<T>(x[e]);
+            if (c.at + e >= c.lo && c.at + e < c.hi) row[c.at + e] = round_to<T>(x[e]);
     }
 };
 
@@ -66,12 +72,12 @@ __global__ __launch_bounds__(256) void k_embed_rows(const T* __restrict__ table,
     const int v = tokens[r];
     const bool known = (unsigned)v < (unsigned)vocab;
     O* o = out + (size_t)r * ld_out;
-    int lo[H], hi[H];
-    my_columns<C, H>(o, blockIdx.y, wide_log2, d, lo, hi);
+    Cols cols[H];
+    my_columns<C, H>(o, blockIdx.y, wide_log2, d, cols);
     Piece<T, C> in[H];
 #pragma unroll
     for (int h = 0; h < H; ++h)
-        if (known) in[h].template load<false>(table + (size_t)v * ld_table, lo[h], hi[h]);
+        if (known) in[h].template load<false>(table + (size_t)v * ld_table, cols[h], d);
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         float x[C];
@@ -81,7 +87,7 @@ __global__ __launch_bounds__(256) void k_embed_rows(const T* __restrict__ table,
         Piece<O, C> res;
         res.v.set(x);
         // the next reader is on any of the 8 XCDs, so little is lost: 8192 rows of 4096 bf16 into float 37 us, evict-first 26
-        res.template store<true>(o, lo[h], hi[h]);
+        res.template store<true>(o, cols[h]);
     }
 }
 
@@ -228,7 +234,7 @@ __device__ __forceinline__ void clear_rows(T* __restrict__ dtable, size_t ld, in
         if (!empty[k]) continue;
         T* o = dtable + (size_t)(r0 + k * per) * ld;
         const int shift = (int)((uintptr_t)o % 16 / sizeof(T));
-        zero.template store<true>(o, max(0, piece * C - shift), min(d, piece * C - shift + C));
+        zero.template store<true>(o, cols_of<C>(max(0, piece * C - shift), min(d, piece * C - shift + C), d));
     }
 }
 template <int THREADS> static int64_t clear_blocks(const Clear& c) {
@@ -248,9 +254,9 @@ __global__ __launch_bounds__(1024) void k_group_and_clear(const int* __restrict_
 
 // x += rows index(0) .. index(count - 1) of m in that order, FLIGHT rows in flight, as they lie in memory.  The indices come a group
 // of lanes at a time, so that no row waits for its own: `width` lanes (a power of two) of a wave share the rows, and all of
-// them have to be here, those without columns (lo >= hi) too.
+// them have to be here, those without columns too.  d: columns of a row of m.
 template <int FLIGHT, int C, int H, typename G, typename Index>
-__device__ __forceinline__ void sum_rows(const G* __restrict__ m, size_t ld, int count, int width, Index index, const int (&lo)[H], const int (&hi)[H],
+__device__ __forceinline__ void sum_rows(const G* __restrict__ m, size_t ld, int d, int count, int width, Index index, const Cols (&cols)[H],
                                          float (&x)[H][C]) {
     const int lane = threadIdx.x & 63, mine = lane & (width - 1), base = lane - mine;
     for (int p0 = 0; p0 < count; p0 += width) {
@@ -262,7 +268,7 @@ __device__ __forceinline__ void sum_rows(const G* __restrict__ m, size_t ld, int
                 const int row = __shfl(r, base + min(p + k, many - 1), kWave);
                 if (p + k < many)
 #pragma unroll
-                    for (int h = 0; h < H; ++h) y[k][h].template load<true>(m + (size_t)row * ld, lo[h], hi[h]);
+                    for (int h = 0; h < H; ++h) y[k][h].template load<true>(m + (size_t)row * ld, cols[h], d);
             }
 #pragma unroll
             for (int k = 0; k < FLIGHT; ++k)
@@ -308,8 +314,8 @@ __device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const Grad
     const Place head = a.places[from], tail = a.places[guess - 1];
     const int total = *a.total, to = min(total, guess);
     if (from >= to) return;
-    int lo[H], hi[H];
-    my_columns<C, H>((const G*)nullptr, slice, a.wide_log2, a.d, lo, hi);
+    Cols cols[H];
+    my_columns<C, H>((const G*)nullptr, slice, a.wide_log2, a.d, cols);
     const Place ends[2] = {head, to == guess ? tail : a.places[to - 1]};
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -317,15 +323,16 @@ __device__ __forceinline__ void sum_chunk(const G* __restrict__ dout, const Grad
         if (run.count <= a.c.size || s != (run.start > from)) continue;       // slot 1: it begins behind the chunk's first place
         const int p = max(from, run.start), end = min(to, run.start + run.count);
         float x[H][C] = {};
-        sum_rows<kFlight, C, H>(dout, a.ld_dout, end - p, min(64, 1 << a.wide_log2), [&](int i) { return a.places[p + i].row; }, lo, hi, x);
+        sum_rows<kFlight, C, H>(dout, a.ld_dout, a.d, end - p, min(64, 1 << a.wide_log2), [&](int i) { return a.places[p + i].row; }, cols, x);
         float* part = a.c.part + ((size_t)k * 2 + s) * a.c.ld;
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int e = 0; e < C; e += 4) {
+                const Cols& c = cols[h];
                 Piece<float, 4> o;
                 o.v.set({x[h][e], x[h][e + 1], x[h][e + 2], x[h][e + 3]});
-                if (lo[h] + e < hi[h]) o.template store<false>(part, lo[h] + e, min(hi[h], lo[h] + e + 4));
+                o.template store<false>(part, Cols{c.at + e, max(c.lo, c.at + e), min(c.hi, c.at + e + 4)});
             }
     }
 }
@@ -370,8 +377,8 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
     int at = p0 + __ffsll((unsigned long long)begins) - 1;
     const int last = 63 - __clzll((long long)begins), many = __shfl(w.count, base + last, kWave);
     const int end = p0 + last + (a.c.count > 0 && many > a.c.size ? 0 : many);
-    int lo[H], hi[H];
-    my_columns<C, H>((const T*)nullptr, slice, a.wide_log2, a.d, lo, hi);
+    Cols cols[H];
+    my_columns<C, H>((const T*)nullptr, slice, a.wide_log2, a.d, cols);
     // rows in the order of their places, kBatch in flight; a run is stored where the next begins
     constexpr int kBatch = ACCUMULATE ? 4 : 8;
     float x[H][C];
@@ -387,7 +394,7 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
             for (int e = 0; e < C; ++e) f[e] = ACCUMULATE ? f[e] + a.scale * x[h][e] : a.scale * x[h][e];
             Piece<T, C> res;
             res.v.set(f);
-            res.template store<false>(o, lo[h], hi[h]);
+            res.template store<false>(o, cols[h]);
         }
     };
     // the places of the first batch are there already; those of the others come while the rows of the one before do
@@ -411,8 +418,8 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
             if (at + k < end)
 #pragma unroll
                 for (int h = 0; h < H; ++h) {
-                    row[k][h].template load<true>(dout + (size_t)r * a.ld_dout, lo[h], hi[h]);
-                    if (ACCUMULATE && token[k] >= 0) had[k][h].template load<false>(dtable + (size_t)token[k] * a.ld_table, lo[h], hi[h]);
+                    row[k][h].template load<true>(dout + (size_t)r * a.ld_dout, cols[h], a.d);
+                    if (ACCUMULATE && token[k] >= 0) had[k][h].template load<false>(dtable + (size_t)token[k] * a.ld_table, cols[h], a.d);
                 }
         }
         if (at + kBatch < end) q = batch(at + kBatch);
@@ -447,7 +454,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_long_runs(T* __restrict__ dtab
     __shared__ float part[4][kJoinThreads];
     __shared__ int s_token[kMaxSubs], s_n;
     __shared__ Run s_run[kMaxSubs];
-    const int t = threadIdx.x, w = t / LANES, lo[1] = {(int)(blockIdx.y * LANES + t % LANES) * 4}, hi[1] = {min(a.d, lo[0] + 4)};
+    const int t = threadIdx.x, w = t / LANES, lo = (blockIdx.y * LANES + t % LANES) * 4;
+    const Cols cols[1] = {{lo, lo, min(a.d, lo + 4)}};        // the sums' rows are padded to fours
     if (t == 0) s_n = 0;
     __syncthreads();
     if (t < a.b.subs) {
@@ -463,8 +471,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_long_runs(T* __restrict__ dtab
         const Run run = s_run[j];
         const int first = run.start / a.c.size, chunks = (run.start + run.count - 1) / a.c.size - first + 1, slot = run.start > first * a.c.size;
         float x[1][4] = {};
-        sum_rows<kFlight, 4, 1>(a.c.part, a.c.ld, max(0, (chunks - w + WORKERS - 1) / WORKERS), LANES,
-                                [&](int i) { const int c = w + WORKERS * i; return (first + c) * 2 + (c == 0 ? slot : 0); }, lo, hi, x);
+        sum_rows<kFlight, 4, 1>(a.c.part, a.c.ld, (int)a.c.ld, max(0, (chunks - w + WORKERS - 1) / WORKERS), LANES,
+                                [&](int i) { const int c = w + WORKERS * i; return (first + c) * 2 + (c == 0 ? slot : 0); }, cols, x);
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[e][t] = x[0][e];
         __syncthreads();
@@ -476,13 +484,13 @@ __global__ __launch_bounds__(kJoinThreads) void k_long_runs(T* __restrict__ dtab
             Piece<T, 4> res;
             float f[4] = {};
             if (ACCUMULATE) {
-                res.template load<false>(o, lo[0], hi[0]);
+                res.template load<false>(o, cols[0], a.d);
                 res.v.get(f);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] += a.scale * x[0][e];
             res.v.set(f);
-            res.template store<false>(o, lo[0], hi[0]);
+            res.template store<false>(o, cols[0]);
         }
         __syncthreads();
     }
@@ -515,14 +523,14 @@ __global__ __launch_bounds__(256) void k_few_rows_grad(const G* __restrict__ dou
     // the list is the wave's own; its lanes run together, but what one has written another may read only behind this
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     T* o = dtable + (size_t)v * ld_table;
-    int lo[H], hi[H];
-    my_columns<C, H>(o, blockIdx.y, wide_log2, d, lo, hi);
+    Cols cols[H];
+    my_columns<C, H>(o, blockIdx.y, wide_log2, d, cols);
     Piece<T, C> old[H];
     if (ACCUMULATE)
 #pragma unroll
-        for (int h = 0; h < H; ++h) old[h].template load<false>(o, lo[h], hi[h]);
+        for (int h = 0; h < H; ++h) old[h].template load<false>(o, cols[h], d);
     float x[H][C] = {};
-    sum_rows<kFlight, C, H>(dout, ld_dout, count, width, [&](int j) { return (int)rows[j]; }, lo, hi, x);
+    sum_rows<kFlight, C, H>(dout, ld_dout, d, count, width, [&](int j) { return (int)rows[j]; }, cols, x);
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         float f[C];
@@ -530,7 +538,7 @@ __global__ __launch_bounds__(256) void k_few_rows_grad(const G* __restrict__ dou
 #pragma unroll
         for (int e = 0; e < C; ++e) f[e] = ACCUMULATE ? f[e] + scale * x[h][e] : scale * x[h][e];
         old[h].v.set(f);
-        old[h].template store<false>(o, lo[h], hi[h]);
+        old[h].template store<false>(o, cols[h]);
     }
 }
 
