@@ -15,12 +15,13 @@ template <typename A, typename B> struct Shape {
     static constexpr int C = sizeof(A) == 2 && sizeof(B) == 2 ? 8 : 4, H = 8 / C;
 };
 struct Grid { int wide_log2, slices; };
-// p, ld: what the pieces go by (my_columns); rows that start off a boundary may have a piece more.
-template <typename T> static Grid grid_of(const T* p, size_t ld, int d, int C, int H) {
+// p, ld: what the pieces go by (my_columns); rows that start off a boundary may have a piece more.  At most 2^most threads side by
+// side.
+template <typename T> static Grid grid_of(const T* p, size_t ld, int d, int C, int H, int most = 8) {
     const bool on_boundary = (uintptr_t)p % (C * sizeof(T)) == 0 && ld % C == 0;
     const int pieces = (d + (on_boundary ? C - 1 : 2 * C - 2)) / C;
     int lg = 3;
-    while (lg < 8 && (H << lg) < pieces) ++lg;
+    while (lg < most && (H << lg) < pieces) ++lg;
     return Grid{lg, (pieces + (H << lg) - 1) / (H << lg)};
 }
 // Row and column numbers are ints.
@@ -496,41 +497,70 @@ __global__ __launch_bounds__(kJoinThreads) void k_long_runs(T* __restrict__ dtab
     }
 }
 
-// Up to kFewRows rows: no grouping ahead.  A thread group a row; that of a token's first row finds the others and sums them.
-constexpr int kFewRows = 256;
+// Few rows: no grouping ahead.  A workgroup a row; that of a token's first row finds the others, deals them to its groups of `wide`
+// threads, and joins their sums.  The longest run possible is what limits it: up to 16 round trips of kFlight rows for a
+// group (1000 rows of 4096, half of them one token, 50 us so and 31 by grouping first; 512 rows 27 and 28).
+constexpr int kFewRows = 2048;
+static bool few_rows(int rows, int d) { return rows <= kFewRows && rows <= 16 * kFlight * (256 >> grid_of((const float*)nullptr, 0, d, 4, 2, 6).wide_log2); }
+
 template <typename G, typename T, bool ACCUMULATE>
 __global__ __launch_bounds__(256) void k_few_rows_grad(const G* __restrict__ dout, size_t ld_dout, const int* __restrict__ tokens, T* __restrict__ dtable,
                                                        size_t ld_table, float scale, int n, int d, int vocab, int wide_log2) {
-    constexpr int C = Shape<G, T>::C, H = Shape<G, T>::H;
-    __shared__ int s_tok[kFewRows];
-    __shared__ uint8_t s_rows[4][8][kFewRows];          // of a wave's groups (8 at most)
-    const int t = threadIdx.x;
-    s_tok[t] = t < n ? tokens[t] : -1;
-    __syncthreads();
-    const int i = blockIdx.x * (256 >> wide_log2) + (t >> wide_log2);
-    const int lane = t & 63, width = min(64, 1 << wide_log2), mine = lane & (width - 1), base = lane - mine;
-    const int v = i < n ? s_tok[i] : -1;
+    constexpr int C = Shape<G, T>::C, H = Shape<G, T>::H, EACH = kFewRows / 256;
+    __shared__ uint16_t s_rows[kFewRows];
+    __shared__ int s_wave[4];
+    __shared__ float part[8][256];
+    const int t = threadIdx.x, w = t >> 6, lane = t & 63, v = tokens[blockIdx.x];
     if ((unsigned)v >= (unsigned)vocab) return;
-    uint8_t* rows = s_rows[t >> 6][base / width];
-    int count = 0;
-    for (int j0 = 0; j0 < n; j0 += width) {
-        const bool same = j0 + mine < n && s_tok[j0 + mine] == v;
-        const uint64_t all = __ballot(same) >> base & (~0ull >> (64 - width));
-        if (count == 0 && all && j0 + __ffsll((unsigned long long)all) - 1 < i) return;      // an earlier row's
-        if (same) rows[count + __popcll(all & ((1ull << mine) - 1))] = (uint8_t)(j0 + mine);
-        count += __popcll(all);
-    }
-    // the list is the wave's own; its lanes run together, but what one has written another may read only behind this
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     T* o = dtable + (size_t)v * ld_table;
     Cols cols[H];
-    my_columns<C, H>(o, blockIdx.y, wide_log2, d, cols);
+    my_columns<C, H>((const T*)nullptr, blockIdx.y, wide_log2, d, cols);
+    const int group = t >> wide_log2, groups = 256 >> wide_log2;
     Piece<T, C> old[H];
-    if (ACCUMULATE)
+    if (ACCUMULATE && group == 0)
 #pragma unroll
         for (int h = 0; h < H; ++h) old[h].template load<false>(o, cols[h], d);
+    // the rows of the token, in ascending order: a thread looks at EACH neighbours
+    bool same[EACH];
+    int many = 0;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int j = t * EACH + k;
+        same[k] = j < n && tokens[j] == v;
+        many += same[k];
+    }
+    int sum = many;
+#pragma unroll
+    for (int e = 1; e < 64; e <<= 1) {
+        const int x = __shfl_up(sum, e, kWave);
+        if (lane >= e) sum += x;
+    }
+    if (lane == 63) s_wave[w] = sum;
+    __syncthreads();
+    int at = sum - many, count = 0;
+    for (int k = 0; k < 4; ++k) {
+        if (k < w) at += s_wave[k];
+        count += s_wave[k];
+    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if (same[k]) s_rows[at++] = (uint16_t)(t * EACH + k);
+    __syncthreads();
+    if (s_rows[0] != blockIdx.x) return;                 // an earlier row's
     float x[H][C] = {};
-    sum_rows<kFlight, C, H>(dout, ld_dout, d, count, width, [&](int j) { return (int)rows[j]; }, cols, x);
+    sum_rows<kFlight, C, H>(dout, ld_dout, d, max(0, (count - group + groups - 1) / groups), 1 << wide_log2,
+                            [&](int j) { return (int)s_rows[group + groups * j]; }, cols, x);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int e = 0; e < C; ++e) part[h * C + e][t] = x[h][e];
+    __syncthreads();
+    if (group > 0) return;
+    for (int g = 1; g < min(count, groups); ++g)
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int e = 0; e < C; ++e) x[h][e] += part[h * C + e][(g << wide_log2) + t];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         float f[C];
@@ -589,7 +619,7 @@ static GradScratch grad_scratch(int rows, int d, int vocab) {
     s.bytes = s.part + (rows > size ? (size_t)((rows + size - 1) / size) * 2 * up((size_t)d * sizeof(float)) : 0);
     return s;
 }
-size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return rows <= kFewRows ? 0 : grad_scratch(rows, d, vocab).bytes; }
+size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return few_rows(rows, d) ? 0 : grad_scratch(rows, d, vocab).bytes; }
 
 // Rows of the table that are cleared beside the grouping: 32 MB, what goes out in the 6 us that 8192 tokens take.
 static int rows_cleared_first(size_t row_bytes, int rows, int vocab) {
@@ -602,7 +632,7 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
                              int vocab) {
     const Grid z = grid_of(dtable, a.ld_table, a.d, 16 / sizeof(T), 1);
     const int first = ACCUMULATE ? 0 : rows_cleared_first(a.d * sizeof(T), rows, vocab);
-    if (rows > 0 && rows <= kFewRows) {
+    if (rows > 0 && few_rows(rows, a.d)) {
         if (!ACCUMULATE) {
             const Clear whole{0, vocab, z.wide_log2, z.slices};
             if (clear_blocks<1024>(whole) > INT32_MAX) return hipErrorInvalidValue;
@@ -611,10 +641,9 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
-        const Grid g = grid_of(dtable, a.ld_table, a.d, Shape<G, T>::C, Shape<G, T>::H);
-        const int per = 256 >> g.wide_log2;
-        k_few_rows_grad<G, T, ACCUMULATE><<<dim3((rows + per - 1) / per, g.slices), 256, 0, st>>>(dout, a.ld_dout, tokens, dtable, a.ld_table, a.scale, rows,
-                                                                                                a.d, vocab, g.wide_log2);
+        const Grid g = grid_of((const T*)nullptr, 0, a.d, Shape<G, T>::C, Shape<G, T>::H, 6);
+        k_few_rows_grad<G, T, ACCUMULATE><<<dim3(rows, g.slices), 256, 0, st>>>(dout, a.ld_dout, tokens, dtable, a.ld_table, a.scale, rows, a.d, vocab,
+                                                                              g.wide_log2);
         return hipGetLastError();
     }
     const Clear beside{0, first, z.wide_log2, z.slices};

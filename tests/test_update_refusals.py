@@ -40,7 +40,7 @@ def test_embed(bad):
     assert R.lib().rlhf_op_embed(*dict(EMBED, **bad).values()) == R.RLHF_EINVAL
 
 
-EGRAD = dict(gdt=0, tdt=0, dout=A, ld=64, tokens=B, scale=1.0, acc=0, dtable=D, ld_table=64, scratch=E, rows=1000, d=64, vocab=10, stream=None)
+EGRAD = dict(gdt=0, tdt=0, dout=A, ld=64, tokens=B, scale=1.0, acc=0, dtable=D, ld_table=64, scratch=E, rows=3000, d=64, vocab=10, stream=None)
 
 
 @pytest.mark.parametrize("bad", [
@@ -84,7 +84,7 @@ def test_struct_layout():
 def test_scratch_sizes_of_nothing():
     L = _R().lib()
     assert L.rlhf_op_policy_loss_scratch_floats(0, 100) == 0 and L.rlhf_op_embed_grad_scratch_bytes(0, 8, 8) == 0
-    assert L.rlhf_op_embed_grad_scratch_bytes(1000, 8, 8) > 0
+    assert L.rlhf_op_embed_grad_scratch_bytes(3000, 8, 8) > 0
     assert L.rlhf_op_policy_loss_scratch_floats(5, 100) >= 15 and L.rlhf_op_grad_norm_scratch_doubles(None, 0) >= 0
 
 
