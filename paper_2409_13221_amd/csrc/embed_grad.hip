@@ -213,11 +213,12 @@ __device__ __forceinline__ Run run_of(const Run* runs, const Buckets& b, int v) 
 }
 
 // Zeros for the rows [from, to) of the table that have no token (runs == NULL: for all), by workgroups of THREADS threads,
-// kZeroRows rows a thread.  `wide` threads lie over a row, a slice of it if it is wider.
-struct Clear { int from, to, wide_log2, slices; };
+// kZeroRows rows a thread.  `wide` threads lie over a row, a slice of it if it is wider.  ld, d: the table's, or those of the
+// same memory as rows of another length, the last of which ends where all `elements` do.
+struct Clear { int from, to, wide_log2, slices, d; size_t ld, elements; };
 constexpr int kZeroRows = 8;
 template <int THREADS, typename T>
-__device__ __forceinline__ void clear_rows(T* __restrict__ dtable, size_t ld, int d, const Clear& c, unsigned block, const Run* runs, const Buckets& b) {
+__device__ __forceinline__ void clear_rows(T* __restrict__ dtable, const Clear& c, unsigned block, const Run* runs, const Buckets& b) {
     constexpr int C = 16 / sizeof(T);
     const int per = THREADS >> c.wide_log2, slice = block % c.slices;
     const int r0 = c.from + (int)(block / c.slices) * (per * kZeroRows) + (threadIdx.x >> c.wide_log2);
@@ -233,8 +234,9 @@ __device__ __forceinline__ void clear_rows(T* __restrict__ dtable, size_t ld, in
 #pragma unroll
     for (int k = 0; k < kZeroRows; ++k) {
         if (!empty[k]) continue;
-        T* o = dtable + (size_t)(r0 + k * per) * ld;
-        const int shift = (int)((uintptr_t)o % 16 / sizeof(T));
+        const size_t at = (size_t)(r0 + k * per) * c.ld;
+        T* o = dtable + at;
+        const int shift = (int)((uintptr_t)o % 16 / sizeof(T)), d = c.elements ? (int)min((size_t)c.d, c.elements - at) : c.d;
         zero.template store<true>(o, cols_of<C>(max(0, piece * C - shift), min(d, piece * C - shift + C), d));
     }
 }
@@ -246,11 +248,10 @@ template <int THREADS> static int64_t clear_blocks(const Clear& c) {
 // The grouping, and beside it (workgroups behind the buckets) zeros for as many rows of the table as go out in its time.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_group_and_clear(const int* __restrict__ tokens, int n, int vocab, Buckets b, Place* __restrict__ places,
-                                                          Run* __restrict__ runs, int* __restrict__ total, T* __restrict__ dtable, size_t ld,
-                                                          int d, Clear clear) {
+                                                          Run* __restrict__ runs, int* __restrict__ total, T* __restrict__ dtable, Clear clear) {
     const int groups = n > 0 ? b.parts << b.log2 : 0;
     if ((int)blockIdx.x < groups) group_tokens(tokens, n, vocab, b, blockIdx.x / b.parts, blockIdx.x % b.parts, places, runs, total);
-    else clear_rows<1024>(dtable, ld, d, clear, blockIdx.x - groups, nullptr, b);
+    else clear_rows<1024>(dtable, clear, blockIdx.x - groups, nullptr, b);
 }
 
 // x += rows index(0) .. index(count - 1) of m in that order, FLIGHT rows in flight, as they lie in memory.  The indices come a group
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
     if (!ACCUMULATE && a.clear_blocks > 0) {
         const uint64_t all = a.table_blocks + a.clear_blocks;
         const unsigned before = (unsigned)((uint64_t)block * a.clear_blocks / all);
-        if ((uint64_t)(block + 1ull) * a.clear_blocks / all > before) return clear_rows<256>(dtable, a.ld_table, a.d, a.clear, before, a.runs, a.b);
+        if ((uint64_t)(block + 1ull) * a.clear_blocks / all > before) return clear_rows<256>(dtable, a.clear, before, a.runs, a.b);
         block -= before;
     }
     const int per = 256 >> a.wide_log2, chunk_groups = (a.c.count + per - 1) / per, slice = block % a.slices;
@@ -499,7 +500,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_long_runs(T* __restrict__ dtab
 
 // Few rows: no grouping ahead.  A workgroup a row; that of a token's first row finds the others, deals them to its groups of `wide`
 // threads, and joins their sums.  The longest run possible is what limits it: up to 16 round trips of kFlight rows for a
-// group (1000 rows of 4096, half of them one token, 50 us so and 31 by grouping first; 512 rows 27 and 28).
+// group (512 rows of 4096, added to a table: 15 us, 27 if half of them are one token, 40 if all; grouped first, 25 to 31 us
+// whatever the tokens are).
 constexpr int kFewRows = 2048;
 static bool few_rows(int rows, int d) { return rows <= kFewRows && rows <= 16 * kFlight * (256 >> grid_of((const float*)nullptr, 0, d, 4, 2, 6).wide_log2); }
 
@@ -627,17 +629,26 @@ static int rows_cleared_first(size_t row_bytes, int rows, int vocab) {
     return rows > 0 && first < (size_t)vocab ? (int)first : vocab;
 }
 
+// The table's first rows, all to be cleared.  Rows behind each other in memory are cleared as rows of 4 KB, whatever their length
+// (41617 rows of 51 bf16: 8.5 us by rows).
+template <typename T> static Clear first_rows(const T* dtable, size_t ld, int d, int rows) {
+    constexpr int L = 4096 / sizeof(T);
+    const size_t elements = (size_t)rows * d, lines = (elements + L - 1) / L;
+    const bool flat = ld == (size_t)d && lines <= 1 << 30;
+    const Grid g = flat ? grid_of(dtable, L, L, 16 / sizeof(T), 1) : grid_of(dtable, ld, d, 16 / sizeof(T), 1);
+    if (flat) return Clear{0, (int)lines, g.wide_log2, g.slices, L, L, elements};
+    return Clear{0, rows, g.wide_log2, g.slices, d, ld, 0};
+}
+
 template <typename G, typename T, bool ACCUMULATE>
 static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int* tokens, GradArgs a, Place* places, Run* runs, int* total, int rows,
                              int vocab) {
-    const Grid z = grid_of(dtable, a.ld_table, a.d, 16 / sizeof(T), 1);
     const int first = ACCUMULATE ? 0 : rows_cleared_first(a.d * sizeof(T), rows, vocab);
     if (rows > 0 && few_rows(rows, a.d)) {
         if (!ACCUMULATE) {
-            const Clear whole{0, vocab, z.wide_log2, z.slices};
+            const Clear whole = first_rows(dtable, a.ld_table, a.d, vocab);
             if (clear_blocks<1024>(whole) > INT32_MAX) return hipErrorInvalidValue;
-            k_group_and_clear<T><<<(unsigned)clear_blocks<1024>(whole), 1024, 0, st>>>(tokens, 0, vocab, a.b, places, runs, total, dtable, a.ld_table, a.d,
-                                                                                      whole);
+            k_group_and_clear<T><<<(unsigned)clear_blocks<1024>(whole), 1024, 0, st>>>(tokens, 0, vocab, a.b, places, runs, total, dtable, whole);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
@@ -646,8 +657,9 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
                                                                               g.wide_log2);
         return hipGetLastError();
     }
-    const Clear beside{0, first, z.wide_log2, z.slices};
-    a.clear = Clear{first, ACCUMULATE ? first : vocab, z.wide_log2, z.slices};
+    const Clear beside = first_rows(dtable, a.ld_table, a.d, first);
+    const Grid z = grid_of(dtable, a.ld_table, a.d, 16 / sizeof(T), 1);
+    a.clear = Clear{first, ACCUMULATE ? first : vocab, z.wide_log2, z.slices, a.d, a.ld_table, 0};
     const int64_t group_blocks = (rows > 0 ? (int64_t)a.b.parts << a.b.log2 : 0) + clear_blocks<1024>(beside), clear = clear_blocks<256>(a.clear);
     const Grid g = grid_of((const T*)nullptr, 0, a.d, Shape<G, T>::C, Shape<G, T>::H);     // its pieces go by columns
     a.wide_log2 = g.wide_log2;
@@ -658,8 +670,8 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
     const int64_t windows = (rows + a.window * per - 1) / (a.window * per);
     const int64_t table = ((a.c.count + per - 1) / per + (windows + 7) / 8 * 8) * g.slices;
     if (group_blocks > INT32_MAX || table + clear > INT32_MAX) return hipErrorInvalidValue;
-    k_group_and_clear<T><<<(unsigned)group_blocks, 1024, group_lds_bytes(a.b), st>>>(tokens, rows, vocab, a.b, places, runs, total, dtable, a.ld_table,
-                                                                                    a.d, beside);
+    k_group_and_clear<T><<<(unsigned)group_blocks, 1024, group_lds_bytes(a.b), st>>>(tokens, rows, vocab, a.b, places, runs, total, dtable,
+                                                                                    beside);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || rows <= 0) return e;
     a.table_blocks = (unsigned)table;
