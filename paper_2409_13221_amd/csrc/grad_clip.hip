@@ -97,7 +97,13 @@ __global__ __launch_bounds__(256) void k_sum_squares(Pack pk, double* __restrict
 __global__ __launch_bounds__(1024) void k_norm_finish(const double* __restrict__ part, int n, float* __restrict__ norm) {
     __shared__ double red[16];
     double s = 0.;
-    for (int i = threadIdx.x; i < n; i += 1024) s += part[i];
+    for (int i = threadIdx.x; i < n; i += 1024 * 8) {
+        double v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = i + k * 1024 < n ? part[i + k * 1024] : 0.;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += v[k];
+    }
     s = block_sum_double(s, red);
     if (threadIdx.x == 0) norm[0] = (float)sqrt(s);
 }
