@@ -666,7 +666,7 @@ def rlhf_op_embed(table, tokens, out, scale: float = 1.0) -> None:
 
 def rlhf_op_embed_grad(dout, tokens, dtable, scale: float = 1.0, accumulate: bool = False, scratch=None) -> None:
     """dtable[v] = scale * sum of dout[r] over the rows with tokens[r] == v, added to dtable[v] with accumulate; dout [rows, d], dtable
-    [vocab, d].  scratch: uint8, rlhf_op_embed_grad_scratch_bytes entries."""
+    [vocab, d].  scratch: uint8, rlhf_op_embed_grad_scratch_bytes entries (few rows need none)."""
     import torch
     (vocab, d), rows = dtable.shape, tokens.numel()
     _on_device(dout, tokens, dtable, scratch)

@@ -32,7 +32,7 @@ template <typename T, int N = 16 / sizeof(T)> struct Vec {
     uint32_t w[WORDS];
     typedef uint32_t Words __attribute__((ext_vector_type(WORDS), aligned(2), may_alias));
     // ONCE: what nobody reads again soon, evict-first in the L2 (policy loss of 8192 x 32000 bf16 201 -> 181 us).  A store of
-    // that kind has to fill its lines together with its neighbours (lanes 32 bytes apart: 80 -> 230 us for 524 MB).
+    // that kind has to fill its lines together with its neighbours (lanes 32 bytes apart: 97 -> 227 us for 524 MB of zeros).
     template <bool ONCE> __device__ __forceinline__ void load(const T* p) {
         const Words q = ONCE ? __builtin_nontemporal_load((const Words*)p) : *(const Words*)p;
 #pragma unroll

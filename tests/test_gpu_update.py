@@ -395,6 +395,24 @@ def test_embed_grad(gdt, tdt, accumulate, rows, d, vocab, kind):
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["tail", "one", "each", "padded"])
+@pytest.mark.parametrize("rows,d", [(512, 300), (513, 300), (1024, 200), (1025, 200), (2048, 100), (2049, 100), (2048, 7), (2047, 64), (512, 4101)])
+def test_embed_grad_where_few_rows_end(rows, d, kind, accumulate):
+    R = _R()
+    r = np.random.default_rng(rows + d)
+    vocab = 3000
+    tok = _tokens(r, rows, vocab, kind)
+    dout = torch.from_numpy(r.normal(size=(rows, d)).astype(np.float32)).cuda()
+    start = torch.from_numpy(r.normal(size=(vocab, d)).astype(np.float32)).half().cuda()
+    got, again = start.clone(), start.clone()
+    for g in (got, again):
+        R.rlhf_op_embed_grad(dout, torch.from_numpy(tok).cuda(), g, scale=0.7, accumulate=accumulate)
+    torch.cuda.synchronize()
+    _egrad_check(_np(got), _np(dout), tok, vocab, 0.7, "half", _np(start) if accumulate else None)
+    assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("d,vocab", [(40, 90), (1025, 33000), (4104, 50), (300, 70001)])
 @pytest.mark.parametrize("lengths", [[1] * 255, [1] * 256, [1] * 257, [31, 32, 33, 63, 64, 65, 95, 96, 97, 1, 2], [8] * 100, [64] * 20, [1, 640, 1], [33] * 30,
                                      [500, 7, 500], [2000, 32, 1, 96]], ids=lambda l: f"{len(l)}x{l[0]}")
