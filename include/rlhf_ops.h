@@ -223,7 +223,8 @@ int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* dout, int64_
 
 /* The gradients of a model: n_tensors entries in HOST memory, read before a call returns.  src: n elements of dtype
  * (RLHF_FP32, RLHF_BF16, 2 = IEEE half), contiguous.  dst: where the clipped gradient goes, in the same type: src itself,
- * or memory that overlaps no other entry's; NULL where only the norm is taken. */
+ * or memory that no entry's src or other dst shares; NULL where only the norm is taken.  Clipping refuses a list whose
+ * dst are not so, the same gradient listed twice in place among them; the norm counts each entry, whatever it shares. */
 typedef struct rlhf_tensor {
     const void* src;
     void* dst;

@@ -683,7 +683,8 @@ def rlhf_op_embed_grad(dout, tokens, dtable, scale: float = 1.0, accumulate: boo
 
 class rlhf_tensor_list:
     """The gradients of a model for rlhf_op_grad_norm and rlhf_op_clip_grads: contiguous tensors, and where each goes when it is
-    clipped (None: in place).  Holds on to the tensors, whose memory must stay where it is."""
+    clipped (None: in place).  Holds on to the tensors, whose memory must stay where it is: gradients that are made anew, as
+    after zero_grad(set_to_none=True), need a new list.  One gradient of tied weights is listed once."""
 
     def __init__(self, src, dst=None):
         self.src = list(src)

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 #include <new>
@@ -353,11 +354,31 @@ static bool grad_tensors(const rlhf_tensor* t, int n, bool write, std::vector<Gr
         const int dt = act_of(t[i].dtype);
         if (dt < 0 || t[i].n < 0) return false;
         if (t[i].n == 0) continue;
-        const size_t bytes = (size_t)t[i].n * elem_bytes(dt);
         if (!t[i].src || !aligned(t[i].src, elem_bytes(dt)) || (write && !t[i].dst) || !aligned(t[i].dst, elem_bytes(dt)))
             return false;
-        if (write && t[i].dst != t[i].src && overlap(t[i].src, bytes, t[i].dst, bytes)) return false;
         out->push_back(GradTensor{t[i].src, t[i].dst, (size_t)t[i].n, dt});
+    }
+    return true;
+}
+
+// Whether every dst is memory of its own: shared with no other entry, and with its own src only as a whole.  Where two entries
+// write the same memory, or one writes what another reads, the workgroups' order would decide what is scaled, and how often.
+static bool apart(const std::vector<GradTensor>& v) {
+    struct Range { uintptr_t from, to; bool write; };
+    std::vector<Range> r;
+    r.reserve(2 * v.size());
+    for (const GradTensor& t : v) {
+        const size_t bytes = t.n * elem_bytes(t.dtype);
+        r.push_back({(uintptr_t)t.dst, (uintptr_t)t.dst + bytes, true});
+        if (t.src != t.dst) r.push_back({(uintptr_t)t.src, (uintptr_t)t.src + bytes, false});
+    }
+    const auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
+    if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
+    uintptr_t end = 0, written = 0;               // of all ranges so far, and of those that are written
+    for (const Range& x : r) {
+        if (x.from < (x.write ? end : written)) return false;
+        end = std::max(end, x.to);
+        if (x.write) written = std::max(written, x.to);
     }
     return true;
 }
@@ -379,7 +400,7 @@ extern "C" int rlhf_op_grad_norm(const rlhf_tensor* tensors, int n_tensors, floa
 
 extern "C" int rlhf_op_clip_grads(const rlhf_tensor* tensors, int n_tensors, const float* norm, float max_norm, void* stream) try {
     std::vector<GradTensor> v;
-    if (!norm || !(max_norm > 0.f) || !grad_tensors(tensors, n_tensors, true, &v)) return RLHF_EINVAL;
+    if (!norm || !(max_norm > 0.f) || !grad_tensors(tensors, n_tensors, true, &v) || !apart(v)) return RLHF_EINVAL;
     return status_of(launch_clip_grads((hipStream_t)stream, v.data(), (int)v.size(), norm, max_norm));
 } catch (const std::bad_alloc&) {
     return RLHF_ENOMEM;

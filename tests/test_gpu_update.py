@@ -580,6 +580,26 @@ def test_norm_of_nothing_and_zeros():
     assert float(norm) == 0.0 and not z.any()
 
 
+def test_a_gradient_listed_twice_is_counted_twice_and_not_clipped():
+    """Tied weights have one gradient: a list that holds it twice is refused before anything is scaled."""
+    R = _R()
+    t = _grads(3, [(1000,), (37, 11)], ("fp32",))
+    before = [_np(x) for x in t]
+    lst, norm = R.rlhf_tensor_list([t[0], t[1], t[0]]), torch.zeros(1, device="cuda")
+    R.rlhf_op_grad_norm(lst, norm)
+    with pytest.raises(R.RlhfError) as e:
+        R.rlhf_op_clip_grads(lst, norm, 0.1)
+    assert e.value.code == R.RLHF_EINVAL
+    flat = torch.full((3000,), 5.0, device="cuda")
+    with pytest.raises(R.RlhfError):
+        R.rlhf_op_clip_grads(R.rlhf_tensor_list([t[0], t[1].view(-1)], [flat[:1000], flat[999:1406]]), norm, 0.1)
+    torch.cuda.synchronize()
+    want = U.grad_norm([before[0], before[1], before[0]])
+    assert abs(float(norm) - want) <= 1.001 * E * want and (flat == 5.0).all()
+    for x, b in zip(t, before):
+        np.testing.assert_array_equal(_np(x), b)
+
+
 def test_norm_combined_between_the_calls():
     """The norm that clipping goes by is the caller's: here as of two ranks with the same gradients."""
     R = _R()

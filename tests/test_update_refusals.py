@@ -63,6 +63,31 @@ def test_grad_list(entry):
         assert R.lib().rlhf_op_grad_norm_scratch_doubles(arr, 2) == 0
 
 
+@pytest.mark.parametrize("entries", [
+    [(A, A, 100), (A, A, 100)], [(A, A, 100), (B, B, 50), (A + 200, A + 200, 10)], [(A, B, 100), (D, B, 100)], [(A, B, 100), (D, B + 399, 1)],
+    [(A, B, 100), (B, D, 100)], [(D, D, 10), (B, A, 100), (A + 396, E, 100)], [(A, A, 100), (A, B, 100)], [(A, A + 400 - 4, 100)],
+    [(A + 4, A, 100)], [(B, B, 5)] + [(A + 400 * k, A + 400 * k, 100) for k in range(300)] + [(A + 400 * 200 - 4, E, 1)],
+], ids=lambda e: f"{len(e)}")
+def test_clipping_refuses_memory_that_two_entries_share(entries):
+    """A gradient listed twice in place would be scaled once or twice, as its workgroups happen to run."""
+    R = _R()
+    arr = (R.rlhf_tensor * len(entries))(*(R.rlhf_tensor(s, d, n, 0) for s, d, n in entries))
+    assert R.lib().rlhf_op_clip_grads(arr, len(entries), E + (1 << 20), 1.0, None) == R.RLHF_EINVAL
+
+
+@pytest.mark.parametrize("entries", [
+    [(A, A, 100), (A + 400, A + 400, 100), (A - 400, A - 400, 100)], [(A, B, 100), (A, D, 100), (A + 200, E, 10)], [(A, A, 0), (A, A, 100)],
+    [(A, A + 400, 100), (A + 800, A + 1200, 100)],
+], ids=str)
+def test_clipping_takes_neighbours_and_sources_listed_twice(entries):
+    R = _R()
+    arr = (R.rlhf_tensor * len(entries))(*(R.rlhf_tensor(s, d, n, 0) for s, d, n in entries))
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not memory: only without a device does nothing read them")
+    assert R.lib().rlhf_op_clip_grads(arr, len(entries), E + (1 << 20), 1.0, None) == R.RLHF_EDEVICE
+
+
 def test_grad_arguments():
     R = _R()
     L, arr = R.lib(), (R.rlhf_tensor * 1)(R.rlhf_tensor(A, A, 100, 0))
