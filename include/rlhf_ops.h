@@ -221,8 +221,8 @@ int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* dout, int64_
                        int accumulate, void* dtable, int64_t ld_table, void* scratch, int rows, int d, int vocab,
                        void* stream);
 
-/* The gradients of a model: n_tensors entries in HOST memory, read before a call returns.  src: n elements of dtype
- * (RLHF_FP32, RLHF_BF16, 2 = IEEE half), contiguous.  dst: where the clipped gradient goes, in the same type: src itself,
+/* The gradients of a model: n_tensors entries in HOST memory, read before a call returns.  src: n elements (fewer than
+ * 2^40) of dtype (RLHF_FP32, RLHF_BF16, 2 = IEEE half), contiguous.  dst: where the clipped gradient goes, in the same type: src itself,
  * or memory that no entry's src or other dst shares; NULL where only the norm is taken.  Clipping refuses a list whose
  * dst are not so, the same gradient listed twice in place among them; the norm counts each entry, whatever it shares. */
 typedef struct rlhf_tensor {

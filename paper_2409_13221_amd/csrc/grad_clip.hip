@@ -15,7 +15,8 @@ constexpr int kPackTensors = 128;
 struct PackTensor {
     const void* src;
     void* dst;
-    uint64_t n : 40, first : 22, dtype : 2;        // elements, the tensor's first chunk, type: 24 bytes in all, 3 KB a launch
+    // elements, the tensor's first chunk (at most 16384 of vectors_of and one more a tensor), type: 24 bytes in all, 3 KB a launch
+    uint64_t n : 40, first : 22, dtype : 2;
 };
 struct Pack {
     PackTensor t[kPackTensors];
@@ -179,7 +180,6 @@ static hipError_t each_pack(const GradTensor* t, int n, bool backwards, Launch l
         size_t chunks = 0;
         for (int i = 0; i < pk.tensors; ++i) {
             const GradTensor& g = t[at + i];
-            if (g.n >> 40 || chunks >> 22) return hipErrorInvalidValue;
             pk.t[i] = PackTensor{g.src, g.dst, g.n, chunks, (uint64_t)g.dtype};
             chunks += chunks_of(g, vectors);
         }

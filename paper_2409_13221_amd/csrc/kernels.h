@@ -257,6 +257,8 @@ size_t embed_grad_scratch_bytes(int rows, int d, int vocab);
 hipError_t launch_embed_grad(hipStream_t st, int gdt, int tdt, const void* dout, size_t ld_dout, const int* tokens, float scale,
                              bool accumulate, void* dtable, size_t ld_table, void* scratch, int rows, int d, int vocab);
 
+// n below kMaxGradElements, which the caller checks for the whole list: launches go out before its end has been looked at.
+constexpr int64_t kMaxGradElements = 1ll << 40;
 struct GradTensor { const void* src; void* dst; size_t n; int dtype; };
 size_t grad_norm_scratch_doubles(const GradTensor* t, int n);
 hipError_t launch_grad_norm(hipStream_t st, const GradTensor* t, int n, float* norm, double* scratch);

@@ -352,7 +352,7 @@ static bool grad_tensors(const rlhf_tensor* t, int n, bool write, std::vector<Gr
     out->reserve((size_t)n);
     for (int i = 0; i < n; ++i) {
         const int dt = act_of(t[i].dtype);
-        if (dt < 0 || t[i].n < 0) return false;
+        if (dt < 0 || t[i].n < 0 || t[i].n >= kMaxGradElements) return false;
         if (t[i].n == 0) continue;
         if (!t[i].src || !aligned(t[i].src, elem_bytes(dt)) || (write && !t[i].dst) || !aligned(t[i].dst, elem_bytes(dt)))
             return false;

@@ -75,6 +75,18 @@ def test_clipping_refuses_memory_that_two_entries_share(entries):
     assert R.lib().rlhf_op_clip_grads(arr, len(entries), E + (1 << 20), 1.0, None) == R.RLHF_EINVAL
 
 
+@pytest.mark.parametrize("n", [1 << 40, 1 << 62, (1 << 63) - 1])
+@pytest.mark.parametrize("at", [0, 140, 299])
+def test_a_count_beyond_any_memory_is_refused_before_a_launch(at, n):
+    """Lists go out 128 tensors a launch: a bad entry behind the first 128 must not leave some of the others clipped."""
+    R = _R()
+    arr = (R.rlhf_tensor * 300)(*(R.rlhf_tensor(A + 400 * k, A + 400 * k, 100, 0) for k in range(300)))
+    arr[at] = R.rlhf_tensor(B, B, n, 0)
+    assert R.lib().rlhf_op_clip_grads(arr, 300, E, 1.0, None) == R.RLHF_EINVAL
+    assert R.lib().rlhf_op_grad_norm(arr, 300, E, E + 8, None) == R.RLHF_EINVAL
+    assert R.lib().rlhf_op_grad_norm_scratch_doubles(arr, 300) == 0
+
+
 @pytest.mark.parametrize("entries", [
     [(A, A, 100), (A + 400, A + 400, 100), (A - 400, A - 400, 100)], [(A, B, 100), (A, D, 100), (A + 200, E, 10)], [(A, A, 0), (A, A, 100)],
     [(A, A + 400, 100), (A + 800, A + 1200, 100)],
