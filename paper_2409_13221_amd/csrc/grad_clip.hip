@@ -160,8 +160,9 @@ static size_t chunks_of(const GradTensor& t, size_t vectors) {
 }
 
 size_t grad_norm_scratch_doubles(const GradTensor* t, int n) {
+    const size_t vectors = vectors_of(t, n);
     size_t c = 0;
-    for (int i = 0; i < n; ++i) c += chunks_of(t[i], vectors_of(t, n));
+    for (int i = 0; i < n; ++i) c += chunks_of(t[i], vectors);
     return c;
 }
 

@@ -87,6 +87,16 @@ def test_a_count_beyond_any_memory_is_refused_before_a_launch(at, n):
     assert R.lib().rlhf_op_grad_norm_scratch_doubles(arr, 300) == 0
 
 
+def test_scratch_of_a_long_list_takes_one_pass():
+    """A pass over the list for each of its entries would be 4 * 10^10 steps."""
+    import time
+    R, n = _R(), 200000
+    arr = (R.rlhf_tensor * n)(*(R.rlhf_tensor(A, A, 5000, k % 3) for k in range(n)))
+    t = time.perf_counter()
+    doubles = R.lib().rlhf_op_grad_norm_scratch_doubles(arr, n)
+    assert doubles == n and time.perf_counter() - t < 2.0
+
+
 @pytest.mark.parametrize("entries", [
     [(A, A, 100), (A + 400, A + 400, 100), (A - 400, A - 400, 100)], [(A, B, 100), (A, D, 100), (A + 200, E, 10)], [(A, A, 0), (A, A, 100)],
     [(A, A + 400, 100), (A + 800, A + 1200, 100)],
