@@ -177,7 +177,8 @@ int rlhf_op_head_dot(int act_dtype, int w_dtype, const void* xn, const void* w, 
 
 /* ---- the Actor's update, as the training stage takes it up from the stage's results: the loss on the logits of a
  * forward pass with its gradient, the embedding lookup with its gradient, and the norm and clipping of all
- * gradients.  All of them can be captured into a graph; a scratch buffer belongs to one call at a time (calls
+ * gradients.  Columns of one buffer, side by side, do not overlap (row strides of the same number of bytes; of different ones, matrices
+ * that interleave count as overlapping).  All of them can be captured into a graph; a scratch buffer belongs to one call at a time (calls
  * ordered on one stream may share it, graphs that may run at the same time may not). */
 
 /* Clipped policy loss with a KL term towards the Reference, on logits, forward and gradient in one pass.  Row r of logits

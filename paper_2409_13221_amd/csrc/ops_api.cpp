@@ -277,14 +277,19 @@ extern "C" int rlhf_op_bf16_to_half(const void* src, void* dst, int64_t n, void*
 
 // ---- the Actor's update
 
-static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return x < y + nb && y < x + na;
-}
 static size_t elem_bytes(int dt) { return dt == kF32 ? 4 : 2; }
-// bytes from the first to behind the last element of a matrix
-static size_t span(int rows, int cols, int64_t ld, int dt) {
-    return rows > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem_bytes(dt) : 0;
+// A matrix that an operator reads or writes: its elements lie in `rows` pieces of `width` bytes, `step` bytes apart.
+struct Matrix { uintptr_t at; size_t rows, width, step; };
+static Matrix matrix(const void* p, int rows, int cols, int64_t ld, int dt) {
+    return Matrix{(uintptr_t)p, (size_t)rows, (size_t)cols * elem_bytes(dt), (size_t)ld * elem_bytes(dt)};
+}
+// Matrices that share an element, or might (of different steps, and interleaved).
+static bool overlap(const Matrix& a, const Matrix& b) {
+    if (a.rows == 0 || b.rows == 0) return false;
+    if (a.at >= b.at + (b.rows - 1) * b.step + b.width || b.at >= a.at + (a.rows - 1) * a.step + a.width) return false;
+    if (a.step != b.step) return true;
+    const size_t behind = a.at <= b.at ? (b.at - a.at) % a.step : (a.step - (a.at - b.at) % a.step) % a.step;     // b's columns, behind a's
+    return behind < a.width || behind + b.width > a.step;
 }
 static bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 
@@ -305,7 +310,7 @@ extern "C" int rlhf_op_policy_loss(int logit_dtype, const void* logits, int64_t 
         return RLHF_EINVAL;
     if (!aligned(logits, elem_bytes(dt)) || !aligned(dlogits, elem_bytes(dt))) return RLHF_EINVAL;
     if (dlogits && !(dlogits == logits && ld_grad == ld) &&
-        overlap(logits, span(rows, vocab, ld, dt), dlogits, span(rows, vocab, ld_grad, dt)))
+        overlap(matrix(logits, rows, vocab, ld, dt), matrix(dlogits, rows, vocab, ld_grad, dt)))
         return RLHF_EINVAL;
     PolicyArgs a;
     a.logits = logits; a.ld = (size_t)ld; a.tokens = tokens;
@@ -322,7 +327,7 @@ extern "C" int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, 
     if (tdt < 0 || odt < 0 || rows < 0 || d < 1 || vocab < 1 || ld_table < d || ld_out < d) return RLHF_EINVAL;
     if (rows == 0) return RLHF_OK;
     if (!table || !tokens || !out || !aligned(table, elem_bytes(tdt)) || !aligned(out, elem_bytes(odt)) ||
-        overlap(table, span(vocab, d, ld_table, tdt), out, span(rows, d, ld_out, odt)))
+        overlap(matrix(table, vocab, d, ld_table, tdt), matrix(out, rows, d, ld_out, odt)))
         return RLHF_EINVAL;
     return status_of(launch_embed_rows((hipStream_t)stream, tdt, odt, table, (size_t)ld_table, tokens, scale, out,
                                        (size_t)ld_out, rows, d, vocab));
@@ -340,7 +345,7 @@ extern "C" int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* d
         !aligned(dtable, elem_bytes(tdt)))
         return RLHF_EINVAL;
     if (rows > 0 && (!dout || !tokens || (!scratch && embed_grad_scratch_bytes(rows, d, vocab) > 0) || !aligned(dout, elem_bytes(gdt)) || !aligned(scratch, 16) ||
-                     overlap(dout, span(rows, d, ld_dout, gdt), dtable, span(vocab, d, ld_table, tdt))))
+                     overlap(matrix(dout, rows, d, ld_dout, gdt), matrix(dtable, vocab, d, ld_table, tdt))))
         return RLHF_EINVAL;
     return status_of(launch_embed_grad((hipStream_t)stream, gdt, tdt, dout, (size_t)ld_dout, tokens, scale, accumulate != 0,
                                        dtable, (size_t)ld_table, scratch, rows, d, vocab));

@@ -150,6 +150,42 @@ def test_policy_loss_in_place_and_guard_columns(dtype, rows, vocab, pad):
         assert (out[:, vocab:] == 5.0).all() and base[:, vocab:].isnan().all()
 
 
+@pytest.mark.parametrize("rows,vocab", [(5, 200), (7, 3001), (3, 32000), (2, 190001)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_policy_loss_side_by_side(dtype, rows, vocab):
+    """Logits and gradient as columns of one buffer, neighbours of each other: each stays inside its own."""
+    c = _policy_case(13, rows, vocab, dtype)
+    both = torch.full((rows, 2 * vocab + 1), 5.0, device="cuda", dtype=TDT[dtype])
+    both[:, :vocab] = c["logits"]
+    lp, stats = torch.empty(rows, device="cuda"), torch.empty(4, device="cuda")
+    _R().rlhf_op_policy_loss(both[:, :vocab], c["tokens"], c["lp_old"], c["adv"], lp, stats, dlogits=both[:, vocab:2 * vocab], lp_ref=c["lp_ref"],
+                             weight=c["weight"], kl_coef=0.1)
+    torch.cuda.synchronize()
+    assert torch.equal(both[:, :vocab], c["logits"]) and (both[:, 2 * vocab] == 5.0).all()
+    # (a row off its boundary is dealt to the threads otherwise, so that its sum may round otherwise: no comparison of bits)
+    _policy_check(c, (lp, stats, both[:, vocab:2 * vocab]), dtype, kl_coef=0.1)
+
+
+@pytest.mark.parametrize("rows,d", [(40, 33), (3000, 100)])
+def test_embedding_side_by_side(rows, d):
+    """Table and rows as columns of one buffer."""
+    R = _R()
+    r = np.random.default_rng(rows)
+    both = torch.from_numpy(r.normal(size=(rows, 2 * d)).astype(np.float32)).cuda()
+    table, out = both[:, :d], both[:, d:]
+    before, tok = _np(table), _tokens(r, rows, rows, "padded")
+    tk = torch.from_numpy(tok).cuda()
+    R.rlhf_op_embed(table, tk, out, scale=2.0)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(_np(table), before)
+    rows_out = _np(out)
+    np.testing.assert_array_equal(rows_out, U.embed(before, tok, 2.0))
+    R.rlhf_op_embed_grad(out, tk, table, scale=2.0)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(_np(out), rows_out)
+    _egrad_check(_np(table), rows_out, tok, rows, 2.0, "fp32")
+
+
 @pytest.mark.parametrize("vocab", [33, 32000, 140001])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
 def test_policy_loss_left_out_rows(dtype, vocab):

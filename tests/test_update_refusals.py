@@ -28,6 +28,29 @@ def test_policy_loss(bad):
     assert R.lib().rlhf_op_policy_loss(*dict(POLICY, **bad).values()) == R.RLHF_EINVAL
 
 
+SIDE_BY_SIDE = "columns of one buffer, side by side, share no element: launched, which fails here for want of a device"
+
+
+def _launches(rc):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not memory: only without a device does nothing read them")
+    return rc() == _R().RLHF_EDEVICE
+
+
+@pytest.mark.parametrize("cols,overlap", [(100, False), (101, False), (99, True), (102, True), (150, True), (-100, False), (-101, False), (-99, True), (-102, True), (0, False),
+                                          (301, False), (300, True), (700, True)])
+def test_policy_loss_side_by_side(cols, overlap):
+    """Logits and gradient as columns of one buffer with rows of 201, the gradient `cols` columns behind (0: in place)."""
+    R = _R()
+    args = dict(POLICY, ld=201, ld_grad=201, dlogits=A + 4 * cols).values()
+    rc = lambda: R.lib().rlhf_op_policy_loss(*args)
+    if overlap:
+        assert rc() == R.RLHF_EINVAL
+    else:
+        assert _launches(rc), SIDE_BY_SIDE
+
+
 EMBED = dict(tdt=0, odt=1, table=A, ld=64, tokens=B, scale=1.0, out=D, ld_out=64, rows=8, d=64, vocab=10, stream=None)
 
 
@@ -50,6 +73,19 @@ EGRAD = dict(gdt=0, tdt=0, dout=A, ld=64, tokens=B, scale=1.0, acc=0, dtable=D, 
 def test_embed_grad(bad):
     R = _R()
     assert R.lib().rlhf_op_embed_grad(*dict(EGRAD, **bad).values()) == R.RLHF_EINVAL
+
+
+@pytest.mark.parametrize("cols,overlap", [(64, False), (63, True), (-64, False), (-65, True), (193, True), (192, False)])
+def test_embedding_side_by_side(cols, overlap):
+    """Table and rows as columns of one buffer with rows of 128."""
+    R = _R()
+    calls = [lambda: R.lib().rlhf_op_embed(*dict(EMBED, odt=0, ld=128, ld_out=128, out=A + 4 * cols).values()),
+             lambda: R.lib().rlhf_op_embed_grad(*dict(EGRAD, ld=128, ld_table=128, dtable=A + 4 * cols).values())]
+    for rc in calls:
+        if overlap:
+            assert rc() == R.RLHF_EINVAL
+        else:
+            assert _launches(rc), SIDE_BY_SIDE
 
 
 @pytest.mark.parametrize("entry", [(None, D, 4, 0), (A, D, -1, 0), (A, D, 4, 3), (A + 2, D, 4, 0), (A, D + 2, 4, 0), (A, A + 8, 4, 0), (A, None, 4, 0)])
