@@ -215,7 +215,8 @@ int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, int64_t ld_
  * (zeros where no row has the token); with accumulate != 0 that sum is added to dtable[v] instead and rows of other
  * tokens are left as they are.  The rows of a token are summed in float, in an order that depends on the tokens alone:
  * the same call gives the same bits.  Rows with tokens outside [0, vocab) count for nothing.  Types and strides as
- * above, dout in dout_dtype, dtable in table_dtype.  dout and dtable must not overlap.
+ * above, dout in dout_dtype, dtable in table_dtype.  dout and dtable must not overlap.  Matrices of hundreds of GB, which no launch
+ * covers, are refused before anything is written.
  * scratch: rlhf_op_embed_grad_scratch_bytes(rows, d, vocab) bytes, 16-byte aligned (none for few rows: NULL will do). */
 int64_t rlhf_op_embed_grad_scratch_bytes(int rows, int d, int vocab);
 int rlhf_op_embed_grad(int dout_dtype, int table_dtype, const void* dout, int64_t ld_dout, const int32_t* tokens, float scale,

@@ -2,6 +2,8 @@
 // rows of 4096 bf16 17 us = 5.6 TB/s.  The gradient is bound by memory where the table is large (8192 rows of 4096 bf16 into
 // 32000 x 4096 float 123 us = 4.8 TB/s, into bf16 76 us), and by the round trips that depend on each other where it is small
 // (tokens, places, rows, chunks: 32768 rows of 768 half, half of them one token, 55 us where memory alone would take 18).
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "vec.h"
@@ -594,8 +596,12 @@ static void embed_rows(hipStream_t st, const T* table, size_t ld_table, const in
                        int vocab) {
     const Grid g = grid_of(out, ld_out, d, Shape<T, O>::C, Shape<T, O>::H);
     const int per = 256 >> g.wide_log2;
-    k_embed_rows<T, O><<<dim3((rows + per - 1) / per, g.slices), 256, 0, st>>>(table, ld_table, tokens, out, ld_out, scale, rows, d, vocab,
-                                                                              g.wide_log2);
+    const int64_t most = kLaunchThreads / 256 * per;
+    for (int64_t first = 0; first < rows; first += most) {
+        const int part = (int)std::min<int64_t>(most, rows - first);
+        k_embed_rows<T, O><<<dim3((part + per - 1) / per, g.slices), 256, 0, st>>>(table, ld_table, tokens + first, out + first * ld_out, ld_out, scale,
+                                                                                  part, d, vocab, g.wide_log2);
+    }
 }
 
 hipError_t launch_embed_rows(hipStream_t st, int tdt, int odt, const void* table, size_t ld_table, const int* tokens, float scale,
@@ -652,7 +658,7 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
     if (rows > 0 && few_rows(rows, a.d)) {
         if (!ACCUMULATE) {
             const Clear whole = first_rows(dtable, a.ld_table, a.d, vocab);
-            if (clear_blocks<1024>(whole) > INT32_MAX) return hipErrorInvalidValue;
+            if (clear_blocks<1024>(whole) > kLaunchThreads / 1024) return hipErrorInvalidValue;
             k_group_and_clear<T><<<(unsigned)clear_blocks<1024>(whole), 1024, 0, st>>>(tokens, 0, vocab, a.b, places, runs, total, dtable, whole);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
@@ -674,7 +680,7 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
     a.window = rows >= 8192 ? 8 : rows >= 1024 ? rows / 1024 : 1;
     const int64_t windows = (rows + a.window * per - 1) / (a.window * per);
     const int64_t table = ((a.c.count + per - 1) / per + (windows + 7) / 8 * 8) * g.slices;
-    if (group_blocks > INT32_MAX || table + clear > INT32_MAX) return hipErrorInvalidValue;
+    if (group_blocks > kLaunchThreads / 1024 || table + clear > kLaunchThreads / 256) return hipErrorInvalidValue;
     k_group_and_clear<T><<<(unsigned)group_blocks, 1024, group_lds_bytes(a.b), st>>>(tokens, rows, vocab, a.b, places, runs, total, dtable,
                                                                                     beside);
     hipError_t e = hipGetLastError();

@@ -233,6 +233,7 @@ hipError_t launch_gae(hipStream_t st, const float* lp_actor, const float* lp_ref
                       const GaePowers& pw, float* adv, float* ret);
 
 // ---- the Actor's update (include/rlhf_ops.h states what each computes)
+constexpr int64_t kLaunchThreads = (1ll << 32) - 1;       // of a launch along x at most: HIP refuses more
 struct PolicyArgs {
     const void* logits;         // [rows, vocab], row stride ld
     size_t ld;
@@ -244,7 +245,8 @@ struct PolicyArgs {
     void* grad;                 // [rows, vocab], row stride ld_grad; or NULL
     size_t ld_grad;
     float* lp;                  // [rows]
-    float* terms;               // [3][rows]: w * policy, w * kl, w * cut
+    float* terms;               // [3][terms_ld]: w * policy, w * kl, w * cut
+    size_t terms_ld;
     int rows, vocab;
     float lo, hi, kl_coef, grad_scale;      // lo, hi: bounds of the ratio
 };

@@ -315,7 +315,7 @@ extern "C" int rlhf_op_policy_loss(int logit_dtype, const void* logits, int64_t 
     PolicyArgs a;
     a.logits = logits; a.ld = (size_t)ld; a.tokens = tokens;
     a.weight = weight; a.lp_old = lp_old; a.lp_ref = lp_ref; a.adv = adv;
-    a.grad = dlogits; a.ld_grad = (size_t)ld_grad; a.lp = lp; a.terms = scratch;
+    a.grad = dlogits; a.ld_grad = (size_t)ld_grad; a.lp = lp; a.terms = scratch; a.terms_ld = (size_t)rows;
     a.rows = rows; a.vocab = vocab;
     a.lo = 1.f - clip_low; a.hi = 1.f + clip_high; a.kl_coef = kl_coef; a.grad_scale = grad_scale;
     return status_of(launch_policy_loss((hipStream_t)stream, dt, a, stats));

@@ -3,6 +3,8 @@
 // exponentials before the first element of the gradient, and nothing else of itself.  Logits are read once and gradients
 // written once, which is what bounds it: 8192 rows of 32000 bf16 (a tenth left out) 187 us = 5.3 TB/s, without gradient 4096
 // rows of 32000 float (a tenth left out) 74 us = 6.4 TB/s.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "vec.h"
@@ -69,8 +71,8 @@ __device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, fl
     const RowLoss o = row_loss(a, r, w, l);
     a.lp[r] = l;
     a.terms[r] = o.policy;
-    a.terms[(size_t)a.rows + r] = o.kl;
-    a.terms[(size_t)2 * a.rows + r] = o.cut;
+    a.terms[a.terms_ld + r] = o.kl;
+    a.terms[2 * a.terms_ld + r] = o.cut;
     out[0] = o.slope * a.grad_scale * (1.f - __expf(zy - M) / S);
     out[1] = -o.slope * a.grad_scale / S;
 }
@@ -83,7 +85,7 @@ template <typename T> __device__ __forceinline__ int columns_before(const T* row
 
 template <typename T>
 __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, int t, int threads) {
-    if (t < 3) a.terms[(size_t)t * a.rows + r] = 0.f;
+    if (t < 3) a.terms[t * a.terms_ld + r] = 0.f;
     if (t == 0) a.lp[r] = 0.f;
     if (!g) return;
     constexpr int N = 16 / sizeof(T);
@@ -288,15 +290,33 @@ static void policy_rows(hipStream_t st, const PolicyArgs& a) {
     k_policy_long_row<T><<<a.rows, 1024, 0, st>>>(a);
 }
 
-hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, float* stats) {
-    if (a.vocab > 1 << 30 || a.rows > 1 << 30) return hipErrorInvalidValue;          // row and column numbers are ints
-    if (a.rows > 0) {
-        if (dtype == kBF16) policy_rows<bf16_t>(st, a);
-        else if (dtype == kF16) policy_rows<f16_t>(st, a);
-        else policy_rows<float>(st, a);
+// The rows in turns of what one launch holds at the threads a row that policy_rows takes: a wave's 64 (four rows a workgroup), up to 1024.
+template <typename T>
+static hipError_t policy_parts(hipStream_t st, const PolicyArgs& a) {
+    const int64_t most = a.vocab < (8 * 64 + 1) * (16 / (int)sizeof(T)) ? kLaunchThreads / 256 * 4 : kLaunchThreads / 1024;
+    for (int64_t first = 0; first < a.rows; first += most) {
+        PolicyArgs p = a;
+        p.logits = (const T*)a.logits + first * a.ld;
+        p.grad = a.grad ? (T*)a.grad + first * a.ld_grad : nullptr;
+        p.tokens += first;
+        p.weight = a.weight ? a.weight + first : nullptr;
+        p.lp_old += first;
+        p.lp_ref = a.lp_ref ? a.lp_ref + first : nullptr;
+        p.adv += first;
+        p.lp += first;
+        p.terms += first;
+        p.rows = (int)std::min<int64_t>(most, a.rows - first);
+        policy_rows<T>(st, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
+    return hipSuccess;
+}
+
+hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, float* stats) {
+    if (a.vocab > 1 << 30 || a.rows > 1 << 30) return hipErrorInvalidValue;          // row and column numbers are ints
+    const hipError_t e = dtype == kBF16 ? policy_parts<bf16_t>(st, a) : dtype == kF16 ? policy_parts<f16_t>(st, a) : policy_parts<float>(st, a);
+    if (e != hipSuccess) return e;
     const int blocks = stats_blocks(a.rows);
     float* part = a.terms + (size_t)3 * a.rows;
     if (blocks > 0) k_policy_stats<1024><<<blocks, 1024, 0, st>>>(a.terms, a.rows, kStatsRows, a.kl_coef, part, nullptr);

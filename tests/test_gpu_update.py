@@ -350,6 +350,29 @@ def test_policy_loss_offsets_beyond_32_bits():
     assert torch.equal(d, want[2]) and torch.equal(lp, want[0]) and torch.equal(stats, want[1])
 
 
+def test_policy_loss_of_more_rows_than_a_launch_has_waves():
+    """A launch has fewer than 2^32 threads, 64 of them a row at the least."""
+    rows = 2 ** 26 + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.randn(rows, 2, device="cuda", generator=g)
+    tok = torch.randint(0, 2, (rows,), device="cuda", dtype=torch.int32, generator=g)
+    adv, w = torch.randn(rows, device="cuda", generator=g), torch.full((rows,), 2.0 ** -26, device="cuda")
+    l = torch.log_softmax(z.double(), 1)
+    p = torch.exp(l)
+    l = l.gather(1, tok.long()[:, None])[:, 0]
+    lp, stats, d = torch.full((rows,), 7.0, device="cuda"), torch.full((4,), 7.0, device="cuda"), torch.full_like(z, 7.0)
+    _R().rlhf_op_policy_loss(z, tok, l.float(), adv, lp, stats, dlogits=d, weight=w, grad_scale=2.0 ** 26)
+    torch.cuda.synchronize()
+    # |l| is at most 12: l by _policy_check's tolerance, the ratio by that and the rounding of lp_old
+    tol = E * (64 + 8 * 12)
+    assert float((lp.double() - l).abs().max()) <= tol
+    a = adv.double()
+    want = -float(a.sum()) * 2.0 ** -26
+    assert abs(float(stats[1]) - want) <= 2 * tol * float(a.abs().sum()) * 2.0 ** -26 and float(stats[3]) == 0.0
+    dl = p.mul_(a[:, None]).scatter_add_(1, tok.long()[:, None], -a[:, None])           # -A (onehot - p)
+    assert float((d.double() - dl).abs().sub_(4 * tol * a.abs()[:, None]).max()) <= 0.0
+
+
 # ------------------------------------------------------------------------------- embedding and gradient
 
 def _tokens(r, rows, vocab, kind):
@@ -392,6 +415,18 @@ def test_embed_token_beyond_the_vocabulary_and_no_rows():
     assert out[0].isnan().all() and not out[1].any() and (out[2] == 1).all()
     R.rlhf_op_embed(table, torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, 10, device="cuda"))
     torch.cuda.synchronize()
+
+
+def test_embed_of_more_rows_than_a_launch_has_threads():
+    """A launch has fewer than 2^32 threads, 8 of them a row at the least."""
+    rows, vocab = 2 ** 29 + 77, 7
+    table = torch.arange(1, vocab + 1, device="cuda", dtype=torch.bfloat16)[:, None]
+    tok = torch.arange(rows, device="cuda", dtype=torch.int32).remainder_(vocab)
+    out = torch.zeros(rows, 1, device="cuda", dtype=torch.bfloat16)
+    _R().rlhf_op_embed(table, tok, out, scale=0.5)
+    torch.cuda.synchronize()
+    for i in range(0, rows, 2 ** 27):
+        assert torch.equal(out[i:i + 2 ** 27, 0].float(), (tok[i:i + 2 ** 27] + 1).float() * 0.5)
 
 
 def _egrad_check(got, dout, tok, vocab, scale, odt, start=None):
@@ -514,6 +549,23 @@ def test_embedding_offsets_beyond_32_bits(rows):
     R.rlhf_op_embed_grad(out, tk, table)
     torch.cuda.synchronize()
     _egrad_check(_np(table), _np(out), tok, vocab, 1.0, "fp32")
+
+
+@pytest.mark.parametrize("rows", [100, 3000])
+def test_embedding_gradient_of_the_largest_vocabulary(rows):
+    R = _R()
+    r = np.random.default_rng(rows)
+    vocab = 2 ** 30
+    tok = r.integers(0, vocab, rows).astype(np.int32)
+    tok[:40], tok[40] = vocab - 1, 0
+    dout = r.integers(-8, 9, (rows, 1)).astype(np.float32)                  # sums are exact in every order
+    got = torch.full((vocab, 1), float("nan"), dtype=torch.half, device="cuda")
+    R.rlhf_op_embed_grad(torch.from_numpy(dout).cuda(), torch.from_numpy(tok).cuda(), got)
+    torch.cuda.synchronize()
+    used = np.unique(tok)
+    want = U.embed_grad(dout, np.searchsorted(used, tok), len(used))
+    np.testing.assert_array_equal(_np(got[torch.from_numpy(used.astype(np.int64)).cuda()]), want)
+    assert not got.isnan().any() and int(got.count_nonzero()) == np.count_nonzero(want)
 
 
 # -------------------------------------------------------------------------------- gradient norm, clipping

@@ -75,6 +75,15 @@ def test_embed_grad(bad):
     assert R.lib().rlhf_op_embed_grad(*dict(EGRAD, **bad).values()) == R.RLHF_EINVAL
 
 
+@pytest.mark.parametrize("big", [dict(vocab=1 << 20, d=1 << 22, ld=1 << 22, ld_table=1 << 22), dict(vocab=1 << 20, d=1 << 22, ld=1 << 22, ld_table=1 << 23, rows=100),
+                                 dict(rows=1 << 28, d=1 << 20, ld=1 << 20, ld_table=1 << 20, acc=1), dict(rows=(1 << 30) + 1), dict(vocab=(1 << 30) + 1),
+                                 dict(d=(1 << 22) + 1, ld=1 << 23, ld_table=1 << 23)], ids=str)
+def test_embed_grad_refuses_what_no_launch_holds(big):
+    """A launch has fewer than 2^32 threads: a second one that fails would leave the table half written."""
+    R = _R()
+    assert R.lib().rlhf_op_embed_grad(*dict(EGRAD, dtable=1 << 60, **big).values()) == R.RLHF_EINVAL
+
+
 @pytest.mark.parametrize("cols,overlap", [(64, False), (63, True), (-64, False), (-65, True), (193, True), (192, False)])
 def test_embedding_side_by_side(cols, overlap):
     """Table and rows as columns of one buffer with rows of 128."""
