@@ -233,7 +233,7 @@ hipError_t launch_gae(hipStream_t st, const float* lp_actor, const float* lp_ref
                       const GaePowers& pw, float* adv, float* ret);
 
 // ---- the Actor's update (include/rlhf_ops.h states what each computes)
-constexpr int64_t kLaunchThreads = (1ll << 32) - 1;       // of a launch along x at most: HIP refuses more
+constexpr int64_t kLaunchThreads = (1ll << 32) - 1;       // of a launch along x at most: more wrap at 2^32, and no error says so
 struct PolicyArgs {
     const void* logits;         // [rows, vocab], row stride ld
     size_t ld;

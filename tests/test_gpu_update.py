@@ -351,7 +351,7 @@ def test_policy_loss_offsets_beyond_32_bits():
 
 
 def test_policy_loss_of_more_rows_than_a_launch_has_waves():
-    """A launch has fewer than 2^32 threads, 64 of them a row at the least."""
+    """A launch has fewer than 2^32 threads, 64 of them a row at the least; of a larger one only the rest beyond 2^32 would run."""
     rows = 2 ** 26 + 5
     g = torch.Generator(device="cuda").manual_seed(1)
     z = torch.randn(rows, 2, device="cuda", generator=g)

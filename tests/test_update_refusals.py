@@ -79,7 +79,7 @@ def test_embed_grad(bad):
                                  dict(rows=1 << 28, d=1 << 20, ld=1 << 20, ld_table=1 << 20, acc=1), dict(rows=(1 << 30) + 1), dict(vocab=(1 << 30) + 1),
                                  dict(d=(1 << 22) + 1, ld=1 << 23, ld_table=1 << 23)], ids=str)
 def test_embed_grad_refuses_what_no_launch_holds(big):
-    """A launch has fewer than 2^32 threads: a second one that fails would leave the table half written."""
+    """A launch has fewer than 2^32 threads; of a larger one only the rest beyond 2^32 would run, without an error."""
     R = _R()
     assert R.lib().rlhf_op_embed_grad(*dict(EGRAD, dtable=1 << 60, **big).values()) == R.RLHF_EINVAL
 
