@@ -194,8 +194,9 @@ int rlhf_op_head_dot(int act_dtype, int w_dtype, const void* xn, const void* w, 
  * Everything is float until the gradient is rounded once.  The rows are summed in a fixed order.
  * A row with weight 0 or a negative token is left out: its logits and its other inputs, whatever they hold, are not used,
  * lp[r] = 0, its gradient is zero.  Logits of -inf have probability 0; where the token's own is, lp[r] = -inf, the ratio is 0 and the
- * KL towards lp_ref infinite.  A row whose result is not a number (all
- * logits -inf, a logit of +inf, NaN, a token of vocab or more) makes lp[r], its gradient and stats NaN.
+ * KL towards lp_ref infinite, and with kl_coef > 0 the row's gradient is not finite.  A row whose result is not a number (all
+ * logits -inf, a logit of +inf, NaN among its inputs, a token of vocab or more) makes lp[r], its gradient and stats NaN; lp[r] is a
+ * number where it does not depend on what is none (adv; lp_old of -inf beside l = -inf), and so is the KL's sum (0 without lp_ref).
  * Columns of dlogits behind vocab are left as they are.  clip_low in [0, 1], clip_high >= 0, kl_coef >= 0.  rows and vocab at most
  * 2^30.
  * scratch: rlhf_op_policy_loss_scratch_floats(rows, vocab) floats. */

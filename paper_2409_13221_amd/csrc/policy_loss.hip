@@ -20,7 +20,7 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, int r, float w,
     const auto times = [adv](float x) { return adv == 0.f && x == x ? 0.f : x * adv; };    // 0, for a ratio that overflows too
     const float u = times(rho), c = times(held);
     const bool cut = u > c;
-    RowLoss o{-(cut ? c : u) * w, 0.f, cut ? w : 0.f, cut ? 0.f : -u * w};
+    RowLoss o{-(cut ? c : u) * w, 0.f, cut ? w : u == u ? 0.f : u, cut ? 0.f : -u * w};
     if (a.lp_ref) {
         const float x = a.lp_ref[r] - l, em = expm1f(x);
         o.kl = (x == INFINITY ? x : em - x) * w;               // a token of probability 0

@@ -252,6 +252,38 @@ def test_policy_loss_rows_that_are_no_number(vocab):
     assert torch.equal(got[0][good], want[0][good]) and torch.equal(got[2][good], want[2][good])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("vocab", [1, 40, 32001, 140001, 200003])
+@pytest.mark.parametrize("what", ["-inf", "inf", "nan", "token", "both -inf", "adv"])
+def test_policy_loss_of_a_row_that_is_no_number(what, vocab, dtype):
+    """The whole row's gradient and all of the sums are NaN; without a Reference the KL's stays zero."""
+    c = _policy_case(14, 5, vocab, dtype, masked=0.0)
+    z, y = c["logits"], int(c["tokens"][2])
+    if what == "-inf":
+        z[2] = float("-inf")
+    elif what == "token":
+        c["tokens"][2] = vocab
+    elif what == "both -inf":            # the token has probability 0 now, as it had: their ratio is no number
+        if vocab == 1:
+            return
+        z[2, y], c["lp_old"][2], c["lp_ref"][2] = float("-inf"), float("-inf"), float("-inf")
+    elif what == "adv":
+        c["adv"][2] = float("nan")
+    else:
+        z[2, vocab - 1] = float(what)
+    for ref in (True, False):
+        if not ref:
+            del c["lp_ref"]
+        lp, stats, d = _policy_run(c, kl_coef=0.1 if ref else 0.0)
+        if what == "both -inf":
+            assert float(lp[2]) == float("-inf")
+        elif what != "adv":
+            assert lp[2].isnan()
+        assert d[2].isnan().all() and torch.isfinite(d[[0, 1, 3, 4]]).all()
+        assert stats[[0, 1, 3]].isnan().all()
+        assert float(stats[2]) == 0.0 if not ref else bool(stats[2].isnan()) == (what != "adv")
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("vocab", [1, 40, 63, 5003, 32001, 140001])
 def test_policy_loss_writes_nothing_for_tokens_beyond_the_vocabulary(dtype, vocab):
