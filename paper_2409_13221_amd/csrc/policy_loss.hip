@@ -232,39 +232,48 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
     if (y < V && (in < (unsigned)whole ? in / N % 1024 == (unsigned)t : y == odd)) g[(int)in] = round_to<T>(s_row[0]);
 }
 
-// Sums of the rows' terms in a fixed order: `rows` rows a workgroup, to out[3][workgroups], or for one workgroup to stats.  The threads'
-// sums meet in LDS, where a wave each takes one of the three: a third of the lane exchanges one after the other.
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void k_policy_stats(const float* __restrict__ terms, int n, int rows, float kl_coef,
-                                                          float* __restrict__ out, float* __restrict__ stats) {
+// Sums of the terms v [3][n] in a fixed order and in double: `each` of a kind a workgroup, to out[3][workgroups], or for one workgroup to
+// stats.  The threads' sums meet in LDS, where a wave each takes one of the three: a third of the lane exchanges one after
+// the other.
+template <int THREADS, typename V>
+__global__ __launch_bounds__(THREADS) void k_policy_stats(const V* __restrict__ v, int n, int each, float kl_coef, double* __restrict__ out,
+                                                          float* __restrict__ stats) {
     __shared__ double part[3][THREADS], sum[3];
-    const unsigned t = threadIdx.x, w = t >> 6, lane = t & 63, lo = blockIdx.x * (unsigned)rows, hi = min((unsigned)n, lo + (unsigned)rows);
+    const unsigned t = threadIdx.x, w = t >> 6, lane = t & 63, lo = blockIdx.x * (unsigned)each, hi = min((unsigned)n, lo + (unsigned)each);
     double s[3] = {0., 0., 0.};
     for (unsigned i = lo + t; i < hi; i += THREADS)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) s[k] += terms[(size_t)k * n + i];
+        for (int k = 0; k < 3; ++k) s[k] += v[(size_t)k * n + i];
 #pragma unroll
     for (int k = 0; k < 3; ++k) part[k][t] = s[k];
     __syncthreads();
     if (w < 3) {
-        double v = 0.;
+        double x = 0.;
 #pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) v += part[w][i * 64 + lane];
+        for (int i = 0; i < THREADS / 64; ++i) x += part[w][i * 64 + lane];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-        if (lane == 0) sum[w] = v;
+        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
+        if (lane == 0) sum[w] = x;
     }
     __syncthreads();
     if (t >= 3) return;
-    if (!stats) { out[t * gridDim.x + blockIdx.x] = (float)sum[t]; return; }
+    if (!stats) { out[t * gridDim.x + blockIdx.x] = sum[t]; return; }
     stats[1 + t] = (float)sum[t];
     if (t == 0) stats[0] = (float)(sum[0] + (kl_coef != 0.f ? kl_coef * sum[1] : 0.));
 }
+template <typename V> static void last_stats(hipStream_t st, const V* v, int n, float kl_coef, float* stats) {
+    if (n <= 1024) k_policy_stats<256, V><<<1, 256, 0, st>>>(v, n, n, kl_coef, nullptr, stats);
+    else k_policy_stats<1024, V><<<1, 1024, 0, st>>>(v, n, n, kl_coef, nullptr, stats);
+}
 
-// More rows than this are summed in two steps.
+// More rows than this are summed in two steps.  Scratch: the rows' terms, and the first step's sums, doubles of two floats each from the next
+// boundary of a double on.
 constexpr int kStatsRows = 8192;
 static int stats_blocks(int rows) { return rows > kStatsRows ? (rows + kStatsRows - 1) / kStatsRows : 0; }
-size_t policy_scratch_floats(int rows, int vocab) { return 3 * ((size_t)rows + stats_blocks(rows)); }
+size_t policy_scratch_floats(int rows, int vocab) {
+    const size_t blocks = stats_blocks(rows);
+    return 3 * ((size_t)rows + 2 * blocks) + (blocks > 0 ? 1 : 0);
+}
 
 // As few threads as hold a row with up to 8 vectors each: waves that wait for one another cost more than vectors.  us, with
 // gradient: 8192 rows of 4096 bf16: a wave a row 24.9, 2 waves 25.6, 4 28.3, 8 37.5; of 8192: 4 waves 45.9, 8 49.7, a wave 52.2;
@@ -318,12 +327,13 @@ hipError_t launch_policy_loss(hipStream_t st, int dtype, const PolicyArgs& a, fl
     const hipError_t e = dtype == kBF16 ? policy_parts<bf16_t>(st, a) : dtype == kF16 ? policy_parts<f16_t>(st, a) : policy_parts<float>(st, a);
     if (e != hipSuccess) return e;
     const int blocks = stats_blocks(a.rows);
-    float* part = a.terms + (size_t)3 * a.rows;
-    if (blocks > 0) k_policy_stats<1024><<<blocks, 1024, 0, st>>>(a.terms, a.rows, kStatsRows, a.kl_coef, part, nullptr);
-    const float* terms = blocks > 0 ? part : a.terms;
-    const int n = blocks > 0 ? blocks : a.rows;
-    if (n <= 1024) k_policy_stats<256><<<1, 256, 0, st>>>(terms, n, n, a.kl_coef, nullptr, stats);
-    else k_policy_stats<1024><<<1, 1024, 0, st>>>(terms, n, n, a.kl_coef, nullptr, stats);
+    if (blocks > 0) {
+        double* sums = (double*)(((uintptr_t)(a.terms + (size_t)3 * a.rows) + 7) / 8 * 8);
+        k_policy_stats<1024, float><<<blocks, 1024, 0, st>>>(a.terms, a.rows, kStatsRows, a.kl_coef, sums, nullptr);
+        last_stats(st, sums, blocks, a.kl_coef, stats);
+    } else {
+        last_stats(st, a.terms, a.rows, a.kl_coef, stats);
+    }
     return hipGetLastError();
 }
 

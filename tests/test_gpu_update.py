@@ -116,6 +116,24 @@ def test_policy_loss_sums_of_many_rows(rows):
     _policy_check(c, _policy_run(c, kl_coef=0.1), "fp32", kl_coef=0.1)
 
 
+@pytest.mark.parametrize("rows", [8192, 16384, 50000])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_policy_loss_sums_that_cancel(rows, offset):
+    """One column: l = 0, ratio 1, and each row's term is -A to the bit.  Sums are held in double until the end, at any number of rows and
+    with scratch on any boundary of a float."""
+    R = _R()
+    z, f = torch.zeros(rows, 1, device="cuda"), torch.zeros(rows, device="cuda")
+    adv = torch.zeros(rows, device="cuda")
+    adv[0], adv[1], adv[rows // 2], adv[-1] = 2.0 ** 24, 1.0, -2.0 ** 24, 2.0 ** -10
+    need = R.lib().rlhf_op_policy_loss_scratch_floats(rows, 1)
+    scratch = torch.full((need + offset + 8,), 3.0, device="cuda")
+    lp, stats = torch.full((rows,), 7.0, device="cuda"), torch.full((4,), 7.0, device="cuda")
+    R.rlhf_op_policy_loss(z, torch.zeros(rows, dtype=torch.int32, device="cuda"), f, adv, lp, stats, scratch=scratch[offset:offset + need])
+    torch.cuda.synchronize()
+    assert stats.tolist() == [-(1.0 + 2.0 ** -10)] * 2 + [0.0, 0.0] and not lp.any()
+    assert (scratch[offset + need:] == 3.0).all() and (scratch[:offset] == 3.0).all()
+
+
 @pytest.mark.parametrize("rows,vocab", [(3, 100), (40, 32000), (2, 140001)])
 @pytest.mark.parametrize("dtype", ["fp32", "half"])
 def test_policy_loss_without_gradient_and_options(dtype, rows, vocab):
