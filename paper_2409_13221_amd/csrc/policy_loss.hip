@@ -45,9 +45,10 @@ struct Running {
     }
 };
 
-// What joins the waves of a row (up to 16): maximum and sum of exp(z - maximum).  Every 16 lanes hold all waves' pairs.
+// What joins the waves of a row (up to 16): the maximum M, zy among it, and the sum R of exp(z - M) without zy's.  Every 16 lanes hold
+// all waves' pairs.
 template <int WAVES>
-__device__ __forceinline__ void join_row(const Running& run, float (*red)[2], float& M, float& S) {
+__device__ __forceinline__ void join_row(const Running& run, float zy, float (*red)[2], float& M, float& R) {
     const int lane = threadIdx.x & 63;
     float m = wave_max(run.m);
     float s = wave_sum(run.s * __expf(run.m - (m == -INFINITY ? 0.f : m)));
@@ -57,23 +58,25 @@ __device__ __forceinline__ void join_row(const Running& run, float (*red)[2], fl
         m = red[lane % WAVES][0];
         s = red[lane % WAVES][1];
     }
-    M = m;
+    M = fmaxf(m, zy);
 #pragma unroll
     for (int o = 1; o < WAVES; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, kWave));
-    S = s * __expf(m - M);                         // a row of -inf alone gives NaN
+    R = s * __expf(m - M);                         // a row of -inf alone gives NaN
 #pragma unroll
-    for (int o = 1; o < WAVES; o <<= 1) S += __shfl_xor(S, o, kWave);
+    for (int o = 1; o < WAVES; o <<= 1) R += __shfl_xor(R, o, kWave);
 }
 
 // Scalars of a row, by its first thread: outputs, and the gradient's factors (at the token, elsewhere) to `out`.
-__device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, float w, float zy, float M, float S, float* out) {
-    const float l = y < a.vocab ? zy - M - logf(S) : NAN;
+__device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, float w, float zy, float M, float R, float* out) {
+    const float top = __expf(zy - M), S = R + top;
+    // log of the sum and of what its rounding lost, all of R where that is far below a top of 1
+    const float l = y < a.vocab ? zy - M - (logf(S) + (R - (S - top)) * __builtin_amdgcn_rcpf(S)) : NAN;
     const RowLoss o = row_loss(a, r, w, l);
     a.lp[r] = l;
     a.terms[r] = o.policy;
     a.terms[a.terms_ld + r] = o.kl;
     a.terms[2 * a.terms_ld + r] = o.cut;
-    out[0] = o.slope * a.grad_scale * (1.f - __expf(zy - M) / S);
+    out[0] = o.slope * a.grad_scale * (R / S);
     out[1] = -o.slope * a.grad_scale / S;
 }
 
@@ -82,6 +85,21 @@ __device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, fl
 template <typename T> __device__ __forceinline__ int columns_before(const T* row, int vocab) {
     return min((int)((0 - (uintptr_t)row) % 16 / sizeof(T)), vocab);
 }
+
+// The columns of a row outside the threads' streams of vectors, a thread each: those before and behind the vectors, and the vector that
+// holds the token (`skip` of its vectors' columns; ~0u where the token is outside them).  The token's own is kept out of the sums:
+// of a token that has nearly all of the probability, what matters is what it leaves, and that cannot be had from a sum that holds the
+// token's 1 (a token 20 above 32000 others: gradient and log-prob off by 1e-3 of themselves, so 3e-7).  A branch or a select on it in
+// each vector of the stream would spill it; a vector left out costs nothing.
+struct Single {
+    unsigned skip;
+    int column;                  // of this thread; the row's length or more where it has none
+    template <int N> static __device__ __forceinline__ Single of(int y, int head, unsigned whole, int vocab, int t) {
+        const unsigned in = y - head, skip = in < whole ? in / N * N : ~0u;
+        const int token = skip != ~0u && t < 3 * N ? head + (int)skip + t - 2 * N : vocab;
+        return Single{skip, t >= 2 * N ? token : t < head ? t : t + (int)whole};
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, int t, int threads) {
@@ -108,7 +126,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
     constexpr int N = 16 / sizeof(T);
     __shared__ float red[THREADS / 64][2];
     __shared__ float s_row[2];
-    const int r = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / THREADS : 0), t = threadIdx.x % THREADS, V = a.vocab;
+    const int r = blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0), t = threadIdx.x % THREADS, V = a.vocab;
     if (ROWS > 1 && r >= a.rows) return;
     const T* z = (const T*)a.logits + (size_t)r * a.ld;
     T* g = a.grad ? (T*)a.grad + (size_t)r * a.ld_grad : nullptr;
@@ -117,18 +135,17 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
     if (y < 0 || w == 0.f) return left_out_row<T>(a, r, g, t, THREADS);
     const int head = columns_before<T>(g ? g : z, V);
     const unsigned whole = (V - head) / N * N;
-    const int odd = t < head ? t : t + (int)whole;
+    const Single one = Single::of<N>(y, head, whole, V, t);
     z += head;
     if (g) g += head;
     Vec<T> x[IT];
-    float xl[1] = {-INFINITY};
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         const unsigned i = (it * THREADS + t) * N;
-        if (i < whole) x[it].template load<true>(z + i);
+        if (i < whole && i != one.skip) x[it].template load<true>(z + i);
         else x[it].fill(-INFINITY);
     }
-    if (odd < V) xl[0] = to_f32<T>(z[odd - head]);
+    const float xl = one.column < V ? to_f32<T>(z[one.column - head]) : -INFINITY;
     const float zy = to_f32<T>(z[min(y, V - 1) - head]);
     Running run;
 #pragma unroll
@@ -138,33 +155,33 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
         run.add(f);
         x[it].forget();
     }
-    run.add(xl);
-    float M, S, row[2];
-    join_row<THREADS / 64>(run, red, M, S);
+    const float others[1] = {one.column == y ? -INFINITY : xl};
+    run.add(others);
+    float M, R, row[2];
+    join_row<THREADS / 64>(run, zy, red, M, R);
     if (ROWS > 1) {
-        finish_row(a, r, y, w, zy, M, S, row);
+        finish_row(a, r, y, w, zy, M, R, row);
         if (!g) return;
     } else {
-        if (t == 0) finish_row(a, r, y, w, zy, M, S, s_row);
+        if (t == 0) finish_row(a, r, y, w, zy, M, R, s_row);
         if (!g) return;
         __syncthreads();
         row[0] = s_row[0];
         row[1] = s_row[1];
     }
+    if (one.column < V) g[one.column - head] = round_to<T>(one.column == y ? row[0] : row[1] * __expf(xl - M));
+    int again = t;                                 // columns are numbered anew for the stores: kept, 22 of them would spill
+    asm volatile("" : "+v"(again));
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-        const unsigned i = (it * THREADS + t) * N;
+        const unsigned i = (it * THREADS + again) * N;
         float f[N];
         x[it].get(f);
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = row[1] * __expf(f[e] - M);
         x[it].set(f);
-        if (i < whole) x[it].template store<true>(g + i);
+        if (i < whole && i != one.skip) x[it].template store<true>(g + i);
     }
-    if (odd < V) g[odd - head] = round_to<T>(row[1] * __expf(xl[0] - M));
-    // the token's own column, by the thread that has just written it
-    const unsigned in = y - head;
-    if (y < V && (in < whole ? in / N % THREADS == (unsigned)t : y == odd)) g[(int)in] = round_to<T>(row[0]);
 }
 
 // Rows that no workgroup's registers hold (beyond 90000 floats, 180000 of 16 bits): read once for the statistics, and again, out of
@@ -181,8 +198,9 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
     const float w = a.weight ? a.weight[r] : 1.f;
     if (y < 0 || w == 0.f) return left_out_row<T>(a, r, g, t, 1024);
     const float zy = to_f32<T>(z[min(y, V - 1)]);
-    const int head = columns_before<T>(g ? g : z, V), whole = (V - head) / N * N, odd = t < head ? t : t + whole;
-    const float xl[1] = {odd < V ? to_f32<T>(z[odd]) : -INFINITY};
+    const int head = columns_before<T>(g ? g : z, V), whole = (V - head) / N * N;
+    const Single one = Single::of<N>(y, head, whole, V, t);
+    const float xl = one.column < V ? to_f32<T>(z[one.column]) : -INFINITY, others[1] = {one.column == y ? -INFINITY : xl};
     z += head;
     if (g) g += head;
     Running run;
@@ -191,7 +209,7 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             const int i = i0 + (it * 1024 + t) * N;
-            if (i < whole) x[it].template load<false>(z + i);
+            if (i < whole && (unsigned)i != one.skip) x[it].template load<false>(z + i);
             else x[it].fill(-INFINITY);
         }
 #pragma unroll
@@ -201,10 +219,10 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
             run.add(f);
         }
     }
-    run.add(xl);
-    float M, S;
-    join_row<16>(run, red, M, S);
-    if (t == 0) finish_row(a, r, y, w, zy, M, S, s_row);
+    run.add(others);
+    float M, R;
+    join_row<16>(run, zy, red, M, R);
+    if (t == 0) finish_row(a, r, y, w, zy, M, R, s_row);
     if (!g) return;
     __syncthreads();
     const float f = s_row[1];
@@ -213,7 +231,7 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             const int i = i0 + (it * 1024 + t) * N;
-            if (i < whole) x[it].template load<true>(z + i);
+            if (i < whole && (unsigned)i != one.skip) x[it].template load<true>(z + i);
         }
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
@@ -224,12 +242,10 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
 #pragma unroll
             for (int e = 0; e < N; ++e) d[e] = f * __expf(d[e] - M);
             x[it].set(d);
-            x[it].template store<true>(g + i);
+            if ((unsigned)i != one.skip) x[it].template store<true>(g + i);
         }
     }
-    if (odd < V) g[odd - head] = round_to<T>(f * __expf(xl[0] - M));
-    const unsigned in = y - head;
-    if (y < V && (in < (unsigned)whole ? in / N % 1024 == (unsigned)t : y == odd)) g[(int)in] = round_to<T>(s_row[0]);
+    if (one.column < V) g[one.column - head] = round_to<T>(one.column == y ? s_row[0] : f * __expf(xl - M));
 }
 
 // Sums of the terms v [3][n] in a fixed order and in double: `each` of a kind a workgroup, to out[3][workgroups], or for one workgroup to

@@ -331,6 +331,44 @@ def test_policy_loss_token_out_of_reach_and_huge_ratios():
     assert abs(float(stats[0]) - want) <= 4 * E * abs(want)
 
 
+@pytest.mark.parametrize("vocab", [2, 9, 50, 255, 1023, 4097, 8200, 20003, 32000, 65537, 140001, 200003])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("above", [6.0, 14.0, 25.0, 60.0])
+def test_policy_loss_of_confident_tokens(dtype, vocab, above):
+    """A token that holds nearly all of the probability: what it leaves, R of 1, is as precise as any other sum, and with it
+    l = -log(1 + R) and the token's gradient, a share R / (1 + R) of the slope.
+
+    A term of R is exp(-x) at a distance x of up to `above` and the spread of the others: off by (2 x + 4) E, and the sum by (V / 256 + 64) E of
+    itself, as in _policy_check; logarithm, quotient and products by 8 E more."""
+    r = np.random.default_rng(int(vocab + above))
+    rows = 12
+    z = torch.from_numpy(r.uniform(-4, 0, size=(rows, vocab + 1)).astype(np.float32)).to(TDT[dtype])
+    # at the row's ends, where columns stand outside vectors, next to them, and in between
+    y = np.array([0, 1, 3, 7, 8, vocab - 1, vocab - 2, vocab - 5, vocab - 9, vocab // 2, vocab // 3, vocab - 16]) % vocab
+    z[torch.arange(rows), torch.from_numpy(y)] = above
+    c = dict(logits=z.cuda()[:, :vocab], tokens=torch.from_numpy(y.astype(np.int32)).cuda(), adv=torch.full((rows,), -2.0, device="cuda"))
+    logp = U.log_softmax(_np(c["logits"]))
+    at = np.arange(rows), y
+    rest = logp.copy()
+    rest[at] = -np.inf
+    share = np.exp(rest).sum(1)                         # R / (1 + R), without a difference from 1
+    l = np.log1p(-share)
+    c["lp_old"] = torch.from_numpy(l.astype(np.float32)).cuda()
+    scale = 2.0 ** 15 if dtype == "half" else 1.0
+    lp, stats, d = _policy_run(c, grad_scale=scale)
+    tol = E * (vocab / 256 + 64 + 2 * (above + 4) + 4 + 8)
+    off = np.abs(_np(lp) - l)
+    assert (off <= tol * np.abs(l)).all(), (off / np.abs(l)).max()
+    # slope -rho A = 2 rho, with rho = exp(l - lp_old): lp_old is off by E |l|, which the reference has too
+    rho = np.exp(l - _np(c["lp_old"]))
+    want = 2.0 * scale * rho * share
+    u, tiny = HALF_STEP[dtype], TINY[dtype]
+    off = np.abs(_np(d)[at] - want)
+    assert (off <= (2 * tol + 1.01 * u) * want + tiny).all(), (off / want).max()
+    if dtype == "fp32":                                 # a row's gradient sums to zero: as exactly as its columns are known
+        assert (np.abs(_np(d).sum(1)) <= 2 * (2 * tol + u) * want).all()
+
+
 def test_policy_loss_kl_of_a_token_out_of_reach():
     c = _policy_case(12, 3, 50, "fp32", masked=0.0)
     c["logits"][1, int(c["tokens"][1])] = float("-inf")
