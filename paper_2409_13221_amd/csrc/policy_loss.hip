@@ -29,7 +29,9 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, int r, float w,
     return o;
 }
 
-// Running maximum m and sum s of exp(z - m) of a thread's logits; m = -inf, s = 0 to begin with.
+// Running maximum m and sum s of exp(z - m) of a thread's logits; m = -inf, s = 0 to begin with.  __expf rounds x log2 e, which makes a term
+// off by |x| 2^-24 of itself, either way: a sum, whose weight lies near the maximum, does not show it (float rows of 32000, 64 of them:
+// with the gradient's exponential here too 12.6 us, so 11.2; log-probs 7.8e-8 off in both).
 struct Running {
     float m = -INFINITY, s = 0.f;
     template <int N> __device__ __forceinline__ void add(const float (&x)[N]) {
@@ -80,6 +82,16 @@ __device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, fl
     out[1] = -o.slope * a.grad_scale / S;
 }
 
+// exp(x) of a distance x <= 0 from the maximum, as the gradient shows it column by column.  Gradients of 16 bits are rounded to 2^-9 and
+// 2^-12 of themselves, beside which __expf is exact; of float ones it would be the largest error (2.7e-6 of themselves, so 1.2e-6).
+template <typename T> __device__ __forceinline__ float exp_of(float x) {
+    if (sizeof(T) == 2) return __expf(x);
+    constexpr float hi = 1.44269504f, lo = 1.44269504088896340736 - (double)hi;        // log2 e
+    const float t = x * hi, p = __builtin_amdgcn_exp2f(t);
+    const float lost = fminf(fmaxf(fmaf(x, lo, fmaf(x, hi, -t)), -1.f), 1.f);          // of x log2 e by its rounding; a number where t is -inf
+    return fmaf(p, lost * 0.693147181f, p);
+}
+
 // The vectors of a row start where what is written of it, or else what is read, reaches a 16-byte boundary; the few columns
 // before and behind them go to a thread each.
 template <typename T> __device__ __forceinline__ int columns_before(const T* row, int vocab) {
@@ -89,7 +101,7 @@ template <typename T> __device__ __forceinline__ int columns_before(const T* row
 // The columns of a row outside the threads' streams of vectors, a thread each: those before and behind the vectors, and the vector that
 // holds the token (`skip` of its vectors' columns; ~0u where the token is outside them).  The token's own is kept out of the sums:
 // of a token that has nearly all of the probability, what matters is what it leaves, and that cannot be had from a sum that holds the
-// token's 1 (a token 20 above 32000 others: gradient and log-prob off by 1e-3 of themselves, so 3e-7).  A branch or a select on it in
+// token's 1 (a token 20 above 32000 others: gradient and log-prob off by 1e-3 of themselves, so 5e-7).  A branch or a select on it in
 // each vector of the stream would spill it; a vector left out costs nothing.
 struct Single {
     unsigned skip;
@@ -169,7 +181,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
         row[0] = s_row[0];
         row[1] = s_row[1];
     }
-    if (one.column < V) g[one.column - head] = round_to<T>(one.column == y ? row[0] : row[1] * __expf(xl - M));
+    if (one.column < V) g[one.column - head] = round_to<T>(one.column == y ? row[0] : row[1] * exp_of<T>(xl - M));
     int again = t;                                 // columns are numbered anew for the stores: kept, 22 of them would spill
     asm volatile("" : "+v"(again));
 #pragma unroll
@@ -178,7 +190,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
         float f[N];
         x[it].get(f);
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = row[1] * __expf(f[e] - M);
+        for (int e = 0; e < N; ++e) f[e] = row[1] * exp_of<T>(f[e] - M);
         x[it].set(f);
         if (i < whole && i != one.skip) x[it].template store<true>(g + i);
     }
@@ -240,12 +252,12 @@ __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
             float d[N];
             x[it].get(d);
 #pragma unroll
-            for (int e = 0; e < N; ++e) d[e] = f * __expf(d[e] - M);
+            for (int e = 0; e < N; ++e) d[e] = f * exp_of<T>(d[e] - M);
             x[it].set(d);
             if ((unsigned)i != one.skip) x[it].template store<true>(g + i);
         }
     }
-    if (one.column < V) g[one.column - head] = round_to<T>(one.column == y ? s_row[0] : f * __expf(xl - M));
+    if (one.column < V) g[one.column - head] = round_to<T>(one.column == y ? s_row[0] : f * exp_of<T>(xl - M));
 }
 
 // Sums of the terms v [3][n] in a fixed order and in double: `each` of a kind a workgroup, to out[3][workgroups], or for one workgroup to

@@ -369,6 +369,29 @@ def test_policy_loss_of_confident_tokens(dtype, vocab, above):
         assert (np.abs(_np(d).sum(1)) <= 2 * (2 * tol + u) * want).all()
 
 
+@pytest.mark.parametrize("vocab", [64, 1000, 20000, 60000, 80000, 100000])
+def test_policy_loss_of_unlikely_columns(vocab):
+    """Float rows: a probability of exp(-80) is as precise as one of a half.  The logits are multiples of 2^-10, so that their distance x
+    from the maximum is exact: exp(-x) is off by 2 E (a product x log2 e rounded to float would make it x E), the sum by at most
+    (V / 256 + 16) E, slope, quotient and products by 11 E together."""
+    r = np.random.default_rng(vocab)
+    rows = 6
+    z = -np.floor(r.uniform(1, 85, size=(rows, vocab)) * 1024) / 1024
+    y = r.integers(0, vocab, rows)
+    z[np.arange(rows), y] = 0.0
+    logp = U.log_softmax(z)
+    l = logp[np.arange(rows), y]
+    f = lambda a: torch.from_numpy(np.asarray(a, np.float32)).cuda()
+    c = dict(logits=f(z), tokens=torch.from_numpy(y.astype(np.int32)).cuda(), adv=f(-np.ones(rows)), lp_old=f(l))
+    got = _policy_run(c, clip_low=1.0, clip_high=float("inf"))
+    want = -np.exp(l - _np(c["lp_old"]))[:, None] * np.exp(logp)
+    want[np.arange(rows), y] = 0.0
+    have = _np(got[2])
+    have[np.arange(rows), y] = 0.0
+    off = np.abs(have - want)
+    assert (off <= E * (vocab / 256 + 29) * np.abs(want)).all(), (off / np.maximum(np.abs(want), 1e-45)).max() / E
+
+
 def test_policy_loss_kl_of_a_token_out_of_reach():
     c = _policy_case(12, 3, 50, "fp32", masked=0.0)
     c["logits"][1, int(c["tokens"][1])] = float("-inf")
