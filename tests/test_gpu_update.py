@@ -594,6 +594,30 @@ def test_embed_grad_where_few_rows_end(rows, d, kind, accumulate):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("gdt,tdt", [("fp32", "fp32"), ("bf16", "fp32"), ("half", "bf16")])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("rows,d,vocab,kind", [
+    (511, 600, 3, "one"), (2048, 60, 4, "tail"), (700, 300, 2, "any"), (5000, 1030, 3, "any"), (9000, 40, 5, "tail"), (40000, 1028, 4, "tail"), (65536, 64, 3, "any"),
+    (65537, 64, 3, "any"), (70001, 8, 3, "one"), (70001, 1030, 2, "any"), (90000, 1024, 7, "tail"), (140000, 33, 1000, "tail"), (270000, 9, 50, "tail"),
+    (270000, 1100, 6, "padded")])
+def test_embed_grad_counts_every_row_once(gdt, tdt, accumulate, rows, d, vocab, kind):
+    """Small whole numbers: sums (below 2^24) and the scale of a half are exact in any order, so that a row dropped, doubled or joined to another
+    run shows, however long the run."""
+    R = _R()
+    g = torch.Generator().manual_seed(rows + d)
+    tok = torch.from_numpy(_tokens(np.random.default_rng(rows + d), rows, vocab, kind))
+    dout = torch.randint(1, 17, (rows, d), generator=g, dtype=torch.int8)
+    start = torch.randint(-50, 51, (vocab, d), generator=g).to(TDT[tdt])
+    got = start.cuda() if accumulate else torch.full((vocab, d), float("nan"), dtype=TDT[tdt], device="cuda")
+    R.rlhf_op_embed_grad(dout.cuda().to(TDT[gdt]), tok.cuda(), got, scale=0.5, accumulate=accumulate)
+    torch.cuda.synchronize()
+    want = torch.zeros(vocab + 1, d, dtype=torch.int32)
+    want.index_add_(0, torch.where(tok < 0, vocab, tok.long()), dout.int())
+    want = want[:vocab].double() * 0.5 + (start.double() if accumulate else 0.0)
+    # one rounding of the exact sum (the sum itself is a float: 270000 * 16 is below 2^24, its half with a whole number added as well)
+    assert torch.equal(got.cpu(), want.float().to(TDT[tdt]))
+
+
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("d,vocab", [(40, 90), (1025, 33000), (4104, 50), (300, 70001)])
 @pytest.mark.parametrize("lengths", [[1] * 255, [1] * 256, [1] * 257, [31, 32, 33, 63, 64, 65, 95, 96, 97, 1, 2], [8] * 100, [64] * 20, [1, 640, 1], [33] * 30,
