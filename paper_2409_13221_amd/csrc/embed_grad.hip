@@ -292,13 +292,13 @@ __device__ __forceinline__ void sum_rows(const G* __restrict__ m, size_t ld, int
     }
 }
 
-// The order is cut into chunks.  A run of more places than a chunk has is long: workgroups of their own sum what each chunk holds of
+// The order is cut into chunks, of 32 places or more (what is grouped has over 512 rows).  A run of more places than a chunk has is long: workgroups of their own sum what each chunk holds of
 // it (of at most two long runs: one that began before the chunk, one that begins in it), and k_long_runs joins the sums.
 constexpr int kFlight = 8;
 struct Chunks {
     float* part;            // [chunks][2][ld]
     size_t ld;
-    int size, count;        // count: 0 where no run can be long
+    int size, count;
 };
 
 struct GradArgs {
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(256) void k_table_grad(const G* __restrict__ dout, 
     if (begins == 0) return;
     int at = p0 + __ffsll((unsigned long long)begins) - 1;
     const int last = 63 - __clzll((long long)begins), many = __shfl(w.count, base + last, kWave);
-    const int end = p0 + last + (a.c.count > 0 && many > a.c.size ? 0 : many);
+    const int end = p0 + last + (many > a.c.size ? 0 : many);
     Cols cols[H];
     my_columns<C, H>((const T*)nullptr, slice, a.wide_log2, a.d, cols);
     // rows in the order of their places, kBatch in flight; a run is stored where the next begins
@@ -628,7 +628,7 @@ static GradScratch grad_scratch(int rows, int d, int vocab) {
     s.places = up(((size_t)b.subs << b.log2) * sizeof(Run));
     s.total = s.places + (size_t)rows * sizeof(Place);
     s.part = s.total + 16;
-    s.bytes = s.part + (rows > size ? (size_t)((rows + size - 1) / size) * 2 * up((size_t)d * sizeof(float)) : 0);
+    s.bytes = s.part + (size_t)((rows + size - 1) / size) * 2 * up((size_t)d * sizeof(float));
     return s;
 }
 size_t embed_grad_scratch_bytes(int rows, int d, int vocab) { return few_rows(rows, d) ? 0 : grad_scratch(rows, d, vocab).bytes; }
@@ -689,7 +689,7 @@ static hipError_t embed_grad(hipStream_t st, const G* dout, T* dtable, const int
     a.clear_blocks = (unsigned)clear;
     k_table_grad<G, T, ACCUMULATE><<<(unsigned)(table + clear), 256, 0, st>>>(dout, dtable, a);
     e = hipGetLastError();
-    if (e != hipSuccess || a.c.count == 0) return e;
+    if (e != hipSuccess) return e;
     const int groups = 1 << a.b.log2;
     if (a.d <= 1024) k_long_runs<T, ACCUMULATE, 16><<<dim3(groups, (a.d + 63) / 64), kJoinThreads, 0, st>>>(dtable, a);
     else k_long_runs<T, ACCUMULATE, 64><<<dim3(groups, (a.d + 255) / 256), kJoinThreads, 0, st>>>(dtable, a);
@@ -708,7 +708,7 @@ hipError_t launch_embed_grad(hipStream_t st, int gdt, int tdt, const void* dout,
     a.places = places; a.total = total; a.runs = runs;
     a.b = buckets_of(vocab);
     a.c = Chunks{(float*)((char*)scratch + g.part), ((size_t)d + 3) / 4 * 4, chunk_size(rows), 0};
-    if (rows > a.c.size) a.c.count = (rows + a.c.size - 1) / a.c.size;
+    a.c.count = (rows + a.c.size - 1) / a.c.size;
     a.ld_dout = ld_dout; a.ld_table = ld_table; a.scale = scale; a.rows = rows; a.d = d;
     hipError_t e = hipSuccess;
     RLHF_TYPES2(gdt, tdt, (e = accumulate ? embed_grad<X, Y, true>(st, (const X*)dout, (Y*)dtable, tokens, a, places, runs, total, rows, vocab)
