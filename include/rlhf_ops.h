@@ -191,7 +191,8 @@ int rlhf_op_head_dot(int act_dtype, int w_dtype, const void* xn, const void* w, 
  *   lp[r]    = l
  *   dlogits[r] = grad_scale * d loss / d logits[r], in logit_dtype, row stride ld_grad; NULL: no gradient is taken.  It may be
  *              the logits themselves (same ld), else the two must not overlap.
- * Everything is float until the gradient is rounded once.  The rows are summed in a fixed order.
+ * Everything is float until the gradient is rounded once, the sums over rows double.  All sums have a fixed order (which columns meet
+ * first goes by where a row lies between 16-byte boundaries): the same call gives the same bits.
  * A row with weight 0 or a negative token is left out: its logits and its other inputs, whatever they hold, are not used,
  * lp[r] = 0, its gradient is zero.  Logits of -inf have probability 0; where the token's own is, lp[r] = -inf, the ratio is 0 and the
  * KL towards lp_ref infinite, and with kl_coef > 0 the row's gradient is not finite.  A row whose result is not a number (all
@@ -214,7 +215,7 @@ int rlhf_op_embed(int table_dtype, int out_dtype, const void* table, int64_t ld_
 
 /* Its gradient: dtable[v] = scale * (sum of dout[r] over the rows r with tokens[r] == v), every row of dtable written
  * (zeros where no row has the token); with accumulate != 0 that sum is added to dtable[v] instead and rows of other
- * tokens are left as they are.  The rows of a token are summed in float, in an order that depends on the tokens alone:
+ * tokens are left as they are.  The rows of a token are summed in float, in an order that depends on the tokens and sizes alone:
  * the same call gives the same bits.  Rows with tokens outside [0, vocab) count for nothing.  Types and strides as
  * above, dout in dout_dtype, dtable in table_dtype.  dout and dtable must not overlap.  Matrices of hundreds of GB, which no launch
  * covers, are refused before anything is written.

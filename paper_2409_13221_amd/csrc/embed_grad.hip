@@ -94,7 +94,9 @@ __global__ __launch_bounds__(256) void k_embed_rows(const T* __restrict__ table,
     }
 }
 
-// ---- gradient: rows grouped by token, then every token's rows summed in ascending order.
+// ---- gradient: rows grouped by token, then every token's rows summed, in float and in an order that follows from the tokens and sizes: a run
+// up to a chunk long in ascending order; a longer one chunk by chunk, the chunks' sums joined by workers that take every WORKERS-th; few
+// rows (k_few_rows_grad) dealt to a workgroup's groups in turn, the groups' sums joined.
 // The vocabulary is dealt to 2^log2 buckets by its low bits (frequent tokens have neighbouring ids), `subs` tokens each, and the
 // rows to `parts` parts, 256 workgroups together unless the vocabulary is large.  A workgroup for each bucket and part reads
 // all tokens out of the L2, counts its bucket's and how many lie in earlier buckets, and puts the rows of its part into their
