@@ -130,7 +130,7 @@ __device__ __forceinline__ void left_out_row(const PolicyArgs& a, int r, T* g, i
 // sum as it arrives, so that the exponentials hide behind the loads; the gradient takes them anew from the logits, which
 // costs less than room for them in 32 bits would: a 16-bit row of 32000 is 16 registers of 1024 threads, and two such workgroups
 // on a compute unit keep one's stores beside the other's loads (3000 rows of 50000 bf16: in 32 bits, one workgroup, 178 us;
-// packed, two, 119).  From 13 vectors a thread on there is room for one: 1500 rows of 100003 half 131 us = 4.6 TB/s.
+// packed, two, 119).  From 13 vectors a thread on there is room for one: 1500 rows of 100003 half, all kept, 135 us = 4.4 TB/s.
 // ROWS rows of THREADS threads each in a workgroup; more than one only where a row is one wave's.
 template <typename T, int IT, int THREADS, int ROWS, int WAVES_PER_SIMD>
 __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(PolicyArgs a) {
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(THREADS * ROWS, WAVES_PER_SIMD) void k_policy_row(P
 }
 
 // Rows that no workgroup's registers hold (beyond 90000 floats, 180000 of 16 bits): read once for the statistics, and again, out of
-// the caches, for the gradient.  1000 rows of 160000 bf16 read so 134 us, 4.8 TB/s of what has to be read and written.
+// the caches, for the gradient.  700 rows of 200000 bf16 133 us, of 300000 215 = 3.9 TB/s of what has to be read and written.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_policy_long_row(PolicyArgs a) {
     constexpr int N = 16 / sizeof(T), IT = 4;
@@ -304,18 +304,23 @@ size_t policy_scratch_floats(int rows, int vocab) {
 }
 
 // As few threads as hold a row with up to 8 vectors each: waves that wait for one another cost more than vectors.  us, with
-// gradient: 8192 rows of 4096 bf16: a wave a row 24.9, 2 waves 25.6, 4 28.3, 8 37.5; of 8192: 4 waves 45.9, 8 49.7, a wave 52.2;
-// of 32000: 8 waves 181, 4 with 16 vectors 184, 16 with 4 187; 65536 rows of 1000: 4 rows of a wave 52.7, a workgroup each 79.
-// Beyond 8 vectors of 1024 threads, as many as needed: 1500 rows of 100003 half: 13 141, 16 150, 25 of 512 threads 148.
+// gradient, all rows kept: 8192 rows of 4096 bf16: a wave a row 28.0, 2 waves 30.8, 4 31.5, 8 40.1; of 8192: 4 waves 50.8, 8 54.6, a wave
+// 57.8; of 16000: 8 waves 93, 16 122; of 32000: 8 waves 187, 4 with 16 vectors 190, 16 with 4 193.  Four rows of a wave share a workgroup
+// where they are float (16384 rows of 2000 float 54.7, a workgroup each 57.1; of bf16 35.5 and 34.1, 65536 rows of 1000 bf16 65.4
+// and 60.6).
+// Beyond 8 vectors of 1024 threads, as many as needed (1200 rows of 104000 bf16: 13 106, 16 109; of 128256: 16 130, 22 136).  Rows that
+// fit are kept in registers, which loses only next to where two workgroups a compute unit end, and there little (us, registers and read
+// twice, 1200 rows: 65535 bf16 65 and 73, 70000 84 and 80, 85000 96 and 96, 104000 106 and 114, 128256 130 and 143, 160000 162 and
+// 178, 180000 183 and 212; float 32771 72 and 74, 50257 105 and 113, 60000 114 and 133, 90000 173 and 208).
 template <typename T>
 static void policy_rows(hipStream_t st, const PolicyArgs& a) {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = 16 / sizeof(T), SHARE = sizeof(T) == 4 ? 4 : 1;
 #define RLHF_POLICY(IT, THREADS, ROWS, WAVES) \
     if (a.vocab < (IT * THREADS + 1) * N)     \
         return k_policy_row<T, IT, THREADS, ROWS, WAVES><<<(a.rows + ROWS - 1) / ROWS, THREADS * ROWS, 0, st>>>(a)
-    RLHF_POLICY(2, 64, 4, 8);
-    RLHF_POLICY(4, 64, 4, 8);
-    RLHF_POLICY(8, 64, 4, 8);
+    RLHF_POLICY(2, 64, SHARE, 8);
+    RLHF_POLICY(4, 64, SHARE, 8);
+    RLHF_POLICY(8, 64, SHARE, 8);
     RLHF_POLICY(4, 256, 1, 8);
     RLHF_POLICY(4, 512, 1, 8);
     RLHF_POLICY(8, 512, 1, 8);
@@ -327,7 +332,8 @@ static void policy_rows(hipStream_t st, const PolicyArgs& a) {
     k_policy_long_row<T><<<a.rows, 1024, 0, st>>>(a);
 }
 
-// The rows in turns of what one launch holds at the threads a row that policy_rows takes: a wave's 64 (four rows a workgroup), up to 1024.
+// The rows in turns of what one launch holds at the threads a row that policy_rows takes: a wave's 64 (of up to four rows a workgroup), or up
+// to 1024.
 template <typename T>
 static hipError_t policy_parts(hipStream_t st, const PolicyArgs& a) {
     const int64_t most = a.vocab < (8 * 64 + 1) * (16 / (int)sizeof(T)) ? kLaunchThreads / 256 * 4 : kLaunchThreads / 1024;
