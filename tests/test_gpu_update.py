@@ -484,6 +484,24 @@ def test_policy_loss_of_more_rows_than_a_launch_has_waves():
     assert float((d.double() - dl).abs().sub_(4 * tol * a.abs()[:, None]).max()) <= 0.0
 
 
+def test_policy_loss_of_more_rows_than_a_launch_has_workgroups():
+    """Rows of more than a wave: equal logits, in place over them (34 GB), every log-prob -log(vocab) and every gradient's row 1/vocab but for the
+    token's."""
+    rows, vocab = 2 ** 22 + 3, 4104
+    z = torch.zeros(rows, vocab, device="cuda", dtype=torch.bfloat16)
+    tok = torch.arange(rows, device="cuda", dtype=torch.int32).remainder_(vocab)
+    l = -np.log(float(vocab))
+    adv, lp, stats = torch.ones(rows, device="cuda"), torch.full((rows,), 7.0, device="cuda"), torch.full((4,), 7.0, device="cuda")
+    _R().rlhf_op_policy_loss(z, tok, torch.full((rows,), l, device="cuda"), adv, lp, stats, dlogits=z, clip_high=float("inf"))
+    torch.cuda.synchronize()
+    tol = E * (vocab / 256 + 64 + 4 * abs(l))
+    assert float((lp.double() - l).abs().max()) <= tol and abs(float(stats[0]) + rows) <= 2 * tol * rows
+    for first in (0, 2 ** 22 - 100, rows - 100):
+        d, at = z[first:first + 100].double(), tok[first:first + 100].long()[:, None]
+        want = torch.full_like(d, 1.0 / vocab).scatter_(1, at, 1.0 / vocab - 1.0)
+        assert ((d - want).abs() <= (2 * tol + 1.01 * 2.0 ** -8) * want.abs()).all()
+
+
 # ------------------------------------------------------------------------------- embedding and gradient
 
 def _tokens(r, rows, vocab, kind):
