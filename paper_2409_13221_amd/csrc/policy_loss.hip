@@ -82,8 +82,8 @@ __device__ __forceinline__ void finish_row(const PolicyArgs& a, int r, int y, fl
     out[1] = -o.slope * a.grad_scale / S;
 }
 
-// exp(x) of a distance x <= 0 from the maximum, as the gradient shows it column by column.  Gradients of 16 bits are rounded to 2^-9 and
-// 2^-12 of themselves, beside which __expf is exact; of float ones it would be the largest error (2.7e-6 of themselves, so 1.2e-6).
+// exp(x) of a distance x <= 0 from the maximum, as the gradient shows it column by column.  Gradients of 16 bits are rounded to 2^-8 and
+// 2^-11 of themselves, beside which __expf is exact; of float ones it would be the largest error (2.7e-6 of themselves, so 1.2e-6).
 template <typename T> __device__ __forceinline__ float exp_of(float x) {
     if (sizeof(T) == 2) return __expf(x);
     constexpr float hi = 1.44269504f, lo = 1.44269504088896340736 - (double)hi;        // log2 e
