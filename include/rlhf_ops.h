@@ -114,6 +114,68 @@ int rlhf_op_flash_attention(const void* q, const void* k, const void* v, const i
                             const int32_t* tile_q0, const int32_t* tile_len, void* out, int n_tiles,
                             int rows, int n_q_heads, int n_kv_heads, int head_dim, void* stream);
 
+/* ---- attention that reads less of its cache: a sliding window with a few first tokens that stay visible (sinks), for packed passes
+ * and for decode steps, and a KV cache held in 4 bits.
+ *
+ * The query at position i sees key j where j <= i and (j > i - window or j < sinks): the newest `window` tokens, itself among them,
+ * and the first `sinks` ones.  window >= 1, sinks >= 0; a window of at least the longest context (INT32_MAX will do) is causal attention.
+ * Scores are scaled by 1/sqrt(head_dim).  head_dim 64 or 128, n_q_heads a multiple of n_kv_heads (query head h reads KV head
+ * h / (n_q_heads / n_kv_heads)).  act_dtype: RLHF_FP32, RLHF_BF16 or 2 = IEEE half, of all matrices of a call.  Scores, softmax and sums are
+ * float; 16-bit outputs are rounded once.  Matrices have rows of their own stride (ld_*, elements); addresses and strides are
+ * multiples of 16 bytes.  What a query does not see does not reach it, whatever it holds (infinities and NaN too).  At most 2^30 rows
+ * (decode 2^24), 2^16 heads and layers, fewer than 2^27 pages. */
+
+/* Packed causal attention of a pass with a window: q, out [rows, n_q_heads*head_dim], k, v [rows, n_kv_heads*head_dim], e.g. columns
+ * of one QKV buffer.  Tiles as in rlhf_op_flash_attention: tile i covers rows tile_start[i] + tile_q0[i] .. (at most 128, up to the
+ * end) of the sequence that starts at row tile_start[i] and has tile_len[i] rows.  Rows of no tile are left as they are; a tile that
+ * does not lie within the `rows` rows is skipped.  out must not overlap q, k or v. */
+int rlhf_op_window_attention(int act_dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             const int32_t* tile_start, const int32_t* tile_q0, const int32_t* tile_len, void* out, int64_t ld_out,
+                             int n_tiles, int rows, int window, int sinks, int n_q_heads, int n_kv_heads, int head_dim,
+                             void* stream);
+
+/* Decode attention of one step with a window: row r holds one query at position ctx_len[r] - 1 of the sample whose row of page_table
+ * [n_samples, pt_stride] is row_sample[r]; pool as in rlhf_op_paged_decode_attention, n_pages of them, in act_dtype.  Page-table entries of
+ * pages without a visible token are not read: their pages may have been given back.  ctx_len[r] <= 0 gives a row of zeros.  A row
+ * whose context, sample or visible pages lie outside page table or pool gives NaN; nothing is read out of bounds.
+ * nsplit (1..64): into how many parts a row's visible pages are cut; rlhf_op_window_decode_nsplit gives the library's choice for a step
+ * whose longest context has max_ctx tokens.  scratch: rlhf_op_window_decode_scratch_floats(rows, n_q_heads, head_dim, nsplit) floats,
+ * 16-byte aligned (none for nsplit == 1: NULL will do); it belongs to one call at a time. */
+int rlhf_op_window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks);
+int64_t rlhf_op_window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int nsplit);
+int rlhf_op_window_decode_attention(int act_dtype, const void* q, int64_t ld_q, const void* pool, int n_pages,
+                                    const int32_t* page_table, int pt_stride, int n_samples, const int32_t* row_sample,
+                                    const int32_t* ctx_len, void* out, int64_t ld_out, float* scratch, int rows, int layer, int nsplit,
+                                    int window, int sinks, int n_layers, int n_q_heads, int n_kv_heads, int head_dim, void* stream);
+
+/* A paged KV cache of 4 bits (4.5 with scales: 3.6 times the tokens of a half cache).  64 consecutive dims of one head's K or V of one token
+ * share a scale and a center, IEEE half both: with lo and hi their least and greatest value
+ *   s = half((hi - lo) * (1/15)),  c = half(lo + 8 s)     each operation and 1/15 rounded to float, then to half
+ *   u = (x - c) / s rounded to the nearest whole number (half way: the even one) and clamped to -8 .. 7; 0 where s == 0
+ * and the value held is c + s u.  A group with a NaN, or a magnitude above 65504, becomes NaN as a whole.
+ * A page is 16 tokens, [page][layer][kv_head][18 * head_dim bytes], rlhf_op_kv4_page_bytes in all:
+ *   8 head_dim bytes   K codes: 4 bits u + 8 of token t, dim d = 32 a + 8 b + i, in bits 4 (i % 2) of byte ((16 b + t) * head_dim / 32 + a) * 4 + i / 2
+ *   8 head_dim bytes   V codes: token t = 4 b + i, dim d = 32 a + 16 e + g, in bits 4 e of byte ((16 b + g) * head_dim / 32 + a) * 4 + i
+ *   head_dim bytes     (s, c) of K [head_dim / 64][16 tokens];  head_dim bytes   the same of V
+ * (what a lane of the matrix units needs lies together).  Pools are 16-byte aligned. */
+int64_t rlhf_op_kv4_page_bytes(int n_layers, int n_kv_heads, int head_dim);
+
+/* Appends rows of k, v [rows, n_kv_heads*head_dim] to token slots kv_dst[r] = page*16 + offset of `layer`.  A negative slot, or one
+ * beyond the pool's n_pages, is left out.  The slots of a call are distinct; k and v do not overlap the pool. */
+int rlhf_op_kv4_append(int act_dtype, const void* k, int64_t ld_k, const void* v, int64_t ld_v, const int32_t* kv_dst, void* pool,
+                       int n_pages, int rows, int layer, int n_layers, int n_kv_heads, int head_dim, void* stream);
+
+/* Reads token slots back into rows of k, v, in act_dtype, rounded once (to look at a cache, move it, or run a pass over it).  A negative slot
+ * gives a row of zeros, one beyond the pool a row of NaN.  k, v and the pool do not overlap. */
+int rlhf_op_kv4_read(int act_dtype, const void* pool, int n_pages, const int32_t* kv_src, void* k, int64_t ld_k, void* v, int64_t ld_v,
+                     int rows, int layer, int n_layers, int n_kv_heads, int head_dim, void* stream);
+
+/* rlhf_op_window_decode_attention over such a cache; act_dtype is the type of q and out.  nsplit and scratch as there. */
+int rlhf_op_kv4_decode_attention(int act_dtype, const void* q, int64_t ld_q, const void* pool, int n_pages,
+                                 const int32_t* page_table, int pt_stride, int n_samples, const int32_t* row_sample,
+                                 const int32_t* ctx_len, void* out, int64_t ld_out, float* scratch, int rows, int layer, int nsplit,
+                                 int window, int sinks, int n_layers, int n_q_heads, int n_kv_heads, int head_dim, void* stream);
+
 /* ---- row-wise kernels of the decoder block and of the heads.  act_dtype is the element type of
  * the 16-bit (or float) activations a kernel writes or reads: RLHF_FP32, RLHF_BF16, or 2 = IEEE
  * half.  "nsplit / sstride": a float input given as nsplit partial planes, plane s at x + s *

@@ -150,6 +150,16 @@ def lib() -> C.CDLL:
         L.rlhf_op_gemm_tall_tile.restype = C.c_int
         L.rlhf_op_bf16_to_half.argtypes = [vp, vp, i64, vp]
         L.rlhf_op_bf16_to_half.restype = C.c_int
+        L.rlhf_op_window_attention.argtypes = [C.c_int] + [vp, i64] * 3 + [vp] * 4 + [i64] + [C.c_int] * 7 + [vp]
+        L.rlhf_op_window_decode_nsplit.argtypes = [C.c_int] * 6
+        L.rlhf_op_window_decode_scratch_floats.argtypes = [C.c_int] * 4
+        L.rlhf_op_window_decode_scratch_floats.restype = i64
+        for f in (L.rlhf_op_window_decode_attention, L.rlhf_op_kv4_decode_attention):
+            f.argtypes = [C.c_int, vp, i64, vp, C.c_int, vp, C.c_int, C.c_int, vp, vp, vp, i64, vp] + [C.c_int] * 9 + [vp]
+        L.rlhf_op_kv4_page_bytes.argtypes = [C.c_int] * 3
+        L.rlhf_op_kv4_page_bytes.restype = i64
+        L.rlhf_op_kv4_append.argtypes = [C.c_int, vp, i64, vp, i64, vp, vp] + [C.c_int] * 6 + [vp]
+        L.rlhf_op_kv4_read.argtypes = [C.c_int, vp, C.c_int, vp, vp, i64, vp, i64] + [C.c_int] * 5 + [vp]
         L.rlhf_op_policy_loss_scratch_floats.argtypes = [C.c_int] * 2
         L.rlhf_op_policy_loss.argtypes = [C.c_int, vp, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i64, vp,
                                           C.c_int, C.c_int, vp]
@@ -588,7 +598,7 @@ def rlhf_op_gemm_tall_tile(bid: int, tiles_m: int, tiles_n: int):
     return (tm.value, tn.value) if rc == 1 else None
 
 
-# ------------------------------------------------------------------------- the Actor's update
+# ------------------------------------------------------------------------- attention that reads less of its cache
 
 def _on_device(*tensors) -> None:
     """Kernels are launched on the current device's current stream: every tensor has to be there."""
@@ -623,6 +633,140 @@ def _matrix(t, rows: int, cols: int, what: str) -> int:
         raise ValueError(f"rows of {what} overlap")
     return ld
 
+
+class rlhf_attention_tiles:
+    """The plan of a packed pass for rlhf_op_window_attention: sequences of seq_lens rows, back to back (a length may be 0), cut into
+    tiles of 128 queries.  One plan serves all layers and any number of passes of these lengths."""
+
+    def __init__(self, seq_lens, device="cuda"):
+        import torch
+        lens = np.asarray(list(seq_lens), np.int64)
+        if lens.ndim != 1 or (lens < 0).any() or lens.sum() > 1 << 30:
+            raise ValueError("seq_lens must be lengths >= 0 of at most 2^30 rows in all")
+        n = -(-lens // 128)
+        which = np.repeat(np.arange(len(lens)), n)
+        q0 = (np.arange(len(which)) - np.repeat(np.cumsum(n) - n, n)) * 128
+        self.rows, self.n = int(lens.sum()), len(which)
+        start = np.cumsum(lens) - lens
+        self.tiles = torch.from_numpy(np.stack([start[which], q0, lens[which]]).astype(np.int32)).to(device)
+        self.start, self.q0, self.len = self.tiles
+
+
+NO_WINDOW = 2 ** 31 - 1
+
+
+def _int32(n: int) -> int:
+    """n within what an argument holds: a window or number of sinks beyond it is as good as its greatest value."""
+    return max(-1, min(n, NO_WINDOW))
+
+
+def rlhf_op_window_attention(q, k, v, tiles: rlhf_attention_tiles, out, window: int, sinks: int, n_q_heads: int, n_kv_heads: int,
+                             head_dim: int) -> None:
+    """Packed causal attention in which a query sees the newest `window` tokens (itself among them) and the first `sinks` of its sequence.
+    q, out [rows, n_q_heads*head_dim], k, v [rows, n_kv_heads*head_dim], float32, bfloat16 or float16, e.g. columns of one QKV buffer; the
+    sequences of `tiles` come first, rows behind them are left as they are."""
+    rows, qc, kc = q.shape[0], n_q_heads * head_dim, n_kv_heads * head_dim
+    if tiles.rows > rows:
+        raise ValueError(f"the sequences have {tiles.rows} rows, q has {rows}")
+    if not q.dtype == k.dtype == v.dtype == out.dtype:
+        raise ValueError("q, k, v and out must be of one type")
+    _on_device(q, k, v, out, tiles.tiles)
+    _op_check(lib().rlhf_op_window_attention(
+        _act_code(q), q.data_ptr(), _matrix(q, rows, qc, "q"), k.data_ptr(), _matrix(k, rows, kc, "k"), v.data_ptr(), _matrix(v, rows, kc, "v"),
+        tiles.start.data_ptr(), tiles.q0.data_ptr(), tiles.len.data_ptr(), out.data_ptr(), _matrix(out, rows, qc, "out"), tiles.n, rows,
+        _int32(window), _int32(sinks), n_q_heads, n_kv_heads, head_dim, _stream_ptr()), "rlhf_op_window_attention")
+
+
+def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out, layer, n_layers, n_q_heads, n_kv_heads, head_dim, window, sinks,
+                   max_ctx, nsplit, scratch):
+    import torch
+    rows, qc = q.shape[0], n_q_heads * head_dim
+    if q.dtype != out.dtype:
+        raise ValueError("q and out must be of one type")
+    _on_device(q, pool, page_table, row_sample, ctx_len, out, scratch)
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table must be a contiguous int32 matrix")
+    n_samples, pt_stride = page_table.shape
+    _vector(row_sample, rows, torch.int32, "row_sample")
+    _vector(ctx_len, rows, torch.int32, "ctx_len")
+    L = lib()
+    window, sinks = _int32(window), _int32(sinks)
+    if nsplit is None:
+        longest = pt_stride * 16
+        nsplit = L.rlhf_op_window_decode_nsplit(rows, n_q_heads, n_kv_heads, longest if max_ctx is None else min(max_ctx, longest), window, sinks)
+    if nsplit > 1:
+        need = L.rlhf_op_window_decode_scratch_floats(rows, n_q_heads, head_dim, nsplit)
+        if scratch is None:
+            scratch = torch.empty(need, device=q.device)
+        elif scratch.dtype != torch.float32 or scratch.numel() < need or not scratch.is_contiguous():
+            raise ValueError(f"scratch must be a contiguous float32 tensor of {need} entries")
+    _op_check(getattr(L, name)(
+        _act_code(q), q.data_ptr(), _matrix(q, rows, qc, "q"), pool.data_ptr(), n_pages, page_table.data_ptr(), pt_stride, n_samples,
+        row_sample.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), _matrix(out, rows, qc, "out"), _ptr(scratch), rows, layer, nsplit, window,
+        sinks, n_layers, n_q_heads, n_kv_heads, head_dim, _stream_ptr()), name)
+
+
+def rlhf_op_window_decode_attention(q, pool, page_table, row_sample, ctx_len, out, layer: int, n_layers: int, n_q_heads: int, n_kv_heads: int,
+                                    head_dim: int, window: int = NO_WINDOW, sinks: int = 0, max_ctx: Optional[int] = None,
+                                    nsplit: Optional[int] = None, scratch=None) -> None:
+    """One query a row [rows, n_q_heads*head_dim] against the newest `window` tokens and the first `sinks` of its sample's paged cache, pool
+    [pages, layer, K|V, kv_head, 16, head_dim] of q's type.  max_ctx: bound of ctx_len (known to the caller that grows the contexts), for the
+    choice of nsplit alone.  scratch: float32, rlhf_op_window_decode_scratch_floats entries."""
+    page = n_layers * 2 * n_kv_heads * 16 * head_dim
+    if pool.dtype != q.dtype or not pool.is_contiguous() or page < 1 or pool.numel() % page:
+        raise ValueError("pool must be whole contiguous pages of q's type")
+    _window_decode("rlhf_op_window_decode_attention", q, pool, pool.numel() // page, page_table, row_sample, ctx_len, out, layer, n_layers, n_q_heads,
+                   n_kv_heads, head_dim, window, sinks, max_ctx, nsplit, scratch)
+
+
+def _kv4_pages(pool, n_layers: int, n_kv_heads: int, head_dim: int) -> int:
+    import torch
+    page = lib().rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim)
+    if page == 0 or pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() % page:
+        raise ValueError(f"pool must be whole contiguous pages of {page} bytes (uint8)")
+    return pool.numel() // page
+
+
+def rlhf_op_kv4_page_bytes(n_layers: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of one page (16 tokens of all layers) of a KV cache of 4 bits; 0 for an unsupported shape."""
+    return lib().rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim)
+
+
+def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
+    """Rows of k, v [rows, n_kv_heads*head_dim] into token slots kv_dst (int32, distinct; outside the pool: left out) of the cache of 4 bits."""
+    import torch
+    rows, cols = kv_dst.numel(), n_kv_heads * head_dim
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must be of one type")
+    _on_device(k, v, kv_dst, pool)
+    _vector(kv_dst, rows, torch.int32, "kv_dst")
+    _op_check(lib().rlhf_op_kv4_append(_act_code(k), k.data_ptr(), _matrix(k, rows, cols, "k"), v.data_ptr(), _matrix(v, rows, cols, "v"),
+                                       kv_dst.data_ptr(), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), rows, layer, n_layers,
+                                       n_kv_heads, head_dim, _stream_ptr()), "rlhf_op_kv4_append")
+
+
+def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
+    """Token slots kv_src (int32) of the cache of 4 bits into rows of k, v (zeros for a negative slot, NaN beyond the pool)."""
+    import torch
+    rows, cols = kv_src.numel(), n_kv_heads * head_dim
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must be of one type")
+    _on_device(k, v, kv_src, pool)
+    _vector(kv_src, rows, torch.int32, "kv_src")
+    _op_check(lib().rlhf_op_kv4_read(_act_code(k), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), kv_src.data_ptr(), k.data_ptr(),
+                                     _matrix(k, rows, cols, "k"), v.data_ptr(), _matrix(v, rows, cols, "v"), rows, layer, n_layers, n_kv_heads, head_dim,
+                                     _stream_ptr()), "rlhf_op_kv4_read")
+
+
+def rlhf_op_kv4_decode_attention(q, pool, page_table, row_sample, ctx_len, out, layer: int, n_layers: int, n_q_heads: int, n_kv_heads: int,
+                                 head_dim: int, window: int = NO_WINDOW, sinks: int = 0, max_ctx: Optional[int] = None,
+                                 nsplit: Optional[int] = None, scratch=None) -> None:
+    """rlhf_op_window_decode_attention over a cache of 4 bits (uint8, rlhf_op_kv4_page_bytes a page)."""
+    _window_decode("rlhf_op_kv4_decode_attention", q, pool, _kv4_pages(pool, n_layers, n_kv_heads, head_dim), page_table, row_sample, ctx_len, out,
+                   layer, n_layers, n_q_heads, n_kv_heads, head_dim, window, sinks, max_ctx, nsplit, scratch)
+
+
+# ------------------------------------------------------------------------- the Actor's update
 
 def rlhf_op_policy_loss(logits, tokens, lp_old, adv, lp, stats, dlogits=None, lp_ref=None, weight=None, clip_low: float = 0.2,
                         clip_high: float = 0.2, kl_coef: float = 0.0, grad_scale: float = 1.0, scratch=None) -> None:

@@ -298,6 +298,43 @@ hipError_t launch_flash_attn(hipStream_t st, const void* q, const void* k, const
 hipError_t launch_flash_attn_f32(hipStream_t st, const float* q, const float* k, const float* v, const int* tile_start,
                                  const int* tile_q0, const int* tile_len, float* out, int n_tiles, int longest, const Dims& dm);
 
+// Packed attention with a sliding window and sinks (window_attention.hip); tiles of kFlashTile queries as above.
+struct WindowArgs {
+    const void *q, *k, *v;          // row strides in elements
+    size_t ld_q, ld_k, ld_v;
+    const int *tile_start, *tile_q0, *tile_len;
+    void* out;
+    size_t ld_out;
+    int n_tiles, rows, window, sinks, n_q_heads, n_kv_heads;
+};
+hipError_t launch_window_attention(hipStream_t st, int dtype, int head_dim, const WindowArgs& a);
+
+// Decode attention with a window over the paged pool, of act_dtype or of 4 bits (window_decode.hip).
+struct WindowDecodeArgs {
+    const void* q;
+    const void* pool;
+    const int *page_table, *row_sample, *ctx_len;
+    void* out;
+    float* part;                    // [rows][n_q_heads][nsplit]: (max, sum), then [..][head_dim] accumulators; nsplit > 1
+    size_t ld_q, ld_out;
+    int rows, layer, n_layers, n_q_heads, n_kv_heads, nsplit, window, sinks, n_pages, n_samples, pt_stride;
+};
+int window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks);
+size_t window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int nsplit);
+hipError_t launch_window_decode(hipStream_t st, int dtype, bool four_bits, int head_dim, const WindowDecodeArgs& a);
+
+// Rows of K and V into the cache of 4 bits, and back (kv4.hip).
+struct Kv4Args {
+    void *k, *v;
+    size_t ld_k, ld_v;
+    const int* slot;
+    void* pool;
+    int n_pages, rows, layer, n_layers, n_kv_heads;
+};
+size_t kv4_block_bytes(int head_dim);
+hipError_t launch_kv4_append(hipStream_t st, int dtype, int head_dim, const Kv4Args& a);
+hipError_t launch_kv4_read(hipStream_t st, int dtype, int head_dim, const Kv4Args& a);
+
 size_t pool_page_elems(const Dims& dm);  // elements of one page over all layers
 
 // Error text of a call without a context; rlhf_last_error(NULL) returns it (per thread).

@@ -411,6 +411,132 @@ extern "C" int rlhf_op_clip_grads(const rlhf_tensor* tensors, int n_tensors, con
     return RLHF_ENOMEM;
 }
 
+// ---- attention that reads less of its cache
+
+// Addresses and row strides of matrices of whole 16-byte pieces.
+static bool in_pieces(const void* p, int64_t ld, int dt) { return p && aligned(p, 16) && (size_t)ld * elem_bytes(dt) % 16 == 0; }
+static bool heads_ok(int hq, int hkv, int hd) {
+    return hkv > 0 && hq > 0 && hq % hkv == 0 && hq <= 1 << 16 && (hd == 64 || hd == 128);
+}
+constexpr size_t kMaxPoolBytes = (size_t)1 << 47;       // beyond any address space
+static Matrix bytes_of(const void* p, size_t n) { return Matrix{(uintptr_t)p, n > 0 ? 1u : 0u, n, n}; }
+
+extern "C" int rlhf_op_window_attention(int act_dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                                        const int32_t* tile_start, const int32_t* tile_q0, const int32_t* tile_len, void* out,
+                                        int64_t ld_out, int n_tiles, int rows, int window, int sinks, int n_q_heads, int n_kv_heads,
+                                        int head_dim, void* stream) {
+    const int dt = act_of(act_dtype);
+    if (dt < 0 || n_tiles < 0 || rows < 0 || rows > 1 << 30 || window < 1 || sinks < 0 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
+        return RLHF_EINVAL;
+    const int qc = n_q_heads * head_dim, kc = n_kv_heads * head_dim;
+    if (ld_q < qc || ld_out < qc || ld_k < kc || ld_v < kc) return RLHF_EINVAL;
+    if (n_tiles == 0 || rows == 0) return RLHF_OK;
+    if (!tile_start || !tile_q0 || !tile_len || !in_pieces(q, ld_q, dt) || !in_pieces(k, ld_k, dt) || !in_pieces(v, ld_v, dt) || !in_pieces(out, ld_out, dt))
+        return RLHF_EINVAL;
+    const Matrix o = matrix(out, rows, qc, ld_out, dt);
+    if (overlap(o, matrix(q, rows, qc, ld_q, dt)) || overlap(o, matrix(k, rows, kc, ld_k, dt)) || overlap(o, matrix(v, rows, kc, ld_v, dt)))
+        return RLHF_EINVAL;
+    WindowArgs a;
+    a.q = q; a.k = k; a.v = v; a.ld_q = (size_t)ld_q; a.ld_k = (size_t)ld_k; a.ld_v = (size_t)ld_v;
+    a.tile_start = tile_start; a.tile_q0 = tile_q0; a.tile_len = tile_len;
+    a.out = out; a.ld_out = (size_t)ld_out; a.n_tiles = n_tiles; a.rows = rows;
+    a.window = window; a.sinks = sinks; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads;
+    return status_of(launch_window_attention((hipStream_t)stream, dt, head_dim, a));
+}
+
+extern "C" int rlhf_op_window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks) {
+    if (rows < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || max_ctx < 1 || window < 1 || sinks < 0) return 1;
+    return window_decode_nsplit(rows, n_q_heads, n_kv_heads, max_ctx, window, sinks);
+}
+
+extern "C" int64_t rlhf_op_window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int nsplit) {
+    return rows > 0 && n_q_heads > 0 && head_dim > 0 && nsplit > 1 ? (int64_t)window_decode_scratch_floats(rows, n_q_heads, head_dim, nsplit) : 0;
+}
+
+static int window_decode(bool four_bits, int act_dtype, const void* q, int64_t ld_q, const void* pool, int n_pages, const int32_t* page_table,
+                         int pt_stride, int n_samples, const int32_t* row_sample, const int32_t* ctx_len, void* out, int64_t ld_out,
+                         float* scratch, int rows, int layer, int nsplit, int window, int sinks, int n_layers, int n_q_heads,
+                         int n_kv_heads, int head_dim, void* stream) {
+    const int dt = act_of(act_dtype);
+    if (dt < 0 || rows < 0 || rows > 1 << 24 || nsplit < 1 || nsplit > 64 || window < 1 || sinks < 0 || layer < 0 || layer >= n_layers || n_layers > 1 << 16 ||
+        n_pages < 1 || n_pages >= 1 << 27 || n_samples < 1 || pt_stride < 1 || pt_stride >= 1 << 27 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
+        return RLHF_EINVAL;
+    const int qc = n_q_heads * head_dim;
+    if (ld_q < qc || ld_out < qc) return RLHF_EINVAL;
+    if (rows == 0) return RLHF_OK;
+    if (!pool || !aligned(pool, 16) || !page_table || !row_sample || !ctx_len || !in_pieces(q, ld_q, dt) || !in_pieces(out, ld_out, dt) ||
+        (nsplit > 1 && (!scratch || !aligned(scratch, 16))))
+        return RLHF_EINVAL;
+    const size_t page = four_bits ? (size_t)rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim)
+                                  : (size_t)n_layers * 2 * n_kv_heads * 16 * head_dim * elem_bytes(dt);
+    const Matrix o = matrix(out, rows, qc, ld_out, dt);
+    if (page > kMaxPoolBytes / n_pages || overlap(o, matrix(q, rows, qc, ld_q, dt)) || overlap(o, bytes_of(pool, page * n_pages))) return RLHF_EINVAL;
+    WindowDecodeArgs a;
+    a.q = q; a.pool = pool; a.page_table = page_table; a.row_sample = row_sample; a.ctx_len = ctx_len; a.out = out; a.part = scratch;
+    a.ld_q = (size_t)ld_q; a.ld_out = (size_t)ld_out; a.rows = rows; a.layer = layer; a.n_layers = n_layers;
+    a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.nsplit = nsplit; a.window = window; a.sinks = sinks;
+    a.n_pages = n_pages; a.n_samples = n_samples; a.pt_stride = pt_stride;
+    return status_of(launch_window_decode((hipStream_t)stream, dt, four_bits, head_dim, a));
+}
+
+extern "C" int rlhf_op_window_decode_attention(int act_dtype, const void* q, int64_t ld_q, const void* pool, int n_pages,
+                                               const int32_t* page_table, int pt_stride, int n_samples, const int32_t* row_sample,
+                                               const int32_t* ctx_len, void* out, int64_t ld_out, float* scratch, int rows, int layer,
+                                               int nsplit, int window, int sinks, int n_layers, int n_q_heads, int n_kv_heads,
+                                               int head_dim, void* stream) {
+    return window_decode(false, act_dtype, q, ld_q, pool, n_pages, page_table, pt_stride, n_samples, row_sample, ctx_len, out, ld_out, scratch, rows,
+                         layer, nsplit, window, sinks, n_layers, n_q_heads, n_kv_heads, head_dim, stream);
+}
+
+extern "C" int rlhf_op_kv4_decode_attention(int act_dtype, const void* q, int64_t ld_q, const void* pool, int n_pages,
+                                            const int32_t* page_table, int pt_stride, int n_samples, const int32_t* row_sample,
+                                            const int32_t* ctx_len, void* out, int64_t ld_out, float* scratch, int rows, int layer,
+                                            int nsplit, int window, int sinks, int n_layers, int n_q_heads, int n_kv_heads,
+                                            int head_dim, void* stream) {
+    return window_decode(true, act_dtype, q, ld_q, pool, n_pages, page_table, pt_stride, n_samples, row_sample, ctx_len, out, ld_out, scratch, rows,
+                         layer, nsplit, window, sinks, n_layers, n_q_heads, n_kv_heads, head_dim, stream);
+}
+
+extern "C" int64_t rlhf_op_kv4_page_bytes(int n_layers, int n_kv_heads, int head_dim) {
+    return n_layers > 0 && n_kv_heads > 0 && (head_dim == 64 || head_dim == 128)
+               ? (int64_t)n_layers * n_kv_heads * (int64_t)kv4_block_bytes(head_dim) : 0;
+}
+
+// Checks what append and read share; a row is n_kv_heads * head_dim elements.
+static bool kv4_args(int dt, const void* k, int64_t ld_k, const void* v, int64_t ld_v, const int32_t* slot, const void* pool, int n_pages,
+                     int rows, int layer, int n_layers, int n_kv_heads, int head_dim, bool writes_rows, Kv4Args* a) {
+    if (dt < 0 || rows < 0 || rows > 1 << 30 || n_pages < 1 || n_pages >= 1 << 27 || layer < 0 || layer >= n_layers || n_layers > 1 << 16 ||
+        !heads_ok(n_kv_heads, n_kv_heads, head_dim) || ld_k < (int64_t)n_kv_heads * head_dim || ld_v < (int64_t)n_kv_heads * head_dim)
+        return false;
+    if (rows > 0) {
+        const int cols = n_kv_heads * head_dim;
+        const Matrix mk = matrix(k, rows, cols, ld_k, dt), mv = matrix(v, rows, cols, ld_v, dt);
+        const size_t page = (size_t)rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim);
+        const Matrix mp = bytes_of(pool, page * n_pages);
+        if (page > kMaxPoolBytes / n_pages || !slot || !pool || !aligned(pool, 16) || !in_pieces(k, ld_k, dt) || !in_pieces(v, ld_v, dt) || overlap(mk, mp) || overlap(mv, mp) ||
+            (writes_rows && overlap(mk, mv)))
+            return false;
+    }
+    *a = Kv4Args{(void*)k, (void*)v, (size_t)ld_k, (size_t)ld_v, slot, (void*)pool, n_pages, rows, layer, n_layers, n_kv_heads};
+    return true;
+}
+
+extern "C" int rlhf_op_kv4_append(int act_dtype, const void* k, int64_t ld_k, const void* v, int64_t ld_v, const int32_t* kv_dst, void* pool,
+                                  int n_pages, int rows, int layer, int n_layers, int n_kv_heads, int head_dim, void* stream) {
+    const int dt = act_of(act_dtype);
+    Kv4Args a;
+    if (!kv4_args(dt, k, ld_k, v, ld_v, kv_dst, pool, n_pages, rows, layer, n_layers, n_kv_heads, head_dim, false, &a)) return RLHF_EINVAL;
+    return rows == 0 ? RLHF_OK : status_of(launch_kv4_append((hipStream_t)stream, dt, head_dim, a));
+}
+
+extern "C" int rlhf_op_kv4_read(int act_dtype, const void* pool, int n_pages, const int32_t* kv_src, void* k, int64_t ld_k, void* v, int64_t ld_v,
+                                int rows, int layer, int n_layers, int n_kv_heads, int head_dim, void* stream) {
+    const int dt = act_of(act_dtype);
+    Kv4Args a;
+    if (!kv4_args(dt, k, ld_k, v, ld_v, kv_src, pool, n_pages, rows, layer, n_layers, n_kv_heads, head_dim, true, &a)) return RLHF_EINVAL;
+    return rows == 0 ? RLHF_OK : status_of(launch_kv4_read((hipStream_t)stream, dt, head_dim, a));
+}
+
 extern "C" int rlhf_op_gemm_tall_grid(int tiles_m, int tiles_n) {
     return tiles_m > 0 && tiles_n > 0 ? gemm_tall_grid(tiles_m, tiles_n) : 0;
 }

@@ -1,0 +1,660 @@
+"""Attention with a sliding window and sinks, packed and paged, and the KV cache of 4 bits, against oracle/window.py in float64.
+
+Tolerances.  E = 2^-24 is the half step of float, U that of the output type.  With S = |q| |k| / sqrt(hd) (a sum of hd products, magnitudes)
+the greatest over the keys of a query, and A = the weighted mean of |v|, V the greatest |v|:
+  a score is off by at most hd E S by its products and sums, and by 4 E |z| <= 4 E S by scaling and the multiply-add in front of exp2;
+  a weight, relative to its like, by twice that and 4 E of exp2 and rescaling: t = E (2 (hd + 4) S + 8);
+  a sum of n terms by n / 16 + 32 additions one after the other of E each (pages or tiles of 16 and more keys are joined by trees);
+  where weights are rounded to 16 bits for the matrix units, each by W of itself: half a step of half (2^-11) at most, which bf16
+  reaches with two terms;
+so |o - o_exact| <= (2 t + 2 E (n / 16 + 32) + W) A + (U + 2 E)|o|, where 2 t counts numerator and denominator.  A is at most V; where weights round, A
+is that of the query itself.  Cache of 4 bits: the same with |k| = |c| + 8 |s|, |v| alike, the values that the cache holds being exact."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import window as W
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+TDT = {"fp32": torch.float32, "bf16": torch.bfloat16, "half": torch.float16}
+HALF_STEP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "half": 2.0 ** -11}
+ROUNDED = {"fp32": 0.0, "bf16": 2.0 ** -11, "half": 2.0 ** -11}        # W
+ALL = 2 ** 31 - 1
+
+
+def _R():
+    import paper_2409_13221_amd as R
+    return R
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _normal(r, *shape, dtype="fp32", std=1.0):
+    return torch.from_numpy((r.normal(size=shape) * std).astype(np.float32)).to(TDT[dtype])
+
+
+def _ints(a):
+    return torch.tensor(a, dtype=torch.int32, device="cuda")
+
+
+def _check(got, q, k, v, q_pos, window, sinks, dtype, k_size=None, v_size=None):
+    """got [T, Hq, hd] against attention of q [T, Hq, hd] over k, v [S, Hkv, hd] (float64)."""
+    want = W.attention(q, k, v, q_pos, window, sinks)
+    T, Hq, hd = q.shape
+    G = Hq // k.shape[1]
+    kk, vv = np.abs(k) if k_size is None else k_size, np.abs(v) if v_size is None else v_size
+    ones = np.ones((T, Hq, 1))
+    for t in range(T):
+        at = np.flatnonzero(W.visible([q_pos[t]], len(k), window, sinks)[0])
+        for h in range(Hq):
+            size = kk[at, h // G] @ np.abs(q[t, h]) / np.sqrt(hd)
+            z = k[at, h // G] @ q[t, h] / np.sqrt(hd)
+            p = np.exp(z - z.max())
+            mean = (p / p.sum()) @ vv[at, h // G]
+            tol = (2 * E * (2 * (hd + 4) * size.max() + 8) + 2 * E * (len(at) / 16 + 32) + ROUNDED[dtype]) * mean + (HALF_STEP[dtype] + 2 * E) * np.abs(want[t, h]) + 1e-30
+            if dtype == "half":
+                tol = tol + 2.0 ** -25
+            off = np.abs(got[t, h] - want[t, h])
+            assert (off <= tol).all(), (t, h, q_pos[t], float((off / tol).max()), float(off.max()))
+    return want
+
+
+# ------------------------------------------------------------------------------------------------ packed
+
+def _packed(seed, lens, Hq, Hkv, hd, dtype, behind=0, pad=0):
+    """q, k, v as columns of one buffer with `pad` more columns of NaN, rows behind the sequences of NaN."""
+    r = np.random.default_rng(seed)
+    rows, width = sum(lens), (Hq + 2 * Hkv) * hd
+    buf = torch.full((rows + behind, width + pad), float("nan"), dtype=TDT[dtype])
+    buf[:rows, :width] = _normal(r, rows, width, dtype=dtype)
+    buf[:rows, :Hq * hd] *= 2
+    buf = buf.cuda()
+    return buf[:, :Hq * hd], buf[:, Hq * hd:(Hq + Hkv) * hd], buf[:, (Hq + Hkv) * hd:width]
+
+
+def _packed_run(q, k, v, lens, window, sinks, Hq, Hkv, hd, out=None):
+    R = _R()
+    if out is None:
+        out = torch.full((q.shape[0], Hq * hd), 7.0, device="cuda", dtype=q.dtype)
+    R.rlhf_op_window_attention(q, k, v, R.rlhf_attention_tiles(lens), out, window, sinks, Hq, Hkv, hd)
+    torch.cuda.synchronize()
+    return out
+
+
+def _packed_check(out, q, k, v, lens, window, sinks, Hq, Hkv, hd, dtype, rows=None):
+    """Every sequence, or of it the given positions."""
+    start = 0
+    for n in lens:
+        s = slice(start, start + n)
+        pos = np.arange(n) if rows is None else np.array([i for i in rows if i < n], int)
+        if n:
+            _check(_np(out[s]).reshape(n, Hq, hd)[pos], _np(q[s]).reshape(n, Hq, hd)[pos], _np(k[s]).reshape(n, Hkv, hd), _np(v[s]).reshape(n, Hkv, hd),
+                   pos, window, sinks, dtype)
+        start += n
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(2, 2, 64), (2, 1, 128)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (2, 3), (16, 4), (63, 0), (64, 1), (65, 64), (128, 130), (100, 0), (ALL, 0), (3, ALL)])
+def test_packed(dtype, Hq, Hkv, hd, window, sinks):
+    lens = [1, 17, 128, 0, 129, 64, 200]
+    q, k, v = _packed(hd + window % 97, lens, Hq, Hkv, hd, dtype, behind=3, pad=8)
+    out = _packed_run(q, k, v, lens, window, sinks, Hq, Hkv, hd)
+    _packed_check(out, q, k, v, lens, window, sinks, Hq, Hkv, hd, dtype)
+    assert (out[sum(lens):] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (3, 1), (8, 1), (16, 2), (17, 1), (6, 3)])
+def test_packed_heads(dtype, Hq, Hkv):
+    lens = [40, 150]
+    q, k, v = _packed(Hq, lens, Hq, Hkv, 64, dtype)
+    _packed_check(_packed_run(q, k, v, lens, 30, 2, Hq, Hkv, 64), q, k, v, lens, 30, 2, Hq, Hkv, 64, dtype, rows=[0, 1, 31, 32, 33, 39, 127, 128, 149])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(700, 5), (ALL, 0), (257, 200), (5, 0)])
+def test_packed_long(dtype, hd, window, sinks):
+    lens = [1500, 3]
+    q, k, v = _packed(hd + sinks, lens, 4, 2, hd, dtype)
+    rows = [0, 4, 5, 6, 127, 128, 255, 256, 257, 258, 300, 699, 700, 701, 1023, 1024, 1279, 1280, 1499]
+    _packed_check(_packed_run(q, k, v, lens, window, sinks, 4, 2, hd), q, k, v, lens, window, sinks, 4, 2, hd, dtype, rows=rows)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_packed_hidden_keys_reach_nobody(dtype, bad, hd):
+    """Key 37 of 200 is not finite: it shows in the queries that see it, 37 to 56, and in no other."""
+    lens, window, sinks, Hq, Hkv = [200, 30], 20, 3, 2, 1
+    q, k, v = _packed(5, lens, Hq, Hkv, hd, dtype)
+    for t in (k, v):
+        kk = t.clone()
+        kk[37] = bad
+        a = (q, kk, v) if t is k else (q, k, kk)
+        out = _packed_run(*a, lens, window, sinks, Hq, Hkv, hd)
+        clean = _packed_run(q, k, v, lens, window, sinks, Hq, Hkv, hd)
+        sees = np.arange(230) // 37 == 1
+        sees[57:] = False
+        _packed_check(out, *a, lens, window, sinks, Hq, Hkv, hd, dtype, rows=[0, 5, 20, 35, 36, 57, 58, 60, 63, 64, 100, 128, 199])
+        if t is v or bad != bad:
+            assert not torch.isfinite(out[sees]).any()
+        assert torch.isfinite(clean).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_packed_a_sink_that_is_not_finite_shows_everywhere(dtype):
+    lens = [150]
+    q, k, v = _packed(6, lens, 2, 2, 64, dtype)
+    v[1] = float("nan")
+    out = _packed_run(q, k, v, lens, 10, 2, 2, 2, 64)
+    assert torch.isfinite(out[0]).all() and torch.isnan(out[1:]).all()
+    v[0], v[1] = float("nan"), 0
+    assert torch.isfinite(_packed_run(q, k, v, lens, 10, 0, 2, 2, 64)[10:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_packed_scores_of_great_size(dtype):
+    """Scores of 1e20 and more, all far apart and all negative: the greatest takes it all."""
+    lens = [140]
+    q, k, v = _packed(7, lens, 1, 1, 64, dtype)
+    q[:], k[:] = 0, 0
+    q[:, 0] = 1e17
+    size = 10.0 ** torch.arange(140, device="cuda").remainder(7).add(1).double()
+    k[:, 0] = -size.to(k.dtype)
+    out = _packed_run(q, k, v, lens, 7, 0, 1, 1, 64)
+    for i in (0, 6, 7, 20, 64, 127, 128, 139):
+        lo = max(0, i - 6)
+        best = lo + int(k[lo:i + 1, 0].float().argmax())
+        assert torch.equal(out[i], v[best]), i
+
+
+def test_packed_strides_views_and_streams():
+    """Rows of every second one of a buffer, on a stream of its own."""
+    lens, Hq, Hkv, hd = [90, 140], 4, 2, 64
+    q, k, v = _packed(8, lens, Hq, Hkv, hd, "half")
+    want = _packed_run(q, k, v, lens, 50, 2, Hq, Hkv, hd)
+    wide = lambda t: torch.full((2 * t.shape[0], t.shape[1] + 24), float("nan"), device="cuda", dtype=t.dtype)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        put = []
+        for t in (q, k, v):
+            b = wide(t)
+            b[::2, 8:8 + t.shape[1]] = t
+            put.append(b[::2, 8:8 + t.shape[1]])
+        o = wide(want)
+        _R().rlhf_op_window_attention(*put, _R().rlhf_attention_tiles(lens), o[::2, 16:16 + Hq * hd], 50, 2, Hq, Hkv, hd)
+    s.synchronize()
+    assert torch.equal(o[::2, 16:16 + Hq * hd], want)
+    assert torch.isnan(o[1::2]).all() and torch.isnan(o[::2, :16]).all() and torch.isnan(o[::2, 16 + Hq * hd:]).all()
+
+
+def test_packed_tiles_outside_the_rows_are_skipped():
+    R = _R()
+    q, k, v = _packed(9, [100], 2, 2, 64, "half")
+    t = R.rlhf_attention_tiles([40, 60])
+    t.tiles[:, 0] = _ints([-1, 0, 40])
+    out = torch.full((100, 128), 7.0, device="cuda", dtype=torch.half)
+    R.rlhf_op_window_attention(q, k, v, t, out, 9, 0, 2, 2, 64)
+    t.tiles[:, 0] = _ints([70, 0, 31])
+    R.rlhf_op_window_attention(q, k, v, t, out, 9, 0, 2, 2, 64)
+    t.tiles[:, 0] = _ints([0, -128, 40])
+    R.rlhf_op_window_attention(q, k, v, t, out, 9, 0, 2, 2, 64)
+    t.tiles[:, 0] = _ints([0, 128, 40])
+    R.rlhf_op_window_attention(q, k, v, t, out, 9, 0, 2, 2, 64)
+    assert (out[:40] == 7).all()
+    _check(_np(out[40:]).reshape(60, 2, 64), _np(q[40:]).reshape(60, 2, 64), _np(k[40:]).reshape(60, 2, 64), _np(v[40:]).reshape(60, 2, 64), np.arange(60), 9, 0,
+           "half")
+
+
+# ------------------------------------------------------------------------------------------------ paged
+
+class Paged:
+    """Contexts in a paged pool of garbage, pages in no order, rows in no order of the samples; layer 1 of 3.  Tokens beyond a context,
+    and pages of nobody, hold NaN."""
+
+    def __init__(self, seed, ctx, Hq, Hkv, hd, dtype, four=False, extra=3):
+        R, r = _R(), np.random.default_rng(seed)
+        self.Hq, self.Hkv, self.hd, self.dtype, self.four, self.ctx = Hq, Hkv, hd, dtype, four, ctx
+        self.layers, self.layer = 3, 1
+        rows, width = len(ctx), max(1, -(-max(ctx) // 16)) + 1
+        need = [-(-max(c, 0) // 16) for c in ctx]
+        order = r.permutation(sum(need) + extra)
+        self.n_pages = len(order)
+        self.sample = r.permutation(rows)
+        self.table = np.full((rows, width), -1, np.int32)              # entries of no page: never read
+        self.k, self.v, self.k_size, self.v_size, first = [], [], [], [], 0
+        if four:
+            pool = r.integers(0, 256, (self.n_pages, self.layers, Hkv, 18 * hd)).astype(np.uint8)
+            pool.view(np.float16)[..., 8 * hd:] = np.nan
+        else:
+            pool = torch.full((self.n_pages, self.layers, 2, Hkv, 16, hd), float("nan"), dtype=TDT[dtype])
+        slots = []
+        for i, c in enumerate(ctx):
+            pages = order[first:first + need[i]]
+            first += need[i]
+            self.table[self.sample[i], :need[i]] = pages
+            k, v = (_normal(r, max(c, 0), Hkv, hd, dtype=dtype) for _ in range(2))
+            if not four:
+                for t in range(c):
+                    pool[pages[t // 16], self.layer, 0, :, t % 16] = k[t]
+                    pool[pages[t // 16], self.layer, 1, :, t % 16] = v[t]
+            slots += [int(pages[t // 16]) * 16 + t % 16 for t in range(c)]
+            self.k.append(k), self.v.append(v)
+        self.q = _normal(r, rows, Hq * hd, dtype=dtype, std=2.0).cuda()
+        if four:
+            self.pool = torch.from_numpy(pool).cuda()
+            k, v = torch.cat(self.k).cuda().flatten(1), torch.cat(self.v).cuda().flatten(1)
+            R.rlhf_op_kv4_append(k, v, _ints(slots), self.pool, self.layer, self.layers, Hkv, hd)
+            self.k_size, self.v_size = [], []
+            for i in range(rows):
+                for kv, size in ((self.k, self.k_size), (self.v, self.v_size)):
+                    u, p = W.kv4_quantize(kv[i].float().numpy())
+                    p = np.abs(p.astype(np.float64))
+                    size.append(np.repeat(p[..., 1] + 8 * p[..., 0], 64, -1))
+                    kv[i] = W.kv4_values(u, W.kv4_quantize(kv[i].float().numpy())[1])
+        else:
+            self.pool = pool.cuda()
+            self.k, self.v = [_np(t) for t in self.k], [_np(t) for t in self.v]
+            self.k_size, self.v_size = [np.abs(t) for t in self.k], [np.abs(t) for t in self.v]
+        self.table_d, self.row_d, self.ctx_d = torch.from_numpy(self.table).cuda(), _ints(self.sample), _ints(ctx)
+
+    def run(self, window, sinks, q=None, out=None, **kw):
+        R = _R()
+        q = self.q if q is None else q
+        out = torch.full(q.shape, 7.0, device="cuda", dtype=q.dtype) if out is None else out
+        call = R.rlhf_op_kv4_decode_attention if self.four else R.rlhf_op_window_decode_attention
+        call(q, self.pool, self.table_d, self.row_d, self.ctx_d, out, self.layer, self.layers, self.Hq, self.Hkv, self.hd, window, sinks, **kw)
+        torch.cuda.synchronize()
+        return out
+
+    def check(self, out, window, sinks, rows=None):
+        got, q = (_np(t).reshape(len(self.ctx), self.Hq, self.hd) for t in (out, self.q))
+        for i, c in enumerate(self.ctx):
+            if rows is not None and i not in rows:
+                continue
+            if c <= 0:
+                assert (got[i] == 0).all()
+                continue
+            _check(got[i:i + 1], q[i:i + 1], self.k[i], self.v[i], np.array([c - 1]), window, sinks, self.dtype, self.k_size[i], self.v_size[i])
+
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 255, 256, 257, 300]
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (2, 20), (16, 4), (17, 0), (33, 16), (100, 17), (ALL, 0), (5, ALL)])
+def test_decode(four, dtype, hd, window, sinks):
+    p = Paged(window % 89 + sinks % 7, EDGES, 2, 2, hd, dtype, four)
+    for nsplit in (None, 1, 3):
+        p.check(p.run(window, sinks, nsplit=nsplit), window, sinks)
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (3, 1), (8, 1), (16, 1), (17, 1), (40, 2), (6, 3)])
+def test_decode_heads(four, dtype, Hq, Hkv):
+    p = Paged(Hq, [70, 5, 200], Hq, Hkv, 128, dtype, four)
+    for nsplit in (1, 2):
+        p.check(p.run(60, 4, nsplit=nsplit), 60, 4)
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("nsplit", [None, 1, 2, 7, 64])
+def test_decode_long(four, dtype, nsplit):
+    p = Paged(3, [3000, 1, 1777], 4, 2, 64, dtype, four)
+    for window, sinks in ((ALL, 0), (1500, 40)):
+        p.check(p.run(window, sinks, nsplit=nsplit), window, sinks)
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "half"])
+def test_decode_many_rows(four, dtype):
+    """More rows than the chip holds at once, with and without a bound of the contexts."""
+    r = np.random.default_rng(0)
+    p = Paged(4, r.integers(0, 60, 700).tolist(), 3, 3, 64, dtype, four)
+    a, b = p.run(25, 2), p.run(25, 2, max_ctx=60)
+    p.check(a, 25, 2, rows=range(0, 700, 23))
+    p.check(b, 25, 2, rows=range(0, 700, 23))
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("nsplit", [1, 2])
+def test_decode_pages_without_a_visible_token_are_not_read(four, nsplit):
+    """Their entries point outside the pool, or at pages of NaN."""
+    p = Paged(5, [200, 90], 2, 1, 64, "half", four)
+    want = p.run(40, 18, nsplit=nsplit)
+    for bad in (-5, 1 << 30, p.n_pages, None):
+        t = p.table.copy()
+        t[p.sample[0], 2:10], t[p.sample[1], 2:3] = (bad,) * 2 if bad is not None else (int(np.setdiff1d(np.arange(p.n_pages), p.table)[0]),) * 2
+        p.table_d = torch.from_numpy(t).cuda()
+        assert torch.equal(p.run(40, 18, nsplit=nsplit), want)
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("nsplit", [1, 3])
+@pytest.mark.parametrize("dtype", ["fp32", "half"])
+def test_decode_rows_outside_table_or_pool_are_nan(four, nsplit, dtype):
+    p = Paged(6, [200, 90, 33, 50, 17, 60], 2, 2, 64, dtype, four)
+    want = p.run(ALL, 0, nsplit=nsplit)
+    t = p.table.copy()
+    t[p.sample[0], 7], t[p.sample[1], 5] = p.n_pages, -1
+    p.table_d = torch.from_numpy(t).cuda()
+    p.row_d[2], p.row_d[3] = 6, -1
+    p.ctx_d[4] = 16 * t.shape[1] + 1
+    out = p.run(ALL, 0, nsplit=nsplit)
+    assert torch.isnan(out[:5]).all() and torch.equal(out[5], want[5])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("nsplit", [1, 4])
+def test_decode_is_the_last_row_of_packed(dtype, nsplit):
+    """Same queries, keys and values through both forms."""
+    p = Paged(7, [130, 64, 300], 4, 2, 128, dtype)
+    dec = p.run(70, 5, nsplit=nsplit)
+    rows = sum(p.ctx)
+    q = torch.zeros(rows, 4 * 128, dtype=TDT[dtype], device="cuda")
+    last = np.cumsum(p.ctx) - 1
+    q[last] = p.q
+    k, v = (torch.from_numpy(np.concatenate(t)).to(TDT[dtype]).flatten(1).cuda() for t in (p.k, p.v))
+    pre = _packed_run(q, k, v, p.ctx, 70, 5, 4, 2, 128)[last]
+    bound = 4 * HALF_STEP[dtype] + 2 * ROUNDED[dtype]                    # of each, twice; values up to 4
+    assert (dec.double() - pre.double()).abs().max() <= 4 * bound + 2e-5
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_decode_a_visible_token_that_is_not_finite(four, dtype):
+    p = Paged(8, [100, 100], 2, 2, 64, dtype, four)
+    page, off = int(p.table[p.sample[0], 5]), 3                          # token 83 of row 0
+    if four:
+        half = p.pool.view(torch.float16).view(p.n_pages, p.layers, 2, 9 * 64)
+        half[page, 1, 0, 8 * 64 + 32 + 2 * off:8 * 64 + 32 + 2 * off + 2] = float("nan")       # scale and center of V, first head
+    else:
+        p.pool[page, 1, 1, 0, off] = float("inf")
+    out = p.run(20, 0)
+    assert not torch.isfinite(out[0, :64]).any() and torch.isfinite(out[0, 64:]).all() and torch.isfinite(out[1]).all()
+    assert torch.isfinite(p.run(16, 0)).all()                            # hidden, in a page of which tokens 84 on are seen
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("nsplit", [1, 3])
+def test_decode_strided_and_on_a_stream(four, nsplit):
+    p = Paged(9, [40, 300, 0], 2, 2, 64, "half", four)
+    want = p.run(50, 3, nsplit=nsplit)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        q, o = torch.full((6, 136), float("nan"), device="cuda", dtype=torch.half), torch.full((3, 152), 7.0, device="cuda", dtype=torch.half)
+        q[::2, :128] = p.q
+        scratch = torch.full((_R().lib().rlhf_op_window_decode_scratch_floats(3, 2, 64, nsplit) + 8,), float("nan"), device="cuda")
+        p.run(50, 3, q=q[::2, :128], out=o[:, 8:136], nsplit=nsplit, scratch=scratch)
+    s.synchronize()
+    assert torch.equal(o[:, 8:136], want) and (o[:, :8] == 7).all() and (o[:, 136:] == 7).all()
+    assert torch.isnan(scratch[-8:]).all()
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+def test_decode_offsets_beyond_32_bits(four):
+    """The last pages of a pool of more than 2^32 elements (2^33 bytes; of 4 bits 2^32 + bytes)."""
+    R = _R()
+    Hkv, hd, layers = 8, 128, 64
+    page = R.rlhf_op_kv4_page_bytes(layers, Hkv, hd) if four else layers * 2 * Hkv * 16 * hd
+    n_pages = ((1 << 32) + (1 << 28)) // page + 2
+    p = Paged(10, [40, 17], 8, Hkv, hd, "half", four)
+    pool = torch.empty(n_pages * page, dtype=torch.uint8 if four else torch.half, device="cuda")
+    shape = (n_pages, layers, Hkv, 18 * hd) if four else (n_pages, layers, 2, Hkv, 16, hd)
+    pool = pool.view(shape)
+    pool[n_pages - p.n_pages:, layers - 1] = p.pool[:, p.layer]
+    p.pool, p.layers, p.layer = pool, layers, layers - 1
+    p.table_d += n_pages - p.n_pages
+    p.check(p.run(30, 1), 30, 1)
+    if four:
+        slots = _ints([(n_pages - 1) * 16 + 15, (n_pages - 2) * 16])
+        k, v = _normal(np.random.default_rng(0), 2, Hkv * hd).cuda(), _normal(np.random.default_rng(1), 2, Hkv * hd).cuda()
+        R.rlhf_op_kv4_append(k, v, slots, pool, layers - 1, layers, Hkv, hd)
+        rk, rv = torch.empty_like(k), torch.empty_like(v)
+        R.rlhf_op_kv4_read(pool, slots, rk, rv, layers - 1, layers, Hkv, hd)
+        np.testing.assert_array_equal(_np(rk), W.kv4_round(k.cpu().numpy().reshape(2, Hkv, hd)).reshape(2, -1).astype(np.float32))
+        np.testing.assert_array_equal(_np(rv), W.kv4_round(v.cpu().numpy().reshape(2, Hkv, hd)).reshape(2, -1).astype(np.float32))
+
+
+# ------------------------------------------------------------------------------------------------ cache of 4 bits
+
+def _blocks(k, v, Hkv, hd, slots, n_pages, layers, layer, start):
+    want = start.copy()
+    for i, s in enumerate(slots):
+        if 0 <= s < 16 * n_pages:
+            for h in range(Hkv):
+                W.kv4_write(want[s // 16, layer, h], s % 16, k[i, h], v[i, h])
+    return want
+
+
+def _append_case(seed, rows, Hkv, hd, dtype, n_pages):
+    r = np.random.default_rng(seed)
+    k, v = _normal(r, rows, Hkv, hd, dtype=dtype), _normal(r, rows, Hkv, hd, dtype=dtype, std=5.0)
+    start = r.integers(0, 256, (n_pages, 2, Hkv, 18 * hd)).astype(np.uint8)
+    return r, k, v, start
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("rows,Hkv,hd", [(1, 1, 64), (5, 3, 64), (37, 2, 128), (16, 1, 128), (100, 1, 64)])
+def test_append_writes_its_tokens_and_nothing_else(dtype, rows, Hkv, hd):
+    """Bytes equal to the oracle's, in a pool that held other bytes; slots out of order, some left out."""
+    R, n_pages = _R(), 9
+    r, k, v, start = _append_case(rows + hd, rows, Hkv, hd, dtype, n_pages)
+    slots = r.permutation(16 * n_pages)[:rows]
+    if rows >= 5:
+        slots[1], slots[3], slots[4] = -1, 16 * n_pages, 2 ** 31 - 1
+    pool = torch.from_numpy(start).cuda()
+    R.rlhf_op_kv4_append(k.cuda().flatten(1), v.cuda().flatten(1), _ints(slots.tolist()), pool, 1, 2, Hkv, hd)
+    want = _blocks(k.float().numpy(), v.float().numpy(), Hkv, hd, slots, n_pages, 2, 1, start)
+    np.testing.assert_array_equal(pool.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_append_in_order(dtype):
+    """Whole pages, and pages that a sequence enters and leaves in the middle."""
+    R, n_pages, rows = _R(), 5, 52
+    r, k, v, start = _append_case(3, rows, 2, 64, dtype, n_pages)
+    for first in (0, 5, 16, 28):
+        pool = torch.from_numpy(start).cuda()
+        slots = list(range(first, first + rows))
+        R.rlhf_op_kv4_append(k.cuda().flatten(1), v.cuda().flatten(1), _ints(slots), pool, 0, 2, 2, 64)
+        np.testing.assert_array_equal(pool.cpu().numpy(), _blocks(k.float().numpy(), v.float().numpy(), 2, 64, slots, n_pages, 2, 0, start))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_append_values_at_the_edges_of_the_rounding(dtype):
+    """Groups of one value, of two, of whole steps and halves between them, tiny, huge, far from zero, not finite."""
+    R, r, hd = _R(), np.random.default_rng(5), 128
+    t = TDT[dtype]
+    groups = [np.zeros(64), np.full(64, -0.0), np.full(64, 3.7), np.r_[np.full(63, -1.0), 2.0], np.tile(np.arange(16.0) - 3, 4), np.tile(np.arange(32) / 2.0, 2),
+              np.tile(np.arange(31) * 0.0625, 3)[:64], r.normal(size=64) * 1e-4, r.normal(size=64) * 1e-7, np.tile([5e-8, 0.0], 32), r.normal(size=64) * 1e4,
+              100 + r.normal(size=64) * 1e-3, np.r_[np.full(32, 65504.0), np.full(32, -65504.0)], np.r_[np.nan, np.zeros(63)], np.r_[np.zeros(63), np.inf],
+              np.r_[-np.inf, np.ones(63)], np.tile(np.arange(16.0), 4) * 2.0 ** -20, r.integers(-20, 21, 64) / 8.0, r.integers(-7, 9, 64) * 1.0, np.full(64, 1e-7)]
+    if dtype != "half":
+        groups += [np.r_[np.ones(63), 65600.0], np.r_[np.ones(63), -1e30], r.normal(size=64) * 1e-12]
+    groups += [r.integers(-60, 61, 64) / 4.0 for _ in range(8 + len(groups) % 2)]
+    x = torch.from_numpy(np.stack(groups).reshape(-1, 2 * 64).astype(np.float32)).to(t)
+    rows = x.shape[0]
+    n_pages = -(-rows // 16)
+    start = np.zeros((n_pages, 2, 1, 18 * hd), np.uint8)
+    pool = torch.from_numpy(start).cuda()
+    v = x.flip(0)
+    R.rlhf_op_kv4_append(x.cuda(), v.cuda(), _ints(list(range(rows))), pool, 1, 2, 1, hd)
+    k_oracle, v_oracle = x.float().numpy()[:, None], v.float().numpy()[:, None]
+    want = _blocks(k_oracle, v_oracle, 1, hd, range(rows), n_pages, 2, 1, start)
+    got = pool.cpu().numpy()
+    half = lambda a: a.view(np.float16)[..., 8 * hd:]
+    np.testing.assert_array_equal(half(got), half(want))                 # a NaN for a NaN
+    np.testing.assert_array_equal(got[..., :16 * hd], want[..., :16 * hd])
+    out = [torch.empty(rows, hd, device="cuda") for _ in range(2)]
+    R.rlhf_op_kv4_read(pool, _ints(list(range(rows))), *out, 1, 2, 1, hd)
+    np.testing.assert_array_equal(_np(out[0]), W.kv4_round(k_oracle)[:, 0].astype(np.float32))
+    np.testing.assert_array_equal(_np(out[1]), W.kv4_round(v_oracle)[:, 0].astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_codes_of_many_values(dtype):
+    """A million values on a coarse grid, where exact halves between steps are frequent, and as many off it."""
+    R, hd, Hkv, rows = _R(), 64, 16, 512
+    r = np.random.default_rng(6)
+    x = torch.from_numpy((r.integers(-120, 121, (rows, Hkv * hd)) / 8.0).astype(np.float32)).to(TDT[dtype])
+    y = _normal(r, rows, Hkv * hd, dtype=dtype)
+    pool = torch.zeros(rows // 16, 1, Hkv, 18 * hd, dtype=torch.uint8, device="cuda")
+    slots = _ints(r.permutation(rows).tolist())
+    R.rlhf_op_kv4_append(x.cuda(), y.cuda(), slots, pool, 0, 1, Hkv, hd)
+    out = [torch.empty(rows, Hkv * hd, device="cuda") for _ in range(2)]
+    R.rlhf_op_kv4_read(pool, slots, *out, 0, 1, Hkv, hd)
+    for got, t in zip(out, (x, y)):
+        np.testing.assert_array_equal(_np(got), W.kv4_round(t.float().numpy()).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_read(dtype):
+    """Any slots, some twice, into strided rows; zeros for a negative slot, NaN beyond the pool; one rounding."""
+    R, r, hd, Hkv, n_pages = _R(), np.random.default_rng(7), 128, 3, 6
+    pool = r.integers(0, 256, (n_pages, 2, Hkv, 18 * hd)).astype(np.uint8)
+    pool.view(np.float16)[..., 8 * hd:] = r.normal(size=(n_pages, 2, Hkv, hd)).astype(np.float16)
+    slots = [5, 95, -1, 0, 5, 96, 17, -2 ** 31, 2 ** 31 - 1, 16]
+    k, v = (torch.full((len(slots), Hkv * hd + 16), 7.0, device="cuda", dtype=TDT[dtype]) for _ in range(2))
+    R.rlhf_op_kv4_read(torch.from_numpy(pool).cuda(), _ints(slots), k[:, 8:8 + Hkv * hd], v[:, :Hkv * hd], 1, 2, Hkv, hd)
+    for i, s in enumerate(slots):
+        for h in range(Hkv):
+            want = [np.zeros(hd)] * 2 if s < 0 else [np.full(hd, np.nan)] * 2 if s >= 96 else [a[s % 16] for a in W.kv4_block_values(pool[s // 16, 1, h], hd)]
+            for t, at, w in ((k, 8, want[0]), (v, 0, want[1])):
+                # c + s u is exact in float but where the halves are more than 2^9 apart: one rounding there, one to the type
+                np.testing.assert_allclose(_np(t[i, at + h * hd:at + (h + 1) * hd]), w, rtol=HALF_STEP[dtype] + 1e-7, atol=1e-7)
+    assert (k[:, :8] == 7).all() and (k[:, -8:] == 7).all() and (v[:, Hkv * hd:] == 7).all()
+
+
+def test_append_and_read_strided():
+    R, hd, Hkv, rows = _R(), 64, 2, 40
+    q, k, v = _packed(11, [rows], 4, Hkv, hd, "bf16", pad=8)
+    pools = [torch.zeros(3, 1, Hkv, 18 * hd, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    slots = _ints(list(range(rows)))
+    R.rlhf_op_kv4_append(k, v, slots, pools[0], 0, 1, Hkv, hd)
+    R.rlhf_op_kv4_append(k.contiguous(), v.contiguous(), slots, pools[1], 0, 1, Hkv, hd)
+    assert torch.equal(*pools)
+
+
+# ------------------------------------------------------------------------------------------------ together
+
+def test_a_prompt_and_decode_steps():
+    """A prompt by packed attention, its K and V into both caches, then steps that append a token and attend, all through a window
+    that moves past the prompt; against float64 over the same keys."""
+    R = _R()
+    Hq, Hkv, hd, lens, window, sinks, steps = 4, 2, 64, [35, 20], 24, 3, 30
+    q, k, v = _packed(12, lens, Hq, Hkv, hd, "half")
+    _packed_check(_packed_run(q, k, v, lens, window, sinks, Hq, Hkv, hd), q, k, v, lens, window, sinks, Hq, Hkv, hd, "half")
+    width = 6
+    table = _ints(np.random.default_rng(0).permutation(2 * width).reshape(2, width).tolist())
+    pool = torch.full((2 * width, 1, 2, Hkv, 16, hd), float("nan"), device="cuda", dtype=torch.half)
+    pool4 = torch.full((2 * width, 1, Hkv, 18 * hd), 255, dtype=torch.uint8, device="cuda")
+    slot = lambda s, t: int(table[s, t // 16]) * 16 + t % 16
+
+    def put(kk, vv, slots):
+        R.rlhf_op_kv4_append(kk, vv, _ints(slots), pool4, 0, 1, Hkv, hd)
+        for i, s in enumerate(slots):
+            pool[s // 16, 0, 0, :, s % 16], pool[s // 16, 0, 1, :, s % 16] = kk[i].view(Hkv, hd), vv[i].view(Hkv, hd)
+
+    put(k, v, [slot(s, t) for s in range(2) for t in range(lens[s])])
+    keys = [[_np(k[:35]), _np(v[:35])], [_np(k[35:]), _np(v[35:])]]
+    r, row = np.random.default_rng(13), _ints([1, 0])
+    for step in range(steps):
+        nq, nk, nv = (_normal(r, 2, h * hd, dtype="half").cuda() for h in (Hq, Hkv, Hkv))
+        ctx = [n + step + 1 for n in lens]
+        put(nk, nv, [slot(s, ctx[s] - 1) for s in range(2)])
+        outs = [torch.empty_like(nq) for _ in range(2)]
+        args = (table, row, _ints([ctx[1], ctx[0]]))
+        rows = nq.flip(0).contiguous()
+        R.rlhf_op_window_decode_attention(rows, pool, *args, outs[0], 0, 1, Hq, Hkv, hd, window, sinks, max_ctx=max(ctx))
+        R.rlhf_op_kv4_decode_attention(rows, pool4, *args, outs[1], 0, 1, Hq, Hkv, hd, window, sinks, max_ctx=max(ctx))
+        for s in range(2):
+            keys[s] = [np.concatenate([a, _np(t[s:s + 1])]) for a, t in zip(keys[s], (nk, nv))]
+            kk, vv = (a.reshape(-1, Hkv, hd) for a in keys[s])
+            qq, pos = _np(nq[s]).reshape(1, Hq, hd), np.array([ctx[s] - 1])
+            _check(_np(outs[0][1 - s]).reshape(1, Hq, hd), qq, kk, vv, pos, window, sinks, "half")
+            k4, v4 = W.kv4_round(kk.astype(np.float32)), W.kv4_round(vv.astype(np.float32))
+            size = lambda a: np.repeat(np.abs(W.kv4_quantize(a.astype(np.float32))[1].astype(np.float64)) @ np.array([8.0, 1.0]), 64, -1)
+            _check(_np(outs[1][1 - s]).reshape(1, Hq, hd), qq, k4, v4, pos, window, sinks, "half", size(kk), size(vv))
+
+
+@pytest.mark.parametrize("nsplit", [1, 3])
+def test_captured_and_replayed(nsplit):
+    """Append and both decode attentions in one graph, replayed on new tokens with eager work in between; and two graphs, each with
+    a scratch of its own."""
+    R = _R()
+    p = Paged(14, [100, 40], 4, 2, 64, "half", True)
+    p16 = Paged(14, [100, 40], 4, 2, 64, "half", False)
+    k, v = torch.zeros(2, 128, device="cuda", dtype=torch.half), torch.zeros(2, 128, device="cuda", dtype=torch.half)
+    slots = _ints([int(p.table[p.sample[i], (c - 1) // 16]) * 16 + (c - 1) % 16 for i, c in enumerate(p.ctx)])
+    scratch = [torch.empty(R.lib().rlhf_op_window_decode_scratch_floats(2, 4, 64, nsplit), device="cuda") if nsplit > 1 else None for _ in range(4)]
+    outs = [torch.zeros_like(p.q) for _ in range(4)]
+
+    def work(i):
+        R.rlhf_op_kv4_append(k, v, slots, p.pool, 1, 3, 2, 64)
+        for j, x in ((i, p), (i + 1, p16)):
+            call = R.rlhf_op_kv4_decode_attention if x.four else R.rlhf_op_window_decode_attention
+            call(x.q, x.pool, x.table_d, x.row_d, x.ctx_d, outs[j], 1, 3, 4, 2, 64, 50, 2, nsplit=nsplit, scratch=scratch[j])
+
+    graphs = []
+    for i in (0, 2):
+        g = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            work(i)
+        torch.cuda.current_stream().wait_stream(side)
+        with torch.cuda.graph(g):
+            work(i)
+        graphs.append(g)
+    for step in range(4):
+        r = np.random.default_rng(step)
+        k.copy_(_normal(r, 2, 128, dtype="half")), v.copy_(_normal(r, 2, 128, dtype="half"))
+        p.q.copy_(_normal(r, 2, 256, dtype="half", std=2.0)), p16.q.copy_(p.q)
+        for o in outs:
+            o.fill_(7.0)
+        graphs[step % 2].replay()
+        graphs[1 - step % 2].replay()
+        torch.cuda.synchronize()
+        a, b = p.run(50, 2, nsplit=nsplit), p16.run(50, 2, nsplit=nsplit)
+        assert torch.equal(outs[0], a) and torch.equal(outs[2], a) and torch.equal(outs[1], b) and torch.equal(outs[3], b)
+        last = torch.empty(2, 128, device="cuda", dtype=torch.half)
+        R.rlhf_op_kv4_read(p.pool, slots, last, torch.empty_like(last), 1, 3, 2, 64)
+        np.testing.assert_array_equal(_np(last), _np(torch.from_numpy(W.kv4_round(k.float().cpu().numpy().reshape(2, 2, 64)).reshape(2, 128)).half()))
+
+
+def test_packed_captured_and_replayed():
+    R = _R()
+    lens = [150, 33]
+    q, k, v = _packed(15, lens, 4, 2, 64, "bf16")
+    tiles, out = R.rlhf_attention_tiles(lens), torch.zeros(183, 256, device="cuda", dtype=torch.bfloat16)
+    R.rlhf_op_window_attention(q, k, v, tiles, out, 60, 2, 4, 2, 64)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        R.rlhf_op_window_attention(q, k, v, tiles, out, 60, 2, 4, 2, 64)
+    for step in range(3):
+        q.copy_(torch.randn(q.shape, device="cuda"))
+        out.fill_(7.0)
+        g.replay()
+        assert torch.equal(out, _packed_run(q, k, v, lens, 60, 2, 4, 2, 64))
+
+
+def test_same_call_same_bits():
+    for four in (False, True):
+        p = Paged(16, [900, 1200, 64], 8, 2, 128, "bf16", four)
+        a = p.run(ALL, 0, nsplit=5)
+        for _ in range(3):
+            assert torch.equal(p.run(ALL, 0, nsplit=5), a)
