@@ -31,77 +31,450 @@ __device__ __forceinline__ int row_context(const WindowDecodeArgs& a, int r, con
     return ctx;
 }
 
-// One element of K (or V) of a token of a page.
-template <typename T, int HD> struct PlainCache {
-    const T* p;
-    int heads;
-    __device__ PlainCache(const WindowDecodeArgs& a, int page, int kh)
-        : p((const T*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD), heads(a.n_kv_heads) {}
-    __device__ float k(int t, int d) const { return to_f32<T>(p[t * HD + d]); }
-    __device__ float v(int t, int d) const { return to_f32<T>(p[(size_t)heads * 16 * HD + t * HD + d]); }
-};
-template <int HD> struct FourBitCache {
-    using L = Kv4<HD>;
-    const uint8_t* p;
-    __device__ FourBitCache(const WindowDecodeArgs& a, int page, int kh)
-        : p((const uint8_t*)a.pool + (((size_t)page * a.n_layers + a.layer) * a.n_kv_heads + kh) * L::BLOCK) {}
-    __device__ float value(int at, int bit, int par) const {
-        const f16_t* sc = (const f16_t*)(p + par);
-        return (float)sc[1] + (float)sc[0] * (float)((p[at] >> bit & 15) - 8);
+// ---- a page's K and V of one KV head as operands of the matrix units.  Scores are S^T = K Q^T (16 tokens x 16 query heads): a lane holds
+// tokens 4c .. 4c + 3 of head n, n = lane % 16, c = lane / 16, which is also how O^T += V^T P^T takes the weights: they never leave their lane.
+// Query heads beyond a KV head's own repeat the last one.
+
+typedef f16_t f16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// Every byte of the cache is read once a step: evict-first.
+template <typename V> __device__ __forceinline__ V ld_once(const void* p) { return __builtin_nontemporal_load((const V*)p); }
+
+// Greatest of (sum over) the four lanes that hold a head's tokens.
+__device__ __forceinline__ float head_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float head_sum(float x) {
+    x += __shfl_xor(x, 16, kWave);
+    return x + __shfl_xor(x, 32, kWave);
+}
+
+constexpr float NONE = 1e9f;            // no offset yet
+
+template <typename T> struct Matrix16;
+template <> struct Matrix16<f16_t> {
+    // Weights up to 2^14: what half loses below its normal range is 2^-39 of the greatest.
+    static constexpr float TOP = 14.f;
+    static __device__ __forceinline__ f32x4_t qk(u32x4_t a, u32x4_t b, f32x4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
     }
-    __device__ float k(int t, int d) const { return value(L::k_byte(t, d), L::k_bit(d), L::param(t, d)); }
-    __device__ float v(int t, int d) const { return value(L::v_byte(t, d), L::v_bit(d), L::param(t, d) + L::PARAMS); }
+    static __device__ __forceinline__ f32x4_t pv(u32x2_t a, u32x2_t b, f32x4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, a), __builtin_bit_cast(f16x4_t, b), c, 0, 0, 0);
+    }
+};
+template <> struct Matrix16<bf16_t> {
+    static constexpr float TOP = 0.f;
+    static __device__ __forceinline__ f32x4_t qk(u32x4_t a, u32x4_t b, f32x4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4_t pv(u32x2_t a, u32x2_t b, f32x4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, b), c, 0, 0, 0);
+    }
 };
 
-// A wave takes a row, a query head and a part of the row's visible pages.
-template <typename T, typename Cache, int HD>
-__global__ __launch_bounds__(64) void k_window_decode(WindowDecodeArgs a) {
-    const int lane = threadIdx.x;
-    const int split = blockIdx.x % a.nsplit, h = blockIdx.x / a.nsplit % a.n_q_heads, r = blockIdx.x / a.nsplit / a.n_q_heads;
-    const int kh = h / (a.n_q_heads / a.n_kv_heads);
-    constexpr int D = HD / 64;
+// A 16-bit cache.  K as it lies: a lane has 8 dims of token n.  V: dims D n .. D n + D - 1 (D = HD / 16) of its four tokens, so that a row of V
+// is read by 16 lanes side by side; pairs of tokens are put together by byte permutations.  Weights go in as two terms of the type, which
+// leaves 2^-16 of them and less (their products are exact): the output's own rounding is what is seen.  Matrix units are idle here anyway.
+template <typename T_, int HD_> struct Cache16 {
+    using T = T_;
+    using M = Matrix16<T>;
+    static constexpr int HD = HD_, D = HD / 16, KS = HD / 32;
+    static constexpr float TOP = M::TOP;
+    typedef uint32_t VRow __attribute__((ext_vector_type(D / 2)));
+    struct Query {
+        u32x4_t q[KS];
+        float unit = 1.f;
+        __device__ __forceinline__ void load(const T* p, int c) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) q[s] = *(const u32x4_t*)(p + s * 32 + c * 8);
+        }
+    };
+    struct Sums {
+        f32x4_t acc[D];
+        __device__ __forceinline__ void clear() {
+#pragma unroll
+            for (int d = 0; d < D; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) acc[d] *= f;
+        }
+        // Dims of the head from `put`'s first argument on, as the lane holds them.
+        template <typename F> __device__ __forceinline__ void each(int c, F put) const {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int d = 0; d < D; d += 4) put((4 * c + r) * D + d, f32x4_t{acc[d][r], acc[d + 1][r], acc[d + 2][r], acc[d + 3][r]});
+        }
+        __device__ __forceinline__ void finish() {}
+    };
+    struct Tile {
+        u32x4_t k[KS];
+        VRow v[4];
+        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
+            const T* p = (const T*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
+            const T* pv = p + (size_t)a.n_kv_heads * 16 * HD;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) k[s] = ld_once<u32x4_t>(p + n * HD + s * 32 + c * 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = ld_once<VRow>(pv + (4 * c + i) * HD + n * D);
+        }
+        __device__ __forceinline__ f32x4_t scores(const Query& q) const {
+            f32x4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) s = M::qk(k[i], q.q[i], s);
+            return s;
+        }
+        __device__ __forceinline__ void hide(int i) {
+#pragma unroll
+            for (int w = 0; w < D / 2; ++w) v[i][w] = 0;
+        }
+        __device__ __forceinline__ float spare(float) const { return -TOP; }
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
+            const u32x2_t hi{pack2<T>(p[0], p[1]), pack2<T>(p[2], p[3])};
+            const u32x2_t lo{pack2<T>(p[0] - unpack<T>(hi[0], 0), p[1] - unpack<T>(hi[0], 1)), pack2<T>(p[2] - unpack<T>(hi[1], 0), p[3] - unpack<T>(hi[1], 1))};
+#pragma unroll
+            for (int w = 0; w < D / 2; ++w)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t sel = half ? 0x07060302u : 0x05040100u;
+                    const u32x2_t x{__builtin_amdgcn_perm(v[1][w], v[0][w], sel), __builtin_amdgcn_perm(v[3][w], v[2][w], sel)};
+                    o.acc[2 * w + half] = M::pv(x, lo, M::pv(x, hi, o.acc[2 * w + half]));
+                }
+        }
+    };
+};
+
+// A float cache: k = 4 products, a lane has 4 dims of token n (K), and D dims of its four tokens (V).
+template <int HD_> struct CacheFloat {
+    using T = float;
+    static constexpr int HD = HD_, D = HD / 16;
+    static constexpr float TOP = 0.f;
+    struct Query {
+        f32x4_t q[D];
+        float unit = 1.f;
+        __device__ __forceinline__ void load(const float* p, int c) {
+#pragma unroll
+            for (int s = 0; s < D; ++s) q[s] = *(const f32x4_t*)(p + s * 16 + c * 4);
+        }
+    };
+    using Sums = typename Cache16<f16_t, HD>::Sums;
+    struct Tile {
+        f32x4_t k[D], v[4][D / 4];
+        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
+            const float* p = (const float*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
+            const float* pv = p + (size_t)a.n_kv_heads * 16 * HD;
+#pragma unroll
+            for (int s = 0; s < D; ++s) k[s] = ld_once<f32x4_t>(p + n * HD + s * 16 + c * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < D / 4; ++d) v[i][d] = ld_once<f32x4_t>(pv + (4 * c + i) * HD + n * D + d * 4);
+        }
+        __device__ __forceinline__ f32x4_t scores(const Query& q) const {
+            f32x4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q.q[i][e], s, 0, 0, 0);
+            return s;
+        }
+        __device__ __forceinline__ void hide(int i) {
+#pragma unroll
+            for (int d = 0; d < D / 4; ++d) v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        __device__ __forceinline__ float spare(float) const { return -TOP; }
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < D; ++d) o.acc[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][d / 4][d % 4], p[i], o.acc[d], 0, 0, 0);
+        }
+    };
+};
+
+// A cache of 4 bits.  Codes become halves u = -8 .. 7 by putting their bits into the mantissa of 1024: 9 instructions for 8 of them.  With scale s and
+// center c of each token and 64 dims (group g),
+//   q.k = sum over g of s_g (sum q u) + c_g (sum of q in g),   o = sum over tokens of (p s_g) u + p c_g:
+// the matrix units take q and p s_g, the rest is a few multiply-adds a token.  A query is scaled to have its greatest magnitude in [2^14, 2^15)
+// and taken as halves, exact from half and bfloat16 down to 2^-39 of that; from float in three terms.  Weights p are scaled such that p s_g fits
+// half (spare), in one term, of float calls two.
+template <typename T_, int HD_> struct Cache4 {
+    using T = T_;
+    using L = Kv4<HD_>;
+    static constexpr int HD = HD_, KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 3 : 1;
+    typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
+    // Eight codes of a word as halves, in the order 0 4 1 5 2 6 3 7.
+    static __device__ __forceinline__ void halves(uint32_t x, uint32_t (&h)[4]) {
+        typedef f16_t pair __attribute__((ext_vector_type(2)));
+        const auto low = [](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair, (w & 0x000F000Fu) | 0x64006400u) - pair{1032, 1032}); };
+        const auto high = [](uint32_t w) {
+            const pair v = __builtin_bit_cast(pair, (w & 0x00F000F0u) | 0x64006400u), f{0.0625, 0.0625}, o{-72, -72};
+            return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, f, o));
+        };
+        h[0] = low(x);
+        h[1] = high(x);
+        h[2] = low(x >> 8);
+        h[3] = high(x >> 8);
+    }
+    struct Query {
+        u32x4_t q[KS][TERMS];
+        float sum[GROUPS], unit;
+        __device__ __forceinline__ void load(const T* p, int c) {
+            float f[KS][8], m = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                load8<T>(p + s * 32 + c * 8, f[s]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(f[s][e]));
+            }
+            m = head_max(m);
+            const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
+            unit = ldexpf(1.f, -up);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                sum[g] = 0.f;
+#pragma unroll
+                for (int s = 2 * g; s < 2 * g + 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[g] += f[s][e] = ldexpf(f[s][e], up);
+                sum[g] = head_sum(sum[g]);
+            }
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t h = pack2<f16_t>(f[s][e], f[s][e + 4]);
+                        q[s][t][e] = h;
+                        f[s][e] -= unpack<f16_t>(h, 0);
+                        f[s][e + 4] -= unpack<f16_t>(h, 1);
+                    }
+        }
+    };
+    struct Sums {
+        f32x4_t acc[HD / 16];
+        float center[GROUPS];
+        __device__ __forceinline__ void clear() {
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) center[g] = 0.f;
+        }
+        __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) acc[d] *= f;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) center[g] *= f;
+        }
+        __device__ __forceinline__ void finish() {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) center[g] = head_sum(center[g]);
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) acc[d] += center[d / 4];
+        }
+        template <typename F> __device__ __forceinline__ void each(int c, F put) const {
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) put(16 * d + 4 * c, acc[d]);
+        }
+    };
+    struct Tile {
+        Codes k, v;
+        u32x4_t kp[GROUPS], vp[GROUPS];            // (scale, center) of the lane's four tokens
+        static __device__ __forceinline__ float scale_of(uint32_t w) { return unpack<f16_t>(w, 0); }
+        static __device__ __forceinline__ float center_of(uint32_t w) { return unpack<f16_t>(w, 1); }
+        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
+            const uint8_t* p = (const uint8_t*)a.pool + (((size_t)page * a.n_layers + a.layer) * a.n_kv_heads + kh) * L::BLOCK;
+            k = ld_once<Codes>(p + (16 * c + n) * L::PIECE);
+            v = ld_once<Codes>(p + L::V_CODES + (16 * c + n) * L::PIECE);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                kp[g] = ld_once<u32x4_t>(p + L::param(4 * c, 64 * g));
+                vp[g] = ld_once<u32x4_t>(p + L::PARAMS + L::param(4 * c, 64 * g));
+            }
+        }
+        __device__ __forceinline__ f32x4_t scores(const Query& q) const {
+            f32x4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                f32x4_t raw{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 2 * g; i < 2 * g + 2; ++i) {
+                    uint32_t h[4];
+                    halves(k[i], h);
+                    const u32x4_t x{h[0], h[1], h[2], h[3]};
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) raw = Matrix16<f16_t>::qk(x, q.q[i][t], raw);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[r] = fmaf(scale_of(kp[g][r]), raw[r], fmaf(center_of(kp[g][r]), q.sum[g], s[r]));
+            }
+            return s;
+        }
+        __device__ __forceinline__ void hide(int i) {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) vp[g][i] = 0;
+        }
+        // What to add to the reference (log2) so that p s stays below 2^15: `now` where it does.
+        __device__ __forceinline__ float spare(float now) const {
+            float s = 0.f;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s = fmaxf(s, fabsf(scale_of(vp[g][r])));
+            const float most = s * __builtin_amdgcn_exp2f(-now);
+            if (!__any(!(most < 32768.f)) && now != NONE) return now;
+            s = wave_max(s);
+            return s > 0.f ? (float)ilogbf(s) - 9.f : -14.f;
+        }
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                float w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    w[r] = p[r] * scale_of(vp[g][r]);
+                    o.center[g] = fmaf(p[r], center_of(vp[g][r]), o.center[g]);
+                }
+                const u32x2_t hi{pack2<f16_t>(w[0], w[2]), pack2<f16_t>(w[1], w[3])};
+                u32x2_t lo{0, 0};
+                if (TERMS > 1)
+                    lo = u32x2_t{pack2<f16_t>(w[0] - unpack<f16_t>(hi[0], 0), w[2] - unpack<f16_t>(hi[0], 1)),
+                                 pack2<f16_t>(w[1] - unpack<f16_t>(hi[1], 0), w[3] - unpack<f16_t>(hi[1], 1))};
+#pragma unroll
+                for (int i = 2 * g; i < 2 * g + 2; ++i) {
+                    uint32_t h[4];
+                    halves(v[i], h);                       // tokens (0, 2) of dims 32 i + n, of dims 32 i + 16 + n, then (1, 3) alike
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const u32x2_t x{h[e], h[2 + e]};
+                        f32x4_t& acc = o.acc[2 * i + e];
+                        acc = Matrix16<f16_t>::pv(x, hi, acc);
+                        if (TERMS > 1) acc = Matrix16<f16_t>::pv(x, lo, acc);
+                    }
+                }
+            }
+        }
+    };
+};
+
+// A workgroup takes a row, a KV head (up to 16 of its query heads) and a part of the row's visible pages; its waves take these in turn, a page in
+// flight while one is worked on, and meet in LDS.  m: greatest score; weights are exp2(z - ref), ref = m + spare in log2.
+template <typename C, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a) {
+    using T = typename C::T;
+    constexpr int HD = C::HD;
+    extern __shared__ float lds[];                 // [WAVES][heads][HD] sums, then [WAVES][heads] references, [WAVES][heads] weights
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
+    const int G = a.n_q_heads / a.n_kv_heads, blocks = (G + 15) / 16;
+    unsigned b = blockIdx.x;
+    const int split = b % a.nsplit;
+    b /= a.nsplit;
+    const int hb = b % blocks;
+    b /= blocks;
+    const int kh = b % a.n_kv_heads, r = b / a.n_kv_heads, h0 = kh * G + hb * 16, heads = min(16, G - hb * 16), room = min(16, G);
     const int* table = nullptr;
     const int ctx = row_context(a, r, table);
-    const T* q = (const T*)a.q + (size_t)r * a.ld_q + (size_t)h * HD;
-    float m = -INFINITY, l = 0.f, acc[D] = {};
+    float m = -INFINITY, l = 0.f, ref = -INFINITY, off = NONE;
+    typename C::Sums o;
+    o.clear();
     bool lost = ctx < 0;
     if (ctx > 0) {
+        typename C::Query q;
+        q.load((const T*)a.q + (size_t)r * a.ld_q + (size_t)(h0 + min(n, heads - 1)) * HD, c);
+        const float unit = q.unit * (1.44269504088896f * rsqrtf((float)HD));
         const Visible see(ctx, a.window, a.sinks);
         const int from = (int)((int64_t)see.n_pages * split / a.nsplit), to = (int)((int64_t)see.n_pages * (split + 1) / a.nsplit);
-        for (int i = from; i < to; ++i) {
-            const int pi = see.page(i), id = table[pi];
-            if (id < 0 || id >= a.n_pages) { lost = true; break; }
-            const Cache c(a, id, kh);
-            float s = -INFINITY;
-            if (lane < 16 && see.sees(pi * 16 + lane)) {
-                s = 0.f;
-                for (int d = 0; d < HD; ++d) s += to_f32<T>(q[d]) * c.k(lane, d);
-                s *= rsqrtf((float)HD);
+        const int mine = to - from > wave ? (to - from - wave + WAVES - 1) / WAVES : 0;
+        int ids = 0;                               // of the next 64 pages, one a lane
+        const auto index = [&](int j) { return see.page(from + wave + j * WAVES); };
+        const auto fetch = [&](typename C::Tile& t, int j) {
+            if (j % 64 == 0) ids = j + lane < mine ? table[index(j + lane)] : 0;
+            int id = __builtin_amdgcn_readlane(ids, j % 64);
+            if ((unsigned)id >= (unsigned)a.n_pages) { lost = true; id = 0; }
+            t.load(a, id, kh, n, c);
+        };
+        const auto step = [&](typename C::Tile& t, int j) {
+            f32x4_t s = t.scores(q);
+            const int first = index(j) * 16;
+            if (first + 15 >= ctx || !(first >= see.lo || first + 15 < see.sinks)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!see.sees(first + 4 * c + i)) {
+                        s[i] = -INFINITY;
+                        t.hide(i);
+                    }
             }
-            const float mn = fmaxf(m, wave_max(s)), ref = mn == -INFINITY ? 0.f : mn, keep = expf(m - ref);
-            const float p = lane < 16 && see.sees(pi * 16 + lane) ? expf(s - ref) : 0.f;
+            const float mn = fmaxf(m, head_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+            off = t.spare(off);
+            const float rn = mn == -INFINITY ? 0.f : fmaf(mn, unit, off);
+            if (__any(!(rn == ref))) {
+                const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - rn);
+                l *= keep;
+                o.scale(keep);
+                ref = rn;
+            }
             m = mn;
-            l = l * keep + wave_sum(p);
+            f32x4_t p;
 #pragma unroll
-            for (int e = 0; e < D; ++e) acc[e] *= keep;
-            for (int t = 0; t < 16; ++t) {
-                const float pt = __shfl(p, t, kWave);
-                if (!see.sees(pi * 16 + t)) continue;
-#pragma unroll
-                for (int e = 0; e < D; ++e) acc[e] += pt * c.v(t, e * 64 + lane);
+            for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], unit, -rn));
+            l += (p[0] + p[1]) + (p[2] + p[3]);
+            t.add(p, o);
+        };
+        typename C::Tile t0, t1;
+        if (mine > 0) fetch(t0, 0);
+        for (int j = 0; j < mine; j += 2) {
+            if (j + 1 < mine) fetch(t1, j + 1);
+            step(t0, j);
+            if (j + 1 < mine) {
+                if (j + 2 < mine) fetch(t0, j + 2);
+                step(t1, j + 1);
             }
         }
     }
     if (lost) l = NAN;
-    if (a.nsplit == 1) {
-        T* o = (T*)a.out + (size_t)r * a.ld_out + (size_t)h * HD;
+    l = head_sum(l);
+    o.finish();
+    if (m == -INFINITY) ref = -INFINITY;           // nothing seen, or scores of -inf alone
+    float* s_ref = lds + WAVES * room * HD;
+    float* s_l = s_ref + WAVES * room;
+    if (n < heads) {
+        o.each(c, [&](int d, f32x4_t x) { *(f32x4_t*)(lds + (wave * room + n) * HD + d) = x; });
+        if (c == 0) {
+            s_ref[wave * room + n] = ref;
+            s_l[wave * room + n] = l;
+        }
+    }
+    __syncthreads();
+    const size_t slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
+    for (int i = threadIdx.x; i < heads * (HD / 4); i += WAVES * 64) {
+        const int h = i / (HD / 4), d = i % (HD / 4) * 4;
+        float top = -INFINITY, sum = 0.f;
+        f32x4_t x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < D; ++e) o[e * 64 + lane] = round_to<T>(ctx == 0 ? 0.f : acc[e] / l);
-    } else {
-        const size_t slot = blockIdx.x, slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
-        if (lane == 0) { a.part[2 * slot] = m; a.part[2 * slot + 1] = l; }
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_ref[w * room + h]);
 #pragma unroll
-        for (int e = 0; e < D; ++e) a.part[2 * slots + slot * HD + e * 64 + lane] = acc[e];
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_ref[w * room + h] - top);
+            sum += f * s_l[w * room + h];
+            x += f * *(const f32x4_t*)(lds + (w * room + h) * HD + d);
+        }
+        if (a.nsplit == 1) {
+            T* out = (T*)a.out + (size_t)r * a.ld_out + (size_t)(h0 + h) * HD + d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = round_to<T>(ctx == 0 ? 0.f : x[e] / sum);
+        } else {
+            const size_t slot = ((size_t)r * a.n_q_heads + h0 + h) * a.nsplit + split;
+            if (d == 0) { a.part[2 * slot] = top; a.part[2 * slot + 1] = sum; }
+            *(f32x4_t*)(a.part + 2 * slots + slot * HD + d) = x;
+        }
     }
 }
 
@@ -116,7 +489,7 @@ __global__ __launch_bounds__(64) void k_window_join(WindowDecodeArgs a) {
     for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, ml[s].x);
     const float ref = m == -INFINITY ? 0.f : m;
     for (int s = 0; s < a.nsplit; ++s) {
-        const float w = expf(ml[s].x - ref);
+        const float w = __builtin_amdgcn_exp2f(ml[s].x - ref);
         l += w * ml[s].y;
 #pragma unroll
         for (int e = 0; e < D; ++e) acc[e] += w * a.part[2 * slots + (slot + s) * HD + e * 64 + lane];
@@ -127,20 +500,27 @@ __global__ __launch_bounds__(64) void k_window_join(WindowDecodeArgs a) {
     for (int e = 0; e < D; ++e) o[e * 64 + lane] = round_to<T>(empty ? 0.f : acc[e] / l);
 }
 
+// Waves of a workgroup; four where 16 heads' sums of eight would take more than 64 KB of LDS.
+static int decode_waves(int group) { return group > 8 ? 4 : 8; }
+
 int window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks) {
     const int64_t pages = std::min<int64_t>((max_ctx + 15ll) / 16, (sinks + 15ll) / 16 + (window + 15ll) / 16 + 1);
-    const int64_t blocks = (int64_t)rows * n_q_heads;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({64, pages / 4, 2048 / blocks}));
+    const int group = n_q_heads / n_kv_heads, waves = decode_waves(group);
+    const int64_t blocks = (int64_t)rows * n_kv_heads * ((group + 15) / 16);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({64, pages / (2 * waves), 4096 / waves / blocks}));
 }
 
 size_t window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int nsplit) {
     return (size_t)rows * n_q_heads * nsplit * (head_dim + 2);
 }
 
-template <typename T, bool FOUR, int HD>
+template <typename C>
 static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
-    using Cache = std::conditional_t<FOUR, FourBitCache<HD>, PlainCache<T, HD>>;
-    const int most = (int)std::min<int64_t>(std::max<int64_t>(1, kLaunchThreads / 64 / a.n_q_heads / a.nsplit), 1 << 24);
+    using T = typename C::T;
+    const int group = a.n_q_heads / a.n_kv_heads, waves = decode_waves(group);
+    const int64_t blocks = (int64_t)a.n_kv_heads * ((group + 15) / 16) * a.nsplit;
+    const int most = (int)std::min<int64_t>(kLaunchThreads / (64 * waves) / std::max<int64_t>(blocks, a.n_q_heads), 1 << 24);
+    const size_t lds = (size_t)waves * std::min(16, group) * (C::HD + 2) * sizeof(float);
     for (int first = 0; first < a.rows; first += most) {
         WindowDecodeArgs p = a;
         p.q = (const T*)a.q + (size_t)first * a.ld_q;
@@ -148,25 +528,27 @@ static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
         p.row_sample += first;
         p.ctx_len += first;
         p.rows = std::min(most, a.rows - first);
-        const unsigned heads = (unsigned)p.rows * (unsigned)a.n_q_heads;
-        k_window_decode<T, Cache, HD><<<heads * a.nsplit, 64, 0, st>>>(p);
-        if (a.nsplit > 1) k_window_join<T, HD><<<heads, 64, 0, st>>>(p);
+        const unsigned grid = (unsigned)(p.rows * blocks);
+        if (waves == 8) k_window_decode<C, 8><<<grid, 512, lds, st>>>(p);
+        else k_window_decode<C, 4><<<grid, 256, lds, st>>>(p);
+        if (a.nsplit > 1) k_window_join<T, C::HD><<<(unsigned)p.rows * (unsigned)a.n_q_heads, 64, 0, st>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-template <typename T>
-static hipError_t decode_typed(hipStream_t st, bool four, int hd, const WindowDecodeArgs& a) {
-    if (four) return hd == 128 ? decode_rows<T, true, 128>(st, a) : decode_rows<T, true, 64>(st, a);
-    return hd == 128 ? decode_rows<T, false, 128>(st, a) : decode_rows<T, false, 64>(st, a);
-}
-
 hipError_t launch_window_decode(hipStream_t st, int dtype, bool four_bits, int head_dim, const WindowDecodeArgs& a) {
-    return dtype == kBF16 ? decode_typed<bf16_t>(st, four_bits, head_dim, a)
-         : dtype == kF16  ? decode_typed<f16_t>(st, four_bits, head_dim, a)
-                          : decode_typed<float>(st, four_bits, head_dim, a);
+#define RLHF_DECODE(HD)                                                                                           \
+    if (head_dim == HD) {                                                                                         \
+        if (dtype == kBF16) return four_bits ? decode_rows<Cache4<bf16_t, HD>>(st, a) : decode_rows<Cache16<bf16_t, HD>>(st, a); \
+        if (dtype == kF16) return four_bits ? decode_rows<Cache4<f16_t, HD>>(st, a) : decode_rows<Cache16<f16_t, HD>>(st, a);    \
+        return four_bits ? decode_rows<Cache4<float, HD>>(st, a) : decode_rows<CacheFloat<HD>>(st, a);            \
+    }
+    RLHF_DECODE(64)
+    RLHF_DECODE(128)
+#undef RLHF_DECODE
+    return hipErrorInvalidValue;
 }
 
 }  // namespace rlhf
