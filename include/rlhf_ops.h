@@ -128,7 +128,7 @@ int rlhf_op_flash_attention(const void* q, const void* k, const void* v, const i
 /* Packed causal attention of a pass with a window: q, out [rows, n_q_heads*head_dim], k, v [rows, n_kv_heads*head_dim], e.g. columns
  * of one QKV buffer.  Tiles as in rlhf_op_flash_attention: tile i covers rows tile_start[i] + tile_q0[i] .. (at most 128, up to the
  * end) of the sequence that starts at row tile_start[i] and has tile_len[i] rows.  Rows of no tile are left as they are; a tile that
- * does not lie within the `rows` rows is skipped.  out must not overlap q, k or v. */
+ * does not lie within the `rows` rows is skipped.  out must not overlap q, k or v; ld_k and ld_v are below 2^25. */
 int rlhf_op_window_attention(int act_dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                              const int32_t* tile_start, const int32_t* tile_q0, const int32_t* tile_len, void* out, int64_t ld_out,
                              int n_tiles, int rows, int window, int sinks, int n_q_heads, int n_kv_heads, int head_dim,

@@ -1,6 +1,7 @@
 // Packed causal attention with a sliding window and sinks (the formulas are in include/rlhf_ops.h).
 #include <algorithm>
 
+#include "attn_tile.h"
 #include "common.h"
 #include "kernels.h"
 #include "vec.h"
@@ -58,17 +59,269 @@ __device__ __forceinline__ bool tile_of(const WindowArgs& a, int tile, int& s0, 
     return s0 >= 0 && q0 >= 0 && len <= a.rows - s0 && q0 < len;
 }
 
+// Workgroup -> (tile, query head).  The heads of a KV head and the neighbouring tiles read the same keys: XCD x (workgroups x modulo 8) takes the
+// x-th eighth of them in the order KV head, tile, query head.
+__device__ __forceinline__ void window_work(const WindowArgs& a, int& tile, int& h) {
+    const unsigned n = (unsigned)a.n_tiles * (unsigned)a.n_q_heads, x = blockIdx.x % 8, i = blockIdx.x / 8;
+    const unsigned w = x * (n / 8) + min(x, n % 8) + i;
+    const unsigned G = a.n_q_heads / a.n_kv_heads, per = (unsigned)a.n_tiles * G;
+    tile = (int)(w % per / G);
+    h = (int)(w / per * G + w % G);
+}
+
+// Key tiles of SIZE keys that queries first .. last see any of: 0 .. n_sink - 1 and from `from` on.
+template <int SIZE> struct KeyTiles {
+    int n_sink, from, n;
+    __device__ __forceinline__ KeyTiles(int first, int last, int window, int sinks) {
+        from = max(0, first - window + 1) / SIZE;
+        n_sink = min(from, sinks / SIZE + (sinks % SIZE != 0));
+        n = n_sink + last / SIZE - from + 1;
+    }
+    __device__ __forceinline__ int at(int j) const { return j < n_sink ? j : from + j - n_sink; }
+};
+
+__device__ __forceinline__ bool window_sees(const WindowArgs& a, int i, int j) { return j <= i && (j > i - a.window || j < a.sinks); }
+
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+__device__ __forceinline__ uint32_t lds_address(void* p) { return (uint32_t)(size_t)(lds_ptr_t)p; }
+// 16 bytes a lane from base + offset to LDS, `to` and on: 1024 bytes of a wave.  Written out, as the builtin makes the compiler wait for all loads in
+// flight before it reads LDS; whoever reads waits for vmcnt and the workgroup first.  (It has no register to come back to; m0 has no other use in
+// these kernels.)
+__device__ __forceinline__ void load_to_lds(u32x4_t base, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ u32x4_t buffer_base(const void* p) {
+    return u32x4_t{(uint32_t)(uintptr_t)p, (uint32_t)((uintptr_t)p >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00020000u};
+}
+typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
+
+// 16-bit types: 128 queries of a head a workgroup, 32 a wave, against 64 keys at a time.  K and V go from memory to LDS directly, one tile ahead;
+// V is transposed as it is read from LDS.  References of the weights follow the running maximum only where these would leave their
+// range, so that most tiles do not rescale the sums.  A key that is hidden from a query has weight 0, and 0 times what is not a number is none: a
+// wave whose result is not finite takes its queries again one by one, over visible keys alone.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_window_rows(WindowArgs a) {
-    int s0, q0, len;
-    if (!tile_of(a, blockIdx.x / a.n_q_heads, s0, q0, len)) return;
-    const int h = blockIdx.x % a.n_q_heads, lane = threadIdx.x & 63;
-    for (int i = q0 + (threadIdx.x >> 6); i < min(len, q0 + kFlashTile); i += 4) window_row<T, HD>(a, s0, i, h, lane);
+__global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
+    using M = Matrix16<T>;
+    constexpr int KS = HD / 32, DF = HD / 16, CH = HD / 8, ROWS = 64 / CH, LOADS = 16 / ROWS, TILE = 64 * HD;
+    constexpr float START = M::TOP > 0.f ? 6.f : 0.f, MOST = M::TOP > 0.f ? M::TOP : 20.f;      // log2 of the greatest weight at a new reference, and ever
+    __shared__ __attribute__((aligned(16))) T sK[2][TILE], sV[2][TILE];
+    int tile, h, s0, q0, len;
+    window_work(a, tile, h);
+    if (!tile_of(a, tile, s0, q0, len)) return;
+    const int kh = h / (a.n_q_heads / a.n_kv_heads);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
+    const float unit = rsqrtf((float)HD) * 1.44269504088896f;
+    const T* kb = (const T*)a.k + (size_t)s0 * a.ld_k + (size_t)kh * HD;
+    const T* vb = (const T*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
+    const uint32_t ldk = (uint32_t)a.ld_k * 2, ldv = (uint32_t)a.ld_v * 2;
+
+    // A load of a wave fills ROWS rows of a tile; place p of row t holds 16-byte piece p ^ (t % 16) of K and, in pairs, p ^ 2 (t % 8) of V (of 64 dims
+    // ^ (t / 2 % 8) and ^ 2 (t / 2 % 4)), so that fragment reads spread over the banks.
+    const int lrow = wave * ROWS + lane / CH, place = lane % CH;
+    const int kpiece = CH == 16 ? place ^ (lrow & 15) : place ^ ((lrow >> 1) & 7), vpiece = CH == 16 ? place ^ ((lrow & 7) << 1) : place ^ (((lrow >> 1) & 3) << 1);
+    const auto fetch = [&](int kt, int buf) {
+        const u32x4_t rk = buffer_base(kb + (size_t)kt * 64 * a.ld_k), rv = buffer_base(vb + (size_t)kt * 64 * a.ld_v);
+        const int last = min(63, len - 1 - kt * 64);               // rows behind the sequence: its last one
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t row = min(lrow + i * 4 * ROWS, last);
+            load_to_lds(rk, row * ldk + kpiece * 16, lds_address(&sK[buf][(wave + i * 4) * ROWS * HD]));
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t row = min(lrow + i * 4 * ROWS, last);
+            load_to_lds(rv, row * ldv + vpiece * 16, lds_address(&sV[buf][(wave + i * 4) * ROWS * HD]));
+        }
+    };
+
+    const int w0 = q0 + wave * 32;                 // this wave's queries
+    u32x4_t q[2][KS];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const T* p = (const T*)a.q + (size_t)(s0 + min(w0 + m * 16 + n, len - 1)) * a.ld_q + (size_t)h * HD + c * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[m][s] = *(const u32x4_t*)(p + s * 32);
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[0][s]), "+v"(q[1][s]));              // here, not in the loop, where a wait for them would be one for K and V
+    f32x4_t o[DF][2];
+#pragma unroll
+    for (int d = 0; d < DF; ++d)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) o[d][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float ref[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
+    const KeyTiles<64> keys(q0, min(q0 + kFlashTile, len) - 1, a.window, a.sinks);
+    const int vt = 4 * c + (n >> 2);               // token (modulo 16) and 32-byte pair of pieces of a lane's reads of V
+    const int vswap = CH == 16 ? vt & 7 : (vt >> 1) & 3;
+
+    fetch(keys.at(0), 0);
+    for (int j = 0; j < keys.n; ++j) {
+        const int kt = keys.at(j), buf = j & 1, first = kt * 64, last = first + 63;
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        __syncthreads();                           // tile j is there, and nobody reads tile j - 1 any more
+        if (j + 1 < keys.n) fetch(keys.at(j + 1), buf ^ 1);
+        if (first > w0 + 31 || (last <= w0 - a.window && first >= a.sinks)) continue;       // nothing that this wave sees
+        f32x4_t s[4][2];
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) s[f][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                const int row = f * 16 + n, p = CH == 16 ? (k * 4 + c) ^ n : (k * 4 + c) ^ ((n >> 1) & 7);
+                const u32x4_t x = *(const u32x4_t*)&sK[buf][row * HD + p * 8];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) s[f][m] = M::qk(x, q[m][k], s[f][m]);
+            }
+        if (last > w0 || !(first > w0 + 31 - a.window || last < a.sinks)) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!window_sees(a, w0 + m * 16 + n, first + f * 16 + 4 * c + r)) s[f][m][r] = -INFINITY;
+        }
+        float top[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            float x = fmaxf(fmaxf(s[0][m][0], s[0][m][1]), fmaxf(s[0][m][2], s[0][m][3]));
+#pragma unroll
+            for (int f = 1; f < 4; ++f) x = fmaxf(x, fmaxf(fmaxf(s[f][m][0], s[f][m][1]), fmaxf(s[f][m][2], s[f][m][3])));
+            top[m] = column_max(x) * unit;
+        }
+        if (__any(top[0] > ref[0] + MOST || top[1] > ref[1] + MOST)) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const float now = top[m] > ref[m] + MOST ? top[m] - START : ref[m], keep = __builtin_amdgcn_exp2f(ref[m] - now);
+                ref[m] = now;
+                l[m] *= keep;
+#pragma unroll
+                for (int d = 0; d < DF; ++d) o[d][m] *= keep;
+            }
+        }
+        u32x4_t p[2][2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                float w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(fmaf(s[f][m][r], unit, -ref[m]));
+                l[m] += (w[0] + w[1]) + (w[2] + w[3]);
+                p[m][f >> 1][(f & 1) * 2] = pack2<T>(w[0], w[1]);
+                p[m][f >> 1][(f & 1) * 2 + 1] = pack2<T>(w[2], w[3]);
+            }
+#pragma unroll
+        for (int d = 0; d < DF; ++d)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                T* at = &sV[buf][(u * 32 + vt) * HD + (d ^ vswap) * 16 + (n & 3) * 4];
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * HD));
+                const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) o[d][m] = M::qk(u32x4_t{x[0], x[1], y[0], y[1]}, p[m][u], o[d][m]);
+            }
+    }
+
+    float odd = 0.f;                               // not a number where a result is not finite
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const float inv = 1.f / column_sum(l[m]);
+        const int i = w0 + m * 16 + n;
+        if (i >= len) continue;
+        T* out = (T*)a.out + (size_t)(s0 + i) * a.ld_out + (size_t)h * HD + 4 * c;
+#pragma unroll
+        for (int d = 0; d < DF; ++d) {
+            const f32x4_t x = o[d][m] * inv;
+            odd += 0.f * ((x[0] + x[1]) + (x[2] + x[3]));
+            *(u32x2_t*)(out + d * 16) = u32x2_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+        }
+    }
+    if (__any(odd != 0.f))
+        for (int i = w0; i < min(w0 + 32, len); ++i) window_row<T, HD>(a, s0, i, h, lane);
+}
+
+// Float: 16 queries a wave, 16 keys at a time from the L2 straight into the matrix units' registers, the next ones in flight; bound by the
+// float matrix rate (a 64th of the half one a lane).  What is hidden is kept out as above.
+template <int HD>
+__global__ __launch_bounds__(512) void k_window_float(WindowArgs a) {
+    using Tile = FloatTile<HD>;
+    constexpr int D = HD / 16;
+    int tile, h, s0, q0, len;
+    window_work(a, tile, h);
+    if (!tile_of(a, tile, s0, q0, len)) return;
+    const int kh = h / (a.n_q_heads / a.n_kv_heads);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
+    const int w0 = q0 + wave * 16;
+    if (w0 >= len) return;
+    const float* kb = (const float*)a.k + (size_t)s0 * a.ld_k + (size_t)kh * HD;
+    const float* vb = (const float*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
+    const float unit = rsqrtf((float)HD) * 1.44269504088896f;
+    FloatQuery<HD> q;
+    q.load((const float*)a.q + (size_t)(s0 + min(w0 + n, len - 1)) * a.ld_q + (size_t)h * HD, c);
+    f32x4_t o[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float ref = -INFINITY, l = 0.f;
+    const KeyTiles<16> keys(w0, min(w0 + 16, len) - 1, a.window, a.sinks);
+    const auto fetch = [&](Tile& t, int j) {
+        const int kt = keys.at(j);
+        t.template load<false>(kb + (size_t)kt * 16 * a.ld_k, a.ld_k, vb + (size_t)kt * 16 * a.ld_v, a.ld_v, min(15, len - 1 - kt * 16), n, c);
+    };
+    const auto step = [&](const Tile& t, int j) {
+        const int first = keys.at(j) * 16;
+        f32x4_t s = t.scores(q);
+        if (first + 15 > w0 || !(first > w0 + 15 - a.window || first + 15 < a.sinks)) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!window_sees(a, w0 + n, first + 4 * c + r)) s[r] = -INFINITY;
+        }
+        const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * unit;
+        if (__any(top > ref)) {
+            const float now = fmaxf(top, ref), keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+            ref = now;
+            l *= keep;
+#pragma unroll
+            for (int d = 0; d < D; ++d) o[d] *= keep;
+        }
+        const float at = ref == -INFINITY ? 0.f : ref;
+        f32x4_t p;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -at));
+        l += (p[0] + p[1]) + (p[2] + p[3]);
+        t.add(p, o);
+    };
+    Tile t0, t1;
+    fetch(t0, 0);
+    for (int j = 0; j < keys.n; j += 2) {
+        if (j + 1 < keys.n) fetch(t1, j + 1);
+        step(t0, j);
+        if (j + 1 < keys.n) {
+            if (j + 2 < keys.n) fetch(t0, j + 2);
+            step(t1, j + 1);
+        }
+    }
+    const float inv = 1.f / column_sum(l);
+    float odd = 0.f;
+    if (w0 + n < len) {
+        float* out = (float*)a.out + (size_t)(s0 + w0 + n) * a.ld_out + (size_t)h * HD;
+        Tile::each(o, c, [&](int d, f32x4_t x) {
+            x *= inv;
+            odd += 0.f * ((x[0] + x[1]) + (x[2] + x[3]));
+            *(f32x4_t*)(out + d) = x;
+        });
+    }
+    if (__any(odd != 0.f))
+        for (int i = w0; i < min(w0 + 16, len); ++i) window_row<float, HD>(a, s0, i, h, lane);
 }
 
 template <typename T>
 static hipError_t window_typed(hipStream_t st, int head_dim, const WindowArgs& a) {
-    const int most = (int)std::min<int64_t>(kLaunchThreads / 256 / a.n_q_heads, 1 << 30);
+    constexpr int THREADS = sizeof(T) == 4 ? 512 : 256;
+    const int most = (int)std::min<int64_t>(kLaunchThreads / THREADS / a.n_q_heads, 1 << 30);
     for (int first = 0; first < a.n_tiles; first += most) {
         WindowArgs p = a;
         p.tile_start += first;
@@ -76,8 +329,13 @@ static hipError_t window_typed(hipStream_t st, int head_dim, const WindowArgs& a
         p.tile_len += first;
         p.n_tiles = std::min(most, a.n_tiles - first);
         const unsigned blocks = (unsigned)p.n_tiles * (unsigned)a.n_q_heads;
-        if (head_dim == 128) k_window_rows<T, 128><<<blocks, 256, 0, st>>>(p);
-        else k_window_rows<T, 64><<<blocks, 256, 0, st>>>(p);
+        if constexpr (sizeof(T) == 4) {
+            if (head_dim == 128) k_window_float<128><<<blocks, 512, 0, st>>>(p);
+            else k_window_float<64><<<blocks, 512, 0, st>>>(p);
+        } else {
+            if (head_dim == 128) k_window_flash<T, 128><<<blocks, 256, 0, st>>>(p);
+            else k_window_flash<T, 64><<<blocks, 256, 0, st>>>(p);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

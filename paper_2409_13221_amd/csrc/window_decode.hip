@@ -2,6 +2,7 @@
 // (include/rlhf_ops.h).
 #include <algorithm>
 
+#include "attn_tile.h"
 #include "common.h"
 #include "kernels.h"
 #include "kv4.h"
@@ -31,52 +32,13 @@ __device__ __forceinline__ int row_context(const WindowDecodeArgs& a, int r, con
     return ctx;
 }
 
-// ---- a page's K and V of one KV head as operands of the matrix units.  Scores are S^T = K Q^T (16 tokens x 16 query heads): a lane holds
-// tokens 4c .. 4c + 3 of head n, n = lane % 16, c = lane / 16, which is also how O^T += V^T P^T takes the weights: they never leave their lane.
-// Query heads beyond a KV head's own repeat the last one.
-
-typedef f16_t f16x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+// ---- a page's K and V of one KV head as operands of the matrix units (attn_tile.h); a column is a query head, those beyond a KV head's own
+// repeat the last one.
 
 // Every byte of the cache is read once a step: evict-first.
 template <typename V> __device__ __forceinline__ V ld_once(const void* p) { return __builtin_nontemporal_load((const V*)p); }
 
-// Greatest of (sum over) the four lanes that hold a head's tokens.
-__device__ __forceinline__ float head_max(float x) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float head_sum(float x) {
-    x += __shfl_xor(x, 16, kWave);
-    return x + __shfl_xor(x, 32, kWave);
-}
-
 constexpr float NONE = 1e9f;            // no offset yet
-
-template <typename T> struct Matrix16;
-template <> struct Matrix16<f16_t> {
-    // Weights up to 2^14: what half loses below its normal range is 2^-39 of the greatest.
-    static constexpr float TOP = 14.f;
-    static __device__ __forceinline__ f32x4_t qk(u32x4_t a, u32x4_t b, f32x4_t c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ f32x4_t pv(u32x2_t a, u32x2_t b, f32x4_t c) {
-        return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, a), __builtin_bit_cast(f16x4_t, b), c, 0, 0, 0);
-    }
-};
-template <> struct Matrix16<bf16_t> {
-    static constexpr float TOP = 0.f;
-    static __device__ __forceinline__ f32x4_t qk(u32x4_t a, u32x4_t b, f32x4_t c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ f32x4_t pv(u32x2_t a, u32x2_t b, f32x4_t c) {
-        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, b), c, 0, 0, 0);
-    }
-};
 
 // A 16-bit cache.  K as it lies: a lane has 8 dims of token n.  V: dims D n .. D n + D - 1 (D = HD / 16) of its four tokens, so that a row of V
 // is read by 16 lanes side by side; pairs of tokens are put together by byte permutations.  Weights go in as two terms of the type, which
@@ -105,13 +67,8 @@ template <typename T_, int HD_> struct Cache16 {
 #pragma unroll
             for (int d = 0; d < D; ++d) acc[d] *= f;
         }
-        // Dims of the head from `put`'s first argument on, as the lane holds them.
-        template <typename F> __device__ __forceinline__ void each(int c, F put) const {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int d = 0; d < D; d += 4) put((4 * c + r) * D + d, f32x4_t{acc[d][r], acc[d + 1][r], acc[d + 2][r], acc[d + 3][r]});
-        }
+        // Four dims at a time: put(dim, values).
+        template <typename F> __device__ __forceinline__ void each(int c, F put) const { FloatTile<HD>::each(acc, c, put); }
         __device__ __forceinline__ void finish() {}
     };
     struct Tile {
@@ -151,51 +108,22 @@ template <typename T_, int HD_> struct Cache16 {
     };
 };
 
-// A float cache: k = 4 products, a lane has 4 dims of token n (K), and D dims of its four tokens (V).
 template <int HD_> struct CacheFloat {
     using T = float;
-    static constexpr int HD = HD_, D = HD / 16;
-    static constexpr float TOP = 0.f;
-    struct Query {
-        f32x4_t q[D];
-        float unit = 1.f;
-        __device__ __forceinline__ void load(const float* p, int c) {
-#pragma unroll
-            for (int s = 0; s < D; ++s) q[s] = *(const f32x4_t*)(p + s * 16 + c * 4);
-        }
-    };
+    static constexpr int HD = HD_;
+    using Query = FloatQuery<HD>;
     using Sums = typename Cache16<f16_t, HD>::Sums;
-    struct Tile {
-        f32x4_t k[D], v[4][D / 4];
+    struct Tile : FloatTile<HD> {
         __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
             const float* p = (const float*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
-            const float* pv = p + (size_t)a.n_kv_heads * 16 * HD;
-#pragma unroll
-            for (int s = 0; s < D; ++s) k[s] = ld_once<f32x4_t>(p + n * HD + s * 16 + c * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int d = 0; d < D / 4; ++d) v[i][d] = ld_once<f32x4_t>(pv + (4 * c + i) * HD + n * D + d * 4);
-        }
-        __device__ __forceinline__ f32x4_t scores(const Query& q) const {
-            f32x4_t s{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < D; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q.q[i][e], s, 0, 0, 0);
-            return s;
+            FloatTile<HD>::template load<true>(p, HD, p + (size_t)a.n_kv_heads * 16 * HD, HD, 15, n, c);
         }
         __device__ __forceinline__ void hide(int i) {
 #pragma unroll
-            for (int d = 0; d < D / 4; ++d) v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int d = 0; d < HD / 64; ++d) this->v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        __device__ __forceinline__ float spare(float) const { return -TOP; }
-        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int d = 0; d < D; ++d) o.acc[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][d / 4][d % 4], p[i], o.acc[d], 0, 0, 0);
-        }
+        __device__ __forceinline__ float spare(float) const { return 0.f; }
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const { FloatTile<HD>::add(p, o.acc); }
     };
 };
 
@@ -234,7 +162,7 @@ template <typename T_, int HD_> struct Cache4 {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(f[s][e]));
             }
-            m = head_max(m);
+            m = column_max(m);
             const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
             unit = ldexpf(1.f, -up);
 #pragma unroll
@@ -244,7 +172,7 @@ template <typename T_, int HD_> struct Cache4 {
                 for (int s = 2 * g; s < 2 * g + 2; ++s)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[g] += f[s][e] = ldexpf(f[s][e], up);
-                sum[g] = head_sum(sum[g]);
+                sum[g] = column_sum(sum[g]);
             }
 #pragma unroll
             for (int s = 0; s < KS; ++s)
@@ -276,7 +204,7 @@ template <typename T_, int HD_> struct Cache4 {
         }
         __device__ __forceinline__ void finish() {
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) center[g] = head_sum(center[g]);
+            for (int g = 0; g < GROUPS; ++g) center[g] = column_sum(center[g]);
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) acc[d] += center[d / 4];
         }
@@ -412,7 +340,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
                         t.hide(i);
                     }
             }
-            const float mn = fmaxf(m, head_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+            const float mn = fmaxf(m, column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
             off = t.spare(off);
             const float rn = mn == -INFINITY ? 0.f : fmaf(mn, unit, off);
             if (__any(!(rn == ref))) {
@@ -440,7 +368,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
         }
     }
     if (lost) l = NAN;
-    l = head_sum(l);
+    l = column_sum(l);
     o.finish();
     if (m == -INFINITY) ref = -INFINITY;           // nothing seen, or scores of -inf alone
     float* s_ref = lds + WAVES * room * HD;
