@@ -35,8 +35,21 @@ __device__ __forceinline__ int row_context(const WindowDecodeArgs& a, int r, con
 // ---- a page's K and V of one KV head as operands of the matrix units (attn_tile.h); a column is a query head, those beyond a KV head's own
 // repeat the last one.
 
-// Every byte of the cache is read once a step: evict-first.
-template <typename V> __device__ __forceinline__ V ld_once(const void* p) { return __builtin_nontemporal_load((const V*)p); }
+// A page's K and V of one KV head as a buffer that ends behind them, or, of a page that is not there, at once: such loads give zeros and touch no
+// memory.  Every byte is read once a step: evict-first.
+struct PageBuffer {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ PageBuffer(const void* base, uint32_t size) : r(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)size, 0x00020000)) {}
+    template <typename V> __device__ __forceinline__ V get(uint32_t lane, uint32_t at, uint32_t plane = 0) const {
+        if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(lane + at), (int)plane, 2));
+        else return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(r, (int)(lane + at), (int)plane, 2));
+    }
+};
+template <typename T, int HD> __device__ __forceinline__ PageBuffer plain_page(const WindowDecodeArgs& a, int page, int kh, bool there, uint32_t& plane) {
+    const T* p = (const T*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
+    plane = (uint32_t)a.n_kv_heads * (16 * HD * sizeof(T));
+    return PageBuffer(p, there ? plane + 16 * HD * sizeof(T) : 0);
+}
 
 constexpr float NONE = 1e9f;            // no offset yet
 
@@ -74,13 +87,13 @@ template <typename T_, int HD_> struct Cache16 {
     struct Tile {
         u32x4_t k[KS];
         VRow v[4];
-        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
-            const T* p = (const T*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
-            const T* pv = p + (size_t)a.n_kv_heads * 16 * HD;
+        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, bool there, int n, int c) {
+            uint32_t plane;
+            const PageBuffer b = plain_page<T, HD>(a, page, kh, there, plane);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) k[s] = ld_once<u32x4_t>(p + n * HD + s * 32 + c * 8);
+            for (int s = 0; s < KS; ++s) k[s] = b.get<u32x4_t>((n * HD + c * 8) * 2, s * 64);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = ld_once<VRow>(pv + (4 * c + i) * HD + n * D);
+            for (int i = 0; i < 4; ++i) v[i] = b.get<VRow>((4 * c * HD + n * D) * 2, i * HD * 2, plane);
         }
         __device__ __forceinline__ f32x4_t scores(const Query& q) const {
             f32x4_t s{0.f, 0.f, 0.f, 0.f};
@@ -92,8 +105,9 @@ template <typename T_, int HD_> struct Cache16 {
 #pragma unroll
             for (int w = 0; w < D / 2; ++w) v[i][w] = 0;
         }
-        __device__ __forceinline__ float spare(float) const { return -TOP; }
-        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
+        __device__ __forceinline__ float spare() const { return -TOP; }
+        __device__ __forceinline__ bool too_large(const f32x4_t&) const { return false; }
+        __device__ __forceinline__ void add(const f32x4_t& p, const Query&, Sums& o) const {
             const u32x2_t hi{pack2<T>(p[0], p[1]), pack2<T>(p[2], p[3])};
             const u32x2_t lo{pack2<T>(p[0] - unpack<T>(hi[0], 0), p[1] - unpack<T>(hi[0], 1)), pack2<T>(p[2] - unpack<T>(hi[1], 0), p[3] - unpack<T>(hi[1], 1))};
 #pragma unroll
@@ -114,16 +128,24 @@ template <int HD_> struct CacheFloat {
     using Query = FloatQuery<HD>;
     using Sums = typename Cache16<f16_t, HD>::Sums;
     struct Tile : FloatTile<HD> {
-        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
-            const float* p = (const float*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
-            FloatTile<HD>::template load<true>(p, HD, p + (size_t)a.n_kv_heads * 16 * HD, HD, 15, n, c);
+        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, bool there, int n, int c) {
+            uint32_t plane;
+            const PageBuffer b = plain_page<float, HD>(a, page, kh, there, plane);
+            constexpr int D = HD / 16;
+#pragma unroll
+            for (int s = 0; s < D; ++s) this->k[s] = b.get<f32x4_t>((n * HD + c * 4) * 4, s * 64);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < D / 4; ++d) this->v[i][d] = b.get<f32x4_t>((4 * c * HD + n * D) * 4, (i * HD + d * 4) * 4, plane);
         }
         __device__ __forceinline__ void hide(int i) {
 #pragma unroll
             for (int d = 0; d < HD / 64; ++d) this->v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        __device__ __forceinline__ float spare(float) const { return 0.f; }
-        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const { FloatTile<HD>::add(p, o.acc); }
+        __device__ __forceinline__ float spare() const { return 0.f; }
+        __device__ __forceinline__ bool too_large(const f32x4_t&) const { return false; }
+        __device__ __forceinline__ void add(const f32x4_t& p, const Query&, Sums& o) const { FloatTile<HD>::add(p, o.acc); }
     };
 };
 
@@ -138,12 +160,13 @@ template <typename T_, int HD_> struct Cache4 {
     using L = Kv4<HD_>;
     static constexpr int HD = HD_, KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 3 : 1;
     typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
-    // Eight codes of a word as halves, in the order 0 4 1 5 2 6 3 7.
-    static __device__ __forceinline__ void halves(uint32_t x, uint32_t (&h)[4]) {
+    // Eight codes of a word as halves, in the order 0 4 1 5 2 6 3 7.  `magic`, 1024 twice, comes in a vector register: with the mask in a scalar one,
+    // and-or is one instruction.
+    static __device__ __forceinline__ void halves(uint32_t x, uint32_t magic, uint32_t (&h)[4]) {
         typedef f16_t pair __attribute__((ext_vector_type(2)));
-        const auto low = [](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair, (w & 0x000F000Fu) | 0x64006400u) - pair{1032, 1032}); };
-        const auto high = [](uint32_t w) {
-            const pair v = __builtin_bit_cast(pair, (w & 0x00F000F0u) | 0x64006400u), f{0.0625, 0.0625}, o{-72, -72};
+        const auto low = [magic](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair, (w & 0x000F000Fu) | magic) - pair{1032, 1032}); };
+        const auto high = [magic](uint32_t w) {
+            const pair v = __builtin_bit_cast(pair, (w & 0x00F000F0u) | magic), f{0.0625, 0.0625}, o{-72, -72};
             return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, f, o));
         };
         h[0] = low(x);
@@ -151,10 +174,17 @@ template <typename T_, int HD_> struct Cache4 {
         h[2] = low(x >> 8);
         h[3] = high(x >> 8);
     }
+    static __device__ __forceinline__ uint32_t magic() {
+        uint32_t m = 0x64006400u;
+        asm("" : "+v"(m));
+        return m;
+    }
     struct Query {
         u32x4_t q[KS][TERMS];
         float sum[GROUPS], unit;
+        uint32_t magic;
         __device__ __forceinline__ void load(const T* p, int c) {
+            magic = Cache4::magic();
             float f[KS][8], m = 0.f;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
@@ -218,17 +248,17 @@ template <typename T_, int HD_> struct Cache4 {
         u32x4_t kp[GROUPS], vp[GROUPS];            // (scale, center) of the lane's four tokens
         static __device__ __forceinline__ float scale_of(uint32_t w) { return unpack<f16_t>(w, 0); }
         static __device__ __forceinline__ float center_of(uint32_t w) { return unpack<f16_t>(w, 1); }
-        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, int n, int c) {
-            const uint8_t* p = (const uint8_t*)a.pool + (((size_t)page * a.n_layers + a.layer) * a.n_kv_heads + kh) * L::BLOCK;
-            k = ld_once<Codes>(p + (16 * c + n) * L::PIECE);
-            v = ld_once<Codes>(p + L::V_CODES + (16 * c + n) * L::PIECE);
+        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, bool there, int n, int c) {
+            const PageBuffer b((const uint8_t*)a.pool + (((size_t)page * a.n_layers + a.layer) * a.n_kv_heads + kh) * L::BLOCK, there ? L::BLOCK : 0);
+            k = b.get<Codes>((16 * c + n) * L::PIECE, 0);
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                kp[g] = ld_once<u32x4_t>(p + L::param(4 * c, 64 * g));
-                vp[g] = ld_once<u32x4_t>(p + L::PARAMS + L::param(4 * c, 64 * g));
-            }
+            for (int g = 0; g < GROUPS; ++g) kp[g] = b.get<u32x4_t>(16 * c, L::param(0, 64 * g));
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) vp[g] = b.get<u32x4_t>(16 * c, L::PARAMS + L::param(0, 64 * g));
+            v = b.get<Codes>((16 * c + n) * L::PIECE, L::V_CODES);
         }
         __device__ __forceinline__ f32x4_t scores(const Query& q) const {
+            const uint32_t m = q.magic;
             f32x4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
@@ -236,7 +266,7 @@ template <typename T_, int HD_> struct Cache4 {
 #pragma unroll
                 for (int i = 2 * g; i < 2 * g + 2; ++i) {
                     uint32_t h[4];
-                    halves(k[i], h);
+                    halves(k[i], m, h);
                     const u32x4_t x{h[0], h[1], h[2], h[3]};
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t) raw = Matrix16<f16_t>::qk(x, q.q[i][t], raw);
@@ -250,25 +280,34 @@ template <typename T_, int HD_> struct Cache4 {
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) vp[g][i] = 0;
         }
-        // What to add to the reference (log2) so that p s stays below 2^15: `now` where it does.
-        __device__ __forceinline__ float spare(float now) const {
+        // What to add to the reference (log2) for p s of at most 2^10 here.
+        __device__ __forceinline__ float spare() const {
             float s = 0.f;
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s = fmaxf(s, fabsf(scale_of(vp[g][r])));
-            const float most = s * __builtin_amdgcn_exp2f(-now);
-            if (!__any(!(most < 32768.f)) && now != NONE) return now;
             s = wave_max(s);
             return s > 0.f ? (float)ilogbf(s) - 9.f : -14.f;
         }
-        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
+        __device__ __forceinline__ float weight(const f32x4_t& p, int g, int r) const { return fmaf(p[r], scale_of(vp[g][r]), 0.f); }
+        // Whether a p s leaves half: no more than one page in many has scales 2^5 times those that the reference was chosen for.
+        __device__ __forceinline__ bool too_large(const f32x4_t& p) const {
+            float s = 0.f;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s = fmaxf(s, fabsf(weight(p, g, r)));
+            return __any(s > 32768.f);
+        }
+        __device__ __forceinline__ void add(const f32x4_t& p, const Query& q, Sums& o) const {
+            const uint32_t m = q.magic;
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 float w[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    w[r] = p[r] * scale_of(vp[g][r]);
+                    w[r] = weight(p, g, r);
                     o.center[g] = fmaf(p[r], center_of(vp[g][r]), o.center[g]);
                 }
                 const u32x2_t hi{pack2<f16_t>(w[0], w[2]), pack2<f16_t>(w[1], w[3])};
@@ -279,7 +318,7 @@ template <typename T_, int HD_> struct Cache4 {
 #pragma unroll
                 for (int i = 2 * g; i < 2 * g + 2; ++i) {
                     uint32_t h[4];
-                    halves(v[i], h);                       // tokens (0, 2) of dims 32 i + n, of dims 32 i + 16 + n, then (1, 3) alike
+                    halves(v[i], m, h);                     // tokens (0, 2) of dims 32 i + n, of dims 32 i + 16 + n, then (1, 3) alike
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const u32x2_t x{h[e], h[2 + e]};
@@ -321,13 +360,12 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
         const Visible see(ctx, a.window, a.sinks);
         const int from = (int)((int64_t)see.n_pages * split / a.nsplit), to = (int)((int64_t)see.n_pages * (split + 1) / a.nsplit);
         const int mine = to - from > wave ? (to - from - wave + WAVES - 1) / WAVES : 0;
-        int ids = 0;                               // of the next 64 pages, one a lane
         const auto index = [&](int j) { return see.page(from + wave + j * WAVES); };
-        const auto fetch = [&](typename C::Tile& t, int j) {
-            if (j % 64 == 0) ids = j + lane < mine ? table[index(j + lane)] : 0;
-            int id = __builtin_amdgcn_readlane(ids, j % 64);
-            if ((unsigned)id >= (unsigned)a.n_pages) { lost = true; id = 0; }
-            t.load(a, id, kh, n, c);
+        const auto page = [&](int j) { return table[index(min(j, mine - 1))]; };
+        const auto fetch = [&](typename C::Tile& t, int id, bool more) {
+            const bool inside = (unsigned)id < (unsigned)a.n_pages;
+            lost |= !inside;
+            t.load(a, inside ? id : 0, kh, inside && more, n, c);
         };
         const auto step = [&](typename C::Tile& t, int j) {
             f32x4_t s = t.scores(q);
@@ -341,29 +379,39 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
                     }
             }
             const float mn = fmaxf(m, column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
-            off = t.spare(off);
-            const float rn = mn == -INFINITY ? 0.f : fmaf(mn, unit, off);
-            if (__any(!(rn == ref))) {
-                const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - rn);
-                l *= keep;
-                o.scale(keep);
-                ref = rn;
-            }
-            m = mn;
+            if (off == NONE) off = t.spare();
             f32x4_t p;
+#pragma unroll 1
+            for (int again = 0; again < 2; ++again) {              // twice where the offset is chosen anew
+                const float rn = mn == -INFINITY ? 0.f : fmaf(mn, unit, off);
+                if (__any(!(rn == ref))) {
+                    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - rn);
+                    l *= keep;
+                    o.scale(keep);
+                    ref = rn;
+                }
+                m = mn;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], unit, -rn));
+                for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], unit, -rn));
+                if (!t.too_large(p)) break;
+                off = t.spare();
+            }
             l += (p[0] + p[1]) + (p[2] + p[3]);
-            t.add(p, o);
+            t.add(p, q, o);
         };
-        typename C::Tile t0, t1;
-        if (mine > 0) fetch(t0, 0);
-        for (int j = 0; j < mine; j += 2) {
-            if (j + 1 < mine) fetch(t1, j + 1);
-            step(t0, j);
-            if (j + 1 < mine) {
-                if (j + 2 < mine) fetch(t0, j + 2);
-                step(t1, j + 1);
+        // Two pages in flight, their numbers one step ahead.  Loads behind the last page are issued too, of nothing: so every wait in the loop is for a known
+        // number of loads.
+        if (mine > 0) {
+            typename C::Tile t0, t1;
+            int id0 = page(0), id1 = page(1);
+            fetch(t0, id0, true);
+            for (int j = 0; j < mine; j += 2) {
+                fetch(t1, id1, j + 1 < mine);
+                id0 = page(j + 2);
+                id1 = page(j + 3);
+                step(t0, j);
+                fetch(t0, id0, j + 2 < mine);
+                if (j + 1 < mine) step(t1, j + 1);
             }
         }
     }
@@ -406,26 +454,31 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
     }
 }
 
-// The parts of a (row, query head) joined, a wave each.
-template <typename T, int HD>
-__global__ __launch_bounds__(64) void k_window_join(WindowDecodeArgs a) {
-    const int lane = threadIdx.x, h = blockIdx.x % a.n_q_heads, r = blockIdx.x / a.n_q_heads;
-    constexpr int D = HD / 64;
+// The parts of a (row, query head) joined: a wave each, or of many parts four, whose sums meet in LDS.
+template <typename T, int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) {
+    constexpr int LANES = HD / 4, GROUPS = WAVES * 64 / LANES;         // a group of lanes takes every GROUPS-th part, four dims a lane
+    __shared__ f32x4_t s_x[GROUPS][LANES];
+    __shared__ float s_w[64], s_l;
+    const int t = threadIdx.x, g = t / LANES, d = t % LANES * 4, h = blockIdx.x % a.n_q_heads, r = blockIdx.x / a.n_q_heads;
     const size_t slot = (size_t)blockIdx.x * a.nsplit, slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
-    const float2* ml = (const float2*)a.part + slot;
-    float m = -INFINITY, l = 0.f, acc[D] = {};
-    for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, ml[s].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    for (int s = 0; s < a.nsplit; ++s) {
-        const float w = __builtin_amdgcn_exp2f(ml[s].x - ref);
-        l += w * ml[s].y;
-#pragma unroll
-        for (int e = 0; e < D; ++e) acc[e] += w * a.part[2 * slots + (slot + s) * HD + e * 64 + lane];
+    if (t < 64) {                                                      // nsplit <= 64
+        const float2 ml = t < a.nsplit ? ((const float2*)a.part)[slot + t] : make_float2(-INFINITY, 0.f);
+        const float m = wave_max(ml.x), w = __builtin_amdgcn_exp2f(ml.x - (m == -INFINITY ? 0.f : m)), l = wave_sum(w * ml.y);
+        s_w[t] = w;
+        if (t == 0) s_l = l;
     }
+    __syncthreads();
+    f32x4_t x{0.f, 0.f, 0.f, 0.f};
+    for (int s = g; s < a.nsplit; s += GROUPS) x += s_w[s] * *(const f32x4_t*)(a.part + 2 * slots + (slot + s) * HD + d);
+    s_x[g][d / 4] = x;
+    __syncthreads();
+    if (t >= LANES) return;
+    for (int i = 1; i < GROUPS; ++i) x += s_x[i][t];
     const bool empty = a.ctx_len[r] <= 0;
-    T* o = (T*)a.out + (size_t)r * a.ld_out + (size_t)h * HD;
+    T* o = (T*)a.out + (size_t)r * a.ld_out + (size_t)h * HD + d;
 #pragma unroll
-    for (int e = 0; e < D; ++e) o[e * 64 + lane] = round_to<T>(empty ? 0.f : acc[e] / l);
+    for (int e = 0; e < 4; ++e) o[e] = round_to<T>(empty ? 0.f : x[e] / s_l);
 }
 
 // Waves of a workgroup; four where 16 heads' sums of eight would take more than 64 KB of LDS.
@@ -459,7 +512,9 @@ static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
         const unsigned grid = (unsigned)(p.rows * blocks);
         if (waves == 8) k_window_decode<C, 8><<<grid, 512, lds, st>>>(p);
         else k_window_decode<C, 4><<<grid, 256, lds, st>>>(p);
-        if (a.nsplit > 1) k_window_join<T, C::HD><<<(unsigned)p.rows * (unsigned)a.n_q_heads, 64, 0, st>>>(p);
+        const unsigned heads = (unsigned)p.rows * (unsigned)a.n_q_heads;
+        if (a.nsplit > 8) k_window_join<T, C::HD, 4><<<heads, 256, 0, st>>>(p);
+        else if (a.nsplit > 1) k_window_join<T, C::HD, 1><<<heads, 64, 0, st>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
