@@ -47,7 +47,6 @@ template <> struct Matrix16<bf16_t> {
 // side by side; sums o[d] hold dim D (4c + r) + d in element r.
 template <int HD> struct FloatQuery {
     f32x4_t q[HD / 16];
-    float unit = 1.f;
     __device__ __forceinline__ void load(const float* p, int c) {
 #pragma unroll
         for (int s = 0; s < HD / 16; ++s) q[s] = *(const f32x4_t*)(p + s * 16 + c * 4);

@@ -32,6 +32,53 @@ __device__ __forceinline__ int row_context(const WindowDecodeArgs& a, int r, con
     return ctx;
 }
 
+// A workgroup's row, KV head, up to 16 of its query heads from h0 on (of `room` in LDS), and part of the row's visible pages.
+struct DecodeWork {
+    int split, r, kh, h0, heads, room;
+    __device__ __forceinline__ explicit DecodeWork(const WindowDecodeArgs& a) {
+        const int G = a.n_q_heads / a.n_kv_heads, blocks = (G + 15) / 16;
+        unsigned b = blockIdx.x;
+        split = b % a.nsplit;
+        b /= a.nsplit;
+        const int hb = b % blocks;
+        b /= blocks;
+        kh = b % a.n_kv_heads;
+        r = b / a.n_kv_heads;
+        h0 = kh * G + hb * 16;
+        heads = min(16, G - hb * 16);
+        room = min(16, G);
+    }
+};
+
+// The waves' sums, references and weights in LDS joined: to the output, or as one of nsplit parts.
+template <typename T, int HD, int WAVES>
+__device__ __forceinline__ void join_waves(const WindowDecodeArgs& a, const DecodeWork& w, int ctx, const float* lds) {
+    const float *s_ref = lds + WAVES * w.room * HD, *s_l = s_ref + WAVES * w.room;
+    const size_t slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
+    for (int i = threadIdx.x; i < w.heads * (HD / 4); i += WAVES * 64) {
+        const int h = i / (HD / 4), d = i % (HD / 4) * 4;
+        float top = -INFINITY, sum = 0.f;
+        f32x4_t x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) top = fmaxf(top, s_ref[k * w.room + h]);
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_ref[k * w.room + h] - top);
+            sum += f * s_l[k * w.room + h];
+            x += f * *(const f32x4_t*)(lds + (k * w.room + h) * HD + d);
+        }
+        if (a.nsplit == 1) {
+            T* out = (T*)a.out + (size_t)w.r * a.ld_out + (size_t)(w.h0 + h) * HD + d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = round_to<T>(ctx == 0 ? 0.f : x[e] / sum);
+        } else {
+            const size_t slot = ((size_t)w.r * a.n_q_heads + w.h0 + h) * a.nsplit + w.split;
+            if (d == 0) { a.part[2 * slot] = top; a.part[2 * slot + 1] = sum; }
+            *(f32x4_t*)(a.part + 2 * slots + slot * HD + d) = x;
+        }
+    }
+}
+
 // ---- a page's K and V of one KV head as operands of the matrix units (attn_tile.h); a column is a query head, those beyond a KV head's own
 // repeat the last one.
 
@@ -45,13 +92,29 @@ struct PageBuffer {
         else return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(r, (int)(lane + at), (int)plane, 2));
     }
 };
-template <typename T, int HD> __device__ __forceinline__ PageBuffer plain_page(const WindowDecodeArgs& a, int page, int kh, bool there, uint32_t& plane) {
-    const T* p = (const T*)a.pool + (((size_t)page * a.n_layers + a.layer) * 2 * a.n_kv_heads + kh) * 16 * HD;
-    plane = (uint32_t)a.n_kv_heads * (16 * HD * sizeof(T));
-    return PageBuffer(p, there ? plane + 16 * HD * sizeof(T) : 0);
+// A lane's byte offsets in a page, of K and of V.  opaque(): what is added to them stays an immediate of the loads, not a register each.
+struct LaneOffsets {
+    uint32_t k, v;
+    __device__ __forceinline__ LaneOffsets opaque() const {
+        LaneOffsets o = *this;
+        asm volatile("" : "+v"(o.k), "+v"(o.v));
+        return o;
+    }
+};
+template <typename T, int HD> __device__ __forceinline__ LaneOffsets plain_offsets(int n, int c) {
+    return LaneOffsets{(n * HD + c * (16 / (uint32_t)sizeof(T))) * (uint32_t)sizeof(T), (4 * c * HD + n * (HD / 16)) * (uint32_t)sizeof(T)};
 }
-
-constexpr float NONE = 1e9f;            // no offset yet
+// Where the pages of a layer and KV head lie: page i at first + i * stride, V `plane` bytes behind K, `size` bytes in all.
+struct Pages {
+    const uint8_t* first;
+    size_t stride;
+    uint32_t plane, size;
+    __device__ __forceinline__ PageBuffer at(int page, bool there) const { return PageBuffer(first + (size_t)page * stride, there ? size : 0); }
+};
+template <typename T, int HD> __device__ __forceinline__ Pages plain_pages(const WindowDecodeArgs& a, int kh) {
+    const size_t tile = 16 * HD * sizeof(T), layer = 2 * tile * a.n_kv_heads;
+    return Pages{(const uint8_t*)a.pool + a.layer * layer + kh * tile, layer * a.n_layers, (uint32_t)(tile * a.n_kv_heads), (uint32_t)(tile * a.n_kv_heads + tile)};
+}
 
 // A 16-bit cache.  K as it lies: a lane has 8 dims of token n.  V: dims D n .. D n + D - 1 (D = HD / 16) of its four tokens, so that a row of V
 // is read by 16 lanes side by side; pairs of tokens are put together by byte permutations.  Weights go in as two terms of the type, which
@@ -59,12 +122,13 @@ constexpr float NONE = 1e9f;            // no offset yet
 template <typename T_, int HD_> struct Cache16 {
     using T = T_;
     using M = Matrix16<T>;
-    static constexpr int HD = HD_, D = HD / 16, KS = HD / 32;
-    static constexpr float TOP = M::TOP;
+    static constexpr int HD = HD_, D = HD / 16, KS = HD / 32, SIMD_WAVES = 4;
+    static constexpr float START = M::TOP > 0.f ? 6.f : 0.f, MOST = M::TOP > 0.f ? M::TOP : 20.f;
     typedef uint32_t VRow __attribute__((ext_vector_type(D / 2)));
+    static __device__ __forceinline__ LaneOffsets offsets(int n, int c) { return plain_offsets<T, HD>(n, c); }
+    static __device__ __forceinline__ Pages pages(const WindowDecodeArgs& a, int kh) { return plain_pages<T, HD>(a, kh); }
     struct Query {
         u32x4_t q[KS];
-        float unit = 1.f;
         __device__ __forceinline__ void load(const T* p, int c) {
 #pragma unroll
             for (int s = 0; s < KS; ++s) q[s] = *(const u32x4_t*)(p + s * 32 + c * 8);
@@ -82,18 +146,16 @@ template <typename T_, int HD_> struct Cache16 {
         }
         // Four dims at a time: put(dim, values).
         template <typename F> __device__ __forceinline__ void each(int c, F put) const { FloatTile<HD>::each(acc, c, put); }
-        __device__ __forceinline__ void finish() {}
     };
     struct Tile {
         u32x4_t k[KS];
         VRow v[4];
-        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, bool there, int n, int c) {
-            uint32_t plane;
-            const PageBuffer b = plain_page<T, HD>(a, page, kh, there, plane);
+        __device__ __forceinline__ void load(const Pages& pages, int page, bool there, const LaneOffsets& lane) {
+            const PageBuffer b = pages.at(page, there);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) k[s] = b.get<u32x4_t>((n * HD + c * 8) * 2, s * 64);
+            for (int s = 0; s < KS; ++s) k[s] = b.get<u32x4_t>(lane.k, s * 64);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = b.get<VRow>((4 * c * HD + n * D) * 2, i * HD * 2, plane);
+            for (int i = 0; i < 4; ++i) v[i] = b.get<VRow>(lane.v, i * HD * 2, pages.plane);
         }
         __device__ __forceinline__ f32x4_t scores(const Query& q) const {
             f32x4_t s{0.f, 0.f, 0.f, 0.f};
@@ -105,9 +167,7 @@ template <typename T_, int HD_> struct Cache16 {
 #pragma unroll
             for (int w = 0; w < D / 2; ++w) v[i][w] = 0;
         }
-        __device__ __forceinline__ float spare() const { return -TOP; }
-        __device__ __forceinline__ bool too_large(const f32x4_t&) const { return false; }
-        __device__ __forceinline__ void add(const f32x4_t& p, const Query&, Sums& o) const {
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
             const u32x2_t hi{pack2<T>(p[0], p[1]), pack2<T>(p[2], p[3])};
             const u32x2_t lo{pack2<T>(p[0] - unpack<T>(hi[0], 0), p[1] - unpack<T>(hi[0], 1)), pack2<T>(p[2] - unpack<T>(hi[1], 0), p[3] - unpack<T>(hi[1], 1))};
 #pragma unroll
@@ -124,248 +184,62 @@ template <typename T_, int HD_> struct Cache16 {
 
 template <int HD_> struct CacheFloat {
     using T = float;
-    static constexpr int HD = HD_;
+    static constexpr int HD = HD_, SIMD_WAVES = HD == 64 ? 4 : 2;
+    static constexpr float START = 0.f, MOST = 20.f;
     using Query = FloatQuery<HD>;
+    static __device__ __forceinline__ LaneOffsets offsets(int n, int c) { return plain_offsets<float, HD>(n, c); }
+    static __device__ __forceinline__ Pages pages(const WindowDecodeArgs& a, int kh) { return plain_pages<float, HD>(a, kh); }
     using Sums = typename Cache16<f16_t, HD>::Sums;
     struct Tile : FloatTile<HD> {
-        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, bool there, int n, int c) {
-            uint32_t plane;
-            const PageBuffer b = plain_page<float, HD>(a, page, kh, there, plane);
+        __device__ __forceinline__ void load(const Pages& pages, int page, bool there, const LaneOffsets& lane) {
+            const PageBuffer b = pages.at(page, there);
             constexpr int D = HD / 16;
 #pragma unroll
-            for (int s = 0; s < D; ++s) this->k[s] = b.get<f32x4_t>((n * HD + c * 4) * 4, s * 64);
+            for (int s = 0; s < D; ++s) this->k[s] = b.get<f32x4_t>(lane.k, s * 64);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int d = 0; d < D / 4; ++d) this->v[i][d] = b.get<f32x4_t>((4 * c * HD + n * D) * 4, (i * HD + d * 4) * 4, plane);
+                for (int d = 0; d < D / 4; ++d) this->v[i][d] = b.get<f32x4_t>(lane.v, (i * HD + d * 4) * 4, pages.plane);
         }
         __device__ __forceinline__ void hide(int i) {
 #pragma unroll
             for (int d = 0; d < HD / 64; ++d) this->v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        __device__ __forceinline__ float spare() const { return 0.f; }
-        __device__ __forceinline__ bool too_large(const f32x4_t&) const { return false; }
-        __device__ __forceinline__ void add(const f32x4_t& p, const Query&, Sums& o) const { FloatTile<HD>::add(p, o.acc); }
-    };
-};
-
-// A cache of 4 bits.  Codes become halves u = -8 .. 7 by putting their bits into the mantissa of 1024: 9 instructions for 8 of them.  With scale s and
-// center c of each token and 64 dims (group g),
-//   q.k = sum over g of s_g (sum q u) + c_g (sum of q in g),   o = sum over tokens of (p s_g) u + p c_g:
-// the matrix units take q and p s_g, the rest is a few multiply-adds a token.  A query is scaled to have its greatest magnitude in [2^14, 2^15)
-// and taken as halves, exact from half and bfloat16 down to 2^-39 of that; from float in three terms.  Weights p are scaled such that p s_g fits
-// half (spare), in one term, of float calls two.
-template <typename T_, int HD_> struct Cache4 {
-    using T = T_;
-    using L = Kv4<HD_>;
-    static constexpr int HD = HD_, KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 3 : 1;
-    typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
-    // Eight codes of a word as halves, in the order 0 4 1 5 2 6 3 7.  `magic`, 1024 twice, comes in a vector register: with the mask in a scalar one,
-    // and-or is one instruction.
-    static __device__ __forceinline__ void halves(uint32_t x, uint32_t magic, uint32_t (&h)[4]) {
-        typedef f16_t pair __attribute__((ext_vector_type(2)));
-        const auto low = [magic](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair, (w & 0x000F000Fu) | magic) - pair{1032, 1032}); };
-        const auto high = [magic](uint32_t w) {
-            const pair v = __builtin_bit_cast(pair, (w & 0x00F000F0u) | magic), f{0.0625, 0.0625}, o{-72, -72};
-            return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, f, o));
-        };
-        h[0] = low(x);
-        h[1] = high(x);
-        h[2] = low(x >> 8);
-        h[3] = high(x >> 8);
-    }
-    static __device__ __forceinline__ uint32_t magic() {
-        uint32_t m = 0x64006400u;
-        asm("" : "+v"(m));
-        return m;
-    }
-    struct Query {
-        u32x4_t q[KS][TERMS];
-        float sum[GROUPS], unit;
-        uint32_t magic;
-        __device__ __forceinline__ void load(const T* p, int c) {
-            magic = Cache4::magic();
-            float f[KS][8], m = 0.f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                load8<T>(p + s * 32 + c * 8, f[s]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(f[s][e]));
-            }
-            m = column_max(m);
-            const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
-            unit = ldexpf(1.f, -up);
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                sum[g] = 0.f;
-#pragma unroll
-                for (int s = 2 * g; s < 2 * g + 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[g] += f[s][e] = ldexpf(f[s][e], up);
-                sum[g] = column_sum(sum[g]);
-            }
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t h = pack2<f16_t>(f[s][e], f[s][e + 4]);
-                        q[s][t][e] = h;
-                        f[s][e] -= unpack<f16_t>(h, 0);
-                        f[s][e + 4] -= unpack<f16_t>(h, 1);
-                    }
-        }
-    };
-    struct Sums {
-        f32x4_t acc[HD / 16];
-        float center[GROUPS];
-        __device__ __forceinline__ void clear() {
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) center[g] = 0.f;
-        }
-        __device__ __forceinline__ void scale(float f) {
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d) acc[d] *= f;
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) center[g] *= f;
-        }
-        __device__ __forceinline__ void finish() {
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) center[g] = column_sum(center[g]);
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d) acc[d] += center[d / 4];
-        }
-        template <typename F> __device__ __forceinline__ void each(int c, F put) const {
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d) put(16 * d + 4 * c, acc[d]);
-        }
-    };
-    struct Tile {
-        Codes k, v;
-        u32x4_t kp[GROUPS], vp[GROUPS];            // (scale, center) of the lane's four tokens
-        static __device__ __forceinline__ float scale_of(uint32_t w) { return unpack<f16_t>(w, 0); }
-        static __device__ __forceinline__ float center_of(uint32_t w) { return unpack<f16_t>(w, 1); }
-        __device__ __forceinline__ void load(const WindowDecodeArgs& a, int page, int kh, bool there, int n, int c) {
-            const PageBuffer b((const uint8_t*)a.pool + (((size_t)page * a.n_layers + a.layer) * a.n_kv_heads + kh) * L::BLOCK, there ? L::BLOCK : 0);
-            k = b.get<Codes>((16 * c + n) * L::PIECE, 0);
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) kp[g] = b.get<u32x4_t>(16 * c, L::param(0, 64 * g));
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) vp[g] = b.get<u32x4_t>(16 * c, L::PARAMS + L::param(0, 64 * g));
-            v = b.get<Codes>((16 * c + n) * L::PIECE, L::V_CODES);
-        }
-        __device__ __forceinline__ f32x4_t scores(const Query& q) const {
-            const uint32_t m = q.magic;
-            f32x4_t s{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                f32x4_t raw{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 2 * g; i < 2 * g + 2; ++i) {
-                    uint32_t h[4];
-                    halves(k[i], m, h);
-                    const u32x4_t x{h[0], h[1], h[2], h[3]};
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t) raw = Matrix16<f16_t>::qk(x, q.q[i][t], raw);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[r] = fmaf(scale_of(kp[g][r]), raw[r], fmaf(center_of(kp[g][r]), q.sum[g], s[r]));
-            }
-            return s;
-        }
-        __device__ __forceinline__ void hide(int i) {
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) vp[g][i] = 0;
-        }
-        // What to add to the reference (log2) for p s of at most 2^10 here.
-        __device__ __forceinline__ float spare() const {
-            float s = 0.f;
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s = fmaxf(s, fabsf(scale_of(vp[g][r])));
-            s = wave_max(s);
-            return s > 0.f ? (float)ilogbf(s) - 9.f : -14.f;
-        }
-        __device__ __forceinline__ float weight(const f32x4_t& p, int g, int r) const { return fmaf(p[r], scale_of(vp[g][r]), 0.f); }
-        // Whether a p s leaves half: no more than one page in many has scales 2^5 times those that the reference was chosen for.
-        __device__ __forceinline__ bool too_large(const f32x4_t& p) const {
-            float s = 0.f;
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s = fmaxf(s, fabsf(weight(p, g, r)));
-            return __any(s > 32768.f);
-        }
-        __device__ __forceinline__ void add(const f32x4_t& p, const Query& q, Sums& o) const {
-            const uint32_t m = q.magic;
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                float w[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    w[r] = weight(p, g, r);
-                    o.center[g] = fmaf(p[r], center_of(vp[g][r]), o.center[g]);
-                }
-                const u32x2_t hi{pack2<f16_t>(w[0], w[2]), pack2<f16_t>(w[1], w[3])};
-                u32x2_t lo{0, 0};
-                if (TERMS > 1)
-                    lo = u32x2_t{pack2<f16_t>(w[0] - unpack<f16_t>(hi[0], 0), w[2] - unpack<f16_t>(hi[0], 1)),
-                                 pack2<f16_t>(w[1] - unpack<f16_t>(hi[1], 0), w[3] - unpack<f16_t>(hi[1], 1))};
-#pragma unroll
-                for (int i = 2 * g; i < 2 * g + 2; ++i) {
-                    uint32_t h[4];
-                    halves(v[i], m, h);                     // tokens (0, 2) of dims 32 i + n, of dims 32 i + 16 + n, then (1, 3) alike
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const u32x2_t x{h[e], h[2 + e]};
-                        f32x4_t& acc = o.acc[2 * i + e];
-                        acc = Matrix16<f16_t>::pv(x, hi, acc);
-                        if (TERMS > 1) acc = Matrix16<f16_t>::pv(x, lo, acc);
-                    }
-                }
-            }
-        }
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const { FloatTile<HD>::add(p, o.acc); }
     };
 };
 
 // A workgroup takes a row, a KV head (up to 16 of its query heads) and a part of the row's visible pages; its waves take these in turn, a page in
-// flight while one is worked on, and meet in LDS.  m: greatest score; weights are exp2(z - ref), ref = m + spare in log2.
+// flight while one is worked on, and meet in LDS.  Weights are exp2(z - ref), z the score in log2; ref follows the greatest score of its column only
+// where a weight would leave its range: most pages take no exchange between lanes.
 template <typename C, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a) {
+__global__ __launch_bounds__(WAVES * 64, C::SIMD_WAVES) void k_window_decode(WindowDecodeArgs a) {
     using T = typename C::T;
     constexpr int HD = C::HD;
     extern __shared__ float lds[];                 // [WAVES][heads][HD] sums, then [WAVES][heads] references, [WAVES][heads] weights
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
-    const int G = a.n_q_heads / a.n_kv_heads, blocks = (G + 15) / 16;
-    unsigned b = blockIdx.x;
-    const int split = b % a.nsplit;
-    b /= a.nsplit;
-    const int hb = b % blocks;
-    b /= blocks;
-    const int kh = b % a.n_kv_heads, r = b / a.n_kv_heads, h0 = kh * G + hb * 16, heads = min(16, G - hb * 16), room = min(16, G);
+    const DecodeWork w(a);
     const int* table = nullptr;
-    const int ctx = row_context(a, r, table);
-    float m = -INFINITY, l = 0.f, ref = -INFINITY, off = NONE;
+    const int ctx = row_context(a, w.r, table);
+    float l = 0.f, ref = -INFINITY;                // ref: -inf as long as nothing but scores of -inf was seen
     typename C::Sums o;
     o.clear();
     bool lost = ctx < 0;
     if (ctx > 0) {
         typename C::Query q;
-        q.load((const T*)a.q + (size_t)r * a.ld_q + (size_t)(h0 + min(n, heads - 1)) * HD, c);
-        const float unit = q.unit * (1.44269504088896f * rsqrtf((float)HD));
+        q.load((const T*)a.q + (size_t)w.r * a.ld_q + (size_t)(w.h0 + min(n, w.heads - 1)) * HD, c);
+        const float unit = 1.44269504088896f * rsqrtf((float)HD);
         const Visible see(ctx, a.window, a.sinks);
-        const int from = (int)((int64_t)see.n_pages * split / a.nsplit), to = (int)((int64_t)see.n_pages * (split + 1) / a.nsplit);
+        const int from = (int)((int64_t)see.n_pages * w.split / a.nsplit), to = (int)((int64_t)see.n_pages * (w.split + 1) / a.nsplit);
         const int mine = to - from > wave ? (to - from - wave + WAVES - 1) / WAVES : 0;
+        const Pages pages = C::pages(a, w.kh);
         const auto index = [&](int j) { return see.page(from + wave + j * WAVES); };
+        const LaneOffsets offsets = C::offsets(n, c);
         const auto page = [&](int j) { return table[index(min(j, mine - 1))]; };
         const auto fetch = [&](typename C::Tile& t, int id, bool more) {
             const bool inside = (unsigned)id < (unsigned)a.n_pages;
             lost |= !inside;
-            t.load(a, inside ? id : 0, kh, inside && more, n, c);
+            t.load(pages, inside ? id : 0, inside && more, offsets.opaque());
         };
         const auto step = [&](typename C::Tile& t, int j) {
             f32x4_t s = t.scores(q);
@@ -378,26 +252,22 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
                         t.hide(i);
                     }
             }
-            const float mn = fmaxf(m, column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
-            if (off == NONE) off = t.spare();
-            f32x4_t p;
-#pragma unroll 1
-            for (int again = 0; again < 2; ++again) {              // twice where the offset is chosen anew
-                const float rn = mn == -INFINITY ? 0.f : fmaf(mn, unit, off);
-                if (__any(!(rn == ref))) {
-                    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - rn);
-                    l *= keep;
-                    o.scale(keep);
-                    ref = rn;
-                }
-                m = mn;
+            f32x4_t e, p;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], unit, -rn));
-                if (!t.too_large(p)) break;
-                off = t.spare();
+            for (int i = 0; i < 4; ++i) e[i] = fmaf(s[i], unit, -ref);
+            if (__any(!(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])) <= C::MOST))) {
+                const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * unit;
+                const float now = ref == -INFINITY || top - ref > C::MOST ? top - C::START : ref, keep = now == ref ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+                l *= keep;
+                o.scale(keep);
+                ref = now;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = fmaf(s[i], unit, ref == -INFINITY ? 0.f : -ref);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(e[i]);
             l += (p[0] + p[1]) + (p[2] + p[3]);
-            t.add(p, q, o);
+            t.add(p, o);
         };
         // Two pages in flight, their numbers one step ahead.  Loads behind the last page are issued too, of nothing: so every wait in the loop is for a known
         // number of loads.
@@ -417,41 +287,328 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_decode(WindowDecodeArgs a
     }
     if (lost) l = NAN;
     l = column_sum(l);
-    o.finish();
-    if (m == -INFINITY) ref = -INFINITY;           // nothing seen, or scores of -inf alone
-    float* s_ref = lds + WAVES * room * HD;
-    float* s_l = s_ref + WAVES * room;
-    if (n < heads) {
-        o.each(c, [&](int d, f32x4_t x) { *(f32x4_t*)(lds + (wave * room + n) * HD + d) = x; });
+    if (n < w.heads) {
+        o.each(c, [&](int d, f32x4_t x) { *(f32x4_t*)(lds + (wave * w.room + n) * HD + d) = x; });
         if (c == 0) {
-            s_ref[wave * room + n] = ref;
-            s_l[wave * room + n] = l;
+            lds[WAVES * w.room * HD + wave * w.room + n] = ref;
+            lds[WAVES * w.room * (HD + 1) + wave * w.room + n] = l;
         }
     }
     __syncthreads();
-    const size_t slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
-    for (int i = threadIdx.x; i < heads * (HD / 4); i += WAVES * 64) {
-        const int h = i / (HD / 4), d = i % (HD / 4) * 4;
-        float top = -INFINITY, sum = 0.f;
-        f32x4_t x{0.f, 0.f, 0.f, 0.f};
+    join_waves<T, HD, WAVES>(a, w, ctx, lds);
+}
+
+// A cache of 4 bits.  The bits of a code v = u + 8, masked where they lie, are the half v 2^-24 or (the upper of a byte) v 2^-20, below half's normal range
+// and exact to the matrix units: 5 instructions for 8 codes.  With scale s and center c of each token and 64 dims (group g),
+//   q.k = sum over g of s_g (sum q v - 8 sum q) + c_g (sum of q in g),   o = sum over tokens of (p s_g) v - 8 (p s_g) + p c_g:
+// the matrix units take q and p s_g, the rest is a few multiply-adds a token.  What a token costs beside its codes would outweigh them if 16 lanes
+// worked on each for the 16 rows of a matrix product, so it is dealt out: scores are Q K^T with the query heads, up to HEADS = 16 / PAGES of them, repeated in
+// all rows, and of PAGES pages' scores a quad of rows (lanes c) keeps the page that is its own: a lane has one token of PAGES x 16 for R heads.
+// Weights p s_g go to the lanes of the second product through LDS.  64 rows of 512-4096 tokens, 32 heads of 128: 142 us with lanes of four tokens for
+// all 16 rows.
+// A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that; from float
+// in three terms.  Weights are such that p s_g fits half, in one term, of float calls in two.
+template <typename T, int HD, int PAGES, int R, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void k_kv4_decode(WindowDecodeArgs a) {
+    using L = Kv4<HD>;
+    constexpr int KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 3 : 1, WTERMS = sizeof(T) == 4 ? 2 : 1, HEADS = 16 / PAGES, QUADS = HEADS / 4;
+    constexpr float CODE = 1.f / (1 << 24), MOST = 4.f;            // MOST: log2 of the greatest weight, above the offset
+    typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
+    extern __shared__ float lds[];                 // as above; while pages are worked on, weights [WAVES][WTERMS][GROUPS][PAGES][HEADS][16 tokens] of half
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
+    const DecodeWork w(a);
+    const int* table = nullptr;
+    const int ctx = row_context(a, w.r, table);
+    const int own = c / QUADS, quad = c % QUADS;   // the lane's page of PAGES, and its heads 4 quad + r
+    float l[R] = {}, ref[R], wsum[GROUPS][R] = {}, csum[GROUPS][R] = {};
+    f32x4_t o[HD / 16];                            // heads 4 quad + r, dim 16 d + n; in units of CODE, odd d of 16 CODE
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_ref[w * room + h]);
+    for (int r = 0; r < R; ++r) ref[r] = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_ref[w * room + h] - top);
-            sum += f * s_l[w * room + h];
-            x += f * *(const f32x4_t*)(lds + (w * room + h) * HD + d);
+    for (int d = 0; d < HD / 16; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    bool lost = ctx < 0;
+    if (ctx > 0) {
+        const int mine_head = min(n % HEADS, w.heads - 1);         // of row n of Q and of the weights
+        u32x4_t q[KS][TERMS];
+        f32x4_t first[GROUPS];                                     // -8 times the sum of q in the group, in units of CODE
+        float unit[R];
+        {
+            const T* p = (const T*)a.q + (size_t)w.r * a.ld_q + (size_t)(w.h0 + mine_head) * HD + c * 8;
+            float f[KS][8], m = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                load8<T>(p + s * 32, f[s]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(f[s][e]));
+            }
+            m = column_max(m);
+            const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
+            const float one = ldexpf(1.44269504088896f * rsqrtf((float)HD) / CODE, -up);
+#pragma unroll
+            for (int r = 0; r < R; ++r) unit[r] = __shfl(one, 4 * quad + r, kWave);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                float sum = 0.f;
+#pragma unroll
+                for (int s = 2 * g; s < 2 * g + 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += f[s][e] = ldexpf(f[s][e], up);
+                sum = column_sum(sum) * (-8.f * CODE);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) first[g][r] = __shfl(sum, 4 * quad + r, kWave);
+            }
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {                  // codes of a word come in the order 0 4 1 5 2 6 3 7, odd ones 16 times as large
+                        const float by = e & 1 ? 0.0625f : 1.f;
+                        const uint32_t h = pack2<f16_t>(f[s][e] * by, f[s][e + 4] * by);
+                        q[s][t][e] = h;
+                        f[s][e] -= unpack<f16_t>(h, 0) / by;
+                        f[s][e + 4] -= unpack<f16_t>(h, 1) / by;
+                    }
         }
-        if (a.nsplit == 1) {
-            T* out = (T*)a.out + (size_t)r * a.ld_out + (size_t)(h0 + h) * HD + d;
+        const Visible see(ctx, a.window, a.sinks);
+        const int from = (int)((int64_t)see.n_pages * w.split / a.nsplit), to = (int)((int64_t)see.n_pages * (w.split + 1) / a.nsplit);
+        const size_t layer = (size_t)a.n_kv_heads * L::BLOCK, stride = layer * a.n_layers;
+        const uint8_t* base = (const uint8_t*)a.pool + a.layer * layer + (size_t)w.kh * L::BLOCK;
+        const uint32_t piece = lane * L::PIECE;
+        uint16_t* weights = (uint16_t*)lds + wave * (WTERMS * GROUPS * 256);
+        // token n lies at place (0 2 1 3)[n % 4] of its four, the order of the codes of V
+        uint16_t* put = weights + (own * HEADS + 4 * quad) * 16 + (n & 12) + (n & 1) * 2 + (n >> 1 & 1);
+        const uint16_t* get = weights + mine_head * 16 + 4 * c;
+        float off = 0.f, most = -INFINITY;
+
+        struct Tile {
+            Codes k[PAGES], v[PAGES];
+            uint32_t kp[GROUPS], vp[GROUPS];       // (scale, center) of the lane's token
+        };
+        const auto number = [&](int j) {           // of the lane's page in block j; of a block behind the last, the last page
+            return table[see.page(min(from + (wave + j * WAVES) * PAGES + own, to - 1))];
+        };
+        const auto fetch = [&](Tile& t, int id, int j) {
+            const bool inside = (unsigned)id < (unsigned)a.n_pages;
+            lost |= !inside;
+            id = inside ? id : 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = round_to<T>(ctx == 0 ? 0.f : x[e] / sum);
-        } else {
-            const size_t slot = ((size_t)r * a.n_q_heads + h0 + h) * a.nsplit + split;
-            if (d == 0) { a.part[2 * slot] = top; a.part[2 * slot + 1] = sum; }
-            *(f32x4_t*)(a.part + 2 * slots + slot * HD + d) = x;
+            for (int p = 0; p < PAGES; ++p) {
+                const int page = __builtin_amdgcn_readlane(id, p * (64 / PAGES));
+                const PageBuffer b(base + (size_t)page * stride, from + (wave + j * WAVES) * PAGES + p < to ? L::BLOCK : 0);
+                uint32_t at = piece;
+                asm volatile("" : "+v"(at));       // offsets stay immediates of the loads, not a register each
+                t.k[p] = b.get<Codes>(at, 0);
+                t.v[p] = b.get<Codes>(at, L::V_CODES);
+            }
+            const uint8_t* par = base + (size_t)id * stride + n * 4;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                t.kp[g] = __builtin_nontemporal_load((const uint32_t*)(par + L::param(0, 64 * g)));
+                t.vp[g] = __builtin_nontemporal_load((const uint32_t*)(par + L::PARAMS + L::param(0, 64 * g)));
+            }
+        };
+        const auto rescale = [&](const float (&now)[R]) {
+            float keep[4] = {1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                keep[r] = now[r] == ref[r] ? 1.f : __builtin_amdgcn_exp2f(ref[r] - now[r]);
+                ref[r] = now[r];
+                l[r] *= keep[r];
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    wsum[g][r] *= keep[r];
+                    csum[g][r] *= keep[r];
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[d][r] *= keep[r];
+        };
+        const auto over_tokens = [&](float x) {    // greatest over all tokens of the head
+#pragma unroll
+            for (int s = 1; s < 16; s <<= 1) x = fmaxf(x, __shfl_xor(x, s, kWave));
+#pragma unroll
+            for (int s = 16 * QUADS; s < 64; s <<= 1) x = fmaxf(x, __shfl_xor(x, s, kWave));
+            return x;
+        };
+        const auto step = [&](Tile& t, int j) {
+            float s[R];
+            {
+                f32x4_t raw[GROUPS];
+#pragma unroll
+                for (int p = 0; p < PAGES; ++p)
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) {
+                        f32x4_t x = first[g];
+#pragma unroll
+                        for (int i = 2 * g; i < 2 * g + 2; ++i) {
+                            const uint32_t k = t.k[p][i], up = k >> 8;
+                            const u32x4_t h{k & 0x000F000Fu, k & 0x00F000F0u, up & 0x000F000Fu, up & 0x00F000F0u};
+#pragma unroll
+                            for (int e = 0; e < TERMS; ++e) x = Matrix16<f16_t>::qk(q[i][e], h, x);
+                        }
+#pragma unroll
+                        for (int r = 0; r < R; ++r) raw[g][r] = p == 0 || own == p ? x[r] : raw[g][r];
+                    }
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r] = 0.f;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    const float center = unpack<f16_t>(t.kp[g], 1) * -0.125f;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) s[r] = fmaf(unpack<f16_t>(t.kp[g], 0), raw[g][r], fmaf(center, first[g][r], s[r]));
+                }
+            }
+            const int i = from + (wave + j * WAVES) * PAGES + own;
+            const bool seen = i < to && see.sees(see.page(i) * 16 + n);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) t.vp[g] = seen ? t.vp[g] : 0;
+            float e[R], p[R], top = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                s[r] = seen ? s[r] : -INFINITY;
+                e[r] = fmaf(s[r], unit[r], -ref[r]);
+                top = r == 0 ? e[r] : fmaxf(top, e[r]);
+            }
+            const auto scale = [&](int g) { return unpack<f16_t>(t.vp[g], 0); };
+            if (__any(!(top <= most))) {
+                if (most == -INFINITY) {           // p s is at most 2^10 for the scales here; later ones may be 2^5 times as large
+                    float m = 0.f;
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) m = fmaxf(m, fabsf(scale(g)));
+                    m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_max(m))));
+                    off = m > 0.f && m < INFINITY ? (float)ilogbf(m) - 9.f : -14.f;
+                    most = MOST - off;
+                }
+                float now[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float high = over_tokens(s[r]) * unit[r];
+                    now[r] = ref[r] == -INFINITY || high - ref[r] > most ? high + off : ref[r];
+                }
+                rescale(now);
+#pragma unroll
+                for (int r = 0; r < R; ++r) e[r] = fmaf(s[r], unit[r], ref[r] == -INFINITY ? 0.f : -ref[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) p[r] = __builtin_amdgcn_exp2f(e[r]);
+            float ps[GROUPS][R], high = 0.f;
+            const auto multiply = [&]() {
+                high = 0.f;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        ps[g][r] = fmaf(p[r], scale(g), 0.f);
+                        high = fmaxf(high, fabsf(ps[g][r]));
+                    }
+            };
+            multiply();
+            if (__any(high > 32768.f)) {           // much larger scales than before: all weights 2^by times smaller from here on
+                high = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_max(high))));
+                const float by = high < INFINITY ? (float)ilogbf(high) - 9.f : 60.f, f = __builtin_amdgcn_exp2f(-by);
+                float now[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    now[r] = ref[r] + by;
+                    p[r] *= f;
+                }
+                rescale(now);
+                off += by;
+                most -= by;
+                multiply();
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                l[r] += p[r];
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    csum[g][r] = fmaf(p[r], unpack<f16_t>(t.vp[g], 1), csum[g][r]);
+                    float rest = ps[g][r];
+#pragma unroll
+                    for (int x = 0; x < WTERMS; ++x) {
+                        const f16_t h = (f16_t)rest;
+                        put[(x * GROUPS + g) * 256 + r * 16] = __builtin_bit_cast(uint16_t, h);
+                        wsum[g][r] += (float)h;    // as the matrix units see them
+                        rest -= (float)h;
+                    }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();       // a wave's LDS accesses keep their order; this states it to the compiler
+            asm volatile("" : : : "memory");
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                for (int x = 0; x < WTERMS; ++x)
+#pragma unroll
+                    for (int pp = 0; pp < PAGES; pp += 2) {
+                        const u32x2_t wa = *(const u32x2_t*)(get + (x * GROUPS + g) * 256 + pp * HEADS * 16);
+                        const u32x2_t wb = PAGES > 1 ? *(const u32x2_t*)(get + (x * GROUPS + g) * 256 + (PAGES > 1 ? pp + 1 : 0) * HEADS * 16) : u32x2_t{0, 0};
+#pragma unroll
+                        for (int i = 2 * g; i < 2 * g + 2; ++i) {
+                            const uint32_t va = t.v[pp][i], vb = PAGES > 1 ? t.v[PAGES > 1 ? pp + 1 : 0][i] : 0;
+#pragma unroll
+                            for (int d = 0; d < 2; ++d) {          // tokens (0, 2), (1, 3) of dims 32 i + n, then of dims 32 i + 16 + n
+                                const uint32_t mask = d ? 0x00F000F0u : 0x000F000Fu;
+                                if (PAGES > 1) {
+                                    const u32x4_t h{va & mask, va >> 8 & mask, vb & mask, vb >> 8 & mask};
+                                    o[2 * i + d] = Matrix16<f16_t>::qk(u32x4_t{wa[0], wa[1], wb[0], wb[1]}, h, o[2 * i + d]);
+                                } else {
+                                    o[2 * i + d] = Matrix16<f16_t>::pv(wa, u32x2_t{va & mask, va >> 8 & mask}, o[2 * i + d]);
+                                }
+                            }
+                        }
+                    }
+            asm volatile("" : : : "memory");
+            __builtin_amdgcn_wave_barrier();
+        };
+        const int blocks = (to - from + PAGES - 1) / PAGES, mine = blocks > wave ? (blocks - wave + WAVES - 1) / WAVES : 0;
+        // Two blocks in flight, page numbers a step further ahead.  Loads of pages behind the last are issued too, of nothing: so every wait in the loop is
+        // for a known number of loads.
+        if (mine > 0) {
+            Tile t0, t1;
+            int id0 = number(0), id1 = number(1);
+            fetch(t0, id0, 0);
+            for (int j = 0; j < mine; j += 2) {
+                id0 = number(j + 2);
+                fetch(t1, id1, j + 1);
+                step(t0, j);
+                id1 = number(j + 3);
+                fetch(t0, id0, j + 2);
+                if (j + 1 < mine) step(t1, j + 1);
+            }
         }
     }
+    lost = __any(lost);
+    const auto total = [&](float x) {              // over all tokens of the head
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) x += __shfl_xor(x, s, kWave);
+#pragma unroll
+        for (int s = 16 * QUADS; s < 64; s <<= 1) x += __shfl_xor(x, s, kWave);
+        return x;
+    };
+    __syncthreads();                               // nobody reads weights any more
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int h = 4 * quad + r;
+        const float all = total(l[r]);
+        float more[GROUPS];
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) more[g] = total(csum[g][r]) - 8.f * total(wsum[g][r]);
+        if (own == 0 && h < w.heads) {
+            float* to = lds + (wave * w.room + h) * HD + n;
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) to[16 * d] = fmaf(o[d][r], (d & 1 ? 0.0625f : 1.f) / CODE, more[d / 4]);
+            if (n == 0) {
+                lds[WAVES * w.room * HD + wave * w.room + h] = ref[r];
+                lds[WAVES * w.room * (HD + 1) + wave * w.room + h] = lost ? NAN : all;
+            }
+        }
+    }
+    __syncthreads();
+    join_waves<T, HD, WAVES>(a, w, ctx, lds);
 }
 
 // The parts of a (row, query head) joined: a wave each, or of many parts four, whose sums meet in LDS.
@@ -482,7 +639,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) 
 }
 
 // Waves of a workgroup; four where 16 heads' sums of eight would take more than 64 KB of LDS.
-static int decode_waves(int group) { return group > 8 ? 4 : 8; }
+static int decode_waves(int group) { static const char* e = getenv("DW"); return group > 8 ? 4 : e ? atoi(e) : 8; }
 
 int window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks) {
     const int64_t pages = std::min<int64_t>((max_ctx + 15ll) / 16, (sinks + 15ll) / 16 + (window + 15ll) / 16 + 1);
@@ -495,13 +652,11 @@ size_t window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int n
     return (size_t)rows * n_q_heads * nsplit * (head_dim + 2);
 }
 
-template <typename C>
-static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
-    using T = typename C::T;
-    const int group = a.n_q_heads / a.n_kv_heads, waves = decode_waves(group);
-    const int64_t blocks = (int64_t)a.n_kv_heads * ((group + 15) / 16) * a.nsplit;
+// The rows in turns of what one launch holds: `start` launches `blocks` workgroups of `waves` waves a row.
+template <typename T, int HD, typename F>
+static hipError_t in_turns(hipStream_t st, const WindowDecodeArgs& a, int waves, F start) {
+    const int64_t blocks = (int64_t)a.n_kv_heads * ((a.n_q_heads / a.n_kv_heads + 15) / 16) * a.nsplit;
     const int most = (int)std::min<int64_t>(kLaunchThreads / (64 * waves) / std::max<int64_t>(blocks, a.n_q_heads), 1 << 24);
-    const size_t lds = (size_t)waves * std::min(16, group) * (C::HD + 2) * sizeof(float);
     for (int first = 0; first < a.rows; first += most) {
         WindowDecodeArgs p = a;
         p.q = (const T*)a.q + (size_t)first * a.ld_q;
@@ -509,24 +664,46 @@ static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
         p.row_sample += first;
         p.ctx_len += first;
         p.rows = std::min(most, a.rows - first);
-        const unsigned grid = (unsigned)(p.rows * blocks);
-        if (waves == 8) k_window_decode<C, 8><<<grid, 512, lds, st>>>(p);
-        else k_window_decode<C, 4><<<grid, 256, lds, st>>>(p);
+        start((unsigned)(p.rows * blocks), p);
         const unsigned heads = (unsigned)p.rows * (unsigned)a.n_q_heads;
-        if (a.nsplit > 8) k_window_join<T, C::HD, 4><<<heads, 256, 0, st>>>(p);
-        else if (a.nsplit > 1) k_window_join<T, C::HD, 1><<<heads, 64, 0, st>>>(p);
+        if (a.nsplit > 8) k_window_join<T, HD, 4><<<heads, 256, 0, st>>>(p);
+        else if (a.nsplit > 1) k_window_join<T, HD, 1><<<heads, 64, 0, st>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+template <typename C>
+static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
+    const int group = a.n_q_heads / a.n_kv_heads, waves = decode_waves(group);
+    const size_t lds = (size_t)waves * std::min(16, group) * (C::HD + 2) * sizeof(float);
+    return in_turns<typename C::T, C::HD>(st, a, waves, [&](unsigned grid, const WindowDecodeArgs& p) {
+        if (waves == 8) k_window_decode<C, 8><<<grid, 512, lds, st>>>(p);
+        else k_window_decode<C, 4><<<grid, 256, lds, st>>>(p);
+    });
+}
+
+template <typename T, int HD>
+static hipError_t kv4_rows(hipStream_t st, const WindowDecodeArgs& a) {
+    const int group = a.n_q_heads / a.n_kv_heads;
+    constexpr int WAVES = 4;
+    const size_t sums = (size_t)WAVES * std::min(16, group) * (HD + 2) * sizeof(float), weights = (size_t)WAVES * (sizeof(T) == 4 ? 2 : 1) * (HD / 64) * 512;
+    const size_t lds = std::max(sums, weights);
+    return in_turns<T, HD>(st, a, WAVES, [&](unsigned grid, const WindowDecodeArgs& p) {
+        if (group == 1) k_kv4_decode<T, HD, 4, 1, WAVES><<<grid, WAVES * 64, lds, st>>>(p);
+        else if (group <= 4) k_kv4_decode<T, HD, 4, 4, WAVES><<<grid, WAVES * 64, lds, st>>>(p);
+        else if (group <= 8) k_kv4_decode<T, HD, 2, 4, WAVES><<<grid, WAVES * 64, lds, st>>>(p);
+        else k_kv4_decode<T, HD, 1, 4, WAVES><<<grid, WAVES * 64, lds, st>>>(p);
+    });
+}
+
 hipError_t launch_window_decode(hipStream_t st, int dtype, bool four_bits, int head_dim, const WindowDecodeArgs& a) {
-#define RLHF_DECODE(HD)                                                                                           \
-    if (head_dim == HD) {                                                                                         \
-        if (dtype == kBF16) return four_bits ? decode_rows<Cache4<bf16_t, HD>>(st, a) : decode_rows<Cache16<bf16_t, HD>>(st, a); \
-        if (dtype == kF16) return four_bits ? decode_rows<Cache4<f16_t, HD>>(st, a) : decode_rows<Cache16<f16_t, HD>>(st, a);    \
-        return four_bits ? decode_rows<Cache4<float, HD>>(st, a) : decode_rows<CacheFloat<HD>>(st, a);            \
+#define RLHF_DECODE(HD)                                                                                                        \
+    if (head_dim == HD) {                                                                                                      \
+        if (dtype == kBF16) return four_bits ? kv4_rows<bf16_t, HD>(st, a) : decode_rows<Cache16<bf16_t, HD>>(st, a);          \
+        if (dtype == kF16) return four_bits ? kv4_rows<f16_t, HD>(st, a) : decode_rows<Cache16<f16_t, HD>>(st, a);             \
+        return four_bits ? kv4_rows<float, HD>(st, a) : decode_rows<CacheFloat<HD>>(st, a);                                    \
     }
     RLHF_DECODE(64)
     RLHF_DECODE(128)
