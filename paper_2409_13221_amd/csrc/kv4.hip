@@ -8,89 +8,169 @@
 
 namespace rlhf {
 
-// The whole number -8 .. 7 nearest to (x - c) / s, the even one half way, in double: in float the quotient would be rounded, and a value next to
-// half way between two steps could go to the other one.
-__device__ __forceinline__ int kv4_code(float x, float s, float c) {
-    if (s == 0.f) return 0;
-    const double d = (double)x - (double)c;
-    double u = rint(d / (double)s);
-    u = u < -8. ? -8. : u > 7. ? 7. : u;
-    return (int)u;
+// What a thread of both kernels has: dims 8 i .. 8 i + 7 (i = lane % (HD / 8)) of one head of one row; 8 threads share a group.  Its K codes are one word of a
+// block.  Its V codes are nibbles of 8 bytes, which the thread with dims 16 further on or back fills up: each of the two moves four of the bytes.
+template <int HD> struct Piece {
+    using L = Kv4<HD>;
+    static constexpr int LANES = HD / 8, ROWS = 64 / LANES;        // of a wave
+    int i, t, d;
+    __device__ __forceinline__ Piece(int lane, int slot) : i(lane % LANES), t(slot & 15), d(i * 8) {}
+    __device__ __forceinline__ int k_word() const { return L::k_byte(t, d); }
+    __device__ __forceinline__ bool upper() const { return i & 2; }          // holds the upper nibbles
+    __device__ __forceinline__ int v_byte(int j) const { return L::v_byte(t, d + (upper() ? 4 : 0) + j); }      // j-th of its four
+    __device__ __forceinline__ int param() const { return L::param(t, d); }
+};
+__device__ __forceinline__ uint32_t other_nibbles(uint32_t x) { return __shfl_xor(x, 2, kWave); }
+// Nibbles 0 .. 3 (upper: 4 .. 7) of lo and hi as the lower and upper ones of four bytes.
+__device__ __forceinline__ uint32_t merge_nibbles(uint32_t lo, uint32_t hi) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x |= (lo >> 4 * j & 15) << 8 * j | (hi >> 4 * j & 15) << (8 * j + 4);
+    return x;
 }
 
-// A wave takes one head's K or V of one row: lanes hold dims lane and lane + 64.
+// The whole number -8 .. 7 nearest to (x - c) / s, the even one half way, in double: the quotient is rounded, but not onto a half that it is not.
+__device__ __forceinline__ float kv4_code(float x, float s, float c) {
+    if (s == 0.f) return 0.f;
+    return (float)fmin(fmax(rint(((double)x - (double)c) / (double)s), -8.), 7.);
+}
+
+// Codes of a thread's 8 values (4 bits each), scale and center of its group.  In float a quotient of up to 8.5 is off by 8.5 x 2^-22 by the difference, the
+// reciprocal and the product; the few that lie within 2^-17 of half way between two steps are taken again in double.
+__device__ __forceinline__ uint32_t kv4_pack(const float (&x)[8], uint32_t& params) {
+    float lo = x[0], hi = x[0], sum = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+        lo = fminf(lo, x[e]);
+        hi = fmaxf(hi, x[e]);
+        sum += x[e];                               // not a number if one of them is not, or infinities of both signs are among them
+    }
+    bool bad = !(fmaxf(-lo, hi) <= 65504.f) || sum != sum;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        lo = fminf(lo, __shfl_xor(lo, o, kWave));
+        hi = fmaxf(hi, __shfl_xor(hi, o, kWave));
+    }
+    bad = __ballot(bad) >> (threadIdx.x & 56) & 255;
+    const f16_t s = bad ? (f16_t)NAN : (f16_t)((hi - lo) * (1.f / 15.f)), c = bad ? (f16_t)NAN : (f16_t)(lo + 8.f * (float)s);
+    params = (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, c) << 16;
+    const float inv = bad || (float)s == 0.f ? 0.f : 1.f / (float)s;
+    float u[8], near = 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float q = bad ? 0.f : (x[e] - (float)c) * inv;
+        u[e] = rintf(q);
+        near = fminf(near, fabsf(fabsf(q - u[e]) - 0.5f));
+        u[e] = fminf(fmaxf(u[e], -8.f), 7.f);
+    }
+    if (__any(near < 0x1p-17f)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = bad ? 0.f : kv4_code(x[e], (float)s, (float)c);
+    }
+    uint32_t code = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) code |= (uint32_t)(u[e] + 8.f) << 4 * e;
+    return code;
+}
+
+// A wave takes one head of 4 rows (of 64 dims: 8), K and V.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_kv4_append(Kv4Args a) {
     using L = Kv4<HD>;
+    using P = Piece<HD>;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r = (int)(w / (2 * a.n_kv_heads)), rest = (int)(w % (2 * a.n_kv_heads)), h = rest >> 1, is_v = rest & 1;
-    if (r >= a.rows) return;
-    const int slot = a.slot[r];
-    if (slot < 0 || slot / 16 >= a.n_pages) return;
-    const T* x = is_v ? (const T*)a.v + (size_t)r * a.ld_v + (size_t)h * HD : (const T*)a.k + (size_t)r * a.ld_k + (size_t)h * HD;
+    const unsigned w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = (int)(w % (unsigned)a.n_kv_heads), r = (int)(w / (unsigned)a.n_kv_heads) * P::ROWS + lane / P::LANES;
+    const int slot = r < a.rows ? a.slot[r] : -1;
+    const bool there = slot >= 0 && slot / 16 < a.n_pages;
+    if (!__any(there)) return;
+    const P p(lane, slot);
+    float k[8] = {}, v[8] = {};
+    if (there) {
+        load8<T>((const T*)a.k + (size_t)r * a.ld_k + (size_t)h * HD + p.d, k);
+        load8<T>((const T*)a.v + (size_t)r * a.ld_v + (size_t)h * HD + p.d, v);
+    }
+    uint32_t pk, pv;
+    const uint32_t ck = kv4_pack(k, pk), cv = kv4_pack(v, pv), other = other_nibbles(cv);
+    if (!there) return;
     uint8_t* block = (uint8_t*)a.pool + (((size_t)(slot / 16) * a.n_layers + a.layer) * a.n_kv_heads + h) * L::BLOCK;
-    const int t = slot % 16;
+    *(uint32_t*)(block + p.k_word()) = ck;
+    const uint32_t bytes = p.upper() ? merge_nibbles(other >> 16, cv >> 16) : merge_nibbles(cv, other);
 #pragma unroll
-    for (int g = 0; g < L::GROUPS; ++g) {
-        const int d = g * 64 + lane;
-        const float f = to_f32<T>(x[d]);
-        const bool bad = __any(!(fabsf(f) <= 65504.f));
-        const float lo = -wave_max(-f), hi = wave_max(f);
-        const f16_t s = bad ? (f16_t)NAN : (f16_t)((hi - lo) * (1.f / 15.f));
-        const f16_t c = bad ? (f16_t)NAN : (f16_t)(lo + 8.f * (float)s);
-        const int u = bad ? 8 : 8 + kv4_code(f, (float)s, (float)c);
-        const int other = __shfl_xor(u, is_v ? 16 : 1, kWave);
-        if (is_v) {
-            if (L::v_bit(d) == 0) block[L::v_byte(t, d)] = (uint8_t)(u | other << 4);
-        } else {
-            if (L::k_bit(d) == 0) block[L::k_byte(t, d)] = (uint8_t)(u | other << 4);
-        }
-        if (lane == 0) {
-            f16_t* p = (f16_t*)(block + L::param(t, d) + is_v * L::PARAMS);
-            p[0] = s;
-            p[1] = c;
-        }
+    for (int j = 0; j < 4; ++j) block[p.v_byte(j)] = (uint8_t)(bytes >> 8 * j);
+    if (p.i % 8 == 0) {
+        *(uint32_t*)(block + p.param()) = pk;
+        *(uint32_t*)(block + p.param() + L::PARAMS) = pv;
+    }
+}
+
+__device__ __forceinline__ void kv4_unpack(uint32_t code, uint32_t params, float (&x)[8]) {
+    const float s = unpack<f16_t>(params, 0), c = unpack<f16_t>(params, 1);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(s, (float)((int)(code >> 4 * e & 15) - 8), c);
+}
+
+template <typename T> __device__ __forceinline__ void put8(T* to, const float (&x)[8]) {
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8; i += N) {
+        float y[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = x[i + e];
+        Vec<T> v;
+        v.set(y);
+        v.template store<false>(to + i);
     }
 }
 
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_kv4_read(Kv4Args a) {
     using L = Kv4<HD>;
+    using P = Piece<HD>;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r = (int)(w / (2 * a.n_kv_heads)), rest = (int)(w % (2 * a.n_kv_heads)), h = rest >> 1, is_v = rest & 1;
-    if (r >= a.rows) return;
-    T* x = is_v ? (T*)a.v + (size_t)r * a.ld_v + (size_t)h * HD : (T*)a.k + (size_t)r * a.ld_k + (size_t)h * HD;
-    const int slot = a.slot[r];
-    const bool inside = slot >= 0 && slot / 16 < a.n_pages;
-    const uint8_t* block = (const uint8_t*)a.pool + (((size_t)(inside ? slot / 16 : 0) * a.n_layers + a.layer) * a.n_kv_heads + h) * L::BLOCK;
-    const int t = slot & 15;
+    const unsigned w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = (int)(w % (unsigned)a.n_kv_heads), r = (int)(w / (unsigned)a.n_kv_heads) * P::ROWS + lane / P::LANES;
+    const int slot = r < a.rows ? a.slot[r] : -1;
+    const bool there = slot >= 0 && slot / 16 < a.n_pages;
+    const P p(lane, slot);
+    const uint8_t* block = (const uint8_t*)a.pool + (((size_t)(there ? slot / 16 : 0) * a.n_layers + a.layer) * a.n_kv_heads + h) * L::BLOCK;
+    uint32_t ck = 0, bytes = 0, pk = 0, pv = 0;
+    if (there) {
+        ck = *(const uint32_t*)(block + p.k_word());
 #pragma unroll
-    for (int g = 0; g < L::GROUPS; ++g) {
-        const int d = g * 64 + lane;
-        float f = slot < 0 ? 0.f : NAN;
-        if (inside) {
-            const int u = (is_v ? block[L::v_byte(t, d)] >> L::v_bit(d) : block[L::k_byte(t, d)] >> L::k_bit(d)) & 15;
-            const f16_t* p = (const f16_t*)(block + L::param(t, d) + is_v * L::PARAMS);
-            f = (float)p[1] + (float)p[0] * (float)(u - 8);
-        }
-        x[d] = round_to<T>(f);
+        for (int j = 0; j < 4; ++j) bytes |= (uint32_t)block[p.v_byte(j)] << 8 * j;
+        pk = *(const uint32_t*)(block + p.param());
+        pv = *(const uint32_t*)(block + p.param() + L::PARAMS);
+    } else if (slot >= 0) {
+        pk = pv = 0x7E007E00u;                     // not a number
     }
+    const uint32_t other = other_nibbles(bytes), lo = p.upper() ? other : bytes, hi = p.upper() ? bytes : other;      // bytes 0 .. 3 and 4 .. 7
+    uint32_t cv = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int at = 8 * j + (p.upper() ? 4 : 0);
+        cv |= (lo >> at & 15) << 4 * j | (hi >> at & 15) << (4 * j + 16);
+    }
+    if (r >= a.rows) return;
+    float x[8];
+    kv4_unpack(ck, pk, x);
+    put8<T>((T*)a.k + (size_t)r * a.ld_k + (size_t)h * HD + p.d, x);
+    kv4_unpack(cv, pv, x);
+    put8<T>((T*)a.v + (size_t)r * a.ld_v + (size_t)h * HD + p.d, x);
 }
 
 size_t kv4_block_bytes(int head_dim) { return (size_t)18 * head_dim; }
 
 template <typename T, bool APPEND>
 static hipError_t kv4_typed(hipStream_t st, int head_dim, const Kv4Args& a) {
-    const int most = (int)std::min<int64_t>(kLaunchThreads / 128 / a.n_kv_heads, 1 << 30);
+    const int each = 512 / head_dim, most = (int)std::min<int64_t>((kLaunchThreads / 64 - 4) / a.n_kv_heads * each, 1 << 30);       // rows of a wave; of a launch
     for (int first = 0; first < a.rows; first += most) {
         Kv4Args p = a;
         p.k = (T*)a.k + (size_t)first * a.ld_k;
         p.v = (T*)a.v + (size_t)first * a.ld_v;
         p.slot += first;
         p.rows = std::min(most, a.rows - first);
-        const unsigned blocks = (unsigned)(((int64_t)p.rows * 2 * a.n_kv_heads + 3) / 4);
+        const unsigned blocks = (unsigned)(((int64_t)((p.rows + each - 1) / each) * a.n_kv_heads + 3) / 4);
         if (APPEND) {
             if (head_dim == 128) k_kv4_append<T, 128><<<blocks, 256, 0, st>>>(p);
             else k_kv4_append<T, 64><<<blocks, 256, 0, st>>>(p);
