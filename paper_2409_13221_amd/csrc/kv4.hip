@@ -21,56 +21,68 @@ template <int HD> struct Piece {
     __device__ __forceinline__ int param() const { return L::param(t, d); }
 };
 __device__ __forceinline__ uint32_t other_nibbles(uint32_t x) { return __shfl_xor(x, 2, kWave); }
-// Nibbles 0 .. 3 (upper: 4 .. 7) of lo and hi as the lower and upper ones of four bytes.
-__device__ __forceinline__ uint32_t merge_nibbles(uint32_t lo, uint32_t hi) {
-    uint32_t x = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x |= (lo >> 4 * j & 15) << 8 * j | (hi >> 4 * j & 15) << (8 * j + 4);
-    return x;
+// Nibbles 0 .. 3 of lo and hi as the lower and upper ones of four bytes.
+__device__ __forceinline__ uint32_t spread_nibbles(uint32_t x) {
+    x = (x | x << 8) & 0x00FF00FFu;
+    return (x | x << 4) & 0x0F0F0F0Fu;
+}
+__device__ __forceinline__ uint32_t merge_nibbles(uint32_t lo, uint32_t hi) { return spread_nibbles(lo & 0xFFFFu) | spread_nibbles(hi & 0xFFFFu) << 4; }
+// Least (greatest) of the 8 threads of a group.
+template <int CTRL> __device__ __forceinline__ float from_lane(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 15, 15, true));
+}
+template <typename F> __device__ __forceinline__ float over_group(float x, F f) {
+    x = f(x, from_lane<0xB1>(x));                  // neighbours, pairs, halves of 8
+    x = f(x, from_lane<0x4E>(x));
+    return f(x, from_lane<0x141>(x));
 }
 
-// The whole number -8 .. 7 nearest to (x - c) / s, the even one half way, in double: the quotient is rounded, but not onto a half that it is not.
-__device__ __forceinline__ float kv4_code(float x, float s, float c) {
-    if (s == 0.f) return 0.f;
-    return (float)fmin(fmax(rint(((double)x - (double)c) / (double)s), -8.), 7.);
+// u, the nearest whole number to q, or the one on q's other side: whichever is nearest to (x - c) / s, which q is within half a step of; the even one half
+// way.  x, c and s are floats and halves: differences and products of this size are exact in double.
+__device__ __forceinline__ float settle(float q, float u, float x, float s, float c) {
+    const float side = q < u ? -1.f : 1.f, rest = (float)fma(-(double)(u + 0.5f * side), (double)s, (double)x - (double)c) * side;
+    const bool odd = (int)u & 1, on = (rest > 0.f) | ((rest == 0.f) & odd);
+    return on ? u + side : u;
 }
 
 // Codes of a thread's 8 values (4 bits each), scale and center of its group.  In float a quotient of up to 8.5 is off by 8.5 x 2^-22 by the difference, the
-// reciprocal and the product; the few that lie within 2^-17 of half way between two steps are taken again in double.
+// reciprocal and the product; those within 2^-17 of half way between two steps are settled exactly.  Rounding to the nearest whole
+// number is the addition of 1.5 x 2^23 (and 8, for the code), whose low bits are then the code.
 __device__ __forceinline__ uint32_t kv4_pack(const float (&x)[8], uint32_t& params) {
-    float lo = x[0], hi = x[0], sum = x[0];
+    float lo = x[0], hi = x[0];                    // not a number if one of them is not
 #pragma unroll
     for (int e = 1; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        sum += x[e];                               // not a number if one of them is not, or infinities of both signs are among them
+        lo = __builtin_elementwise_minimum(lo, x[e]);
+        hi = __builtin_elementwise_maximum(hi, x[e]);
     }
-    bool bad = !(fmaxf(-lo, hi) <= 65504.f) || sum != sum;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-        lo = fminf(lo, __shfl_xor(lo, o, kWave));
-        hi = fmaxf(hi, __shfl_xor(hi, o, kWave));
-    }
-    bad = __ballot(bad) >> (threadIdx.x & 56) & 255;
+    lo = over_group(lo, [](float a, float b) { return __builtin_elementwise_minimum(a, b); });
+    hi = over_group(hi, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
+    const bool bad = !(lo >= -65504.f) || !(hi <= 65504.f);
     const f16_t s = bad ? (f16_t)NAN : (f16_t)((hi - lo) * (1.f / 15.f)), c = bad ? (f16_t)NAN : (f16_t)(lo + 8.f * (float)s);
     params = (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, c) << 16;
-    const float inv = bad || (float)s == 0.f ? 0.f : 1.f / (float)s;
-    float u[8], near = 1.f;
+    const float inv = (float)s == 0.f ? 0.f : __builtin_amdgcn_rcpf((float)s);
+    constexpr float ZERO = 12582912.f;             // 1.5 x 2^23, code 0
+    uint32_t code = 0, base = 0;
+    float off = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float q = bad ? 0.f : (x[e] - (float)c) * inv;
-        u[e] = rintf(q);
-        near = fminf(near, fabsf(fabsf(q - u[e]) - 0.5f));
-        u[e] = fminf(fmaxf(u[e], -8.f), 7.f);
+    for (int e = 7; e >= 0; --e) {
+        const float q = (x[e] - (float)c) * inv, t = q + (ZERO + 8.f);
+        off = fmaxf(off, fabsf(q - (t - (ZERO + 8.f))));
+        code = (code << 4) + __float_as_uint(__builtin_amdgcn_fmed3f(t, ZERO, ZERO + 15.f));
+        base = (base << 4) + 0x4B400000u;
     }
-    if (__any(near < 0x1p-17f)) {
+    code -= base;
+    if (__any(off > 0.5f - 0x1p-17f)) {
+        code = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = bad ? 0.f : kv4_code(x[e], (float)s, (float)c);
+        for (int e = 7; e >= 0; --e) {
+            const float q = (x[e] - (float)c) * inv;
+            float u = q + (ZERO + 8.f) - (ZERO + 8.f);
+            if (__any(fabsf(q - u) > 0.5f - 0x1p-17f)) u = settle(q, u, x[e], (float)s, (float)c);
+            code = code << 4 | (uint32_t)(int)(__builtin_amdgcn_fmed3f(u, -8.f, 7.f) + 8.f);
+        }
     }
-    uint32_t code = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) code |= (uint32_t)(u[e] + 8.f) << 4 * e;
-    return code;
+    return bad || (float)s == 0.f ? 0x88888888u : code;
 }
 
 // A wave takes one head of 4 rows (of 64 dims: 8), K and V.
@@ -85,10 +97,25 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Args a) {
     const bool there = slot >= 0 && slot / 16 < a.n_pages;
     if (!__any(there)) return;
     const P p(lane, slot);
-    float k[8] = {}, v[8] = {};
-    if (there) {
-        load8<T>((const T*)a.k + (size_t)r * a.ld_k + (size_t)h * HD + p.d, k);
-        load8<T>((const T*)a.v + (size_t)r * a.ld_v + (size_t)h * HD + p.d, v);
+    constexpr int N = 16 / sizeof(T);
+    Vec<T> rk[8 / N], rv[8 / N];
+    const T *fk = (const T*)a.k + (size_t)(there ? r : 0) * a.ld_k + (size_t)h * HD + p.d, *fv = (const T*)a.v + (size_t)(there ? r : 0) * a.ld_v + (size_t)h * HD + p.d;
+#pragma unroll
+    for (int i = 0; i < 8 / N; ++i) {
+        rk[i].template load<true>(fk + i * N);
+        rv[i].template load<true>(fv + i * N);
+    }
+    float k[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8 / N; ++i) {
+        float x[N], y[N];
+        rk[i].get(x);
+        rv[i].get(y);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            k[i * N + e] = x[e];
+            v[i * N + e] = y[e];
+        }
     }
     uint32_t pk, pv;
     const uint32_t ck = kv4_pack(k, pk), cv = kv4_pack(v, pv), other = other_nibbles(cv);

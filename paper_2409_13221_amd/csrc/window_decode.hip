@@ -639,7 +639,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) 
 }
 
 // Waves of a workgroup; four where 16 heads' sums of eight would take more than 64 KB of LDS.
-static int decode_waves(int group) { static const char* e = getenv("DW"); return group > 8 ? 4 : e ? atoi(e) : 8; }
+static int decode_waves(int group) { return group > 8 ? 4 : 8; }
 
 int window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks) {
     const int64_t pages = std::min<int64_t>((max_ctx + 15ll) / 16, (sinks + 15ll) / 16 + (window + 15ll) / 16 + 1);
