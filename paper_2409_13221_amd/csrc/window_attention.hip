@@ -59,14 +59,13 @@ __device__ __forceinline__ bool tile_of(const WindowArgs& a, int tile, int& s0, 
     return s0 >= 0 && q0 >= 0 && len <= a.rows - s0 && q0 < len;
 }
 
-// Workgroup -> (tile, query head).  The heads of a KV head and the neighbouring tiles read the same keys: XCD x (workgroups x modulo 8) takes the
-// x-th eighth of them in the order KV head, tile, query head.
-__device__ __forceinline__ void window_work(const WindowArgs& a, int& tile, int& h) {
-    const unsigned n = (unsigned)a.n_tiles * (unsigned)a.n_q_heads, x = blockIdx.x % 8, i = blockIdx.x / 8;
-    const unsigned w = x * (n / 8) + min(x, n % 8) + i;
-    const unsigned G = a.n_q_heads / a.n_kv_heads, per = (unsigned)a.n_tiles * G;
-    tile = (int)(w % per / G);
-    h = (int)(w / per * G + w % G);
+// Workgroup -> (tile, query head).
+__device__ __forceinline__ bool window_work(const WindowArgs& a, int& tile, int& h) {
+    const unsigned G = a.n_q_heads / a.n_kv_heads, i = blockIdx.x / 8, unit = i / G * 8 + blockIdx.x % 8;
+    if (unit >= (unsigned)a.n_tiles * (unsigned)a.n_kv_heads) return false;
+    tile = a.n_tiles - 1 - (int)(unit / a.n_kv_heads);
+    h = (int)(unit % a.n_kv_heads * G + i % G);
+    return true;
 }
 
 // Key tiles of SIZE keys that queries first .. last see any of: 0 .. n_sink - 1 and from `from` on.
@@ -84,11 +83,11 @@ __device__ __forceinline__ bool window_sees(const WindowArgs& a, int i, int j) {
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 __device__ __forceinline__ uint32_t lds_address(void* p) { return (uint32_t)(size_t)(lds_ptr_t)p; }
-// 16 bytes a lane from base + offset to LDS, `to` and on: 1024 bytes of a wave.  Written out, as the builtin makes the compiler wait for all loads in
+// 16 bytes a lane from base + lane + offset to LDS, `to` and on: 1024 bytes of a wave.  Written out, as the builtin makes the compiler wait for all loads in
 // flight before it reads LDS; whoever reads waits for vmcnt and the workgroup first.  (It has no register to come back to; m0 has no other use in
 // these kernels.)
-__device__ __forceinline__ void load_to_lds(u32x4_t base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(base) : "memory");
+__device__ __forceinline__ void load_to_lds(u32x4_t base, uint32_t lane, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(to), "v"(lane), "s"(base), "s"(offset) : "memory");
 }
 __device__ __forceinline__ u32x4_t buffer_base(const void* p) {
     return u32x4_t{(uint32_t)(uintptr_t)p, (uint32_t)((uintptr_t)p >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00020000u};
@@ -100,14 +99,13 @@ typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 // range, so that most tiles do not rescale the sums.  A key that is hidden from a query has weight 0, and 0 times what is not a number is none: a
 // wave whose result is not finite takes its queries again one by one, over visible keys alone.
 template <typename T, int HD>
-__global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
+__global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     using M = Matrix16<T>;
-    constexpr int KS = HD / 32, DF = HD / 16, CH = HD / 8, ROWS = 64 / CH, LOADS = 16 / ROWS, TILE = 64 * HD;
+    constexpr int KT = 32, NF = KT / 16, NU = KT / 32, KS = HD / 32, DF = HD / 16, CH = HD / 8, ROWS = 64 / CH, LOADS = KT / (4 * ROWS), TILE = KT * HD;
     constexpr float START = M::TOP > 0.f ? 6.f : 0.f, MOST = M::TOP > 0.f ? M::TOP : 20.f;      // log2 of the greatest weight at a new reference, and ever
     __shared__ __attribute__((aligned(16))) T sK[2][TILE], sV[2][TILE];
     int tile, h, s0, q0, len;
-    window_work(a, tile, h);
-    if (!tile_of(a, tile, s0, q0, len)) return;
+    if (!window_work(a, tile, h) || !tile_of(a, tile, s0, q0, len)) return;
     const int kh = h / (a.n_q_heads / a.n_kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     const float unit = rsqrtf((float)HD) * 1.44269504088896f;
@@ -119,21 +117,27 @@ __global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
     // ^ (t / 2 % 8) and ^ 2 (t / 2 % 4)), so that fragment reads spread over the banks.
     const int lrow = wave * ROWS + lane / CH, place = lane % CH;
     const int kpiece = CH == 16 ? place ^ (lrow & 15) : place ^ ((lrow >> 1) & 7), vpiece = CH == 16 ? place ^ ((lrow & 7) << 1) : place ^ (((lrow >> 1) & 3) << 1);
+    const uint32_t kat = lrow * ldk + kpiece * 16, vat = lrow * ldv + vpiece * 16;
     const auto fetch = [&](int kt, int buf) {
-        const u32x4_t rk = buffer_base(kb + (size_t)kt * 64 * a.ld_k), rv = buffer_base(vb + (size_t)kt * 64 * a.ld_v);
-        const int last = min(63, len - 1 - kt * 64);               // rows behind the sequence: its last one
+        const u32x4_t rk = buffer_base(kb + (size_t)kt * KT * a.ld_k), rv = buffer_base(vb + (size_t)kt * KT * a.ld_v);
+        const int last = len - 1 - kt * KT;
+        if (last >= KT - 1) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const uint32_t row = min(lrow + i * 4 * ROWS, last);
-            load_to_lds(rk, row * ldk + kpiece * 16, lds_address(&sK[buf][(wave + i * 4) * ROWS * HD]));
-        }
+            for (int i = 0; i < LOADS; ++i) load_to_lds(rk, kat, i * 4 * ROWS * ldk, lds_address(&sK[buf][(wave + i * 4) * ROWS * HD]));
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const uint32_t row = min(lrow + i * 4 * ROWS, last);
-            load_to_lds(rv, row * ldv + vpiece * 16, lds_address(&sV[buf][(wave + i * 4) * ROWS * HD]));
+            for (int i = 0; i < LOADS; ++i) load_to_lds(rv, vat, i * 4 * ROWS * ldv, lds_address(&sV[buf][(wave + i * 4) * ROWS * HD]));
+        } else {                                   // rows behind the sequence: its last one
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const uint32_t row = min(lrow + i * 4 * ROWS, last);
+                load_to_lds(rk, row * ldk + kpiece * 16, 0, lds_address(&sK[buf][(wave + i * 4) * ROWS * HD]));
+                load_to_lds(rv, row * ldv + vpiece * 16, 0, lds_address(&sV[buf][(wave + i * 4) * ROWS * HD]));
+            }
         }
     };
 
+    const KeyTiles<KT> keys(q0, min(q0 + kFlashTile, len) - 1, a.window, a.sinks);
+    fetch(keys.at(0), 0);
     const int w0 = q0 + wave * 32;                 // this wave's queries
     u32x4_t q[2][KS];
 #pragma unroll
@@ -150,26 +154,26 @@ __global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) o[d][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float ref[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
-    const KeyTiles<64> keys(q0, min(q0 + kFlashTile, len) - 1, a.window, a.sinks);
     const int vt = 4 * c + (n >> 2);               // token (modulo 16) and 32-byte pair of pieces of a lane's reads of V
     const int vswap = CH == 16 ? vt & 7 : (vt >> 1) & 3;
 
-    fetch(keys.at(0), 0);
+    if (keys.n > 1) fetch(keys.at(1), 1);
     for (int j = 0; j < keys.n; ++j) {
-        const int kt = keys.at(j), buf = j & 1, first = kt * 64, last = first + 63;
-        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        const int kt = keys.at(j), buf = j & 1, first = kt * KT, last = first + KT - 1;
+        if (j == 0 && keys.n > 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         __syncthreads();                           // tile j is there, and nobody reads tile j - 1 any more
-        if (j + 1 < keys.n) fetch(keys.at(j + 1), buf ^ 1);
+        if (j > 0 && j + 1 < keys.n) fetch(keys.at(j + 1), buf ^ 1);
         if (first > w0 + 31 || (last <= w0 - a.window && first >= a.sinks)) continue;       // nothing that this wave sees
-        f32x4_t s[4][2];
+        f32x4_t s[NF][2];
 #pragma unroll
-        for (int f = 0; f < 4; ++f)
+        for (int f = 0; f < NF; ++f)
 #pragma unroll
             for (int m = 0; m < 2; ++m) s[f][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
+            for (int f = 0; f < NF; ++f) {
                 const int row = f * 16 + n, p = CH == 16 ? (k * 4 + c) ^ n : (k * 4 + c) ^ ((n >> 1) & 7);
                 const u32x4_t x = *(const u32x4_t*)&sK[buf][row * HD + p * 8];
 #pragma unroll
@@ -179,7 +183,7 @@ __global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
+                for (int f = 0; f < NF; ++f)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (!window_sees(a, w0 + m * 16 + n, first + f * 16 + 4 * c + r)) s[f][m][r] = -INFINITY;
@@ -187,26 +191,26 @@ __global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
         float top[2];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            float x = fmaxf(fmaxf(s[0][m][0], s[0][m][1]), fmaxf(s[0][m][2], s[0][m][3]));
+            float x = s[0][m][0];
 #pragma unroll
-            for (int f = 1; f < 4; ++f) x = fmaxf(x, fmaxf(fmaxf(s[f][m][0], s[f][m][1]), fmaxf(s[f][m][2], s[f][m][3])));
-            top[m] = column_max(x) * unit;
+            for (int e = 1; e < 4 * NF; ++e) x = __builtin_elementwise_maximum(x, s[e / 4][m][e % 4]);         // one instruction for two; a score that is no number shows in the result
+            top[m] = x * unit;
         }
         if (__any(top[0] > ref[0] + MOST || top[1] > ref[1] + MOST)) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                const float now = top[m] > ref[m] + MOST ? top[m] - START : ref[m], keep = __builtin_amdgcn_exp2f(ref[m] - now);
+                const float high = column_max(top[m]), now = high > ref[m] + MOST ? high - START : ref[m], keep = __builtin_amdgcn_exp2f(ref[m] - now);
                 ref[m] = now;
                 l[m] *= keep;
 #pragma unroll
                 for (int d = 0; d < DF; ++d) o[d][m] *= keep;
             }
         }
-        u32x4_t p[2][2];
+        u32x4_t p[2][NU];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
+            for (int f = 0; f < NF; ++f) {
                 float w[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(fmaf(s[f][m][r], unit, -ref[m]));
@@ -217,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void k_window_flash(WindowArgs a) {
 #pragma unroll
         for (int d = 0; d < DF; ++d)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < NU; ++u) {
                 T* at = &sV[buf][(u * 32 + vt) * HD + (d ^ vswap) * 16 + (n & 3) * 4];
                 const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * HD));
                 const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
@@ -251,8 +255,7 @@ __global__ __launch_bounds__(512) void k_window_float(WindowArgs a) {
     using Tile = FloatTile<HD>;
     constexpr int D = HD / 16;
     int tile, h, s0, q0, len;
-    window_work(a, tile, h);
-    if (!tile_of(a, tile, s0, q0, len)) return;
+    if (!window_work(a, tile, h) || !tile_of(a, tile, s0, q0, len)) return;
     const int kh = h / (a.n_q_heads / a.n_kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     const int w0 = q0 + wave * 16;
@@ -321,14 +324,14 @@ __global__ __launch_bounds__(512) void k_window_float(WindowArgs a) {
 template <typename T>
 static hipError_t window_typed(hipStream_t st, int head_dim, const WindowArgs& a) {
     constexpr int THREADS = sizeof(T) == 4 ? 512 : 256;
-    const int most = (int)std::min<int64_t>(kLaunchThreads / THREADS / a.n_q_heads, 1 << 30);
+    const int most = (int)std::min<int64_t>((kLaunchThreads / THREADS - 8 * a.n_q_heads) / a.n_q_heads, 1 << 30);
     for (int first = 0; first < a.n_tiles; first += most) {
         WindowArgs p = a;
         p.tile_start += first;
         p.tile_q0 += first;
         p.tile_len += first;
         p.n_tiles = std::min(most, a.n_tiles - first);
-        const unsigned blocks = (unsigned)p.n_tiles * (unsigned)a.n_q_heads;
+        const unsigned blocks = ((unsigned)p.n_tiles * (unsigned)a.n_kv_heads + 7) / 8 * 8 * (unsigned)(a.n_q_heads / a.n_kv_heads);
         if constexpr (sizeof(T) == 4) {
             if (head_dim == 128) k_window_float<128><<<blocks, 512, 0, st>>>(p);
             else k_window_float<64><<<blocks, 512, 0, st>>>(p);
