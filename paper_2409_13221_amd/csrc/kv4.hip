@@ -45,6 +45,13 @@ __device__ __forceinline__ float settle(float q, float u, float x, float s, floa
     return on ? u + side : u;
 }
 
+// A float, rounded as one, to half.  The compiler makes one instruction of a multiply-add and this conversion, which rounds once where the
+// definition rounds twice (one group in some thousands had another scale).
+__device__ __forceinline__ f16_t half_of_float(float x) {
+    asm volatile("" : "+v"(x));
+    return (f16_t)x;
+}
+
 // Codes of a thread's 8 values (4 bits each), scale and center of its group.  In float a quotient of up to 8.5 is off by 8.5 x 2^-22 by the difference, the
 // reciprocal and the product; those within 2^-17 of half way between two steps are settled exactly.  Rounding to the nearest whole
 // number is the addition of 1.5 x 2^23 (and 8, for the code), whose low bits are then the code.
@@ -58,7 +65,7 @@ __device__ __forceinline__ uint32_t kv4_pack(const float (&x)[8], uint32_t& para
     lo = over_group(lo, [](float a, float b) { return __builtin_elementwise_minimum(a, b); });
     hi = over_group(hi, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
     const bool bad = !(lo >= -65504.f) || !(hi <= 65504.f);
-    const f16_t s = bad ? (f16_t)NAN : (f16_t)((hi - lo) * (1.f / 15.f)), c = bad ? (f16_t)NAN : (f16_t)(lo + 8.f * (float)s);
+    const f16_t s = bad ? (f16_t)NAN : half_of_float((hi - lo) * (1.f / 15.f)), c = bad ? (f16_t)NAN : half_of_float(lo + 8.f * (float)s);
     params = (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, c) << 16;
     const float inv = (float)s == 0.f ? 0.f : __builtin_amdgcn_rcpf((float)s);
     constexpr float ZERO = 12582912.f;             // 1.5 x 2^23, code 0

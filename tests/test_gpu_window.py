@@ -521,6 +521,31 @@ def test_codes_of_many_values(dtype):
         np.testing.assert_array_equal(_np(got), W.kv4_round(t.float().numpy()).astype(np.float32))
 
 
+def test_scale_and_center_are_rounded_to_float_and_then_to_half():
+    """Groups whose scale or center would be another half if it were rounded once."""
+    R, r, hd = _R(), np.random.default_rng(8), 64
+    lo = (-r.uniform(1, 4, 400000)).astype(np.float32)
+    hi = r.uniform(1, 4, 400000).astype(np.float32)
+    third = np.float32(np.float32(1) / np.float32(15))
+    f = (hi - lo) * third
+    s = f.astype(np.float16)
+    once = ((hi - lo).astype(np.float64) * np.float64(third)).astype(np.float16) != s
+    c = (lo + np.float32(8) * s.astype(np.float32)).astype(np.float16)
+    once |= (lo.astype(np.float64) + 8 * s.astype(np.float64)).astype(np.float16) != c
+    lo, hi = lo[once], hi[once]
+    assert len(lo) >= 16
+    rows = len(lo) // 16 * 16
+    x = r.uniform(-1, 1, (rows, hd)).astype(np.float32)
+    x[:, 5], x[:, 40] = lo[:rows], hi[:rows]
+    pool = torch.zeros(rows // 16, 1, 1, 18 * hd, dtype=torch.uint8, device="cuda")
+    t = torch.from_numpy(x).cuda()
+    R.rlhf_op_kv4_append(t, -t, _ints(list(range(rows))), pool, 0, 1, 1, hd)
+    out = [torch.empty(rows, hd, device="cuda") for _ in range(2)]
+    R.rlhf_op_kv4_read(pool, _ints(list(range(rows))), *out, 0, 1, 1, hd)
+    np.testing.assert_array_equal(_np(out[0]), W.kv4_round(x).astype(np.float32))
+    np.testing.assert_array_equal(_np(out[1]), W.kv4_round(-x).astype(np.float32))
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
 def test_read(dtype):
     """Any slots, some twice, into strided rows; zeros for a negative slot, NaN beyond the pool; one rounding."""
