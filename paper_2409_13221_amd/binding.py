@@ -364,9 +364,21 @@ def _dt(t) -> int:
     return RLHF_BF16 if t.dtype == torch.bfloat16 else RLHF_FP32
 
 
+_torch = None
+
+
+def _th():
+    """torch, imported by the first call that needs it (an import statement costs 0.3 us each time it is met)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _stream_ptr():
     """The current stream of the current device, without a Stream object around it (2.8 us of host time a call)."""
-    import torch
+    torch = _th()
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
@@ -497,9 +509,14 @@ def rlhf_op_gemm_rope(A, W_qkv, pos, table, q, k=None, v=None, pool=None, kv_dst
               "rlhf_op_gemm_rope")
 
 
+_act_codes = {}
+
+
 def _act_code(t) -> int:
-    import torch
-    return {torch.float32: RLHF_FP32, torch.bfloat16: RLHF_BF16, torch.float16: 2}[t.dtype]
+    if not _act_codes:
+        torch = _th()
+        _act_codes.update({torch.float32: RLHF_FP32, torch.bfloat16: RLHF_BF16, torch.float16: 2})
+    return _act_codes[t.dtype]
 
 
 def _ptr(t):
@@ -602,7 +619,7 @@ def rlhf_op_gemm_tall_tile(bid: int, tiles_m: int, tiles_n: int):
 
 def _on_device(*tensors) -> None:
     """Kernels are launched on the current device's current stream: every tensor has to be there."""
-    import torch
+    torch = _th()
     dev = None
     for t in tensors:
         if t is None:
@@ -626,7 +643,7 @@ def _vector(t, n: int, dtype, what: str):
 
 def _matrix(t, rows: int, cols: int, what: str) -> int:
     """Row stride of a [rows, cols] matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+    if t.dim() != 2 or t.size(0) != rows or t.size(1) != cols or (cols > 1 and t.stride(1) != 1):
         raise ValueError(f"{what} must be [{rows}, {cols}] with contiguous rows")
     ld = t.stride(0) if rows > 1 else cols
     if ld < cols:
@@ -679,8 +696,8 @@ def rlhf_op_window_attention(q, k, v, tiles: rlhf_attention_tiles, out, window: 
 
 def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out, layer, n_layers, n_q_heads, n_kv_heads, head_dim, window, sinks,
                    max_ctx, nsplit, scratch):
-    import torch
-    rows, qc = q.shape[0], n_q_heads * head_dim
+    torch = _th()
+    rows, qc = q.size(0), n_q_heads * head_dim
     if q.dtype != out.dtype:
         raise ValueError("q and out must be of one type")
     _on_device(q, pool, page_table, row_sample, ctx_len, out, scratch)
@@ -720,7 +737,7 @@ def rlhf_op_window_decode_attention(q, pool, page_table, row_sample, ctx_len, ou
 
 
 def _kv4_pages(pool, n_layers: int, n_kv_heads: int, head_dim: int) -> int:
-    import torch
+    torch = _th()
     page = lib().rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim)
     if page == 0 or pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() % page:
         raise ValueError(f"pool must be whole contiguous pages of {page} bytes (uint8)")
@@ -734,7 +751,7 @@ def rlhf_op_kv4_page_bytes(n_layers: int, n_kv_heads: int, head_dim: int) -> int
 
 def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
     """Rows of k, v [rows, n_kv_heads*head_dim] into token slots kv_dst (int32, distinct; outside the pool: left out) of the cache of 4 bits."""
-    import torch
+    torch = _th()
     rows, cols = kv_dst.numel(), n_kv_heads * head_dim
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
@@ -747,7 +764,7 @@ def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads
 
 def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
     """Token slots kv_src (int32) of the cache of 4 bits into rows of k, v (zeros for a negative slot, NaN beyond the pool)."""
-    import torch
+    torch = _th()
     rows, cols = kv_src.numel(), n_kv_heads * head_dim
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")

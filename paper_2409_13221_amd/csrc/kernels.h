@@ -315,7 +315,7 @@ struct WindowDecodeArgs {
     const void* pool;
     const int *page_table, *row_sample, *ctx_len;
     void* out;
-    float* part;                    // [rows][n_q_heads][nsplit]: (max, sum), then [..][head_dim] accumulators; nsplit > 1
+    float* part;                    // [rows][n_q_heads][nsplit][head_dim] sums, then a (reference, weight) pair for each; nsplit > 1
     size_t ld_q, ld_out;
     int rows, layer, n_layers, n_q_heads, n_kv_heads, nsplit, window, sinks, n_pages, n_samples, pt_stride;
 };

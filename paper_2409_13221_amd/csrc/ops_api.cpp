@@ -459,12 +459,12 @@ static int window_decode(bool four_bits, int act_dtype, const void* q, int64_t l
                          int n_kv_heads, int head_dim, void* stream) {
     const int dt = act_of(act_dtype);
     if (dt < 0 || rows < 0 || rows > 1 << 24 || nsplit < 1 || nsplit > 64 || window < 1 || sinks < 0 || layer < 0 || layer >= n_layers || n_layers > 1 << 16 ||
-        n_pages < 1 || n_pages >= 1 << 27 || n_samples < 1 || pt_stride < 1 || pt_stride >= 1 << 27 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
+        n_pages < 0 || n_pages >= 1 << 27 || n_samples < 0 || pt_stride < 0 || pt_stride >= 1 << 27 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
         return RLHF_EINVAL;
     const int qc = n_q_heads * head_dim;
     if (ld_q < qc || ld_out < qc) return RLHF_EINVAL;
     if (rows == 0) return RLHF_OK;
-    if (!pool || !aligned(pool, 16) || !page_table || !row_sample || !ctx_len || !in_pieces(q, ld_q, dt) || !in_pieces(out, ld_out, dt) ||
+    if (n_pages < 1 || n_samples < 1 || pt_stride < 1 || !pool || !aligned(pool, 16) || !page_table || !row_sample || !ctx_len || !in_pieces(q, ld_q, dt) || !in_pieces(out, ld_out, dt) ||
         (nsplit > 1 && (!scratch || !aligned(scratch, 16))))
         return RLHF_EINVAL;
     const size_t page = four_bits ? (size_t)rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim)
@@ -505,7 +505,7 @@ extern "C" int64_t rlhf_op_kv4_page_bytes(int n_layers, int n_kv_heads, int head
 // Checks what append and read share; a row is n_kv_heads * head_dim elements.
 static bool kv4_args(int dt, const void* k, int64_t ld_k, const void* v, int64_t ld_v, const int32_t* slot, const void* pool, int n_pages,
                      int rows, int layer, int n_layers, int n_kv_heads, int head_dim, bool writes_rows, Kv4Args* a) {
-    if (dt < 0 || rows < 0 || rows > 1 << 30 || n_pages < 1 || n_pages >= 1 << 27 || layer < 0 || layer >= n_layers || n_layers > 1 << 16 ||
+    if (dt < 0 || rows < 0 || rows > 1 << 30 || n_pages < 0 || n_pages >= 1 << 27 || layer < 0 || layer >= n_layers || n_layers > 1 << 16 ||
         !heads_ok(n_kv_heads, n_kv_heads, head_dim) || ld_k < (int64_t)n_kv_heads * head_dim || ld_v < (int64_t)n_kv_heads * head_dim)
         return false;
     if (rows > 0) {
@@ -513,7 +513,7 @@ static bool kv4_args(int dt, const void* k, int64_t ld_k, const void* v, int64_t
         const Matrix mk = matrix(k, rows, cols, ld_k, dt), mv = matrix(v, rows, cols, ld_v, dt);
         const size_t page = (size_t)rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim);
         const Matrix mp = bytes_of(pool, page * n_pages);
-        if (page > kMaxPoolBytes / n_pages || !slot || !pool || !aligned(pool, 16) || !in_pieces(k, ld_k, dt) || !in_pieces(v, ld_v, dt) || overlap(mk, mp) || overlap(mv, mp) ||
+        if (n_pages < 1 || page > kMaxPoolBytes / n_pages || !slot || !pool || !aligned(pool, 16) || !in_pieces(k, ld_k, dt) || !in_pieces(v, ld_v, dt) || overlap(mk, mp) || overlap(mv, mp) ||
             (writes_rows && overlap(mk, mv)))
             return false;
     }

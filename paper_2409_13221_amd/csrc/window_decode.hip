@@ -73,8 +73,8 @@ __device__ __forceinline__ void join_waves(const WindowDecodeArgs& a, const Deco
             for (int e = 0; e < 4; ++e) out[e] = round_to<T>(ctx == 0 ? 0.f : x[e] / sum);
         } else {
             const size_t slot = ((size_t)w.r * a.n_q_heads + w.h0 + h) * a.nsplit + w.split;
-            if (d == 0) { a.part[2 * slot] = top; a.part[2 * slot + 1] = sum; }
-            *(f32x4_t*)(a.part + 2 * slots + slot * HD + d) = x;
+            if (d == 0) ((float2*)(a.part + slots * HD))[slot] = make_float2(top, sum);
+            *(f32x4_t*)(a.part + slot * HD + d) = x;
         }
     }
 }
@@ -620,14 +620,14 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) 
     const int t = threadIdx.x, g = t / LANES, d = t % LANES * 4, h = blockIdx.x % a.n_q_heads, r = blockIdx.x / a.n_q_heads;
     const size_t slot = (size_t)blockIdx.x * a.nsplit, slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
     if (t < 64) {                                                      // nsplit <= 64
-        const float2 ml = t < a.nsplit ? ((const float2*)a.part)[slot + t] : make_float2(-INFINITY, 0.f);
+        const float2 ml = t < a.nsplit ? ((const float2*)(a.part + slots * HD))[slot + t] : make_float2(-INFINITY, 0.f);
         const float m = wave_max(ml.x), w = __builtin_amdgcn_exp2f(ml.x - (m == -INFINITY ? 0.f : m)), l = wave_sum(w * ml.y);
         s_w[t] = w;
         if (t == 0) s_l = l;
     }
     __syncthreads();
     f32x4_t x{0.f, 0.f, 0.f, 0.f};
-    for (int s = g; s < a.nsplit; s += GROUPS) x += s_w[s] * *(const f32x4_t*)(a.part + 2 * slots + (slot + s) * HD + d);
+    for (int s = g; s < a.nsplit; s += GROUPS) x += s_w[s] * *(const f32x4_t*)(a.part + (slot + s) * HD + d);
     s_x[g][d / 4] = x;
     __syncthreads();
     if (t >= LANES) return;

@@ -40,8 +40,8 @@ DECODE = dict(dtype=0, q=A, ld_q=512, pool=B, n_pages=50, table=C, pt_stride=9, 
 @pytest.mark.parametrize("name", ["rlhf_op_window_decode_attention", "rlhf_op_kv4_decode_attention"])
 @pytest.mark.parametrize("bad", [
     dict(dtype=3), dict(dtype=-1), dict(q=None), dict(pool=None), dict(table=None), dict(row=None), dict(ctx=None), dict(out=None), dict(scratch=None),
-    dict(scratch=E + 4), dict(ld_q=508), dict(ld_out=500), dict(ld_q=513), dict(q=A + 4), dict(out=D + 8), dict(pool=B + 8), dict(n_pages=0), dict(n_pages=1 << 27),
-    dict(pt_stride=0), dict(pt_stride=1 << 27), dict(n_samples=0), dict(rows=-1), dict(rows=(1 << 24) + 1), dict(layer=-1), dict(layer=2), dict(nsplit=0),
+    dict(scratch=E + 4), dict(ld_q=508), dict(ld_out=500), dict(ld_q=513), dict(q=A + 4), dict(out=D + 8), dict(pool=B + 8), dict(n_pages=0), dict(n_pages=-1), dict(n_pages=1 << 27),
+    dict(pt_stride=0), dict(pt_stride=-1), dict(pt_stride=1 << 27), dict(n_samples=0), dict(n_samples=-1), dict(rows=-1), dict(rows=(1 << 24) + 1), dict(layer=-1), dict(layer=2), dict(nsplit=0),
     dict(nsplit=65), dict(window=0), dict(sinks=-1), dict(hq=3), dict(hkv=0), dict(hd=80), dict(out=A), dict(out=A + 512 * 4), dict(out=B + 16),
     dict(n_layers=1 << 17), dict(n_layers=1 << 16, hq=1 << 14, hkv=1 << 14, ld_q=1 << 21, ld_out=1 << 21, n_pages=1 << 26),
 ], ids=str)
@@ -53,7 +53,7 @@ def test_decode(name, bad):
 @pytest.mark.parametrize("name", ["rlhf_op_window_decode_attention", "rlhf_op_kv4_decode_attention"])
 def test_decode_of_no_rows(name):
     R = _R()
-    assert getattr(R.lib(), name)(*dict(DECODE, rows=0, q=None, pool=None, out=None).values()) == R.RLHF_OK
+    assert getattr(R.lib(), name)(*dict(DECODE, rows=0, n_pages=0, pt_stride=0, n_samples=0, q=None, pool=None, out=None).values()) == R.RLHF_OK
 
 
 APPEND = dict(dtype=0, k=A, ld_k=256, v=B, ld_v=256, slot=C, pool=D, n_pages=50, rows=8, layer=1, n_layers=2, hkv=2, hd=128, stream=None)
@@ -63,7 +63,7 @@ READ = dict(dtype=0, pool=D, n_pages=50, slot=C, k=A, ld_k=256, v=B, ld_v=256, r
 @pytest.mark.parametrize("call", ["append", "read"])
 @pytest.mark.parametrize("bad", [
     dict(dtype=3), dict(dtype=-1), dict(k=None), dict(v=None), dict(slot=None), dict(pool=None), dict(ld_k=252), dict(ld_v=252), dict(ld_k=257), dict(k=A + 4),
-    dict(v=B + 8), dict(pool=D + 8), dict(n_pages=0), dict(n_pages=1 << 27), dict(rows=-1), dict(rows=BIG + 1), dict(layer=-1), dict(layer=2), dict(hkv=0),
+    dict(v=B + 8), dict(pool=D + 8), dict(n_pages=0), dict(n_pages=-1), dict(n_pages=1 << 27), dict(rows=-1), dict(rows=BIG + 1), dict(layer=-1), dict(layer=2), dict(hkv=0),
     dict(hd=32), dict(hd=100), dict(k=D + 16), dict(v=D - 1024), dict(n_layers=1 << 17),
     dict(n_layers=1 << 16, hkv=1 << 14, ld_k=1 << 21, ld_v=1 << 21, n_pages=1 << 26),
 ], ids=str)
@@ -82,7 +82,7 @@ def test_kv4_read_into_rows_that_overlap():
 def test_kv4_of_no_rows(call):
     R = _R()
     base = APPEND if call == "append" else READ
-    assert getattr(R.lib(), f"rlhf_op_kv4_{call}")(*dict(base, rows=0, k=None, v=None, slot=None, pool=None).values()) == R.RLHF_OK
+    assert getattr(R.lib(), f"rlhf_op_kv4_{call}")(*dict(base, rows=0, n_pages=0, k=None, v=None, slot=None, pool=None).values()) == R.RLHF_OK
 
 
 def test_sizes():
