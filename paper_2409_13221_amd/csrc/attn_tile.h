@@ -43,8 +43,8 @@ template <> struct Matrix16<bf16_t> {
     }
 };
 
-// Float: k = 4 products.  A lane has 4 dims of key n (K) and D = HD / 16 dims of its four keys (V), D n .. D n + D - 1, so that a row of V is read by 16 lanes
-// side by side; sums o[d] hold dim D (4c + r) + d in element r.
+// Float: k = 4 products.  A lane has 4 dims of key n (K) and dims 64 i + 4 n .. + 3 of its four keys (V), so that 16 lanes side by side read 256 bytes of a row;
+// element r of sums o[4 i + e] is dim 64 i + 4 (4c + r) + e.
 template <int HD> struct FloatQuery {
     f32x4_t q[HD / 16];
     __device__ __forceinline__ void load(const float* p, int c) {
@@ -52,41 +52,20 @@ template <int HD> struct FloatQuery {
         for (int s = 0; s < HD / 16; ++s) q[s] = *(const f32x4_t*)(p + s * 16 + c * 4);
     }
 };
-template <int HD> struct FloatTile {
-    static constexpr int D = HD / 16;
-    f32x4_t k[D], v[4][D / 4];
-    // Rows 0 .. last of K and V; those behind it are the last one again.
-    template <bool ONCE> __device__ __forceinline__ void load(const float* pk, size_t ldk, const float* pv, size_t ldv, int last, int n, int c) {
-        const auto get = [](const float* p) { return ONCE ? __builtin_nontemporal_load((const f32x4_t*)p) : *(const f32x4_t*)p; };
-        pk += min(n, last) * ldk + c * 4;
+// Four dims at a time: put(dim, values).
+template <int HD, typename F> __device__ __forceinline__ void each_dims(const f32x4_t (&o)[HD / 16], int c, F put) {
 #pragma unroll
-        for (int s = 0; s < D; ++s) k[s] = get(pk + s * 16);
+    for (int i = 0; i < HD / 64; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int r = 0; r < 4; ++r) put(64 * i + 16 * c + 4 * r, f32x4_t{o[4 * i][r], o[4 * i + 1][r], o[4 * i + 2][r], o[4 * i + 3][r]});
+}
+__device__ __forceinline__ void float_scores(const f32x4_t& k, const f32x4_t& q, f32x4_t& s) {
 #pragma unroll
-            for (int d = 0; d < D / 4; ++d) v[i][d] = get(pv + min(4 * c + i, last) * ldv + n * D + d * 4);
-    }
-    __device__ __forceinline__ f32x4_t scores(const FloatQuery<HD>& q) const {
-        f32x4_t s{0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[e], s, 0, 0, 0);
+}
+__device__ __forceinline__ void float_sums(const f32x4_t& v, float p, f32x4_t* o) {
 #pragma unroll
-        for (int i = 0; i < D; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q.q[i][e], s, 0, 0, 0);
-        return s;
-    }
-    __device__ __forceinline__ void add(const f32x4_t& p, f32x4_t (&o)[D]) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int d = 0; d < D; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][d / 4][d % 4], p[i], o[d], 0, 0, 0);
-    }
-    // Four dims at a time, in order: put(dim, values).
-    template <typename F> static __device__ __forceinline__ void each(const f32x4_t (&o)[D], int c, F put) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int d = 0; d < D; d += 4) put((4 * c + r) * D + d, f32x4_t{o[d][r], o[d + 1][r], o[d + 2][r], o[d + 3][r]});
-    }
-};
+    for (int e = 0; e < 4; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], p, o[e], 0, 0, 0);
+}
 
 }  // namespace rlhf

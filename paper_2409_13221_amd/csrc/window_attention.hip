@@ -248,70 +248,77 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
         for (int i = w0; i < min(w0 + 32, len); ++i) window_row<T, HD>(a, s0, i, h, lane);
 }
 
-// Float: 16 queries a wave, 16 keys at a time from the L2 straight into the matrix units' registers, the next ones in flight; bound by the
-// float matrix rate (a 64th of the half one a lane).  What is hidden is kept out as above.
+// Float: 128 queries of a head a workgroup, 16 a wave, against 16 keys at a time, which go to LDS a tile ahead; bound by the float matrix rate (a sixteenth
+// of the half one).  What is hidden is kept out as above.
 template <int HD>
-__global__ __launch_bounds__(512) void k_window_float(WindowArgs a) {
-    using Tile = FloatTile<HD>;
-    constexpr int D = HD / 16;
+__global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
+    constexpr int KT = 16, D = HD / 16, CH = HD / 4, ROWS = 64 / CH, WAVES_EACH = KT / ROWS, TILE = KT * HD;       // WAVES_EACH: waves that load a tile of K
+    __shared__ __attribute__((aligned(16))) float sK[2][TILE], sV[2][TILE];
     int tile, h, s0, q0, len;
     if (!window_work(a, tile, h) || !tile_of(a, tile, s0, q0, len)) return;
     const int kh = h / (a.n_q_heads / a.n_kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     const int w0 = q0 + wave * 16;
-    if (w0 >= len) return;
     const float* kb = (const float*)a.k + (size_t)s0 * a.ld_k + (size_t)kh * HD;
     const float* vb = (const float*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
     const float unit = rsqrtf((float)HD) * 1.44269504088896f;
+    // Place p of row t of K holds 16-byte piece p ^ t, so that a piece of 16 rows spreads over the banks; V lies as it is.  Of 64 dims half the waves load K, the
+    // other half V.
+    const int lw = wave % WAVES_EACH, lrow = lw * ROWS + lane / CH, place = lane % CH;
+    const bool loads_k = wave < WAVES_EACH, loads_v = WAVES_EACH == 8 || !loads_k;
+    const auto fetch = [&](int kt, int buf) {
+        const uint32_t row = min(lrow, len - 1 - kt * KT);           // rows behind the sequence: its last one
+        if (loads_k)
+            load_to_lds(buffer_base(kb + (size_t)kt * KT * a.ld_k), row * (uint32_t)a.ld_k * 4 + (place ^ lrow) * 16, 0, lds_address(&sK[buf][lw * ROWS * HD]));
+        if (loads_v) load_to_lds(buffer_base(vb + (size_t)kt * KT * a.ld_v), row * (uint32_t)a.ld_v * 4 + place * 16, 0, lds_address(&sV[buf][lw * ROWS * HD]));
+    };
+    const KeyTiles<KT> keys(q0, min(q0 + kFlashTile, len) - 1, a.window, a.sinks);
+    fetch(keys.at(0), 0);
     FloatQuery<HD> q;
     q.load((const float*)a.q + (size_t)(s0 + min(w0 + n, len - 1)) * a.ld_q + (size_t)h * HD, c);
+#pragma unroll
+    for (int s = 0; s < D; ++s) asm volatile("" : "+v"(q.q[s]));
     f32x4_t o[D];
 #pragma unroll
     for (int d = 0; d < D; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float ref = -INFINITY, l = 0.f;
-    const KeyTiles<16> keys(w0, min(w0 + 16, len) - 1, a.window, a.sinks);
-    const auto fetch = [&](Tile& t, int j) {
-        const int kt = keys.at(j);
-        t.template load<false>(kb + (size_t)kt * 16 * a.ld_k, a.ld_k, vb + (size_t)kt * 16 * a.ld_v, a.ld_v, min(15, len - 1 - kt * 16), n, c);
-    };
-    const auto step = [&](const Tile& t, int j) {
-        const int first = keys.at(j) * 16;
-        f32x4_t s = t.scores(q);
-        if (first + 15 > w0 || !(first > w0 + 15 - a.window || first + 15 < a.sinks)) {
+    constexpr float MOST = 20.f;
+    float ref = -1e30f, l = 0.f;
+    for (int j = 0; j < keys.n; ++j) {
+        const int buf = j & 1, first = keys.at(j) * KT, last = first + KT - 1;
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        __syncthreads();                           // tile j is there, and nobody reads tile j - 1 any more
+        if (j + 1 < keys.n) fetch(keys.at(j + 1), buf ^ 1);
+        if (w0 >= len || first > w0 + 15 || (last <= w0 - a.window && first >= a.sinks)) continue;      // nothing that this wave sees
+        f32x4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D; ++i) float_scores(*(const f32x4_t*)&sK[buf][n * HD + (((4 * i + c) ^ n) << 2)], q.q[i], s);
+        if (last > w0 || !(first > w0 + 15 - a.window || last < a.sinks)) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 if (!window_sees(a, w0 + n, first + 4 * c + r)) s[r] = -INFINITY;
         }
-        const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * unit;
-        if (__any(top > ref)) {
-            const float now = fmaxf(top, ref), keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+        const float top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[0], s[1]), __builtin_elementwise_maximum(s[2], s[3])) * unit;
+        if (__any(top > ref + MOST)) {
+            const float high = column_max(top), now = high > ref + MOST ? high : ref, keep = __builtin_amdgcn_exp2f(ref - now);
             ref = now;
             l *= keep;
 #pragma unroll
             for (int d = 0; d < D; ++d) o[d] *= keep;
         }
-        const float at = ref == -INFINITY ? 0.f : ref;
         f32x4_t p;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -at));
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -ref));
         l += (p[0] + p[1]) + (p[2] + p[3]);
-        t.add(p, o);
-    };
-    Tile t0, t1;
-    fetch(t0, 0);
-    for (int j = 0; j < keys.n; j += 2) {
-        if (j + 1 < keys.n) fetch(t1, j + 1);
-        step(t0, j);
-        if (j + 1 < keys.n) {
-            if (j + 2 < keys.n) fetch(t0, j + 2);
-            step(t1, j + 1);
-        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int d = 0; d < HD / 64; ++d) float_sums(*(const f32x4_t*)&sV[buf][(4 * c + i) * HD + 64 * d + 4 * n], p[i], o + 4 * d);
     }
     const float inv = 1.f / column_sum(l);
     float odd = 0.f;
     if (w0 + n < len) {
         float* out = (float*)a.out + (size_t)(s0 + w0 + n) * a.ld_out + (size_t)h * HD;
-        Tile::each(o, c, [&](int d, f32x4_t x) {
+        each_dims<HD>(o, c, [&](int d, f32x4_t x) {
             x *= inv;
             odd += 0.f * ((x[0] + x[1]) + (x[2] + x[3]));
             *(f32x4_t*)(out + d) = x;

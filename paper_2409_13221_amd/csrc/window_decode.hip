@@ -102,7 +102,7 @@ struct LaneOffsets {
     }
 };
 template <typename T, int HD> __device__ __forceinline__ LaneOffsets plain_offsets(int n, int c) {
-    return LaneOffsets{(n * HD + c * (16 / (uint32_t)sizeof(T))) * (uint32_t)sizeof(T), (4 * c * HD + n * (HD / 16)) * (uint32_t)sizeof(T)};
+    return LaneOffsets{(n * HD + c * (16 / (uint32_t)sizeof(T))) * (uint32_t)sizeof(T), (4 * c * HD + n * (sizeof(T) == 4 ? 4 : HD / 16)) * (uint32_t)sizeof(T)};
 }
 // Where the pages of a layer and KV head lie: page i at first + i * stride, V `plane` bytes behind K, `size` bytes in all.
 struct Pages {
@@ -145,7 +145,12 @@ template <typename T_, int HD_> struct Cache16 {
             for (int d = 0; d < D; ++d) acc[d] *= f;
         }
         // Four dims at a time: put(dim, values).
-        template <typename F> __device__ __forceinline__ void each(int c, F put) const { FloatTile<HD>::each(acc, c, put); }
+        template <typename F> __device__ __forceinline__ void each(int c, F put) const {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int d = 0; d < D; d += 4) put((4 * c + r) * D + d, f32x4_t{acc[d][r], acc[d + 1][r], acc[d + 2][r], acc[d + 3][r]});
+        }
     };
     struct Tile {
         u32x4_t k[KS];
@@ -184,28 +189,41 @@ template <typename T_, int HD_> struct Cache16 {
 
 template <int HD_> struct CacheFloat {
     using T = float;
-    static constexpr int HD = HD_, SIMD_WAVES = HD == 64 ? 4 : 2;
+    static constexpr int HD = HD_, D = HD / 16, SIMD_WAVES = HD == 64 ? 4 : 2;
     static constexpr float START = 0.f, MOST = 20.f;
     using Query = FloatQuery<HD>;
     static __device__ __forceinline__ LaneOffsets offsets(int n, int c) { return plain_offsets<float, HD>(n, c); }
     static __device__ __forceinline__ Pages pages(const WindowDecodeArgs& a, int kh) { return plain_pages<float, HD>(a, kh); }
-    using Sums = typename Cache16<f16_t, HD>::Sums;
-    struct Tile : FloatTile<HD> {
+    struct Sums : Cache16<f16_t, HD>::Sums {
+        template <typename F> __device__ __forceinline__ void each(int c, F put) const { each_dims<HD>(this->acc, c, put); }
+    };
+    struct Tile {
+        f32x4_t k[D], v[4][HD / 64];
         __device__ __forceinline__ void load(const Pages& pages, int page, bool there, const LaneOffsets& lane) {
             const PageBuffer b = pages.at(page, there);
-            constexpr int D = HD / 16;
 #pragma unroll
-            for (int s = 0; s < D; ++s) this->k[s] = b.get<f32x4_t>(lane.k, s * 64);
+            for (int s = 0; s < D; ++s) k[s] = b.get<f32x4_t>(lane.k, s * 64);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int d = 0; d < D / 4; ++d) this->v[i][d] = b.get<f32x4_t>(lane.v, (i * HD + d * 4) * 4, pages.plane);
+                for (int d = 0; d < HD / 64; ++d) v[i][d] = b.get<f32x4_t>(lane.v, (i * HD + d * 64) * 4, pages.plane);
+        }
+        __device__ __forceinline__ f32x4_t scores(const Query& q) const {
+            f32x4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D; ++i) float_scores(k[i], q.q[i], s);
+            return s;
         }
         __device__ __forceinline__ void hide(int i) {
 #pragma unroll
-            for (int d = 0; d < HD / 64; ++d) this->v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int d = 0; d < HD / 64; ++d) v[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const { FloatTile<HD>::add(p, o.acc); }
+        __device__ __forceinline__ void add(const f32x4_t& p, Sums& o) const {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < HD / 64; ++d) float_sums(v[i][d], p[i], o.acc + 4 * d);
+        }
     };
 };
 
