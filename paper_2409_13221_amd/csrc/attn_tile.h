@@ -10,6 +10,9 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
+// log2 of a weight by a score: log2(e) / sqrt(HD).
+template <int HD> constexpr float kScoreUnit = 1.44269504088896f * (HD == 64 ? 0.125f : 0.0883883476483184f);
+
 // Greatest of (sum over) the four lanes that hold a column.
 __device__ __forceinline__ float column_max(float x) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

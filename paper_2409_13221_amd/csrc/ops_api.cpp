@@ -429,7 +429,7 @@ extern "C" int rlhf_op_window_attention(int act_dtype, const void* q, int64_t ld
     if (dt < 0 || n_tiles < 0 || rows < 0 || rows > 1 << 30 || window < 1 || sinks < 0 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
         return RLHF_EINVAL;
     const int qc = n_q_heads * head_dim, kc = n_kv_heads * head_dim;
-    if (ld_q < qc || ld_out < qc || ld_k < kc || ld_v < kc || ld_k >= 1 << 25 || ld_v >= 1 << 25) return RLHF_EINVAL;     // 64 rows of K in 32 bits
+    if (ld_q < qc || ld_out < qc || ld_k < kc || ld_v < kc || ld_k >= 1 << 25 || ld_v >= 1 << 25) return RLHF_EINVAL;     // the rows of a tile of keys in 32 bits
     if (n_tiles == 0 || rows == 0) return RLHF_OK;
     if (!tile_start || !tile_q0 || !tile_len || !in_pieces(q, ld_q, dt) || !in_pieces(k, ld_k, dt) || !in_pieces(v, ld_v, dt) || !in_pieces(out, ld_out, dt))
         return RLHF_EINVAL;

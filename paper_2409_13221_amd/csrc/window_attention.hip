@@ -94,6 +94,10 @@ __device__ __forceinline__ u32x4_t buffer_base(const void* p) {
 }
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 
+// References beyond this (log2) are off by more than a factor of 2 from the score that they were taken from, and weights then leave the range of
+// their type: such queries are taken again, too.
+constexpr float kFarthest = 0x1p24f;
+
 // 16-bit types: 128 queries of a head a workgroup, 32 a wave, against 64 keys at a time.  K and V go from memory to LDS directly, one tile ahead;
 // V is transposed as it is read from LDS.  References of the weights follow the running maximum only where these would leave their
 // range, so that most tiles do not rescale the sums.  A key that is hidden from a query has weight 0, and 0 times what is not a number is none: a
@@ -108,7 +112,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     if (!window_work(a, tile, h) || !tile_of(a, tile, s0, q0, len)) return;
     const int kh = h / (a.n_q_heads / a.n_kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
-    const float unit = rsqrtf((float)HD) * 1.44269504088896f;
+    constexpr float unit = kScoreUnit<HD>;
     const T* kb = (const T*)a.k + (size_t)s0 * a.ld_k + (size_t)kh * HD;
     const T* vb = (const T*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
     const uint32_t ldk = (uint32_t)a.ld_k * 2, ldv = (uint32_t)a.ld_v * 2;
@@ -154,6 +158,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) o[d][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float ref[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
+    bool far = false;
     const int vt = 4 * c + (n >> 2);               // token (modulo 16) and 32-byte pair of pieces of a lane's reads of V
     const int vswap = CH == 16 ? vt & 7 : (vt >> 1) & 3;
 
@@ -200,6 +205,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 const float high = column_max(top[m]), now = high > ref[m] + MOST ? high - START : ref[m], keep = __builtin_amdgcn_exp2f(ref[m] - now);
+                far |= __any(now != ref[m] && fabsf(now) > kFarthest);
                 ref[m] = now;
                 l[m] *= keep;
 #pragma unroll
@@ -244,7 +250,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
             *(u32x2_t*)(out + d * 16) = u32x2_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
         }
     }
-    if (__any(odd != 0.f))
+    if (far || __any(odd != 0.f))
         for (int i = w0; i < min(w0 + 32, len); ++i) window_row<T, HD>(a, s0, i, h, lane);
 }
 
@@ -261,7 +267,7 @@ __global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
     const int w0 = q0 + wave * 16;
     const float* kb = (const float*)a.k + (size_t)s0 * a.ld_k + (size_t)kh * HD;
     const float* vb = (const float*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
-    const float unit = rsqrtf((float)HD) * 1.44269504088896f;
+    constexpr float unit = kScoreUnit<HD>;
     // Place p of row t of K holds 16-byte piece p ^ t, so that a piece of 16 rows spreads over the banks; V lies as it is.  Of 64 dims half the waves load K, the
     // other half V.
     const int lw = wave % WAVES_EACH, lrow = lw * ROWS + lane / CH, place = lane % CH;
@@ -283,6 +289,7 @@ __global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
     for (int d = 0; d < D; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     constexpr float MOST = 20.f;
     float ref = -1e30f, l = 0.f;
+    bool far = false;
     for (int j = 0; j < keys.n; ++j) {
         const int buf = j & 1, first = keys.at(j) * KT, last = first + KT - 1;
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
@@ -300,6 +307,7 @@ __global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
         const float top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[0], s[1]), __builtin_elementwise_maximum(s[2], s[3])) * unit;
         if (__any(top > ref + MOST)) {
             const float high = column_max(top), now = high > ref + MOST ? high : ref, keep = __builtin_amdgcn_exp2f(ref - now);
+            far |= __any(now != ref && fabsf(now) > kFarthest);
             ref = now;
             l *= keep;
 #pragma unroll
@@ -324,7 +332,7 @@ __global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
             *(f32x4_t*)(out + d) = x;
         });
     }
-    if (__any(odd != 0.f))
+    if (far || __any(odd != 0.f))
         for (int i = w0; i < min(w0 + 16, len); ++i) window_row<float, HD>(a, s0, i, h, lane);
 }
 

@@ -63,7 +63,7 @@ __device__ __forceinline__ void join_waves(const WindowDecodeArgs& a, const Deco
         for (int k = 0; k < WAVES; ++k) top = fmaxf(top, s_ref[k * w.room + h]);
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) {
-            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_ref[k * w.room + h] - top);
+            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((s_ref[k * w.room + h] - top) * kScoreUnit<HD>);
             sum += f * s_l[k * w.room + h];
             x += f * *(const f32x4_t*)(lds + (k * w.room + h) * HD + d);
         }
@@ -228,8 +228,9 @@ template <int HD_> struct CacheFloat {
 };
 
 // A workgroup takes a row, a KV head (up to 16 of its query heads) and a part of the row's visible pages; its waves take these in turn, a page in
-// flight while one is worked on, and meet in LDS.  Weights are exp2(z - ref), z the score in log2; ref follows the greatest score of its column only
-// where a weight would leave its range: most pages take no exchange between lanes.
+// flight while one is worked on, and meet in LDS.  Weights are 2^START exp((s - ref) / sqrt(HD)); ref follows the greatest score of its column only
+// where a weight would leave its range (2^MOST): most pages take no exchange between lanes.  ref is a score itself, and subtracted before scaling: where
+// scores are large, a scaled one's rounding would be a factor of any size.
 template <typename C, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, C::SIMD_WAVES) void k_window_decode(WindowDecodeArgs a) {
     using T = typename C::T;
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(WAVES * 64, C::SIMD_WAVES) void k_window_decode(Win
     if (ctx > 0) {
         typename C::Query q;
         q.load((const T*)a.q + (size_t)w.r * a.ld_q + (size_t)(w.h0 + min(n, w.heads - 1)) * HD, c);
-        const float unit = 1.44269504088896f * rsqrtf((float)HD);
+        constexpr float UNIT = kScoreUnit<HD>, HIGHEST = (C::MOST - C::START) / UNIT;         // HIGHEST: of s - ref
         const Visible see(ctx, a.window, a.sinks);
         const int from = (int)((int64_t)see.n_pages * w.split / a.nsplit), to = (int)((int64_t)see.n_pages * (w.split + 1) / a.nsplit);
         const int mine = to - from > wave ? (to - from - wave + WAVES - 1) / WAVES : 0;
@@ -270,20 +271,17 @@ __global__ __launch_bounds__(WAVES * 64, C::SIMD_WAVES) void k_window_decode(Win
                         t.hide(i);
                     }
             }
-            f32x4_t e, p;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = fmaf(s[i], unit, -ref);
-            if (__any(!(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])) <= C::MOST))) {
-                const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * unit;
-                const float now = ref == -INFINITY || top - ref > C::MOST ? top - C::START : ref, keep = now == ref ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+            f32x4_t d = s - ref, p;
+            if (__any(!(fmaxf(fmaxf(d[0], d[1]), fmaxf(d[2], d[3])) <= HIGHEST))) {
+                const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+                const float now = ref == -INFINITY || top - ref > HIGHEST ? top : ref, keep = now == ref ? 1.f : __builtin_amdgcn_exp2f((ref - now) * UNIT);
                 l *= keep;
                 o.scale(keep);
                 ref = now;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = fmaf(s[i], unit, ref == -INFINITY ? 0.f : -ref);
+                d = s - (ref == -INFINITY ? 0.f : ref);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(e[i]);
+            for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(d[i], UNIT, C::START));
             l += (p[0] + p[1]) + (p[2] + p[3]);
             t.add(p, o);
         };
@@ -339,6 +337,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
     const int ctx = row_context(a, w.r, table);
     const int own = c / QUADS, quad = c % QUADS;   // the lane's page of PAGES, and its heads 4 quad + r
     float l[R] = {}, ref[R], wsum[GROUPS][R] = {}, csum[GROUPS][R] = {};
+    float off = INFINITY;                          // weights are 2^-off exp((s - ref) / sqrt(HD)); infinite: none yet
     f32x4_t o[HD / 16];                            // heads 4 quad + r, dim 16 d + n; in units of CODE, odd d of 16 CODE
 #pragma unroll
     for (int r = 0; r < R; ++r) ref[r] = -INFINITY;
@@ -349,7 +348,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
         const int mine_head = min(n % HEADS, w.heads - 1);         // of row n of Q and of the weights
         u32x4_t q[KS][TERMS];
         f32x4_t first[GROUPS];                                     // -8 times the sum of q in the group, in units of CODE
-        float unit[R];
+        int back[R];                                               // score = 2^back s
         {
             const T* p = (const T*)a.q + (size_t)w.r * a.ld_q + (size_t)(w.h0 + mine_head) * HD + c * 8;
             float f[KS][8], m = 0.f;
@@ -361,9 +360,8 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
             }
             m = column_max(m);
             const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
-            const float one = ldexpf(1.44269504088896f * rsqrtf((float)HD) / CODE, -up);
 #pragma unroll
-            for (int r = 0; r < R; ++r) unit[r] = __shfl(one, 4 * quad + r, kWave);
+            for (int r = 0; r < R; ++r) back[r] = __shfl(24 - up, 4 * quad + r, kWave);
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 float sum = 0.f;
@@ -397,7 +395,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
         // token n lies at place (0 2 1 3)[n % 4] of its four, the order of the codes of V
         uint16_t* put = weights + (own * HEADS + 4 * quad) * 16 + (n & 12) + (n & 1) * 2 + (n >> 1 & 1);
         const uint16_t* get = weights + mine_head * 16 + 4 * c;
-        float off = 0.f, most = -INFINITY;
+        constexpr float UNIT = kScoreUnit<HD>, HIGHEST = MOST / UNIT;
 
         struct Tile {
             Codes k[PAGES], v[PAGES];
@@ -426,12 +424,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
                 t.vp[g] = __builtin_nontemporal_load((const uint32_t*)(par + L::PARAMS + L::param(0, 64 * g)));
             }
         };
-        const auto rescale = [&](const float (&now)[R]) {
-            float keep[4] = {1.f, 1.f, 1.f, 1.f};
+        const auto rescale = [&](const float (&keep)[4]) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                keep[r] = now[r] == ref[r] ? 1.f : __builtin_amdgcn_exp2f(ref[r] - now[r]);
-                ref[r] = now[r];
                 l[r] *= keep[r];
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
@@ -483,35 +478,34 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
             const bool seen = i < to && see.sees(see.page(i) * 16 + n);
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) t.vp[g] = seen ? t.vp[g] : 0;
-            float e[R], p[R], top = -INFINITY;
+            float d[R], p[R], top = -INFINITY;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                s[r] = seen ? s[r] : -INFINITY;
-                e[r] = fmaf(s[r], unit[r], -ref[r]);
-                top = r == 0 ? e[r] : fmaxf(top, e[r]);
+                s[r] = seen ? ldexpf(s[r], back[r]) : -INFINITY;
+                d[r] = s[r] - ref[r];
+                top = r == 0 ? d[r] : fmaxf(top, d[r]);
             }
             const auto scale = [&](int g) { return unpack<f16_t>(t.vp[g], 0); };
-            if (__any(!(top <= most))) {
-                if (most == -INFINITY) {           // p s is at most 2^10 for the scales here; later ones may be 2^5 times as large
+            if (__any(!(top <= HIGHEST))) {
+                if (off == INFINITY) {             // p s is at most 2^10 for the scales here; later ones may be 2^5 times as large
                     float m = 0.f;
 #pragma unroll
                     for (int g = 0; g < GROUPS; ++g) m = fmaxf(m, fabsf(scale(g)));
                     m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_max(m))));
                     off = m > 0.f && m < INFINITY ? (float)ilogbf(m) - 9.f : -14.f;
-                    most = MOST - off;
                 }
-                float now[R];
+                float keep[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const float high = over_tokens(s[r]) * unit[r];
-                    now[r] = ref[r] == -INFINITY || high - ref[r] > most ? high + off : ref[r];
+                    const float high = over_tokens(s[r]), now = ref[r] == -INFINITY || high - ref[r] > HIGHEST ? high : ref[r];
+                    keep[r] = now == ref[r] ? 1.f : __builtin_amdgcn_exp2f((ref[r] - now) * UNIT);
+                    ref[r] = now;
+                    d[r] = s[r] - (now == -INFINITY ? 0.f : now);
                 }
-                rescale(now);
-#pragma unroll
-                for (int r = 0; r < R; ++r) e[r] = fmaf(s[r], unit[r], ref[r] == -INFINITY ? 0.f : -ref[r]);
+                rescale(keep);
             }
 #pragma unroll
-            for (int r = 0; r < R; ++r) p[r] = __builtin_amdgcn_exp2f(e[r]);
+            for (int r = 0; r < R; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(d[r], UNIT, -off));
             float ps[GROUPS][R], high = 0.f;
             const auto multiply = [&]() {
                 high = 0.f;
@@ -527,15 +521,11 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
             if (__any(high > 32768.f)) {           // much larger scales than before: all weights 2^by times smaller from here on
                 high = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_max(high))));
                 const float by = high < INFINITY ? (float)ilogbf(high) - 9.f : 60.f, f = __builtin_amdgcn_exp2f(-by);
-                float now[R];
+                const float keep[4] = {f, f, f, f};
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    now[r] = ref[r] + by;
-                    p[r] *= f;
-                }
-                rescale(now);
+                for (int r = 0; r < R; ++r) p[r] *= f;
+                rescale(keep);
                 off += by;
-                most -= by;
                 multiply();
             }
 #pragma unroll
@@ -600,6 +590,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
         }
     }
     lost = __any(lost);
+    const float whole = off == INFINITY ? 1.f : ldexpf(1.f, (int)off);
     const auto total = [&](float x) {              // over all tokens of the head
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) x += __shfl_xor(x, s, kWave);
@@ -611,14 +602,14 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int h = 4 * quad + r;
-        const float all = total(l[r]);
+        const float all = total(l[r]) * whole;
         float more[GROUPS];
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) more[g] = total(csum[g][r]) - 8.f * total(wsum[g][r]);
         if (own == 0 && h < w.heads) {
             float* to = lds + (wave * w.room + h) * HD + n;
 #pragma unroll
-            for (int d = 0; d < HD / 16; ++d) to[16 * d] = fmaf(o[d][r], (d & 1 ? 0.0625f : 1.f) / CODE, more[d / 4]);
+            for (int d = 0; d < HD / 16; ++d) to[16 * d] = fmaf(o[d][r], (d & 1 ? 0.0625f : 1.f) / CODE, more[d / 4]) * whole;
             if (n == 0) {
                 lds[WAVES * w.room * HD + wave * w.room + h] = ref[r];
                 lds[WAVES * w.room * (HD + 1) + wave * w.room + h] = lost ? NAN : all;
@@ -639,7 +630,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) 
     const size_t slot = (size_t)blockIdx.x * a.nsplit, slots = (size_t)a.rows * a.n_q_heads * a.nsplit;
     if (t < 64) {                                                      // nsplit <= 64
         const float2 ml = t < a.nsplit ? ((const float2*)(a.part + slots * HD))[slot + t] : make_float2(-INFINITY, 0.f);
-        const float m = wave_max(ml.x), w = __builtin_amdgcn_exp2f(ml.x - (m == -INFINITY ? 0.f : m)), l = wave_sum(w * ml.y);
+        const float m = wave_max(ml.x), w = __builtin_amdgcn_exp2f((ml.x - (m == -INFINITY ? 0.f : m)) * kScoreUnit<HD>), l = wave_sum(w * ml.y);
         s_w[t] = w;
         if (t == 0) s_l = l;
     }

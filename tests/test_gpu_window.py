@@ -175,6 +175,21 @@ def test_packed_scores_of_great_size(dtype):
         assert torch.equal(out[i], v[best]), i
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_packed_scores_of_2_to_the_30(dtype, sign):
+    """As far as half goes: scores of 2^26 to 2^30, thousands apart; a rounded one may be off by 2^6."""
+    lens = [140]
+    q, k, v = _packed(14, lens, 1, 1, 64, dtype)
+    q[:] = 8192.0
+    k[:] = (sign * 32 * (1 + torch.arange(140, device="cuda").mul(37).remainder(140)).double())[:, None].to(k.dtype)
+    out = _packed_run(q, k, v, lens, 50, 2, 1, 1, 64)
+    for i in range(140):
+        seen = [j for j in range(i + 1) if j > i - 50 or j < 2]
+        best = seen[int(k[seen, 0].float().argmax())]
+        assert torch.equal(out[i], v[best]), i
+
+
 def test_packed_strides_views_and_streams():
     """Rows of every second one of a buffer, on a stream of its own."""
     lens, Hq, Hkv, hd = [90, 140], 4, 2, 64
@@ -385,6 +400,72 @@ def test_decode_a_visible_token_that_is_not_finite(four, dtype):
     out = p.run(20, 0)
     assert not torch.isfinite(out[0, :64]).any() and torch.isfinite(out[0, 64:]).all() and torch.isfinite(out[1]).all()
     assert torch.isfinite(p.run(16, 0)).all()                            # hidden, in a page of which tokens 84 on are seen
+
+
+def _hold(p, i, k, v):
+    """Other k, v [ctx, Hkv, hd] in the place of context i of a cache of 4 bits."""
+    slots = [int(p.table[p.sample[i], t // 16]) * 16 + t % 16 for t in range(p.ctx[i])]
+    k, v = k.to(TDT[p.dtype]), v.to(TDT[p.dtype])
+    _R().rlhf_op_kv4_append(k.flatten(1).cuda(), v.flatten(1).cuda(), _ints(slots), p.pool, p.layer, p.layers, p.Hkv, p.hd)
+    for kv, to, size in ((k, p.k, p.k_size), (v, p.v, p.v_size)):
+        u, par = W.kv4_quantize(kv.float().numpy())
+        to[i], par = W.kv4_values(u, par), np.abs(par.astype(np.float64))
+        size[i] = np.repeat(par[..., 1] + 8 * par[..., 0], 64, -1)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("Hq", [1, 2])
+@pytest.mark.parametrize("great", [2.0 ** 90, 2.0 ** 115, 2.0 ** 127])
+def test_four_bits_queries_of_great_size(dtype, Hq, great):
+    """One dim of q is so large that the scores, all finite, are far apart: the greatest takes it all."""
+    p = Paged(11, [100, 40], Hq, 1, 64, dtype, four=True)
+    k = torch.zeros(100, 1, 64)
+    k[:, 0, 5] = 2.0 ** -7 * (1 + torch.arange(100).mul(37).remainder(100) / 128)
+    _hold(p, 0, k, torch.from_numpy(np.random.default_rng(1).normal(size=(100, 1, 64))))
+    q = torch.zeros(2, Hq * 64, device="cuda", dtype=TDT[dtype])
+    q[:, 5::64] = great
+    out = _np(p.run(50, 3, q=q))[0].reshape(Hq, 64)
+    seen = np.r_[0:3, 50:100]
+    score = p.k[0][seen, 0, 5]
+    best = seen[score == score.max()]                                   # held alike, their values are averaged
+    want, size = p.v[0][best, 0].mean(0), p.v_size[0][best, 0].mean(0)
+    assert (np.abs(out - want) <= (ROUNDED[dtype] + 8 * E) * size + (HALF_STEP[dtype] + 2 * E) * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 1), (6, 1), (12, 1)])
+@pytest.mark.parametrize("what", ["grow", "fall", "jump", "equal", "tiny"])
+def test_four_bits_values_of_changing_size(dtype, Hq, Hkv, what):
+    """V that grows or falls by 2^20 along a context, jumps by 2^15, has scale 0, or the least that half holds."""
+    n, r = 400, np.random.default_rng(12)
+    p = Paged(13, [n, 33], Hq, Hkv, 128, dtype, four=True)
+    t = np.arange(n)[:, None, None]
+    size = {"grow": 2.0 ** (t / 20 - 10), "fall": 2.0 ** (10 - t / 20), "jump": np.where(t // 70 % 2, 2.0 ** 10, 2.0 ** -5), "equal": 0.0 * t, "tiny": 2.0 ** -22 + 0 * t}[what]
+    v = r.normal(size=(n, Hkv, 128)) * size + (np.where(t < 200, 0.0, 3.0) if what == "equal" else 0.0)
+    _hold(p, 0, torch.from_numpy(r.normal(size=(n, Hkv, 128))), torch.from_numpy(v))
+    for window, sinks, nsplit in ((ALL, 0, 1), (150, 20, 1), (ALL, 0, 3)):
+        p.check(p.run(window, sinks, nsplit=nsplit), window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("great,less", [(2.0 ** 15, 2.0 ** 4), (-2.0 ** 15, 2.0 ** 6), (2.0 ** 60, 1.0), (2.0 ** 100, 2.0 ** 10), (-2.0 ** 60, 1.0)])
+@pytest.mark.parametrize("nsplit", [1, 3])
+def test_decode_scores_of_great_size(dtype, great, less, nsplit):
+    """Finite scores that are far apart: the greatest takes it all."""
+    if dtype == "half" and abs(great) > 65504:
+        pytest.skip("beyond half")
+    p = Paged(15, [200, 40], 2, 1, 64, dtype)
+    q = torch.zeros(2, 128, device="cuda", dtype=TDT[dtype])
+    q[:, ::64] = great
+    for t in range(200):
+        x = less * (1 + t * 37 % 200 / 256)
+        p.pool[int(p.table[p.sample[0], t // 16]), 1, 0, 0, t % 16, 0] = x
+        p.k[0][t, 0, 0] = float(torch.tensor(x).to(TDT[dtype]))
+    out = _np(p.run(100, 3, q=q, nsplit=nsplit))[0].reshape(2, 64)
+    seen = np.r_[0:3, 100:200]
+    score = p.k[0][seen, 0, 0] * np.sign(great)
+    want = p.v[0][seen[score == score.max()], 0].mean(0)
+    assert (np.abs(out - want) <= (HALF_STEP[dtype] + 8 * E) * np.abs(p.v[0][:, 0]).max(0)).all()
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])

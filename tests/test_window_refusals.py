@@ -20,7 +20,7 @@ PACKED = dict(dtype=0, q=A, ld_q=512, k=B, ld_k=256, v=C, ld_v=256, start=D, q0=
     dict(ld_q=508), dict(ld_k=252), dict(ld_v=252), dict(ld_out=508), dict(ld_q=514), dict(ld_k=257), dict(dtype=2, ld_q=516), dict(q=A + 8), dict(k=B + 4),
     dict(v=C + 2), dict(out=E + 8), dict(n_tiles=-1), dict(rows=-1), dict(rows=BIG + 1), dict(window=0), dict(window=-5), dict(sinks=-1), dict(hq=3),
     dict(hq=0), dict(hkv=0), dict(hd=32), dict(hd=96), dict(hd=256), dict(out=A), dict(out=A + 16), dict(out=B), dict(out=C + 1024),
-    dict(hq=1 << 17, hkv=1 << 17, ld_q=1 << 24, ld_k=1 << 24, ld_v=1 << 24, ld_out=1 << 24),
+    dict(hq=1 << 17, hkv=1 << 17, ld_q=1 << 24, ld_k=1 << 24, ld_v=1 << 24, ld_out=1 << 24), dict(ld_k=1 << 25), dict(ld_v=1 << 25),
 ], ids=str)
 def test_window_attention(bad):
     R = _R()
