@@ -650,11 +650,19 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) 
 // Waves of a workgroup; four where 16 heads' sums of eight would take more than 64 KB of LDS.
 static int decode_waves(int group) { return group > 8 ? 4 : 8; }
 
+// Into how many parts the visible pages of a row are cut: none below 6 pages a wave, where joining costs more than it gives (two rows of 12 heads of
+// 64, 700 tokens 7.5 us in one part, 7.8 in four; 1000 tokens 9.2 and 8.2); else a power of two, which leaves the parts of a row's heads on as few XCDs as
+// there are (32 heads of 128, 4000 tokens: 8 parts 16.0 us, 12 18.6, 16 16.2), of a page a wave at least and of 2048 waves in all (8 rows of
+// 8 KV heads, 2000 tokens: 4 parts 15.8 us, 2 21.7, 8 17.2), or 4096 with 32 pages a wave and more (one row of 131072 tokens in 4 bits, 8 KV
+// heads: 64 parts 39 us, 32 44).
 int window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks) {
     const int64_t pages = std::min<int64_t>((max_ctx + 15ll) / 16, (sinks + 15ll) / 16 + (window + 15ll) / 16 + 1);
     const int group = n_q_heads / n_kv_heads, waves = decode_waves(group);
-    const int64_t blocks = (int64_t)rows * n_kv_heads * ((group + 15) / 16);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({64, pages / (2 * waves), 4096 / waves / blocks}));
+    const int64_t all = (int64_t)rows * n_kv_heads * ((group + 15) / 16) * waves;       // in one part each
+    if (pages < 6 * waves) return 1;
+    int n = 1;
+    while (n < 64 && 2 * n * waves <= pages && 2 * n * all <= (pages >= 32 * n * waves ? 4096 : 2048)) n *= 2;
+    return n;
 }
 
 size_t window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int nsplit) {
