@@ -59,7 +59,9 @@ __device__ __forceinline__ bool tile_of(const WindowArgs& a, int tile, int& s0, 
     return s0 >= 0 && q0 >= 0 && len <= a.rows - s0 && q0 < len;
 }
 
-// Workgroup -> (tile, query head).
+// Workgroup -> (tile, query head).  Units of a tile and KV head, whose query heads share K and V, go to the XCDs in turn, so that keys are read into one
+// L2; the last tiles, with the most keys, come first (units side by side: 16384 tokens 1808 -> 1988 us, 2 x 8192 of 32 / 8 heads, window
+// 1024 293 -> 318; tiles from the first: 8192 tokens of 32 heads 542 -> 642).
 __device__ __forceinline__ bool window_work(const WindowArgs& a, int& tile, int& h) {
     const unsigned G = a.n_q_heads / a.n_kv_heads, i = blockIdx.x / 8, unit = i / G * 8 + blockIdx.x % 8;
     if (unit >= (unsigned)a.n_tiles * (unsigned)a.n_kv_heads) return false;
@@ -98,10 +100,14 @@ typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 // their type: such queries are taken again, too.
 constexpr float kFarthest = 0x1p24f;
 
-// 16-bit types: 128 queries of a head a workgroup, 32 a wave, against 64 keys at a time.  K and V go from memory to LDS directly, one tile ahead;
-// V is transposed as it is read from LDS.  References of the weights follow the running maximum only where these would leave their
-// range, so that most tiles do not rescale the sums.  A key that is hidden from a query has weight 0, and 0 times what is not a number is none: a
-// wave whose result is not finite takes its queries again one by one, over visible keys alone.
+// 16-bit types: 128 queries of a head a workgroup, 32 a wave, against 32 keys at a time.  K and V go from memory to LDS directly, one tile ahead;
+// V is transposed as it is read from LDS, and the weights stay in the lanes that made them.  References of the weights follow the running maximum only
+// where these would leave their range, so that most tiles do not rescale the sums.  A key that is hidden from a query has weight 0, and 0 times
+// what is not a number is none: a wave whose result is not finite takes its queries again one by one, over visible keys alone.
+// 32 keys leave registers for three workgroups a compute unit, 64 for two (64 instead: 16384 tokens 1808 -> 1871 us, 16 sequences of 200-800 85 -> 90; heads
+// of 64 gain with long contexts, 4 x 4096 162 -> 150, and lose with short ones, 40 of 1-700 30.5 -> 31.6).
+// 16384 tokens of 64 / 8 heads of 128, window 4096: 1.79 ms, 1.08 PFLOP/s of visible keys, the chip at its power limit (1.6 to 1.9 GHz).
+// 16 sequences of 200-800, window 256: 80 us, 3.3 TB/s where a copy reaches 4.7.  Weights go to the matrix units rounded once to the type.
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     using M = Matrix16<T>;
@@ -117,10 +123,10 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     const T* vb = (const T*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
     const uint32_t ldk = (uint32_t)a.ld_k * 2, ldv = (uint32_t)a.ld_v * 2;
 
-    // A load of a wave fills ROWS rows of a tile; place p of row t holds 16-byte piece p ^ (t % 16) of K and, in pairs, p ^ 2 (t % 8) of V (of 64 dims
-    // ^ (t / 2 % 8) and ^ 2 (t / 2 % 4)), so that fragment reads spread over the banks.
+    // A load of a wave fills ROWS rows of a tile; place p of row t holds 16-byte piece p ^ (t % 16) of K and p ^ 4 (t % 4) of V (of 64 dims
+    // ^ (t / 2 % 8) and ^ 4 (t / 2 % 2)), so that fragment reads spread over the banks.
     const int lrow = wave * ROWS + lane / CH, place = lane % CH;
-    const int kpiece = CH == 16 ? place ^ (lrow & 15) : place ^ ((lrow >> 1) & 7), vpiece = CH == 16 ? place ^ ((lrow & 7) << 1) : place ^ (((lrow >> 1) & 3) << 1);
+    const int kpiece = CH == 16 ? place ^ (lrow & 15) : place ^ ((lrow >> 1) & 7), vpiece = CH == 16 ? place ^ ((lrow & 3) << 2) : place ^ (((lrow >> 1) & 1) << 2);
     const uint32_t kat = lrow * ldk + kpiece * 16, vat = lrow * ldv + vpiece * 16;
     const auto fetch = [&](int kt, int buf) {
         const u32x4_t rk = buffer_base(kb + (size_t)kt * KT * a.ld_k), rv = buffer_base(vb + (size_t)kt * KT * a.ld_v);
@@ -159,8 +165,10 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
         for (int m = 0; m < 2; ++m) o[d][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float ref[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
     bool far = false;
-    const int vt = 4 * c + (n >> 2);               // token (modulo 16) and 32-byte pair of pieces of a lane's reads of V
-    const int vswap = CH == 16 ? vt & 7 : (vt >> 1) & 3;
+    // Token (modulo 16) of a lane's reads of V.  Sums d and d + 1 (even d) of a lane are dims 16 d + 8 c .. + 7, so that it stores 16 bytes at a time (16
+    // sequences of 200-800, 32 heads of 128, window 1: 62.6 -> 58.4 us, 4.5 TB/s).
+    const int vt = 4 * c + (n >> 2);
+    const int vswap = (CH == 16 ? vt & 3 : (vt >> 1) & 1) << 2;
 
     if (keys.n > 1) fetch(keys.at(1), 1);
     for (int j = 0; j < keys.n; ++j) {
@@ -228,7 +236,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
         for (int d = 0; d < DF; ++d)
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
-                T* at = &sV[buf][(u * 32 + vt) * HD + (d ^ vswap) * 16 + (n & 3) * 4];
+                T* at = &sV[buf][(u * 32 + vt) * HD + ((d / 2 * 4 + (n & 3)) ^ vswap) * 8 + (d & 1) * 4];
                 const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * HD));
                 const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
 #pragma unroll
@@ -242,20 +250,21 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
         const float inv = 1.f / column_sum(l[m]);
         const int i = w0 + m * 16 + n;
         if (i >= len) continue;
-        T* out = (T*)a.out + (size_t)(s0 + i) * a.ld_out + (size_t)h * HD + 4 * c;
+        T* out = (T*)a.out + (size_t)(s0 + i) * a.ld_out + (size_t)h * HD + 8 * c;
 #pragma unroll
-        for (int d = 0; d < DF; ++d) {
-            const f32x4_t x = o[d][m] * inv;
-            odd += 0.f * ((x[0] + x[1]) + (x[2] + x[3]));
-            *(u32x2_t*)(out + d * 16) = u32x2_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+        for (int d = 0; d < DF; d += 2) {
+            const f32x4_t x = o[d][m] * inv, y = o[d + 1][m] * inv;
+            odd += 0.f * (((x[0] + x[1]) + (x[2] + x[3])) + ((y[0] + y[1]) + (y[2] + y[3])));
+            *(u32x4_t*)(out + d * 16) = u32x4_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
         }
     }
     if (far || __any(odd != 0.f))
         for (int i = w0; i < min(w0 + 32, len); ++i) window_row<T, HD>(a, s0, i, h, lane);
 }
 
-// Float: 128 queries of a head a workgroup, 16 a wave, against 16 keys at a time, which go to LDS a tile ahead; bound by the float matrix rate (a sixteenth
-// of the half one).  What is hidden is kept out as above.
+// Float: 128 queries of a head a workgroup, 16 a wave, against 16 keys at a time, which go to LDS a tile ahead; bound by the float matrix rate (a tenth
+// of the half one).  What is hidden is kept out as above.  8192 tokens of 64 / 8 heads of 128, window 1024: 2.11 ms, 123 TFLOP/s with the hidden part of
+// the tiles (waves that read keys from memory for themselves: 3.29); 16 sequences of 200-800, 32 heads, window 256: 313 us (456).
 template <int HD>
 __global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
     constexpr int KT = 16, D = HD / 16, CH = HD / 4, ROWS = 64 / CH, WAVES_EACH = KT / ROWS, TILE = KT * HD;       // WAVES_EACH: waves that load a tile of K
