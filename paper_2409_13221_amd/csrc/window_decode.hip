@@ -122,7 +122,7 @@ template <typename T, int HD> __device__ __forceinline__ Pages plain_pages(const
 template <typename T_, int HD_> struct Cache16 {
     using T = T_;
     using M = Matrix16<T>;
-    static constexpr int HD = HD_, D = HD / 16, KS = HD / 32, SIMD_WAVES = 4;
+    static constexpr int HD = HD_, D = HD / 16, KS = HD / 32;
     static constexpr float START = M::TOP > 0.f ? 6.f : 0.f, MOST = M::TOP > 0.f ? M::TOP : 20.f;
     typedef uint32_t VRow __attribute__((ext_vector_type(D / 2)));
     static __device__ __forceinline__ LaneOffsets offsets(int n, int c) { return plain_offsets<T, HD>(n, c); }
@@ -189,7 +189,7 @@ template <typename T_, int HD_> struct Cache16 {
 
 template <int HD_> struct CacheFloat {
     using T = float;
-    static constexpr int HD = HD_, D = HD / 16, SIMD_WAVES = HD == 64 ? 4 : 2;
+    static constexpr int HD = HD_, D = HD / 16;
     static constexpr float START = 0.f, MOST = 20.f;
     using Query = FloatQuery<HD>;
     static __device__ __forceinline__ LaneOffsets offsets(int n, int c) { return plain_offsets<float, HD>(n, c); }
@@ -231,8 +231,10 @@ template <int HD_> struct CacheFloat {
 // flight while one is worked on, and meet in LDS.  Weights are 2^START exp((s - ref) / sqrt(HD)); ref follows the greatest score of its column only
 // where a weight would leave its range (2^MOST): most pages take no exchange between lanes.  ref is a score itself, and subtracted before scaling: where
 // scores are large, a scaled one's rounding would be a factor of any size.
+// Bound by the cache's bytes: 64 rows of 300-2560 tokens, 32 heads of 128, window 1024, half: 157 us, 6.1 TB/s; in float, 16 heads: 164 us.  Registers for
+// two waves a SIMD at least (16 bits take 125: four fit; asked for three, float spills: 297 us).
 template <typename C, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, C::SIMD_WAVES) void k_window_decode(WindowDecodeArgs a) {
+__global__ __launch_bounds__(WAVES * 64, 2) void k_window_decode(WindowDecodeArgs a) {
     using T = typename C::T;
     constexpr int HD = C::HD;
     extern __shared__ float lds[];                 // [WAVES][heads][HD] sums, then [WAVES][heads] references, [WAVES][heads] weights
@@ -320,12 +322,15 @@ __global__ __launch_bounds__(WAVES * 64, C::SIMD_WAVES) void k_window_decode(Win
 // the matrix units take q and p s_g, the rest is a few multiply-adds a token.  What a token costs beside its codes would outweigh them if 16 lanes
 // worked on each for the 16 rows of a matrix product, so it is dealt out: scores are Q K^T with the query heads, up to HEADS = 16 / PAGES of them, repeated in
 // all rows, and of PAGES pages' scores a quad of rows (lanes c) keeps the page that is its own: a lane has one token of PAGES x 16 for R heads.
-// Weights p s_g go to the lanes of the second product through LDS.  64 rows of 512-4096 tokens, 32 heads of 128: 142 us with lanes of four tokens for
-// all 16 rows.
+// Weights p s_g go to the lanes of the second product through LDS.
+// 64 rows of 512-4096 tokens, 32 heads of 128: 113 us, 6.1 TB/s (68 with all pages in L2; lanes of four tokens for all 16 rows: 142).  PAGES goes by the query
+// heads of a KV head, 1, up to 4, up to 8, more: with PAGES = 2 for one head 137, 1 for it 182; for two heads 78 with 4, 81 with 2; for
+// eight (170 MB instead of 680) 47 with 2, 65 with 1: bound by the steps of a wave there, two waves a SIMD.  Waves that ask for registers for three a
+// SIMD: one head 115, eight 217.
 // A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that; from float
 // in three terms.  Weights are such that p s_g fits half, in one term, of float calls in two.
 template <typename T, int HD, int PAGES, int R, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void k_kv4_decode(WindowDecodeArgs a) {
+__global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a) {
     using L = Kv4<HD>;
     constexpr int KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 3 : 1, WTERMS = sizeof(T) == 4 ? 2 : 1, HEADS = 16 / PAGES, QUADS = HEADS / 4;
     constexpr float CODE = 1.f / (1 << 24), MOST = 4.f;            // MOST: log2 of the greatest weight, above the offset
@@ -620,10 +625,10 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && R == 1 ? 3 : 2) void 
     join_waves<T, HD, WAVES>(a, w, ctx, lds);
 }
 
-// The parts of a (row, query head) joined: a wave each, or of many parts four, whose sums meet in LDS.
-template <typename T, int HD, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) {
-    constexpr int LANES = HD / 4, GROUPS = WAVES * 64 / LANES;         // a group of lanes takes every GROUPS-th part, four dims a lane
+// The parts of a (row, query head) joined, by four waves whose sums meet in LDS: of 64 parts (64 heads of 128) 4.3 us, with one wave 10.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_window_join(WindowDecodeArgs a) {
+    constexpr int LANES = HD / 4, GROUPS = 256 / LANES;         // a group of lanes takes every GROUPS-th part, four dims a lane
     __shared__ f32x4_t s_x[GROUPS][LANES];
     __shared__ float s_w[64], s_l;
     const int t = threadIdx.x, g = t / LANES, d = t % LANES * 4, h = blockIdx.x % a.n_q_heads, r = blockIdx.x / a.n_q_heads;
@@ -647,7 +652,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_window_join(WindowDecodeArgs a) 
     for (int e = 0; e < 4; ++e) o[e] = round_to<T>(empty ? 0.f : x[e] / s_l);
 }
 
-// Waves of a workgroup; four where 16 heads' sums of eight would take more than 64 KB of LDS.
+// Waves of a workgroup over a plain cache; four where 16 heads' sums of eight would take more than 64 KB of LDS.  (Four for all: 64 rows of 300-2560, 32 heads
+// of 128 164 us instead of 160, 16 rows of 2000, 12 heads of 64 25.5 instead of 22.4.)
 static int decode_waves(int group) { return group > 8 ? 4 : 8; }
 
 // Into how many parts the visible pages of a row are cut: none below 6 pages a wave, where joining costs more than it gives (two rows of 12 heads of
@@ -683,8 +689,7 @@ static hipError_t in_turns(hipStream_t st, const WindowDecodeArgs& a, int waves,
         p.rows = std::min(most, a.rows - first);
         start((unsigned)(p.rows * blocks), p);
         const unsigned heads = (unsigned)p.rows * (unsigned)a.n_q_heads;
-        if (a.nsplit > 8) k_window_join<T, HD, 4><<<heads, 256, 0, st>>>(p);
-        else if (a.nsplit > 1) k_window_join<T, HD, 1><<<heads, 64, 0, st>>>(p);
+        if (a.nsplit > 1) k_window_join<T, HD><<<heads, 256, 0, st>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -704,7 +709,7 @@ static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
 template <typename T, int HD>
 static hipError_t kv4_rows(hipStream_t st, const WindowDecodeArgs& a) {
     const int group = a.n_q_heads / a.n_kv_heads;
-    constexpr int WAVES = 4;
+    constexpr int WAVES = 4;                       // eight: 64 rows of 512-4096, 32 heads of 128 121 us instead of 115, 131072 tokens 47 instead of 38
     const size_t sums = (size_t)WAVES * std::min(16, group) * (HD + 2) * sizeof(float), weights = (size_t)WAVES * (sizeof(T) == 4 ? 2 : 1) * (HD / 64) * 512;
     const size_t lds = std::max(sums, weights);
     return in_turns<T, HD>(st, a, WAVES, [&](unsigned grid, const WindowDecodeArgs& p) {
