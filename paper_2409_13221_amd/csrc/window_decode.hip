@@ -316,6 +316,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_decode(WindowDecodeArg
     join_waves<T, HD, WAVES>(a, w, ctx, lds);
 }
 
+// Two codes as masked, v 2^-24 or v 2^-20: as they are, or (SHIFT 10) 2^14 times as large.
+template <int SHIFT> __device__ __forceinline__ uint32_t code_pair(uint32_t x) {
+    if constexpr (SHIFT == 24) return x;
+    typedef f16_t f16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, x) * f16x2_t{16384.f, 16384.f});
+}
+
 // A cache of 4 bits.  The bits of a code v = u + 8, masked where they lie, are the half v 2^-24 or (the upper of a byte) v 2^-20, below half's normal range
 // and exact to the matrix units: 5 instructions for 8 codes.  With scale s and center c of each token and 64 dims (group g),
 //   q.k = sum over g of s_g (sum q v - 8 sum q) + c_g (sum of q in g),   o = sum over tokens of (p s_g) v - 8 (p s_g) + p c_g:
@@ -327,15 +334,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_decode(WindowDecodeArg
 // heads of a KV head, 1, up to 4, up to 8, more: with PAGES = 2 for one head 137, 1 for it 182; for two heads 78 with 4, 81 with 2; for
 // eight (170 MB instead of 680) 47 with 2, 65 with 1: bound by the steps of a wave there, two waves a SIMD.  Waves that ask for registers for three a
 // SIMD: one head 115, eight 217.
-// A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that; from float
-// in three terms.  Weights are such that p s_g fits half, in one term, of float calls in two.
+// A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that; weights are
+// such that p s_g fits half.  Of float calls both come in two terms, which leave 2^-24 of them.  The matrix units do not normalize what is below half's
+// normal range before they align a sum, which costs it 6 bits (scores off by 2^-18 of their terms); float calls take codes 2^14 times as large, which
+// keeps those: outputs were off by 4e-5, and are by 4e-7 (one head, 64 rows as above: 123 -> 127 us).
 template <typename T, int HD, int PAGES, int R, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a) {
     using L = Kv4<HD>;
-    constexpr int KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 3 : 1, WTERMS = sizeof(T) == 4 ? 2 : 1, HEADS = 16 / PAGES, QUADS = HEADS / 4;
-    constexpr float CODE = 1.f / (1 << 24), MOST = 4.f;            // MOST: log2 of the greatest weight, above the offset
+    constexpr int KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 2 : 1, HEADS = 16 / PAGES, QUADS = HEADS / 4;
+    constexpr int SHIFT = TERMS > 1 ? 10 : 24;
+    constexpr float CODE = 1.f / (1 << SHIFT), MOST = 4.f;            // MOST: log2 of the greatest weight, above the offset
     typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
-    extern __shared__ float lds[];                 // as above; while pages are worked on, weights [WAVES][WTERMS][GROUPS][PAGES][HEADS][16 tokens] of half
+    extern __shared__ float lds[];                 // as above; while pages are worked on, weights [WAVES][TERMS][GROUPS][PAGES][HEADS][16 tokens] of half
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     const DecodeWork w(a);
     const int* table = nullptr;
@@ -366,7 +376,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
             m = column_max(m);
             const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
 #pragma unroll
-            for (int r = 0; r < R; ++r) back[r] = __shfl(24 - up, 4 * quad + r, kWave);
+            for (int r = 0; r < R; ++r) back[r] = __shfl(SHIFT - up, 4 * quad + r, kWave);
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 float sum = 0.f;
@@ -396,7 +406,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
         const size_t layer = (size_t)a.n_kv_heads * L::BLOCK, stride = layer * a.n_layers;
         const uint8_t* base = (const uint8_t*)a.pool + a.layer * layer + (size_t)w.kh * L::BLOCK;
         const uint32_t piece = lane * L::PIECE;
-        uint16_t* weights = (uint16_t*)lds + wave * (WTERMS * GROUPS * 256);
+        uint16_t* weights = (uint16_t*)lds + wave * (TERMS * GROUPS * 256);
         // token n lies at place (0 2 1 3)[n % 4] of its four, the order of the codes of V
         uint16_t* put = weights + (own * HEADS + 4 * quad) * 16 + (n & 12) + (n & 1) * 2 + (n >> 1 & 1);
         const uint16_t* get = weights + mine_head * 16 + 4 * c;
@@ -463,7 +473,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
 #pragma unroll
                         for (int i = 2 * g; i < 2 * g + 2; ++i) {
                             const uint32_t k = t.k[p][i], up = k >> 8;
-                            const u32x4_t h{k & 0x000F000Fu, k & 0x00F000F0u, up & 0x000F000Fu, up & 0x00F000F0u};
+                            const u32x4_t h{code_pair<SHIFT>(k & 0x000F000Fu), code_pair<SHIFT>(k & 0x00F000F0u), code_pair<SHIFT>(up & 0x000F000Fu),
+                                            code_pair<SHIFT>(up & 0x00F000F0u)};
 #pragma unroll
                             for (int e = 0; e < TERMS; ++e) x = Matrix16<f16_t>::qk(q[i][e], h, x);
                         }
@@ -541,7 +552,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
                     csum[g][r] = fmaf(p[r], unpack<f16_t>(t.vp[g], 1), csum[g][r]);
                     float rest = ps[g][r];
 #pragma unroll
-                    for (int x = 0; x < WTERMS; ++x) {
+                    for (int x = 0; x < TERMS; ++x) {
                         const f16_t h = (f16_t)rest;
                         put[(x * GROUPS + g) * 256 + r * 16] = __builtin_bit_cast(uint16_t, h);
                         wsum[g][r] += (float)h;    // as the matrix units see them
@@ -554,7 +565,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-                for (int x = 0; x < WTERMS; ++x)
+                for (int x = 0; x < TERMS; ++x)
 #pragma unroll
                     for (int pp = 0; pp < PAGES; pp += 2) {
                         const u32x2_t wa = *(const u32x2_t*)(get + (x * GROUPS + g) * 256 + pp * HEADS * 16);
@@ -565,11 +576,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
 #pragma unroll
                             for (int d = 0; d < 2; ++d) {          // tokens (0, 2), (1, 3) of dims 32 i + n, then of dims 32 i + 16 + n
                                 const uint32_t mask = d ? 0x00F000F0u : 0x000F000Fu;
+                                const u32x2_t a2{code_pair<SHIFT>(va & mask), code_pair<SHIFT>(va >> 8 & mask)};
                                 if (PAGES > 1) {
-                                    const u32x4_t h{va & mask, va >> 8 & mask, vb & mask, vb >> 8 & mask};
+                                    const u32x4_t h{a2[0], a2[1], code_pair<SHIFT>(vb & mask), code_pair<SHIFT>(vb >> 8 & mask)};
                                     o[2 * i + d] = Matrix16<f16_t>::qk(u32x4_t{wa[0], wa[1], wb[0], wb[1]}, h, o[2 * i + d]);
                                 } else {
-                                    o[2 * i + d] = Matrix16<f16_t>::pv(wa, u32x2_t{va & mask, va >> 8 & mask}, o[2 * i + d]);
+                                    o[2 * i + d] = Matrix16<f16_t>::pv(wa, a2, o[2 * i + d]);
                                 }
                             }
                         }

@@ -469,6 +469,26 @@ def test_decode_scores_of_great_size(dtype, great, less, nsplit):
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(2, 2, 64), (4, 2, 128), (8, 1, 64), (16, 1, 128)])
+def test_decode_in_float_is_as_near_as_float(four, Hq, Hkv, hd):
+    """The bounds of _check add magnitudes; roundings add as random numbers do.  A score is a sum of some 16 partial sums, each off by up to a step (2 E) of
+    at most 2 S here (codes v = u + 8 are summed, and 8 sum q taken off), so by some 4 * 2 E * 2 S = 16 E S where float products of hd terms in blocks are off by
+    E S or so: 16 times the error of the same formula in float32, in the mean over all outputs, with 2^-22 for exp2 and the weights' terms."""
+    p = Paged(16, [300, 33, 150], Hq, Hkv, hd, "fp32", four)
+    out = _np(p.run(ALL, 0, nsplit=1)).reshape(3, Hq, hd)
+    off, plain, size = 0.0, 0.0, 0.0
+    for i, c in enumerate(p.ctx):
+        q = _np(p.q[i]).reshape(1, Hq, hd)
+        want = W.attention(q, p.k[i], p.v[i], np.array([c - 1]), ALL, 0)[0]
+        kf, vf, qf = (torch.from_numpy(np.asarray(t, np.float32)) for t in (p.k[i].repeat(Hq // Hkv, 1), p.v[i].repeat(Hq // Hkv, 1), q[0]))
+        w = torch.softmax((kf * qf[None]).sum(-1) / np.float32(np.sqrt(hd)), 0)
+        off += ((out[i] - want) ** 2).sum()
+        plain += (((w[..., None] * vf).sum(0).double().numpy() - want) ** 2).sum()
+        size += (want ** 2).sum()
+    assert np.sqrt(off) <= 16 * np.sqrt(plain) + 2.0 ** -22 * np.sqrt(size), (np.sqrt(off / size), np.sqrt(plain / size))
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
 @pytest.mark.parametrize("nsplit", [1, 3])
 def test_decode_strided_and_on_a_stream(four, nsplit):
     p = Paged(9, [40, 300, 0], 2, 2, 64, "half", four)
