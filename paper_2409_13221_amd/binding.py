@@ -651,6 +651,30 @@ def _matrix(t, rows: int, cols: int, what: str) -> int:
     return ld
 
 
+def _stream_with(*tensors) -> int:
+    """The current stream, if all tensors are on the current device: _on_device and _stream_ptr with the device asked for once."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at != dev:
+                if dev is not None or at < 0 or at != _th()._C._cuda_getDevice():
+                    _on_device(*tensors)         # says what is wrong
+                dev = at
+    return _th()._C._cuda_getCurrentRawStream(dev)
+
+
+def _row_stride(t, shape: tuple, what: str) -> int:
+    """_matrix of a call that lasts a few microseconds: shape and strides are asked for once."""
+    rows, cols = shape
+    if t.shape != shape:
+        raise ValueError(f"{what} must be [{rows}, {cols}] with contiguous rows")
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        return _matrix(t, rows, cols, what)      # says what is wrong
+    return ld if rows > 1 else cols
+
+
 class rlhf_attention_tiles:
     """The plan of a packed pass for rlhf_op_window_attention: sequences of seq_lens rows, back to back (a length may be 0), cut into
     tiles of 128 queries.  One plan serves all layers and any number of passes of these lengths."""
@@ -687,11 +711,12 @@ def rlhf_op_window_attention(q, k, v, tiles: rlhf_attention_tiles, out, window: 
         raise ValueError(f"the sequences have {tiles.rows} rows, q has {rows}")
     if not q.dtype == k.dtype == v.dtype == out.dtype:
         raise ValueError("q, k, v and out must be of one type")
-    _on_device(q, k, v, out, tiles.tiles)
+    stream, like_q, like_k = _stream_with(q, k, v, out, tiles.tiles), (rows, qc), (rows, kc)
     _op_check(lib().rlhf_op_window_attention(
-        _act_code(q), q.data_ptr(), _matrix(q, rows, qc, "q"), k.data_ptr(), _matrix(k, rows, kc, "k"), v.data_ptr(), _matrix(v, rows, kc, "v"),
-        tiles.start.data_ptr(), tiles.q0.data_ptr(), tiles.len.data_ptr(), out.data_ptr(), _matrix(out, rows, qc, "out"), tiles.n, rows,
-        _int32(window), _int32(sinks), n_q_heads, n_kv_heads, head_dim, _stream_ptr()), "rlhf_op_window_attention")
+        _act_code(q), q.data_ptr(), _row_stride(q, like_q, "q"), k.data_ptr(), _row_stride(k, like_k, "k"), v.data_ptr(),
+        _row_stride(v, like_k, "v"), tiles.start.data_ptr(), tiles.q0.data_ptr(), tiles.len.data_ptr(), out.data_ptr(),
+        _row_stride(out, like_q, "out"), tiles.n, rows, _int32(window), _int32(sinks), n_q_heads, n_kv_heads, head_dim, stream),
+        "rlhf_op_window_attention")
 
 
 def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out, layer, n_layers, n_q_heads, n_kv_heads, head_dim, window, sinks,
@@ -700,7 +725,7 @@ def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out,
     rows, qc = q.size(0), n_q_heads * head_dim
     if q.dtype != out.dtype:
         raise ValueError("q and out must be of one type")
-    _on_device(q, pool, page_table, row_sample, ctx_len, out, scratch)
+    stream, shape = _stream_with(q, pool, page_table, row_sample, ctx_len, out, scratch), (rows, qc)
     if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
         raise ValueError("page_table must be a contiguous int32 matrix")
     n_samples, pt_stride = page_table.shape
@@ -718,9 +743,9 @@ def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out,
         elif scratch.dtype != torch.float32 or scratch.numel() < need or not scratch.is_contiguous():
             raise ValueError(f"scratch must be a contiguous float32 tensor of {need} entries")
     _op_check(getattr(L, name)(
-        _act_code(q), q.data_ptr(), _matrix(q, rows, qc, "q"), pool.data_ptr(), n_pages, page_table.data_ptr(), pt_stride, n_samples,
-        row_sample.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), _matrix(out, rows, qc, "out"), _ptr(scratch), rows, layer, nsplit, window,
-        sinks, n_layers, n_q_heads, n_kv_heads, head_dim, _stream_ptr()), name)
+        _act_code(q), q.data_ptr(), _row_stride(q, shape, "q"), pool.data_ptr(), n_pages, page_table.data_ptr(), pt_stride, n_samples,
+        row_sample.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), _row_stride(out, shape, "out"), _ptr(scratch), rows, layer, nsplit, window,
+        sinks, n_layers, n_q_heads, n_kv_heads, head_dim, stream), name)
 
 
 def rlhf_op_window_decode_attention(q, pool, page_table, row_sample, ctx_len, out, layer: int, n_layers: int, n_q_heads: int, n_kv_heads: int,
@@ -752,27 +777,29 @@ def rlhf_op_kv4_page_bytes(n_layers: int, n_kv_heads: int, head_dim: int) -> int
 def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
     """Rows of k, v [rows, n_kv_heads*head_dim] into token slots kv_dst (int32, distinct; outside the pool: left out) of the cache of 4 bits."""
     torch = _th()
-    rows, cols = kv_dst.numel(), n_kv_heads * head_dim
+    rows = kv_dst.numel()
+    shape = (rows, n_kv_heads * head_dim)
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
-    _on_device(k, v, kv_dst, pool)
+    stream = _stream_with(k, v, kv_dst, pool)
     _vector(kv_dst, rows, torch.int32, "kv_dst")
-    _op_check(lib().rlhf_op_kv4_append(_act_code(k), k.data_ptr(), _matrix(k, rows, cols, "k"), v.data_ptr(), _matrix(v, rows, cols, "v"),
+    _op_check(lib().rlhf_op_kv4_append(_act_code(k), k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"),
                                        kv_dst.data_ptr(), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), rows, layer, n_layers,
-                                       n_kv_heads, head_dim, _stream_ptr()), "rlhf_op_kv4_append")
+                                       n_kv_heads, head_dim, stream), "rlhf_op_kv4_append")
 
 
 def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
     """Token slots kv_src (int32) of the cache of 4 bits into rows of k, v (zeros for a negative slot, NaN beyond the pool)."""
     torch = _th()
-    rows, cols = kv_src.numel(), n_kv_heads * head_dim
+    rows = kv_src.numel()
+    shape = (rows, n_kv_heads * head_dim)
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
-    _on_device(k, v, kv_src, pool)
+    stream = _stream_with(k, v, kv_src, pool)
     _vector(kv_src, rows, torch.int32, "kv_src")
     _op_check(lib().rlhf_op_kv4_read(_act_code(k), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), kv_src.data_ptr(), k.data_ptr(),
-                                     _matrix(k, rows, cols, "k"), v.data_ptr(), _matrix(v, rows, cols, "v"), rows, layer, n_layers, n_kv_heads, head_dim,
-                                     _stream_ptr()), "rlhf_op_kv4_read")
+                                     _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), rows, layer, n_layers, n_kv_heads, head_dim,
+                                     stream), "rlhf_op_kv4_read")
 
 
 def rlhf_op_kv4_decode_attention(q, pool, page_table, row_sample, ctx_len, out, layer: int, n_layers: int, n_q_heads: int, n_kv_heads: int,
