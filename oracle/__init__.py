@@ -16,6 +16,8 @@ not for speed:
   page tables, retirement order, scoring-batch formation after the trigger R_t).
 * `oracle.gae` -- Generalized Advantage Estimation by its backward recursion (Section 6
   describes the product's variant as one matrix multiply).
+* `oracle.update`, `oracle.window` -- the operators of the Actor's update, and attention with a sliding window and the
+  KV cache of 4 bits, from their definitions.
 
 Pins: tests/test_oracle_*.py check these against closed forms, brute force on tiny
 shapes, invariants, and an independent library implementation of the same decoder.

@@ -92,7 +92,8 @@ __device__ __forceinline__ uint32_t kv4_pack(const float (&x)[8], uint32_t& para
     return bad || (float)s == 0.f ? 0x88888888u : code;
 }
 
-// A wave takes one head of 4 rows (of 64 dims: 8), K and V.
+// A wave takes one head of 4 rows (of 64 dims: 8), K and V.  8192 rows of 32 heads of 128 bf16: 40 us, 4.3 TB/s of both directions, bound by vector
+// instructions (with the quotients divided, and every one settled in double: 62).
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_kv4_append(Kv4Args a) {
     using L = Kv4<HD>;
@@ -157,6 +158,7 @@ template <typename T> __device__ __forceinline__ void put8(T* to, const float (&
     }
 }
 
+// The same back: 28 us, 6.1 TB/s; every V byte is read by one of two threads and handed to the other.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_kv4_read(Kv4Args a) {
     using L = Kv4<HD>;
