@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
         else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         __syncthreads();                           // tile j is there, and nobody reads tile j - 1 any more
         if (j > 0 && j + 1 < keys.n) fetch(keys.at(j + 1), buf ^ 1);
-        if (first > w0 + 31 || (last <= w0 - a.window && first >= a.sinks)) continue;       // nothing that this wave sees
+        if (w0 >= len || first > w0 + 31 || (last <= w0 - a.window && first >= a.sinks)) continue;       // nothing that this wave sees
         f32x4_t s[NF][2];
 #pragma unroll
         for (int f = 0; f < NF; ++f)
