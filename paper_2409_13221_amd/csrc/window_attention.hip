@@ -51,21 +51,25 @@ __device__ void window_row(const WindowArgs& a, int s0, int i, int h, int lane) 
     for (int e = 0; e < D; ++e) o[e * 64 + lane] = round_to<T>(acc[e] / l);
 }
 
-// Whether a tile lies within the rows of the call; what it covers.
-__device__ __forceinline__ bool tile_of(const WindowArgs& a, int tile, int& s0, int& q0, int& len) {
+// Whether a tile lies within the rows of the call and has queries from `part` on; what it covers.
+__device__ __forceinline__ bool tile_of(const WindowArgs& a, int tile, int part, int& s0, int& q0, int& len) {
     s0 = a.tile_start[tile];
     q0 = a.tile_q0[tile];
     len = a.tile_len[tile];
-    return s0 >= 0 && q0 >= 0 && len <= a.rows - s0 && q0 < len;
+    if (s0 < 0 || q0 < 0 || len > a.rows - s0 || q0 >= len) return false;
+    q0 += part;
+    return q0 < len;
 }
 
-// Workgroup -> (tile, query head).  Units of a tile and KV head, whose query heads share K and V, go to the XCDs in turn, so that keys are read into one
-// L2; the last tiles, with the most keys, come first (units side by side: 16384 tokens 1808 -> 1988 us, 2 x 8192 of 32 / 8 heads, window
-// 1024 293 -> 318; tiles from the first: 8192 tokens of 32 heads 542 -> 642).
-__device__ __forceinline__ bool window_work(const WindowArgs& a, int& tile, int& h) {
-    const unsigned G = a.n_q_heads / a.n_kv_heads, i = blockIdx.x / 8, unit = i / G * 8 + blockIdx.x % 8;
+// Workgroup -> (tile, first query in it, query head).  Units of a tile and KV head, whose query heads share K and V, go to the XCDs in turn, so that
+// keys are read into one L2; the last tiles, with the most keys, come first (units side by side: 16384 tokens 1808 -> 1988 us, 2 x 8192 of
+// 32 / 8 heads, window 1024 293 -> 318; tiles from the first: 8192 tokens of 32 heads 542 -> 642).
+template <int QUERIES> __device__ __forceinline__ bool window_work(const WindowArgs& a, int& tile, int& part, int& h) {
+    constexpr unsigned PARTS = kFlashTile / QUERIES;
+    const unsigned G = a.n_q_heads / a.n_kv_heads, all = blockIdx.x / 8, i = all / PARTS, unit = i / G * 8 + blockIdx.x % 8;
     if (unit >= (unsigned)a.n_tiles * (unsigned)a.n_kv_heads) return false;
     tile = a.n_tiles - 1 - (int)(unit / a.n_kv_heads);
+    part = (int)(PARTS - 1 - all % PARTS) * QUERIES;
     h = (int)(unit % a.n_kv_heads * G + i % G);
     return true;
 }
@@ -89,7 +93,7 @@ __device__ __forceinline__ uint32_t lds_address(void* p) { return (uint32_t)(siz
 // flight before it reads LDS; whoever reads waits for vmcnt and the workgroup first.  (It has no register to come back to; m0 has no other use in
 // these kernels.)
 __device__ __forceinline__ void load_to_lds(u32x4_t base, uint32_t lane, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(to), "v"(lane), "s"(base), "s"(offset) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane), "s"(base), "s"(offset) : "memory");
 }
 __device__ __forceinline__ u32x4_t buffer_base(const void* p) {
     return u32x4_t{(uint32_t)(uintptr_t)p, (uint32_t)((uintptr_t)p >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00020000u};
@@ -114,8 +118,8 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     constexpr int KT = 32, NF = KT / 16, NU = KT / 32, KS = HD / 32, DF = HD / 16, CH = HD / 8, ROWS = 64 / CH, LOADS = KT / (4 * ROWS), TILE = KT * HD;
     constexpr float START = M::TOP > 0.f ? 6.f : 0.f, MOST = M::TOP > 0.f ? M::TOP : 20.f;      // log2 of the greatest weight at a new reference, and ever
     __shared__ __attribute__((aligned(16))) T sK[2][TILE], sV[2][TILE];
-    int tile, h, s0, q0, len;
-    if (!window_work(a, tile, h) || !tile_of(a, tile, s0, q0, len)) return;
+    int tile, part, h, s0, q0, len;
+    if (!window_work<kFlashTile>(a, tile, part, h) || !tile_of(a, tile, part, s0, q0, len)) return;
     const int kh = h / (a.n_q_heads / a.n_kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     constexpr float unit = kScoreUnit<HD>;
@@ -262,32 +266,36 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
         for (int i = w0; i < min(w0 + 32, len); ++i) window_row<T, HD>(a, s0, i, h, lane);
 }
 
-// Float: 128 queries of a head a workgroup, 16 a wave, against 16 keys at a time, which go to LDS a tile ahead; bound by the float matrix rate (a tenth
+// Float: 128 or 64 queries of a head a workgroup, 16 a wave, against 16 keys at a time, which go to LDS a tile ahead; bound by the float matrix rate (a tenth
 // of the half one).  What is hidden is kept out as above.  8192 tokens of 64 / 8 heads of 128, window 1024: 2.11 ms, 123 TFLOP/s with the hidden part of
-// the tiles (waves that read keys from memory for themselves: 3.29); 16 sequences of 200-800, 32 heads, window 256: 313 us (456).
-template <int HD>
-__global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
-    constexpr int KT = 16, D = HD / 16, CH = HD / 4, ROWS = 64 / CH, WAVES_EACH = KT / ROWS, TILE = KT * HD;       // WAVES_EACH: waves that load a tile of K
+// the tiles (waves that read keys from memory for themselves: 3.29); 16 sequences of 200-800, 32 heads, window 256: 288 us (456).
+// Four waves where tiles are mostly full: twice as many workgroups, nearer to each other in length (2 x 767, 8 heads of 128: 106 us with eight, 71 with
+// four; 2000 tokens of 32 heads 363, 316; 4 x 4096, 12 of 64, window 1024 457, 409; two instead of four: 104, 404, 433); of short sequences the
+// second half would be empty (256 of 20-60, 32 heads of 128 165, 228; 32 of 100, 40 of 64 42.6, 44.7).
+template <int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 4) void k_window_float(WindowArgs a) {
+    constexpr int KT = 16, D = HD / 16, CH = HD / 4, ROWS = 64 / CH, EACH = KT / ROWS, LOADS = 2 * EACH / WAVES, TILE = KT * HD, QUERIES = 16 * WAVES;
     __shared__ __attribute__((aligned(16))) float sK[2][TILE], sV[2][TILE];
-    int tile, h, s0, q0, len;
-    if (!window_work(a, tile, h) || !tile_of(a, tile, s0, q0, len)) return;
+    int tile, part, h, s0, q0, len;
+    if (!window_work<QUERIES>(a, tile, part, h) || !tile_of(a, tile, part, s0, q0, len)) return;
     const int kh = h / (a.n_q_heads / a.n_kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     const int w0 = q0 + wave * 16;
     const float* kb = (const float*)a.k + (size_t)s0 * a.ld_k + (size_t)kh * HD;
     const float* vb = (const float*)a.v + (size_t)s0 * a.ld_v + (size_t)kh * HD;
     constexpr float unit = kScoreUnit<HD>;
-    // Place p of row t of K holds 16-byte piece p ^ t, so that a piece of 16 rows spreads over the banks; V lies as it is.  Of 64 dims half the waves load K, the
-    // other half V.
-    const int lw = wave % WAVES_EACH, lrow = lw * ROWS + lane / CH, place = lane % CH;
-    const bool loads_k = wave < WAVES_EACH, loads_v = WAVES_EACH == 8 || !loads_k;
+    // Place p of row t of K holds 16-byte piece p ^ t, so that a piece of 16 rows spreads over the banks; V lies as it is.  A load of a wave fills ROWS rows; of
+    // the 2 EACH loads of a tile, K first, a wave takes every WAVES-th.
     const auto fetch = [&](int kt, int buf) {
-        const uint32_t row = min(lrow, len - 1 - kt * KT);           // rows behind the sequence: its last one
-        if (loads_k)
-            load_to_lds(buffer_base(kb + (size_t)kt * KT * a.ld_k), row * (uint32_t)a.ld_k * 4 + (place ^ lrow) * 16, 0, lds_address(&sK[buf][lw * ROWS * HD]));
-        if (loads_v) load_to_lds(buffer_base(vb + (size_t)kt * KT * a.ld_v), row * (uint32_t)a.ld_v * 4 + place * 16, 0, lds_address(&sV[buf][lw * ROWS * HD]));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int load = wave + i * WAVES, first = load % EACH * ROWS, row = first + lane / CH, place = lane % CH;
+            const uint32_t at = min(row, len - 1 - kt * KT);         // rows behind the sequence: its last one
+            if (load < EACH) load_to_lds(buffer_base(kb + (size_t)kt * KT * a.ld_k), at * (uint32_t)a.ld_k * 4 + (place ^ row) * 16, 0, lds_address(&sK[buf][first * HD]));
+            else load_to_lds(buffer_base(vb + (size_t)kt * KT * a.ld_v), at * (uint32_t)a.ld_v * 4 + place * 16, 0, lds_address(&sV[buf][first * HD]));
+        }
     };
-    const KeyTiles<KT> keys(q0, min(q0 + kFlashTile, len) - 1, a.window, a.sinks);
+    const KeyTiles<KT> keys(q0, min(q0 + QUERIES, len) - 1, a.window, a.sinks);
     fetch(keys.at(0), 0);
     FloatQuery<HD> q;
     q.load((const float*)a.q + (size_t)(s0 + min(w0 + n, len - 1)) * a.ld_q + (size_t)h * HD, c);
@@ -345,32 +353,41 @@ __global__ __launch_bounds__(512, 4) void k_window_float(WindowArgs a) {
         for (int i = w0; i < min(w0 + 16, len); ++i) window_row<float, HD>(a, s0, i, h, lane);
 }
 
-template <typename T>
-static hipError_t window_typed(hipStream_t st, int head_dim, const WindowArgs& a) {
-    constexpr int THREADS = sizeof(T) == 4 ? 512 : 256;
-    const int most = (int)std::min<int64_t>((kLaunchThreads / THREADS - 8 * a.n_q_heads) / a.n_q_heads, 1 << 30);
+// A pass in launches of fewer than 2^32 threads, 128 / QUERIES workgroups of THREADS a tile and query head.
+template <int QUERIES, int THREADS, typename F>
+static hipError_t window_launches(const WindowArgs& a, F start) {
+    constexpr int PARTS = kFlashTile / QUERIES;
+    const int each = PARTS * a.n_q_heads, most = (int)std::min<int64_t>((kLaunchThreads / THREADS - 8 * each) / each, 1 << 30);
     for (int first = 0; first < a.n_tiles; first += most) {
         WindowArgs p = a;
         p.tile_start += first;
         p.tile_q0 += first;
         p.tile_len += first;
         p.n_tiles = std::min(most, a.n_tiles - first);
-        const unsigned blocks = ((unsigned)p.n_tiles * (unsigned)a.n_kv_heads + 7) / 8 * 8 * (unsigned)(a.n_q_heads / a.n_kv_heads);
-        if constexpr (sizeof(T) == 4) {
-            if (head_dim == 128) k_window_float<128><<<blocks, 512, 0, st>>>(p);
-            else k_window_float<64><<<blocks, 512, 0, st>>>(p);
-        } else {
-            if (head_dim == 128) k_window_flash<T, 128><<<blocks, 256, 0, st>>>(p);
-            else k_window_flash<T, 64><<<blocks, 256, 0, st>>>(p);
-        }
+        start(((unsigned)p.n_tiles * (unsigned)a.n_kv_heads + 7) / 8 * 8 * (unsigned)(a.n_q_heads / a.n_kv_heads) * PARTS, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+template <int HD> static hipError_t window_float(hipStream_t st, const WindowArgs& a) {
+    if (a.rows > 96ll * a.n_tiles)
+        return window_launches<64, 256>(a, [&](unsigned grid, const WindowArgs& p) { k_window_float<HD, 4><<<grid, 256, 0, st>>>(p); });
+    return window_launches<128, 512>(a, [&](unsigned grid, const WindowArgs& p) { k_window_float<HD, 8><<<grid, 512, 0, st>>>(p); });
+}
+
+template <typename T, int HD> static hipError_t window_typed(hipStream_t st, const WindowArgs& a) {
+    if constexpr (sizeof(T) == 4) return window_float<HD>(st, a);
+    else return window_launches<128, 256>(a, [&](unsigned grid, const WindowArgs& p) { k_window_flash<T, HD><<<grid, 256, 0, st>>>(p); });
+}
+
+template <typename T> static hipError_t window_dims(hipStream_t st, int head_dim, const WindowArgs& a) {
+    return head_dim == 128 ? window_typed<T, 128>(st, a) : window_typed<T, 64>(st, a);
+}
+
 hipError_t launch_window_attention(hipStream_t st, int dtype, int head_dim, const WindowArgs& a) {
-    return dtype == kBF16 ? window_typed<bf16_t>(st, head_dim, a) : dtype == kF16 ? window_typed<f16_t>(st, head_dim, a) : window_typed<float>(st, head_dim, a);
+    return dtype == kBF16 ? window_dims<bf16_t>(st, head_dim, a) : dtype == kF16 ? window_dims<f16_t>(st, head_dim, a) : window_dims<float>(st, head_dim, a);
 }
 
 }  // namespace rlhf
