@@ -664,9 +664,31 @@ __global__ __launch_bounds__(256) void k_window_join(WindowDecodeArgs a) {
     for (int e = 0; e < 4; ++e) o[e] = round_to<T>(empty ? 0.f : x[e] / s_l);
 }
 
-// Waves of a workgroup over a plain cache; four where 16 heads' sums of eight would take more than 64 KB of LDS.  (Four for all: 64 rows of 300-2560, 32 heads
-// of 128 164 us instead of 160, 16 rows of 2000, 12 heads of 64 25.5 instead of 22.4.)
-static int decode_waves(int group) { return group > 8 ? 4 : 8; }
+// Pages that a row may see.
+static int64_t visible_pages(int64_t max_pages, int window, int sinks) {
+    return std::min<int64_t>(max_pages, (sinks + 15ll) / 16 + (window + 15ll) / 16 + 1);
+}
+// Workgroups of a call in one part.
+static int64_t decode_blocks(int rows, int n_q_heads, int n_kv_heads) { return (int64_t)rows * n_kv_heads * ((n_q_heads / n_kv_heads + 15) / 16); }
+
+// Waves of a workgroup over a plain cache: most where contexts are long, four where 16 heads' sums of eight would take more than 64 KB of LDS.
+static int most_waves(int group) { return group > 8 ? 4 : 8; }
+// Eight with 64 pages and more to a row or in parts, four below, and one where eight pages or fewer meet workgroups enough to fill the chip: starting idle
+// waves then costs more than the pages (95 rows of 15-50 tokens, 32 heads of 128: 8 waves 29.4 us, 4 19.8, 1 14.3; 64 rows of 128 tokens 36, 26.4,
+// 25.2; 16 rows of 500 28.3, 26.3, 31.3; 16 rows of 2000, 12 heads of 64 26.1, 26.7, 62).
+static int decode_waves(const WindowDecodeArgs& a) {
+    const int group = a.n_q_heads / a.n_kv_heads;
+    const int64_t pages = visible_pages(a.pt_stride, a.window, a.sinks), blocks = decode_blocks(a.rows, a.n_q_heads, a.n_kv_heads);
+    if (a.nsplit > 1 || pages >= 64) return most_waves(group);
+    return pages <= 8 && blocks >= 1024 ? 1 : 4;
+}
+// Four over 4 bits, or one where workgroups fill the chip and rows are short, or there are so many that long and short ones even out (64 rows of 256 tokens, 32
+// heads of 128: 4 waves 29.4 us, 1 18.2; 64 rows of 300-2560, window 1024 60, 53; 256 rows of 16-2048 238, 208; but 64 rows of 512-4096 138,
+// 147, and 16 rows of 500 12.3, 13.4).  Eight: 64 rows of 512-4096 121 us where four take 115, 131072 tokens 47, 38.
+static int kv4_waves(const WindowDecodeArgs& a) {
+    const int64_t blocks = decode_blocks(a.rows, a.n_q_heads, a.n_kv_heads);
+    return a.nsplit == 1 && ((blocks >= 1024 && visible_pages(a.pt_stride, a.window, a.sinks) <= 96) || blocks >= 4096) ? 1 : 4;
+}
 
 // Into how many parts the visible pages of a row are cut: none below 6 pages a wave, where joining costs more than it gives (two rows of 12 heads of
 // 64, 700 tokens 7.5 us in one part, 7.8 in four; 1000 tokens 9.2 and 8.2); else a power of two, which leaves the parts of a row's heads on as few XCDs as
@@ -674,9 +696,9 @@ static int decode_waves(int group) { return group > 8 ? 4 : 8; }
 // 8 KV heads, 2000 tokens: 4 parts 15.8 us, 2 21.7, 8 17.2), or 4096 with 32 pages a wave and more (one row of 131072 tokens in 4 bits, 8 KV
 // heads: 64 parts 39 us, 32 44).
 int window_decode_nsplit(int rows, int n_q_heads, int n_kv_heads, int max_ctx, int window, int sinks) {
-    const int64_t pages = std::min<int64_t>((max_ctx + 15ll) / 16, (sinks + 15ll) / 16 + (window + 15ll) / 16 + 1);
-    const int group = n_q_heads / n_kv_heads, waves = decode_waves(group);
-    const int64_t all = (int64_t)rows * n_kv_heads * ((group + 15) / 16) * waves;       // in one part each
+    const int64_t pages = visible_pages((max_ctx + 15ll) / 16, window, sinks);
+    const int waves = most_waves(n_q_heads / n_kv_heads);
+    const int64_t all = decode_blocks(rows, n_q_heads, n_kv_heads) * waves;
     if (pages < 6 * waves) return 1;
     int n = 1;
     while (n < 64 && 2 * n * waves <= pages && 2 * n * all <= (pages >= 32 * n * waves ? 4096 : 2048)) n *= 2;
@@ -690,7 +712,7 @@ size_t window_decode_scratch_floats(int rows, int n_q_heads, int head_dim, int n
 // The rows in turns of what one launch holds: `start` launches `blocks` workgroups of `waves` waves a row.
 template <typename T, int HD, typename F>
 static hipError_t in_turns(hipStream_t st, const WindowDecodeArgs& a, int waves, F start) {
-    const int64_t blocks = (int64_t)a.n_kv_heads * ((a.n_q_heads / a.n_kv_heads + 15) / 16) * a.nsplit;
+    const int64_t blocks = decode_blocks(1, a.n_q_heads, a.n_kv_heads) * a.nsplit;
     const int most = (int)std::min<int64_t>(kLaunchThreads / (64 * waves) / std::max<int64_t>(blocks, a.n_q_heads), 1 << 24);
     for (int first = 0; first < a.rows; first += most) {
         WindowDecodeArgs p = a;
@@ -710,18 +732,18 @@ static hipError_t in_turns(hipStream_t st, const WindowDecodeArgs& a, int waves,
 
 template <typename C>
 static hipError_t decode_rows(hipStream_t st, const WindowDecodeArgs& a) {
-    const int group = a.n_q_heads / a.n_kv_heads, waves = decode_waves(group);
-    const size_t lds = (size_t)waves * std::min(16, group) * (C::HD + 2) * sizeof(float);
+    const int waves = decode_waves(a);
+    const size_t lds = (size_t)waves * std::min(16, a.n_q_heads / a.n_kv_heads) * (C::HD + 2) * sizeof(float);
     return in_turns<typename C::T, C::HD>(st, a, waves, [&](unsigned grid, const WindowDecodeArgs& p) {
         if (waves == 8) k_window_decode<C, 8><<<grid, 512, lds, st>>>(p);
-        else k_window_decode<C, 4><<<grid, 256, lds, st>>>(p);
+        else if (waves == 4) k_window_decode<C, 4><<<grid, 256, lds, st>>>(p);
+        else k_window_decode<C, 1><<<grid, 64, lds, st>>>(p);
     });
 }
 
-template <typename T, int HD>
-static hipError_t kv4_rows(hipStream_t st, const WindowDecodeArgs& a) {
+template <typename T, int HD, int WAVES>
+static hipError_t kv4_typed(hipStream_t st, const WindowDecodeArgs& a) {
     const int group = a.n_q_heads / a.n_kv_heads;
-    constexpr int WAVES = 4;                       // eight: 64 rows of 512-4096, 32 heads of 128 121 us instead of 115, 131072 tokens 47 instead of 38
     const size_t sums = (size_t)WAVES * std::min(16, group) * (HD + 2) * sizeof(float), weights = (size_t)WAVES * (sizeof(T) == 4 ? 2 : 1) * (HD / 64) * 512;
     const size_t lds = std::max(sums, weights);
     return in_turns<T, HD>(st, a, WAVES, [&](unsigned grid, const WindowDecodeArgs& p) {
@@ -730,6 +752,11 @@ static hipError_t kv4_rows(hipStream_t st, const WindowDecodeArgs& a) {
         else if (group <= 8) k_kv4_decode<T, HD, 2, 4, WAVES><<<grid, WAVES * 64, lds, st>>>(p);
         else k_kv4_decode<T, HD, 1, 4, WAVES><<<grid, WAVES * 64, lds, st>>>(p);
     });
+}
+
+template <typename T, int HD>
+static hipError_t kv4_rows(hipStream_t st, const WindowDecodeArgs& a) {
+    return kv4_waves(a) == 1 ? kv4_typed<T, HD, 1>(st, a) : kv4_typed<T, HD, 4>(st, a);
 }
 
 hipError_t launch_window_decode(hipStream_t st, int dtype, bool four_bits, int head_dim, const WindowDecodeArgs& a) {

@@ -344,6 +344,18 @@ def test_decode_many_rows(four, dtype):
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(2, 2, 128), (4, 2, 64), (12, 2, 128), (36, 2, 64), (8, 1, 128)])
+def test_decode_many_short_rows(four, dtype, Hq, Hkv, hd):
+    """Rows enough to fill the chip with a wave each: contexts of up to 7 pages, of which at most 5 are seen, and all of them."""
+    r = np.random.default_rng(1)
+    rows = 1030 // Hkv
+    p = Paged(17, r.integers(-1, 112, rows).tolist(), Hq, Hkv, hd, dtype, four)
+    for window, sinks in ((40, 5), (ALL, 0)):
+        p.check(p.run(window, sinks), window, sinks, rows=range(0, rows, 41))
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
 @pytest.mark.parametrize("nsplit", [1, 2])
 def test_decode_pages_without_a_visible_token_are_not_read(four, nsplit):
     """Their entries point outside the pool, or at pages of NaN."""
