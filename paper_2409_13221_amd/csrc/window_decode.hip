@@ -682,12 +682,14 @@ static int decode_waves(const WindowDecodeArgs& a) {
     if (a.nsplit > 1 || pages >= 64) return most_waves(group);
     return pages <= 8 && blocks >= 1024 ? 1 : 4;
 }
-// Four over 4 bits, or one where workgroups fill the chip and rows are short, or there are so many that long and short ones even out (64 rows of 256 tokens, 32
-// heads of 128: 4 waves 29.4 us, 1 18.2; 64 rows of 300-2560, window 1024 60, 53; 256 rows of 16-2048 238, 208; but 64 rows of 512-4096 138,
-// 147, and 16 rows of 500 12.3, 13.4).  Eight: 64 rows of 512-4096 121 us where four take 115, 131072 tokens 47, 38.
+// Four over 4 bits; where workgroups fill the chip one for short rows, and two for longer ones, or where there are so many that long and short ones even out
+// (64 rows of 256 tokens, 32 heads of 128: 4 waves 29.4 us, 2 21.6, 1 18.2; 136 rows of 40-4072, 64 / 8 heads, window 587, float 48.5, 46.5,
+// 51.6; 256 rows of 16-2048, 32 heads 238, 202, 208; but 64 rows of 512-4096 138, 147, 147, and 16 rows of 500 12.3, 12.4, 13.4).  Eight:
+// 64 rows of 512-4096 121 us where four take 115, 131072 tokens 47, 38.
 static int kv4_waves(const WindowDecodeArgs& a) {
-    const int64_t blocks = decode_blocks(a.rows, a.n_q_heads, a.n_kv_heads);
-    return a.nsplit == 1 && ((blocks >= 1024 && visible_pages(a.pt_stride, a.window, a.sinks) <= 96) || blocks >= 4096) ? 1 : 4;
+    const int64_t pages = visible_pages(a.pt_stride, a.window, a.sinks), blocks = decode_blocks(a.rows, a.n_q_heads, a.n_kv_heads);
+    if (a.nsplit > 1 || blocks < 1024) return 4;
+    return pages <= 32 ? 1 : pages <= 96 || blocks >= 4096 ? 2 : 4;
 }
 
 // Into how many parts the visible pages of a row are cut: none below 6 pages a wave, where joining costs more than it gives (two rows of 12 heads of
@@ -756,7 +758,8 @@ static hipError_t kv4_typed(hipStream_t st, const WindowDecodeArgs& a) {
 
 template <typename T, int HD>
 static hipError_t kv4_rows(hipStream_t st, const WindowDecodeArgs& a) {
-    return kv4_waves(a) == 1 ? kv4_typed<T, HD, 1>(st, a) : kv4_typed<T, HD, 4>(st, a);
+    const int waves = kv4_waves(a);
+    return waves == 1 ? kv4_typed<T, HD, 1>(st, a) : waves == 2 ? kv4_typed<T, HD, 2>(st, a) : kv4_typed<T, HD, 4>(st, a);
 }
 
 hipError_t launch_window_decode(hipStream_t st, int dtype, bool four_bits, int head_dim, const WindowDecodeArgs& a) {

@@ -355,6 +355,16 @@ def test_decode_many_short_rows(four, dtype, Hq, Hkv, hd):
         p.check(p.run(window, sinks), window, sinks, rows=range(0, rows, 41))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "half"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(8, 8, 128), (32, 8, 64), (48, 8, 64), (72, 8, 64)])
+def test_four_bits_many_longer_rows(dtype, Hq, Hkv, hd):
+    """Rows of up to 40 pages, two waves each."""
+    r = np.random.default_rng(2)
+    p = Paged(18, (r.integers(0, 640, 128) * (r.random(128) < 0.3)).tolist() + [640], Hq, Hkv, hd, dtype, True)
+    for window, sinks in ((600, 5), (ALL, 0)):
+        p.check(p.run(window, sinks), window, sinks, rows=[*range(0, 128, 13), 128])
+
+
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
 @pytest.mark.parametrize("nsplit", [1, 2])
 def test_decode_pages_without_a_visible_token_are_not_read(four, nsplit):
