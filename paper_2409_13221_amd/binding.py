@@ -675,6 +675,12 @@ def _row_stride(t, shape: tuple, what: str) -> int:
     return ld if rows > 1 else cols
 
 
+def _indices(t, n: int, what: str) -> None:
+    """_vector of int32."""
+    if t.shape != (n,) or t.dtype != _th().int32 or t.stride() != (1,):
+        _vector(t, n, _th().int32, what)         # a contiguous tensor of n entries in another shape will do
+
+
 class rlhf_attention_tiles:
     """The plan of a packed pass for rlhf_op_window_attention: sequences of seq_lens rows, back to back (a length may be 0), cut into
     tiles of 128 queries.  One plan serves all layers and any number of passes of these lengths."""
@@ -729,8 +735,8 @@ def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out,
     if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
         raise ValueError("page_table must be a contiguous int32 matrix")
     n_samples, pt_stride = page_table.shape
-    _vector(row_sample, rows, torch.int32, "row_sample")
-    _vector(ctx_len, rows, torch.int32, "ctx_len")
+    _indices(row_sample, rows, "row_sample")
+    _indices(ctx_len, rows, "ctx_len")
     L = lib()
     window, sinks = _int32(window), _int32(sinks)
     if nsplit is None:
@@ -762,11 +768,11 @@ def rlhf_op_window_decode_attention(q, pool, page_table, row_sample, ctx_len, ou
 
 
 def _kv4_pages(pool, n_layers: int, n_kv_heads: int, head_dim: int) -> int:
-    torch = _th()
-    page = lib().rlhf_op_kv4_page_bytes(n_layers, n_kv_heads, head_dim)
-    if page == 0 or pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() % page:
+    page = 18 * head_dim * n_kv_heads * n_layers                   # rlhf_op_kv4_page_bytes, which costs 0.2 us to ask
+    pages, rest = divmod(pool.numel(), page) if page > 0 else (0, 1)
+    if rest or pool.dtype != _th().uint8 or not pool.is_contiguous():
         raise ValueError(f"pool must be whole contiguous pages of {page} bytes (uint8)")
-    return pool.numel() // page
+    return pages
 
 
 def rlhf_op_kv4_page_bytes(n_layers: int, n_kv_heads: int, head_dim: int) -> int:
@@ -776,13 +782,12 @@ def rlhf_op_kv4_page_bytes(n_layers: int, n_kv_heads: int, head_dim: int) -> int
 
 def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
     """Rows of k, v [rows, n_kv_heads*head_dim] into token slots kv_dst (int32, distinct; outside the pool: left out) of the cache of 4 bits."""
-    torch = _th()
     rows = kv_dst.numel()
     shape = (rows, n_kv_heads * head_dim)
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
     stream = _stream_with(k, v, kv_dst, pool)
-    _vector(kv_dst, rows, torch.int32, "kv_dst")
+    _indices(kv_dst, rows, "kv_dst")
     _op_check(lib().rlhf_op_kv4_append(_act_code(k), k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"),
                                        kv_dst.data_ptr(), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), rows, layer, n_layers,
                                        n_kv_heads, head_dim, stream), "rlhf_op_kv4_append")
@@ -790,13 +795,12 @@ def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads
 
 def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
     """Token slots kv_src (int32) of the cache of 4 bits into rows of k, v (zeros for a negative slot, NaN beyond the pool)."""
-    torch = _th()
     rows = kv_src.numel()
     shape = (rows, n_kv_heads * head_dim)
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
     stream = _stream_with(k, v, kv_src, pool)
-    _vector(kv_src, rows, torch.int32, "kv_src")
+    _indices(kv_src, rows, "kv_src")
     _op_check(lib().rlhf_op_kv4_read(_act_code(k), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), kv_src.data_ptr(), k.data_ptr(),
                                      _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), rows, layer, n_layers, n_kv_heads, head_dim,
                                      stream), "rlhf_op_kv4_read")
