@@ -121,8 +121,9 @@ int rlhf_op_flash_attention(const void* q, const void* k, const void* v, const i
  * and the first `sinks` ones.  window >= 1, sinks >= 0; a window of at least the longest context (INT32_MAX will do) is causal attention.
  * Scores are scaled by 1/sqrt(head_dim).  head_dim 64 or 128, n_q_heads a multiple of n_kv_heads (query head h reads KV head
  * h / (n_q_heads / n_kv_heads)).  act_dtype: RLHF_FP32, RLHF_BF16 or 2 = IEEE half, of all matrices of a call.  Scores, softmax and sums are
- * float; 16-bit outputs are rounded once.  Matrices have rows of their own stride (ld_*, elements); addresses and strides are
- * multiples of 16 bytes.  What a query does not see does not reach it, whatever it holds (infinities and NaN too).  At most 2^30 rows
+ * float.  In 16-bit calls a weight is rounded once for its product with V: in the packed form to the type (outputs are divided by the sum of the rounded
+ * weights, and off by up to half a step of how far the visible values lie apart), over a cache of 4 bits, times the scale of a token's values, to half;
+ * outputs are rounded once.  Matrices have rows of their own stride (ld_*, elements); addresses and strides are multiples of 16 bytes.  What a query does not see does not reach it, whatever it holds (infinities and NaN too).  At most 2^30 rows
  * (decode 2^24), 2^16 heads and layers, fewer than 2^27 pages. */
 
 /* Packed causal attention of a pass with a window: q, out [rows, n_q_heads*head_dim], k, v [rows, n_kv_heads*head_dim], e.g. columns

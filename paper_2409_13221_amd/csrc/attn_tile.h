@@ -27,8 +27,10 @@ __device__ __forceinline__ float column_sum(float x) {
 
 template <typename T> struct Matrix16;
 template <> struct Matrix16<f16_t> {
-    // Weights of up to 2^14: what half loses below its normal range is 2^-39 of the greatest.
+    // Weights of up to 2^14, the greatest of them at least 2^6 (where a reference starts): half a step below half's normal range, 2^-25, is at most
+    // 2^-31 of the greatest.
     static constexpr float TOP = 14.f;
+    static constexpr uint32_t ONES = 0x3C003C00u;
     static __device__ __forceinline__ f32x4_t qk(u32x4_t a, u32x4_t b, f32x4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
     }
@@ -38,6 +40,7 @@ template <> struct Matrix16<f16_t> {
 };
 template <> struct Matrix16<bf16_t> {
     static constexpr float TOP = 0.f;
+    static constexpr uint32_t ONES = 0x3F803F80u;
     static __device__ __forceinline__ f32x4_t qk(u32x4_t a, u32x4_t b, f32x4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
     }

@@ -111,7 +111,9 @@ constexpr float kFarthest = 0x1p24f;
 // 32 keys leave registers for three workgroups a compute unit, 64 for two (64 instead: 16384 tokens 1808 -> 1871 us, 16 sequences of 200-800 85 -> 90; heads
 // of 64 gain with long contexts, 4 x 4096 162 -> 150, and lose with short ones, 40 of 1-700 30.5 -> 31.6).
 // 16384 tokens of 64 / 8 heads of 128, window 4096: 1.79 ms, 1.08 PFLOP/s of visible keys, the chip at its power limit (1.6 to 1.9 GHz).
-// 16 sequences of 200-800, window 256: 80 us, 3.3 TB/s where a copy reaches 4.7.  Weights go to the matrix units rounded once to the type.
+// 16 sequences of 200-800, window 256: 80 us, 3.3 TB/s where a copy reaches 4.7.  Weights go to the matrix units rounded once to the type, of which an
+// output is off by up to half a step of the values' spread (two terms would cost as many products again); what it is divided by is the sum of the rounded
+// weights, by the matrix units too, so that equal values come out as they are.
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     using M = Matrix16<T>;
@@ -167,7 +169,8 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     for (int d = 0; d < DF; ++d)
 #pragma unroll
         for (int m = 0; m < 2; ++m) o[d][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float ref[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
+    f32x4_t l[2] = {};                             // sums of the weights, in every row of the product
+    float ref[2] = {-1e30f, -1e30f};
     bool far = false;
     // Token (modulo 16) of a lane's reads of V.  Sums d and d + 1 (even d) of a lane are dims 16 d + 8 c .. + 7, so that it stores 16 bytes at a time (16
     // sequences of 200-800, 32 heads of 128, window 1: 62.6 -> 58.4 us, 4.5 TB/s).
@@ -232,10 +235,13 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
                 float w[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(fmaf(s[f][m][r], unit, -ref[m]));
-                l[m] += (w[0] + w[1]) + (w[2] + w[3]);
                 p[m][f >> 1][(f & 1) * 2] = pack2<T>(w[0], w[1]);
                 p[m][f >> 1][(f & 1) * 2 + 1] = pack2<T>(w[2], w[3]);
             }
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) l[m] = M::qk(u32x4_t{M::ONES, M::ONES, M::ONES, M::ONES}, p[m][u], l[m]);
 #pragma unroll
         for (int d = 0; d < DF; ++d)
 #pragma unroll
@@ -251,7 +257,7 @@ __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     float odd = 0.f;                               // not a number where a result is not finite
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        const float inv = 1.f / column_sum(l[m]);
+        const float inv = 1.f / l[m][0];
         const int i = w0 + m * 16 + n;
         if (i >= len) continue;
         T* out = (T*)a.out + (size_t)(s0 + i) * a.ld_out + (size_t)h * HD + 8 * c;

@@ -190,6 +190,20 @@ def test_packed_scores_of_2_to_the_30(dtype, sign):
         assert torch.equal(out[i], v[best]), i
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "half"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(2, 0), (3, 1), (40, 4), (700, 5), (ALL, 0)])
+def test_packed_equal_values_come_out_as_they_are(dtype, hd, window, sinks):
+    """All rows of V of a sequence alike: the weights that multiply V are those that the output is divided by, so it is V.  Products and sums in float are off by
+    2 E (n / 16 + 32) <= 2^-16 of it, which no 16-bit rounding of V itself lets through; weights that are summed before they are rounded would be off by
+    half a step of their type (half 2^-11, bf16 2^-8) of a weight, more than the 2^-12 (2^-9) that keep an output at V."""
+    lens = [1500, 70]
+    q, k, v = _packed(21, lens, 4, 2, hd, dtype)
+    v[:1500], v[1500:] = v[0].clone(), v[1500].clone()
+    out = _packed_run(q, k, v, lens, window, sinks, 4, 2, hd)
+    assert torch.equal(out.view(-1, 2, 2, hd), v.reshape(-1, 2, 1, hd).expand(-1, 2, 2, hd))
+
+
 def test_packed_strides_views_and_streams():
     """Rows of every second one of a buffer, on a stream of its own."""
     lens, Hq, Hkv, hd = [90, 140], 4, 2, 64
