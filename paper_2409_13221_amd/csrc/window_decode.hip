@@ -323,8 +323,15 @@ template <int SHIFT> __device__ __forceinline__ uint32_t code_pair(uint32_t x) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, x) * f16x2_t{16384.f, 16384.f});
 }
 
+// The 8 codes of a word of K as the halves v 2^-18, in pairs (0, 4), (1, 5), (2, 6), (3, 7).
+__device__ __forceinline__ u32x4_t key_codes(uint32_t k) {
+    constexpr uint32_t MASK = 0x03C003C0u;
+    return u32x4_t{k << 6 & MASK, k << 2 & MASK, k >> 2 & MASK, k >> 6 & MASK};
+}
+
 // A cache of 4 bits.  The bits of a code v = u + 8, masked where they lie, are the half v 2^-24 or (the upper of a byte) v 2^-20, below half's normal range
-// and exact to the matrix units: 5 instructions for 8 codes.  With scale s and center c of each token and 64 dims (group g),
+// and exact to the matrix units: 5 instructions for 8 codes of V; those of K, which decide exponents, are shifted to the top of the mantissa, 8
+// instructions (below).  With scale s and center c of each token and 64 dims (group g),
 //   q.k = sum over g of s_g (sum q v - 8 sum q) + c_g (sum of q in g),   o = sum over tokens of (p s_g) v - 8 (p s_g) + p c_g:
 // the matrix units take q and p s_g, the rest is a few multiply-adds a token.  What a token costs beside its codes would outweigh them if 16 lanes
 // worked on each for the 16 rows of a matrix product, so it is dealt out: scores are Q K^T with the query heads, up to HEADS = 16 / PAGES of them, repeated in
@@ -336,14 +343,15 @@ template <int SHIFT> __device__ __forceinline__ uint32_t code_pair(uint32_t x) {
 // SIMD: one head 115, eight 217.
 // A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that; weights are
 // such that p s_g fits half.  Of float calls both come in two terms, which leave 2^-24 of them.  The matrix units do not normalize what is below half's
-// normal range before they align a sum, which costs it 6 bits (scores off by 2^-18 of their terms); float calls take codes 2^14 times as large, which
-// keeps those: outputs were off by 4e-5, and are by 4e-7 (one head, 64 rows as above: 123 -> 127 us).
+// normal range before they align a sum: codes v 2^-24 would leave 2^-17 of a score's greatest term (one of 3500: half outputs off by 0.4 %,
+// 13 times what the formula in float32 is), those shifted up leave 2^-23 and less.  They cost 1.5 to 4 % (one head 114 -> 115.5 us, two 78.5 -> 80, eight 47 -> 48.7).  Sums of V lose as much of
+// their greatest term, which is far below the half step that p s_g is rounded by; float calls take codes of V 2^14 times as large (one head 128 us).
 template <typename T, int HD, int PAGES, int R, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a) {
     using L = Kv4<HD>;
     constexpr int KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 2 : 1, HEADS = 16 / PAGES, QUADS = HEADS / 4;
-    constexpr int SHIFT = TERMS > 1 ? 10 : 24;
-    constexpr float CODE = 1.f / (1 << SHIFT), MOST = 4.f;            // MOST: log2 of the greatest weight, above the offset
+    constexpr int K_SHIFT = 18, V_SHIFT = TERMS > 1 ? 10 : 24;
+    constexpr float K_CODE = 1.f / (1 << K_SHIFT), V_CODE = 1.f / (1 << V_SHIFT), MOST = 4.f;         // MOST: log2 of the greatest weight, above the offset
     typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
     extern __shared__ float lds[];                 // as above; while pages are worked on, weights [WAVES][TERMS][GROUPS][PAGES][HEADS][16 tokens] of half
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
@@ -353,7 +361,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
     const int own = c / QUADS, quad = c % QUADS;   // the lane's page of PAGES, and its heads 4 quad + r
     float l[R] = {}, ref[R], wsum[GROUPS][R] = {}, csum[GROUPS][R] = {};
     float off = INFINITY;                          // weights are 2^-off exp((s - ref) / sqrt(HD)); infinite: none yet
-    f32x4_t o[HD / 16];                            // heads 4 quad + r, dim 16 d + n; in units of CODE, odd d of 16 CODE
+    f32x4_t o[HD / 16];                            // heads 4 quad + r, dim 16 d + n; in units of V_CODE, odd d of 16 V_CODE
 #pragma unroll
     for (int r = 0; r < R; ++r) ref[r] = -INFINITY;
 #pragma unroll
@@ -362,7 +370,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
     if (ctx > 0) {
         const int mine_head = min(n % HEADS, w.heads - 1);         // of row n of Q and of the weights
         u32x4_t q[KS][TERMS];
-        f32x4_t first[GROUPS];                                     // -8 times the sum of q in the group, in units of CODE
+        f32x4_t first[GROUPS];                                     // -8 times the sum of q in the group, in units of K_CODE
         int back[R];                                               // score = 2^back s
         {
             const T* p = (const T*)a.q + (size_t)w.r * a.ld_q + (size_t)(w.h0 + mine_head) * HD + c * 8;
@@ -376,7 +384,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
             m = column_max(m);
             const int up = m > 0.f && m < INFINITY ? min(100, 14 - ilogbf(m)) : 0;
 #pragma unroll
-            for (int r = 0; r < R; ++r) back[r] = __shfl(SHIFT - up, 4 * quad + r, kWave);
+            for (int r = 0; r < R; ++r) back[r] = __shfl(K_SHIFT - up, 4 * quad + r, kWave);
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 float sum = 0.f;
@@ -384,7 +392,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
                 for (int s = 2 * g; s < 2 * g + 2; ++s)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum += f[s][e] = ldexpf(f[s][e], up);
-                sum = column_sum(sum) * (-8.f * CODE);
+                sum = column_sum(sum) * (-8.f * K_CODE);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) first[g][r] = __shfl(sum, 4 * quad + r, kWave);
             }
@@ -393,12 +401,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {                  // codes of a word come in the order 0 4 1 5 2 6 3 7, odd ones 16 times as large
-                        const float by = e & 1 ? 0.0625f : 1.f;
-                        const uint32_t h = pack2<f16_t>(f[s][e] * by, f[s][e + 4] * by);
+                    for (int e = 0; e < 4; ++e) {                  // codes of a word come in the order 0 4 1 5 2 6 3 7
+                        const uint32_t h = pack2<f16_t>(f[s][e], f[s][e + 4]);
                         q[s][t][e] = h;
-                        f[s][e] -= unpack<f16_t>(h, 0) / by;
-                        f[s][e + 4] -= unpack<f16_t>(h, 1) / by;
+                        f[s][e] -= unpack<f16_t>(h, 0);
+                        f[s][e + 4] -= unpack<f16_t>(h, 1);
                     }
         }
         const Visible see(ctx, a.window, a.sinks);
@@ -472,9 +479,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
                         f32x4_t x = first[g];
 #pragma unroll
                         for (int i = 2 * g; i < 2 * g + 2; ++i) {
-                            const uint32_t k = t.k[p][i], up = k >> 8;
-                            const u32x4_t h{code_pair<SHIFT>(k & 0x000F000Fu), code_pair<SHIFT>(k & 0x00F000F0u), code_pair<SHIFT>(up & 0x000F000Fu),
-                                            code_pair<SHIFT>(up & 0x00F000F0u)};
+                            const u32x4_t h = key_codes(t.k[p][i]);
 #pragma unroll
                             for (int e = 0; e < TERMS; ++e) x = Matrix16<f16_t>::qk(q[i][e], h, x);
                         }
@@ -576,9 +581,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
 #pragma unroll
                             for (int d = 0; d < 2; ++d) {          // tokens (0, 2), (1, 3) of dims 32 i + n, then of dims 32 i + 16 + n
                                 const uint32_t mask = d ? 0x00F000F0u : 0x000F000Fu;
-                                const u32x2_t a2{code_pair<SHIFT>(va & mask), code_pair<SHIFT>(va >> 8 & mask)};
+                                const u32x2_t a2{code_pair<V_SHIFT>(va & mask), code_pair<V_SHIFT>(va >> 8 & mask)};
                                 if (PAGES > 1) {
-                                    const u32x4_t h{a2[0], a2[1], code_pair<SHIFT>(vb & mask), code_pair<SHIFT>(vb >> 8 & mask)};
+                                    const u32x4_t h{a2[0], a2[1], code_pair<V_SHIFT>(vb & mask), code_pair<V_SHIFT>(vb >> 8 & mask)};
                                     o[2 * i + d] = Matrix16<f16_t>::qk(u32x4_t{wa[0], wa[1], wb[0], wb[1]}, h, o[2 * i + d]);
                                 } else {
                                     o[2 * i + d] = Matrix16<f16_t>::pv(wa, a2, o[2 * i + d]);
@@ -626,7 +631,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
         if (own == 0 && h < w.heads) {
             float* to = lds + (wave * w.room + h) * HD + n;
 #pragma unroll
-            for (int d = 0; d < HD / 16; ++d) to[16 * d] = fmaf(o[d][r], (d & 1 ? 0.0625f : 1.f) / CODE, more[d / 4]) * whole;
+            for (int d = 0; d < HD / 16; ++d) to[16 * d] = fmaf(o[d][r], (d & 1 ? 0.0625f : 1.f) / V_CODE, more[d / 4]) * whole;
             if (n == 0) {
                 lds[WAVES * w.room * HD + wave * w.room + h] = ref[r];
                 lds[WAVES * w.room * (HD + 1) + wave * w.room + h] = lost ? NAN : all;

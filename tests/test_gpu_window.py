@@ -524,6 +524,42 @@ def test_decode_in_float_is_as_near_as_float(four, Hq, Hkv, hd):
     assert np.sqrt(off) <= 16 * np.sqrt(plain) + 2.0 ** -22 * np.sqrt(size), (np.sqrt(off / size), np.sqrt(plain / size))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(2, 2, 64), (4, 2, 128), (8, 1, 64), (16, 1, 128)])
+@pytest.mark.parametrize("dim", [4, 35])
+def test_four_bits_scores_of_large_terms(dtype, Hq, Hkv, hd, dim):
+    """One channel of query and key so large that its term M of a score is some thousands, the same in all scores.  Scores are float all the same.  In float32 the
+    formula rounds some hd partial sums of about M; here it is hd / 32 sums of about 2 M (codes v = u + 8, whose 8 sum q comes off again), each of 32 terms that are
+    cut off at a step of the greatest: 4 times that error, beside the roundings of 16-bit calls, which add as random numbers do: a weight times the scale of
+    its token's values, 2^-11 of it, for the steps s u = v - c that it multiplies, and the output's own half step."""
+    p = Paged(19, [300, 150], Hq, Hkv, hd, dtype, four=True)
+    r = np.random.default_rng(20)
+    q = r.normal(size=(2, Hq, hd))
+    q[..., dim] = 100 * np.sign(q[..., dim])
+    p.q = torch.from_numpy(q.reshape(2, -1)).to(TDT[dtype]).cuda()
+    off, plain, rest, center = 0.0, 0.0, 0.0, []
+    for i, n in enumerate(p.ctx):
+        k = r.normal(size=(n, Hkv, hd)) * 10
+        k[..., dim] = 400
+        v = torch.from_numpy(r.normal(size=(n, Hkv, hd))).to(TDT[dtype])
+        _hold(p, i, torch.from_numpy(k), v)
+        center.append(np.repeat(W.kv4_quantize(v.float().numpy())[1][..., 1].astype(np.float64), 64, -1))
+    out = _np(p.run(ALL, 0, nsplit=1)).reshape(2, Hq, hd)
+    for i in range(2):
+        q = _np(p.q[i]).reshape(Hq, hd)
+        k, v, c = (t[i].repeat(Hq // Hkv, 1) for t in (p.k, p.v, center))
+        z = (k * q).sum(-1) / np.sqrt(hd)
+        w = np.exp(z - z.max(0))
+        w /= w.sum(0)
+        want = (w[..., None] * v).sum(0)
+        kf, vf, qf = (torch.from_numpy(t.astype(np.float32)) for t in (k, v, q))
+        wf = torch.softmax((kf * qf).sum(-1) / np.float32(np.sqrt(hd)), 0)
+        off += ((out[i] - want) ** 2).sum()
+        plain += (((wf[..., None] * vf).sum(0).double().numpy() - want) ** 2).sum()
+        rest += ((ROUNDED[dtype] * w[..., None] * (v - c)) ** 2).sum() + (HALF_STEP[dtype] ** 2 * want ** 2).sum()
+    assert np.sqrt(off) <= 4 * np.sqrt(plain) + np.sqrt(rest), (np.sqrt(off), np.sqrt(plain), np.sqrt(rest))
+
+
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
 @pytest.mark.parametrize("nsplit", [1, 3])
 def test_decode_strided_and_on_a_stream(four, nsplit):
