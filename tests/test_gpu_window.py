@@ -149,6 +149,59 @@ def test_packed_hidden_keys_reach_nobody(dtype, bad, hd):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("hd,long", [(64, 0), (128, 0), (128, 1)])
+def test_packed_hidden_keys_change_nothing(dtype, bad, hd, long):
+    """Key 37 of 200 (or, with tiles that are mostly full, of 1500) is not finite, in all dims or in one of V: what does not see it keeps its bits."""
+    lens, window, sinks, Hq, Hkv = [1500 if long else 200, 30], 20, 3, 4, 2
+    q, k, v = _packed(5, lens, Hq, Hkv, hd, dtype)
+    clean = _packed_run(q, k, v, lens, window, sinks, Hq, Hkv, hd)
+    sees = np.zeros(sum(lens), bool)
+    sees[37:57] = True
+    for what, dims in ((k, slice(None)), (v, slice(None)), (v, slice(hd + 9, hd + 10))):      # dim 9 of the second KV head
+        other = what.clone()
+        other[37, dims] = bad
+        out = _packed_run(q, *((other, v) if what is k else (k, other)), lens, window, sinks, Hq, Hkv, hd)
+        assert torch.equal(out[~sees], clean[~sees])
+        if dims != slice(None):
+            hit = torch.zeros_like(out, dtype=torch.bool)
+            hit.view(-1, Hq, hd)[37:57, 2:, 9] = True
+            assert torch.equal(out[~hit], clean[~hit])
+            assert (torch.isnan(out[hit]) if bad != bad else out[hit] == bad).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_packed_values_that_are_not_finite(dtype):
+    """Per dim: infinities of one sign that a query sees give that infinity, of both or a NaN none, and the other dims are as without them; what a query does not see
+    is not there.  The first keys of 300 hold them, seen for a while."""
+    lens, hd = [300], 64
+    q, k, v = _packed(22, lens, 2, 1, hd, dtype)
+    inf = float("inf")
+    clean = _packed_run(q, k, v, lens, 100, 0, 2, 1, hd)
+    other = v.clone()
+    other[2, 5], other[40, 6], other[3, 7], other[90, 7], other[7, 8], other[50, 8], other[60, 63] = inf, -inf, inf, -inf, inf, inf, float("nan")
+    out = _packed_run(q, k, other, lens, 100, 0, 2, 1, hd).view(-1, 2, hd)
+    want = clean.clone().view(-1, 2, hd)
+    want[2:102, :, 5], want[40:140, :, 6], want[3:103, :, 7], want[90:190, :, 7], want[7:107, :, 8] = inf, -inf, inf, -inf, inf
+    want[90:103, :, 7], want[50:150, :, 8], want[60:160, :, 63] = float("nan"), inf, float("nan")
+    assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(out.nan_to_num(nan=0.0, posinf=inf, neginf=-inf), want.nan_to_num(nan=0.0, posinf=inf, neginf=-inf))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_packed_queries_keep_their_bits_beside_great_scores(dtype):
+    """Every fifth query has scores of some 2^28, too far apart for the references of a tile; the others in its tile keep their bits."""
+    lens, hd = [140], 64
+    q, k, v = _packed(23, lens, 1, 1, hd, dtype)
+    k *= 4096
+    q[:] = q / 4096
+    clean = _packed_run(q, k, v, lens, 50, 2, 1, 1, hd)
+    great = torch.arange(140, device="cuda") % 5 == 0
+    q[great] *= 2.0 ** 24
+    out = _packed_run(q, k, v, lens, 50, 2, 1, 1, hd)
+    assert torch.equal(out[~great], clean[~great]) and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
 def test_packed_a_sink_that_is_not_finite_shows_everywhere(dtype):
     lens = [150]
     q, k, v = _packed(6, lens, 2, 2, 64, dtype)
