@@ -154,6 +154,7 @@ int rlhf_op_window_decode_attention(int act_dtype, const void* q, int64_t ld_q, 
  *   s = half((hi - lo) * (1/15)),  c = half(lo + 8 s)     each operation and 1/15 rounded to float, then to half
  *   u = (x - c) / s rounded to the nearest whole number (half way: the even one) and clamped to -8 .. 7; 0 where s == 0
  * and the value held is c + s u.  A group with a NaN, or a magnitude above 65504, becomes NaN as a whole.
+ * The outermost step of a group next to 65504 may lie beyond it: read or averaged in half it counts as 65504.
  * A page is 16 tokens, [page][layer][kv_head][18 * head_dim bytes], rlhf_op_kv4_page_bytes in all:
  *   8 head_dim bytes   K codes: 4 bits u + 8 of token t, dim d = 32 a + 8 b + i, in bits 4 (i % 2) of byte ((16 b + t) * head_dim / 32 + a) * 4 + i / 2
  *   8 head_dim bytes   V codes: token t = 4 b + i, dim d = 32 a + 16 e + g, in bits 4 e of byte ((16 b + g) * head_dim / 32 + a) * 4 + i

@@ -1,6 +1,8 @@
 // The cache of 4 bits (layout and rounding are stated in include/rlhf_ops.h): where things lie in a block, the 18 * HD bytes of one
 // (page, layer, KV head).
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 
 namespace rlhf {
@@ -17,5 +19,12 @@ template <int HD> struct Kv4 {
     // Scale and center of 64 dims of token t, two halves from this byte on; of V: PARAMS further.
     __host__ __device__ static constexpr int param(int t, int d) { return K_PARAMS + (d / 64 * 16 + t) * 4; }
 };
+
+// A value on its way to T.  A step next to 65504, half's greatest, may lie beyond it, by up to 15 half steps of the scale and one of the center (76), and from 65520 on
+// would round to infinity: it is held to 65504, as the values that went into the cache were.
+template <typename T> __device__ __forceinline__ float within(float x) {
+    if constexpr (std::is_same_v<T, f16_t>) return fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x;
+    else return x;
+}
 
 }  // namespace rlhf

@@ -151,7 +151,7 @@ template <typename T> __device__ __forceinline__ void put8(T* to, const float (&
     for (int i = 0; i < 8; i += N) {
         float y[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[i + e];
+        for (int e = 0; e < N; ++e) y[e] = within<T>(x[i + e]);
         Vec<T> v;
         v.set(y);
         v.template store<false>(to + i);

@@ -70,7 +70,7 @@ __device__ __forceinline__ void join_waves(const WindowDecodeArgs& a, const Deco
         if (a.nsplit == 1) {
             T* out = (T*)a.out + (size_t)w.r * a.ld_out + (size_t)(w.h0 + h) * HD + d;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = round_to<T>(ctx == 0 ? 0.f : x[e] / sum);
+            for (int e = 0; e < 4; ++e) out[e] = round_to<T>(ctx == 0 ? 0.f : within<T>(x[e] / sum));
         } else {
             const size_t slot = ((size_t)w.r * a.n_q_heads + w.h0 + h) * a.nsplit + w.split;
             if (d == 0) ((float2*)(a.part + slots * HD))[slot] = make_float2(top, sum);
@@ -666,7 +666,7 @@ __global__ __launch_bounds__(256) void k_window_join(WindowDecodeArgs a) {
     const bool empty = a.ctx_len[r] <= 0;
     T* o = (T*)a.out + (size_t)r * a.ld_out + (size_t)h * HD + d;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = round_to<T>(empty ? 0.f : x[e] / s_l);
+    for (int e = 0; e < 4; ++e) o[e] = round_to<T>(empty ? 0.f : within<T>(x[e] / s_l));
 }
 
 // Pages that a row may see.

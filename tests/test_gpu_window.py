@@ -732,6 +732,33 @@ def test_append_values_at_the_edges_of_the_rounding(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+def test_values_next_to_the_end_of_half(dtype):
+    """The nearest step to 65504 may lie at 65536 and more: read back into half, or averaged by decode attention there, it is 65504 and no infinity.  (The other types
+    hold it.)"""
+    R, hd, r = _R(), 64, np.random.default_rng(24)
+    x = np.stack([np.r_[np.full(32, 65504.0), np.full(32, -65504.0)], np.r_[np.full(63, 65504.0), 64000.0], np.r_[np.full(63, -65504.0), 65000.0], np.r_[np.full(63, 65504.0), -60000.0],
+                  *np.clip(r.uniform(-1.1, 1.1, (12, 64)), -1, 1) * 65504])
+    t = torch.from_numpy(x.astype(np.float32)).to(TDT["half"])
+    held = W.kv4_round(t.float().numpy())
+    assert (np.abs(held) > 65519).sum() > 100                           # would round to infinity
+    pool = torch.zeros(1, 1, 1, 18 * hd, dtype=torch.uint8, device="cuda")
+    slots = _ints(list(range(16)))
+    R.rlhf_op_kv4_append(t.cuda(), t.cuda(), slots, pool, 0, 1, 1, hd)
+    want = torch.from_numpy(held).to(TDT[dtype])
+    if dtype == "half":
+        want = want.clamp(-65504, 65504)
+    out = torch.empty(2, 16, hd, device="cuda", dtype=TDT[dtype])
+    R.rlhf_op_kv4_read(pool, slots, out[0], out[1], 0, 1, 1, hd)
+    assert torch.equal(out[0].cpu(), want) and torch.equal(out[1].cpu(), want)
+    q, o = torch.zeros(16, hd, device="cuda", dtype=TDT[dtype]), torch.empty(16, hd, device="cuda", dtype=TDT[dtype])
+    for nsplit in (1, 2):                                                # row i sees token i alone
+        R.rlhf_op_kv4_decode_attention(q, pool, _ints([[0]]), _ints([0] * 16), _ints(list(range(1, 17))), o, 0, 1, 1, 1, hd, 1, 0, nsplit=nsplit)
+        assert torch.isfinite(o).all()
+        off = np.abs(_np(o) - _np(want))
+        assert (off <= (HALF_STEP[dtype] + ROUNDED[dtype] + 8 * E) * 2 * np.abs(held).max(1, keepdims=True)).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
 def test_codes_of_many_values(dtype):
     """A million values on a coarse grid, where exact halves between steps are frequent, and as many off it."""
     R, hd, Hkv, rows = _R(), 64, 16, 512
