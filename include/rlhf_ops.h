@@ -124,7 +124,7 @@ int rlhf_op_flash_attention(const void* q, const void* k, const void* v, const i
  * float.  In 16-bit calls a weight is rounded once for its product with V: in the packed form to the type (outputs are divided by the sum of the rounded
  * weights, and off by up to half a step of how far the visible values lie apart), over a cache of 4 bits, times the scale of a token's values, to half;
  * outputs are rounded once.  Matrices have rows of their own stride (ld_*, elements); addresses and strides are multiples of 16 bytes.  What a query does not see does not reach it, whatever it holds (infinities and NaN too).  At most 2^30 rows
- * (decode 2^24), 2^16 heads and layers, fewer than 2^27 pages. */
+ * (decode 2^24) and tiles, 2^16 heads and layers, fewer than 2^27 pages. */
 
 /* Packed causal attention of a pass with a window: q, out [rows, n_q_heads*head_dim], k, v [rows, n_kv_heads*head_dim], e.g. columns
  * of one QKV buffer.  Tiles as in rlhf_op_flash_attention: tile i covers rows tile_start[i] + tile_q0[i] .. (at most 128, up to the

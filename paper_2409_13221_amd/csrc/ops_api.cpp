@@ -426,7 +426,7 @@ extern "C" int rlhf_op_window_attention(int act_dtype, const void* q, int64_t ld
                                         int64_t ld_out, int n_tiles, int rows, int window, int sinks, int n_q_heads, int n_kv_heads,
                                         int head_dim, void* stream) {
     const int dt = act_of(act_dtype);
-    if (dt < 0 || n_tiles < 0 || rows < 0 || rows > 1 << 30 || window < 1 || sinks < 0 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
+    if (dt < 0 || n_tiles < 0 || n_tiles > 1 << 30 || rows < 0 || rows > 1 << 30 || window < 1 || sinks < 0 || !heads_ok(n_q_heads, n_kv_heads, head_dim))
         return RLHF_EINVAL;
     const int qc = n_q_heads * head_dim, kc = n_kv_heads * head_dim;
     if (ld_q < qc || ld_out < qc || ld_k < kc || ld_v < kc || ld_k >= 1 << 25 || ld_v >= 1 << 25) return RLHF_EINVAL;     // the rows of a tile of keys in 32 bits

@@ -27,6 +27,13 @@ def test_window_attention(bad):
     assert R.lib().rlhf_op_window_attention(*dict(PACKED, **bad).values()) == R.RLHF_EINVAL
 
 
+@pytest.mark.parametrize("n_tiles", [BIG + 1, 2 ** 31 - 1])
+def test_window_attention_of_more_tiles_than_rows_can_have(n_tiles):
+    """The count of tiles that launches in turns have done stays within an int."""
+    R = _R()
+    assert R.lib().rlhf_op_window_attention(*dict(PACKED, n_tiles=n_tiles).values()) == R.RLHF_EINVAL
+
+
 @pytest.mark.parametrize("empty", [dict(n_tiles=0), dict(rows=0), dict(rows=0, q=None, k=None, v=None, out=None), dict(n_tiles=0, start=None)], ids=str)
 def test_window_attention_of_nothing(empty):
     R = _R()
