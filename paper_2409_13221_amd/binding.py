@@ -7,6 +7,7 @@ shared library is missing or a call fails, an exception is raised.
 """
 import ctypes as C
 import os
+import operator
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -687,9 +688,13 @@ class rlhf_attention_tiles:
 
     def __init__(self, seq_lens, device="cuda"):
         import torch
-        lens = np.asarray(list(seq_lens), np.int64)
-        if lens.ndim != 1 or (lens < 0).any() or lens.sum() > 1 << 30:
+        try:
+            lens = [operator.index(n) for n in seq_lens]
+        except TypeError:
+            raise ValueError("seq_lens must be whole numbers") from None
+        if min(lens, default=0) < 0 or sum(lens) > 1 << 30:
             raise ValueError("seq_lens must be lengths >= 0 of at most 2^30 rows in all")
+        lens = np.asarray(lens, np.int64)
         n = -(-lens // 128)
         which = np.repeat(np.arange(len(lens)), n)
         q0 = (np.arange(len(which)) - np.repeat(np.cumsum(n) - n, n)) * 128

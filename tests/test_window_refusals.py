@@ -132,3 +132,20 @@ def test_binding_refuses_what_the_library_cannot_see():
         R.rlhf_op_kv4_decode_attention(q[:4], torch.zeros(2, 4, 18 * 64 - 1, dtype=torch.uint8), i[None], i, i, q[:4], 0, 1, 4, 4, 64)
     with pytest.raises(ValueError):                     # pages of another type
         R.rlhf_op_kv4_append(q[:4], q[:4], i, torch.zeros(2, 4, 18 * 64), 0, 1, 4, 64)
+
+
+@pytest.mark.parametrize("lens", [[1.5], [3, 0.0], [2 ** 62] * 4, [2 ** 64], [2 ** 30, 1], [float("nan")], [[3, 4]], ["3"], [None]], ids=str)
+def test_tiles_of_lengths_that_are_none(lens):
+    """No length is cut off to a whole number, and no sum of them wraps."""
+    with pytest.raises(ValueError):
+        _R().rlhf_attention_tiles(lens, "cpu")
+
+
+def test_tiles_of_whole_numbers_of_any_kind():
+    import numpy as np
+    import torch
+    R = _R()
+    for lens in ([3, 130], (3, 130), np.array([3, 130], np.int16), torch.tensor([3, 130]), [np.int64(3), torch.tensor(130)], iter([3, 130])):
+        t = R.rlhf_attention_tiles(lens, "cpu")
+        assert t.rows == 133 and t.start.tolist() == [0, 3, 3] and t.q0.tolist() == [0, 0, 128] and t.len.tolist() == [3, 130, 130]
+    assert R.rlhf_attention_tiles([], "cpu").n == 0 and R.rlhf_attention_tiles([0, 0], "cpu").n == 0
