@@ -91,8 +91,8 @@ __device__ __forceinline__ bool window_sees(const WindowArgs& a, int i, int j) {
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 __device__ __forceinline__ uint32_t lds_address(void* p) { return (uint32_t)(size_t)(lds_ptr_t)p; }
 // 16 bytes a lane from base + lane + offset to LDS, `to` and on: 1024 bytes of a wave.  Written out, as the builtin makes the compiler wait for all loads in
-// flight before it reads LDS; whoever reads waits for vmcnt and the workgroup first.  (It has no register to come back to; m0 has no other use in
-// these kernels.)
+// flight before it reads LDS; whoever reads waits for vmcnt and the workgroup first.  (It has no register to come back to.  m0 is
+// reserved: the compiler keeps nothing in it, warns of it as a clobber, and makes no other use of it in these kernels.)
 __device__ __forceinline__ void load_to_lds(u32x4_t base, uint32_t lane, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane), "s"(base), "s"(offset) : "memory");
 }
