@@ -708,7 +708,8 @@ NO_WINDOW = 2 ** 31 - 1
 
 
 def _int32(n: int) -> int:
-    """n within what an argument holds: a window or number of sinks beyond it is as good as its greatest value."""
+    """n within what an argument holds, where ctypes would take its low bits: a window or number of sinks beyond it is as good as its greatest value, a
+    layer or number of parts is refused there."""
     return max(-1, min(n, NO_WINDOW))
 
 
@@ -747,7 +748,7 @@ def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out,
     if nsplit is None:
         longest = pt_stride * 16
         nsplit = L.rlhf_op_window_decode_nsplit(rows, n_q_heads, n_kv_heads, longest if max_ctx is None else min(max_ctx, longest), window, sinks)
-    if nsplit > 1:
+    if 1 < nsplit <= 64:                           # others are refused
         need = L.rlhf_op_window_decode_scratch_floats(rows, n_q_heads, head_dim, nsplit)
         if scratch is None:
             scratch = torch.empty(need, device=q.device)
@@ -755,7 +756,7 @@ def _window_decode(name, q, pool, n_pages, page_table, row_sample, ctx_len, out,
             raise ValueError(f"scratch must be a contiguous float32 tensor of {need} entries")
     _op_check(getattr(L, name)(
         _act_code(q), q.data_ptr(), _row_stride(q, shape, "q"), pool.data_ptr(), n_pages, page_table.data_ptr(), pt_stride, n_samples,
-        row_sample.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), _row_stride(out, shape, "out"), _ptr(scratch), rows, layer, nsplit, window,
+        row_sample.data_ptr(), ctx_len.data_ptr(), out.data_ptr(), _row_stride(out, shape, "out"), _ptr(scratch), rows, _int32(layer), _int32(nsplit), window,
         sinks, n_layers, n_q_heads, n_kv_heads, head_dim, stream), name)
 
 
@@ -794,7 +795,7 @@ def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads
     stream = _stream_with(k, v, kv_dst, pool)
     _indices(kv_dst, rows, "kv_dst")
     _op_check(lib().rlhf_op_kv4_append(_act_code(k), k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"),
-                                       kv_dst.data_ptr(), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), rows, layer, n_layers,
+                                       kv_dst.data_ptr(), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), rows, _int32(layer), n_layers,
                                        n_kv_heads, head_dim, stream), "rlhf_op_kv4_append")
 
 
@@ -807,7 +808,7 @@ def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: 
     stream = _stream_with(k, v, kv_src, pool)
     _indices(kv_src, rows, "kv_src")
     _op_check(lib().rlhf_op_kv4_read(_act_code(k), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), kv_src.data_ptr(), k.data_ptr(),
-                                     _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), rows, layer, n_layers, n_kv_heads, head_dim,
+                                     _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), rows, _int32(layer), n_layers, n_kv_heads, head_dim,
                                      stream), "rlhf_op_kv4_read")
 
 

@@ -631,6 +631,27 @@ def test_decode_strided_and_on_a_stream(four, nsplit):
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+def test_decode_numbers_that_do_not_fit_an_argument(four):
+    """A layer or number of parts of 2^32 and one is not taken for one, and parts that no call takes need no scratch first."""
+    R = _R()
+    p = Paged(25, [40, 3], 2, 2, 64, "half", four)
+    for bad in (dict(nsplit=2 ** 32 + 1), dict(nsplit=2 ** 32 + 2), dict(nsplit=65), dict(nsplit=2 ** 31 - 1), dict(nsplit=0), dict(nsplit=-1), dict(nsplit=-2 ** 32 + 1)):
+        with pytest.raises(R.RlhfError):
+            p.run(ALL, 0, **bad)
+    for bad in (2 ** 32 + 1, -2 ** 32 + 1, 3, -1):
+        p.layer = bad
+        with pytest.raises(R.RlhfError):
+            p.run(ALL, 0)
+        if four:
+            k, v = (torch.zeros(2, 128, device="cuda", dtype=torch.half) for _ in range(2))
+            with pytest.raises(R.RlhfError):
+                R.rlhf_op_kv4_append(k, v, _ints([0, 1]), p.pool, bad, 3, 2, 64)
+            with pytest.raises(R.RlhfError):
+                R.rlhf_op_kv4_read(p.pool, _ints([0, 1]), k, v, bad, 3, 2, 64)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
 def test_decode_offsets_beyond_32_bits(four):
     """The last pages of a pool of more than 2^32 elements (2^33 bytes; of 4 bits 2^32 + bytes)."""
     R = _R()
