@@ -792,11 +792,11 @@ def rlhf_op_kv4_append(k, v, kv_dst, pool, layer: int, n_layers: int, n_kv_heads
     shape = (rows, n_kv_heads * head_dim)
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
-    stream = _stream_with(k, v, kv_dst, pool)
+    pages, stream = _kv4_pages(pool, n_layers, n_kv_heads, head_dim), _stream_with(k, v, kv_dst, pool)
     _indices(kv_dst, rows, "kv_dst")
     _op_check(lib().rlhf_op_kv4_append(_act_code(k), k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"),
-                                       kv_dst.data_ptr(), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), rows, _int32(layer), n_layers,
-                                       n_kv_heads, head_dim, stream), "rlhf_op_kv4_append")
+                                       kv_dst.data_ptr(), pool.data_ptr(), pages, rows, _int32(layer), n_layers, n_kv_heads, head_dim, stream),
+              "rlhf_op_kv4_append")
 
 
 def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: int, head_dim: int) -> None:
@@ -805,11 +805,10 @@ def rlhf_op_kv4_read(pool, kv_src, k, v, layer: int, n_layers: int, n_kv_heads: 
     shape = (rows, n_kv_heads * head_dim)
     if k.dtype != v.dtype:
         raise ValueError("k and v must be of one type")
-    stream = _stream_with(k, v, kv_src, pool)
+    pages, stream = _kv4_pages(pool, n_layers, n_kv_heads, head_dim), _stream_with(k, v, kv_src, pool)
     _indices(kv_src, rows, "kv_src")
-    _op_check(lib().rlhf_op_kv4_read(_act_code(k), pool.data_ptr(), _kv4_pages(pool, n_layers, n_kv_heads, head_dim), kv_src.data_ptr(), k.data_ptr(),
-                                     _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), rows, _int32(layer), n_layers, n_kv_heads, head_dim,
-                                     stream), "rlhf_op_kv4_read")
+    _op_check(lib().rlhf_op_kv4_read(_act_code(k), pool.data_ptr(), pages, kv_src.data_ptr(), k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(),
+                                     _row_stride(v, shape, "v"), rows, _int32(layer), n_layers, n_kv_heads, head_dim, stream), "rlhf_op_kv4_read")
 
 
 def rlhf_op_kv4_decode_attention(q, pool, page_table, row_sample, ctx_len, out, layer: int, n_layers: int, n_q_heads: int, n_kv_heads: int,

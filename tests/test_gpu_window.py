@@ -958,3 +958,69 @@ def test_same_call_same_bits():
         a = p.run(ALL, 0, nsplit=5)
         for _ in range(3):
             assert torch.equal(p.run(ALL, 0, nsplit=5), a)
+
+
+# ------------------------------------------------------------------------------------------------ refusals that need tensors of a device
+
+BAD_MATRICES = {"fewer rows": lambda t: t[:-1], "fewer columns": lambda t: t[:, :-8], "flat": lambda t: t.flatten(), "more dims": lambda t: t[None], "columns apart": lambda t: t.t().contiguous().t(),
+                "rows that overlap": lambda t: t[:1].expand(t.shape), "rows closer than their length": lambda t: t.as_strided(t.shape, (t.shape[1] - 8, 1)),
+                "half": lambda t: t.half(), "host": lambda t: t.cpu()}
+BAD_VECTORS = {"int64": lambda t: t.long(), "fewer": lambda t: t[:-1], "apart": lambda t: t.repeat_interleave(2)[::2], "float": lambda t: t.float(), "host": lambda t: t.cpu()}
+
+
+def _refused(args, at, bad, call):
+    args = list(args)
+    args[at] = bad(args[at])
+    with pytest.raises(ValueError):
+        call(*args)
+
+
+@pytest.mark.parametrize("bad", BAD_MATRICES)
+def test_matrices_that_are_refused(bad):
+    R = _R()
+    f = BAD_MATRICES[bad]
+    q, k, v, o = (torch.zeros(6, 128, device="cuda") for _ in range(4))
+    tiles = R.rlhf_attention_tiles([4, 1])
+    for at in (1, 2, 3) if bad == "fewer rows" else (0, 1, 2, 3):       # rows of q are those of the call
+        _refused((q, k, v, o), at, f, lambda q, k, v, o: R.rlhf_op_window_attention(q, k, v, tiles, o, 8, 0, 2, 2, 64))
+    pool, four, i = torch.zeros(2, 1, 2, 2, 16, 64, device="cuda"), torch.zeros(2, 2, 18 * 64, device="cuda", dtype=torch.uint8), _ints([0] * 6)
+    for name, p in (("rlhf_op_window_decode_attention", pool), ("rlhf_op_kv4_decode_attention", four)):
+        for at in (0, 1):
+            _refused((q, o), at, f, lambda q, o: getattr(R, name)(q, p, i[None].contiguous(), i, i, o, 0, 1, 2, 2, 64))
+    for at in (0, 1):
+        _refused((k, v), at, f, lambda k, v: R.rlhf_op_kv4_append(k, v, i, four, 0, 1, 2, 64))
+        _refused((k, v), at, f, lambda k, v: R.rlhf_op_kv4_read(four, i, k, v, 0, 1, 2, 64))
+
+
+@pytest.mark.parametrize("bad", BAD_VECTORS)
+def test_vectors_that_are_refused(bad):
+    R = _R()
+    f = BAD_VECTORS[bad]
+    q, k, o = (torch.zeros(6, 128, device="cuda") for _ in range(3))
+    pool, four, i = torch.zeros(2, 1, 2, 2, 16, 64, device="cuda"), torch.zeros(2, 2, 18 * 64, device="cuda", dtype=torch.uint8), _ints([0] * 6)
+    for name, p in (("rlhf_op_window_decode_attention", pool), ("rlhf_op_kv4_decode_attention", four)):
+        for at in (0, 1):
+            _refused((i, i), at, f, lambda row, ctx: getattr(R, name)(q, p, _ints([[0, 1]]), row, ctx, o, 0, 1, 2, 2, 64))
+    if bad != "fewer":                                                  # as many rows as slots: then k has too many
+        _refused((i,), 0, f, lambda s: R.rlhf_op_kv4_append(q, k, s, four, 0, 1, 2, 64))
+        _refused((i,), 0, f, lambda s: R.rlhf_op_kv4_read(four, s, q, k, 0, 1, 2, 64))
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+def test_tables_and_scratch_that_are_refused(four):
+    R = _R()
+    p = Paged(26, [40, 3], 2, 2, 64, "half", four)
+    table = p.table_d
+    for bad in (table.long(), table.flatten(), table.t(), table[None], table.cpu()):
+        p.table_d = bad
+        with pytest.raises(ValueError):
+            p.run(ALL, 0)
+    p.table_d = table
+    need = R.lib().rlhf_op_window_decode_scratch_floats(2, 2, 64, 3)
+    for bad in (torch.empty(need - 1, device="cuda"), torch.empty(need, device="cuda", dtype=torch.half), torch.empty(2 * need, device="cuda")[::2], torch.empty(need)):
+        with pytest.raises(ValueError):
+            p.run(ALL, 0, nsplit=3, scratch=bad)
+    with pytest.raises(R.RlhfError):                                    # not at 16 bytes
+        p.run(ALL, 0, nsplit=3, scratch=torch.empty(need + 4, device="cuda")[1:])
+    whole = p.run(ALL, 0, nsplit=3, scratch=torch.empty(need, device="cuda"))
+    assert torch.equal(whole, p.run(ALL, 0, nsplit=3))

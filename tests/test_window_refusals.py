@@ -149,3 +149,39 @@ def test_tiles_of_whole_numbers_of_any_kind():
         t = R.rlhf_attention_tiles(lens, "cpu")
         assert t.rows == 133 and t.start.tolist() == [0, 3, 3] and t.q0.tolist() == [0, 0, 128] and t.len.tolist() == [3, 130, 130]
     assert R.rlhf_attention_tiles([], "cpu").n == 0 and R.rlhf_attention_tiles([0, 0], "cpu").n == 0
+
+
+@pytest.mark.parametrize("call", ["append", "read", "decode"])
+@pytest.mark.parametrize("bad", ["type", "size", "strides"])
+def test_pools_of_4_bits_are_looked_at_first(call, bad):
+    """By what they are, whatever else is wrong with a call: here all tensors are in host memory."""
+    import torch
+    R = _R()
+    q, i = torch.zeros(4, 256), torch.zeros(4, dtype=torch.int32)
+    pool = {"type": torch.zeros(2, 4, 18 * 64), "size": torch.zeros(2, 4, 18 * 64 - 1, dtype=torch.uint8), "strides": torch.zeros(4, 4, 18 * 64, dtype=torch.uint8)[::2]}[bad]
+    with pytest.raises(ValueError, match="uint8"):
+        if call == "append":
+            R.rlhf_op_kv4_append(q, q, i, pool, 0, 1, 4, 64)
+        elif call == "read":
+            R.rlhf_op_kv4_read(pool, i, q, q.clone(), 0, 1, 4, 64)
+        else:
+            R.rlhf_op_kv4_decode_attention(q, pool, i[None], i, i, q, 0, 1, 4, 4, 64)
+
+
+@pytest.mark.parametrize("call", ["append", "read", "decode", "paged", "packed"])
+def test_tensors_in_host_memory(call):
+    """All else being right."""
+    import torch
+    R = _R()
+    q, o, i, four = torch.zeros(4, 256), torch.zeros(4, 256), torch.zeros(4, dtype=torch.int32), torch.zeros(2, 4, 18 * 64, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="device memory"):
+        if call == "append":
+            R.rlhf_op_kv4_append(q, o, i, four, 0, 1, 4, 64)
+        elif call == "read":
+            R.rlhf_op_kv4_read(four, i, q, o, 0, 1, 4, 64)
+        elif call == "decode":
+            R.rlhf_op_kv4_decode_attention(q, four, i[None], i, i, o, 0, 1, 4, 4, 64)
+        elif call == "paged":
+            R.rlhf_op_window_decode_attention(q, torch.zeros(2, 2, 4, 16, 64), i[None], i, i, o, 0, 1, 4, 4, 64)
+        else:
+            R.rlhf_op_window_attention(q, q, q, R.rlhf_attention_tiles([4], "cpu"), o, 8, 0, 4, 4, 64)
