@@ -848,6 +848,88 @@ def test_append_and_read_strided():
     assert torch.equal(*pools)
 
 
+# ------------------------------------------------------------------------------------------------ launches in turns
+
+MANY = 1 << 16                                                           # heads, the most that a call takes: few rows of them fill a launch of 2^32 threads
+
+
+@pytest.mark.parametrize("dtype,rows", [("half", 260), ("fp32", 130)])
+def test_packed_in_turns(dtype, rows):
+    """Sequences of one token, more than one launch has workgroups for (half: 248 tiles; float: 120): every output is its token's V."""
+    hd, r = 64, np.random.default_rng(27)
+    k, v = (_normal(r, rows, hd, dtype=dtype).cuda() for _ in range(2))
+    q = torch.empty(rows, MANY * hd, device="cuda", dtype=TDT[dtype]).normal_()
+    out = _packed_run(q, k, v, [1] * rows, 1, 0, MANY, 1, hd)
+    off = (out.view(rows, MANY, hd) - v[:, None]).abs_().amax(1)
+    assert (off <= (0 if dtype == "half" else 4 * E) * v.abs()).all()
+    del q, out, off
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("four,dtype,rows,width,nsplit", [(False, "half", 10, 4, 32), (True, "half", 10, 4, 32), (True, "fp32", 10, 4, 32), (False, "half", 130, 64, 1)])
+def test_decode_in_turns(four, dtype, rows, width, nsplit):
+    """More rows than one launch has workgroups for (in 32 parts: 3 rows, over 4 bits 7; in one part 127): every row as in a call of its own, which is one launch, and
+    some heads against float64."""
+    R, hd, r = _R(), 64, np.random.default_rng(28)
+    pages, window = 3, 20 if nsplit > 1 else ALL
+    g = torch.Generator(device="cuda").manual_seed(29)
+    k, v = (torch.empty(16 * pages, MANY * hd, device="cuda", dtype=torch.half).normal_(generator=g) for _ in range(2))
+    if four:
+        pool = torch.zeros(pages, 1, MANY, 18 * hd, dtype=torch.uint8, device="cuda")
+        R.rlhf_op_kv4_append(k, v, _ints(list(range(16 * pages))), pool, 0, 1, MANY, hd)
+    else:
+        put = lambda t: t.view(pages, 16, MANY, hd).transpose(1, 2)
+        pool = torch.stack([put(k), put(v)], 1)[:, None].contiguous().to(TDT[dtype])
+    q = torch.empty(rows, MANY * hd, device="cuda", dtype=TDT[dtype]).normal_(generator=g)
+    table = torch.full((1, width), -1, dtype=torch.int32)
+    table[0, :pages] = torch.tensor([0, 1, 2])
+    table, ctx = table.cuda(), r.integers(1, 16 * pages + 1, rows)
+    ctx[rows // 2] = 0
+    call = R.rlhf_op_kv4_decode_attention if four else R.rlhf_op_window_decode_attention
+    run = lambda a, b, o: call(q[a:b], pool, table, _ints([0] * (b - a)), _ints(ctx[a:b].tolist()), o, 0, 1, MANY, MANY, hd, window, 3, nsplit=nsplit)
+    out, one = torch.full_like(q, 7.0), torch.empty_like(q[:1])
+    run(0, rows, out)
+    for i in range(rows):
+        run(i, i + 1, one)
+        assert torch.equal(out[i], one[0]), i
+    heads = [0, 1, 40000, MANY - 1]
+    some = lambda t, n: _np(t.view(n, MANY, hd)[:, heads])
+    kk, vv = (some(t, 16 * pages) for t in (k, v))
+    size = [None, None]
+    if four:
+        size = [np.repeat(np.abs(W.kv4_quantize(t.astype(np.float32))[1].astype(np.float64)) @ np.array([8.0, 1.0]), 64, -1) for t in (kk, vv)]
+        kk, vv = (W.kv4_round(t.astype(np.float32)) for t in (kk, vv))
+    for i in (0, 2, 3, 6, 7, rows - 1):
+        n = int(ctx[i])
+        if n:
+            _check(some(out[i:i + 1], 1), some(q[i:i + 1], 1), kk[:n], vv[:n], np.array([n - 1]), window, 3, dtype, *(t if t is None else t[:n] for t in size))
+        else:
+            assert (out[i] == 0).all()
+    del k, v, pool, q, out, one
+    torch.cuda.empty_cache()
+
+
+def test_append_in_turns():
+    """8188 rows of 65536 heads, of which one launch has waves for 8184; all but a few are left out."""
+    R, hd, rows = _R(), 64, 8188
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("rows of 69 GB")
+    x = torch.empty(rows, MANY * hd, device="cuda", dtype=torch.half)
+    at = [0, 8183, 8184, rows - 1]
+    slots = torch.full((rows,), -1, dtype=torch.int32)
+    for i, row in enumerate(at):
+        x[row] = torch.randn(MANY * hd, device="cuda")
+        slots[row] = 3 * i + 1
+    pool = torch.zeros(1, 1, MANY, 18 * hd, dtype=torch.uint8, device="cuda")
+    other = pool.clone()
+    R.rlhf_op_kv4_append(x, x, slots.cuda(), pool, 0, 1, MANY, hd)
+    few = x[at].contiguous()
+    del x
+    torch.cuda.empty_cache()
+    R.rlhf_op_kv4_append(few, few, _ints([1, 4, 7, 10]), other, 0, 1, MANY, hd)
+    assert torch.equal(pool, other) and pool.any()
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def test_a_prompt_and_decode_steps():
