@@ -329,6 +329,83 @@ __device__ __forceinline__ u32x4_t key_codes(uint32_t k) {
     return u32x4_t{k << 6 & MASK, k << 2 & MASK, k >> 2 & MASK, k >> 6 & MASK};
 }
 
+// One query head over the pages that a wave has had, value by value in float: weights exp((s - ref) / sqrt(HD)), their sum to *l and what they sum up to
+// o[HD].  For heads of which the weights times scales were too small for half (below).
+template <typename T, int HD, int PAGES, int WAVES>
+__device__ __forceinline__ void kv4_head(const WindowDecodeArgs& a, const DecodeWork& w, const Visible& see, const int* table, int first, int to, int h, float ref,
+                                         float* out, float* l, int lane) {
+    using L = Kv4<HD>;
+    constexpr int KS = HD / 32;
+    typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
+    const int n = lane & 15, c = lane >> 4;
+    const size_t layer = (size_t)a.n_kv_heads * L::BLOCK;
+    float q[KS][8], o[HD / 16] = {}, sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) load8<T>((const T*)a.q + (size_t)w.r * a.ld_q + (size_t)(w.h0 + h) * HD + s * 32 + c * 8, q[s]);
+    for (int j = first; j < to; j += WAVES * PAGES)
+        for (int i = j; i < min(j + PAGES, to); ++i) {
+            const int page = see.page(i), id = table[page];
+            if ((unsigned)id >= (unsigned)a.n_pages) continue;         // the row is lost anyway
+            const uint8_t* block = (const uint8_t*)a.pool + ((size_t)id * a.n_layers + a.layer) * layer + (size_t)w.kh * L::BLOCK;
+            const Codes k = *(const Codes*)(block + lane * L::PIECE), v = *(const Codes*)(block + L::V_CODES + lane * L::PIECE);
+            const bool seen = see.sees(page * 16 + n);
+            float z = 0.f, scale[L::GROUPS], center[L::GROUPS];        // of V of token n
+#pragma unroll
+            for (int g = 0; g < L::GROUPS; ++g) {
+                const uint32_t kp = *(const uint32_t*)(block + n * 4 + L::param(0, 64 * g)), vp = *(const uint32_t*)(block + n * 4 + L::param(0, 64 * g) + L::PARAMS);
+                scale[g] = seen ? unpack<f16_t>(vp, 0) : 0.f;
+                center[g] = seen ? unpack<f16_t>(vp, 1) : 0.f;
+#pragma unroll
+                for (int s = 2 * g; s < 2 * g + 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z = fmaf(q[s][e], fmaf(unpack<f16_t>(kp, 0), (float)((int)(k[s] >> 4 * e & 15) - 8), unpack<f16_t>(kp, 1)), z);
+            }
+            z = column_sum(z);
+            const float p = seen ? __builtin_amdgcn_exp2f((z - ref) * kScoreUnit<HD>) : 0.f;
+            sum += p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {                              // token 4c + e, dims 16 d + n
+                const float pt = __shfl(p, 4 * c + e, kWave);
+#pragma unroll
+                for (int g = 0; g < L::GROUPS; ++g) {
+                    const float st = __shfl(scale[g], 4 * c + e, kWave), ct = __shfl(center[g], 4 * c + e, kWave);
+#pragma unroll
+                    for (int d = 4 * g; d < 4 * g + 4; ++d) o[d] = fmaf(pt, fmaf(st, (float)((int)(v[d / 2] >> (8 * e + 4 * (d & 1)) & 15) - 8), ct), o[d]);
+                }
+            }
+        }
+#pragma unroll
+    for (int s = 1; s < 16; s <<= 1) sum += __shfl_xor(sum, s, kWave);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) {
+        o[d] = column_sum(o[d]);
+        if (c == 0) out[16 * d + n] = o[d];
+    }
+    if (lane == 0) *l = sum;
+}
+
+// The groups (a bit each) in which any of the V scales of what a wave has seen is not 0.
+template <int HD, int PAGES, int WAVES>
+__device__ __forceinline__ uint32_t kv4_scaled(const WindowDecodeArgs& a, const DecodeWork& w, const Visible& see, const int* table, int first, int to, int lane) {
+    using L = Kv4<HD>;
+    uint32_t any = 0;
+    const int n = lane & 15;
+    for (int p = lane >> 4;; p += 4) {             // 16 lanes a page
+        const int i = first + p / PAGES * (WAVES * PAGES) + p % PAGES;
+        if (first + p / PAGES * (WAVES * PAGES) >= to) break;
+        if (i >= to) continue;
+        const int page = see.page(i), id = table[page];
+        if ((unsigned)id >= (unsigned)a.n_pages || !see.sees(page * 16 + n)) continue;
+        const uint8_t* block = (const uint8_t*)a.pool + (((size_t)id * a.n_layers + a.layer) * a.n_kv_heads + w.kh) * L::BLOCK;
+#pragma unroll
+        for (int g = 0; g < L::GROUPS; ++g) any |= unpack<f16_t>(*(const uint32_t*)(block + n * 4 + L::param(0, 64 * g) + L::PARAMS), 0) != 0.f ? 1u << g : 0u;
+    }
+    uint32_t all = 0;
+#pragma unroll
+    for (int g = 0; g < L::GROUPS; ++g) all |= __any(any >> g & 1) ? 1u << g : 0u;
+    return all;
+}
+
 // A cache of 4 bits.  The bits of a code v = u + 8, masked where they lie, are the half v 2^-24 or (the upper of a byte) v 2^-20, below half's normal range
 // and exact to the matrix units: 5 instructions for 8 codes of V; those of K, which decide exponents, are shifted to the top of the mantissa, 8
 // instructions (below).  With scale s and center c of each token and 64 dims (group g),
@@ -341,17 +418,21 @@ __device__ __forceinline__ u32x4_t key_codes(uint32_t k) {
 // heads of a KV head, 1, up to 4, up to 8, more: with PAGES = 2 for one head 137, 1 for it 182; for two heads 78 with 4, 81 with 2; for
 // eight (170 MB instead of 680) 47 with 2, 65 with 1: bound by the steps of a wave there, two waves a SIMD.  Waves that ask for registers for three a
 // SIMD: one head 115, eight 217.
-// A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that; weights are
-// such that p s_g fits half.  Of float calls both come in two terms, which leave 2^-24 of them.  The matrix units do not normalize what is below half's
-// normal range before they align a sum: codes v 2^-24 would leave 2^-17 of a score's greatest term (one of 3500: half outputs off by 0.4 %,
-// 13 times what the formula in float32 is), those shifted up leave 2^-23 and less.  They cost 1.5 to 4 % (one head 114 -> 115.5 us, two 78.5 -> 80, eight 47 -> 48.7).  Sums of V lose as much of
-// their greatest term, which is far below the half step that p s_g is rounded by; float calls take codes of V 2^14 times as large (one head 128 us).
+// A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that.  Of float calls it
+// comes in two terms, as p s_g does, which leave 2^-24.  The matrix units do not normalize what is below half's normal range before they align a sum:
+// codes v 2^-24 would leave 2^-17 of a score's greatest term (one of 3500: half outputs off by 0.4 %, 13 times what the formula in float32 is), those
+// shifted up leave 2^-23 and less (one head 114 -> 115.5 us, two 78.5 -> 80, eight 47 -> 48.7).  Sums of V lose as much of their greatest term, which is far
+// below the half step that p s_g is rounded by; float calls take codes of V 2^14 times as large (one head 127 us).
+// Weights are such that p s_g fits half: 2^10 for the largest scales that come first, less where larger ones follow.  Half a step of the least that half
+// holds is 2^-25, so that heads with less of p s_g than LEAST in a group, 2^-15 of that or (float) 2^-9, are taken again by kv4_head (64 rows of 512-4096
+// tokens: 115.5 us, all heads again 276; where all scales of V are 0, which is looked up first, 151; without this two heads 80 us, with it 82).
 template <typename T, int HD, int PAGES, int R, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a) {
     using L = Kv4<HD>;
     constexpr int KS = HD / 32, GROUPS = L::GROUPS, TERMS = sizeof(T) == 4 ? 2 : 1, HEADS = 16 / PAGES, QUADS = HEADS / 4;
     constexpr int K_SHIFT = 18, V_SHIFT = TERMS > 1 ? 10 : 24;
     constexpr float K_CODE = 1.f / (1 << K_SHIFT), V_CODE = 1.f / (1 << V_SHIFT), MOST = 4.f;         // MOST: log2 of the greatest weight, above the offset
+    constexpr float LEAST = TERMS > 1 ? 1.f : 0x1p-6f;                // of a head's sum of p s_g in half (below)
     typedef uint32_t Codes __attribute__((ext_vector_type(KS)));
     extern __shared__ float lds[];                 // as above; while pages are worked on, weights [WAVES][TERMS][GROUPS][PAGES][HEADS][16 tokens] of half
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
@@ -621,13 +702,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
         return x;
     };
     __syncthreads();                               // nobody reads weights any more
+    uint32_t few = 0;                              // bit 4 g + r: the lane's head has too little of p s_g; 16 further: it has, and nothing
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int h = 4 * quad + r;
         const float all = total(l[r]) * whole;
         float more[GROUPS];
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) more[g] = total(csum[g][r]) - 8.f * total(wsum[g][r]);
+        for (int g = 0; g < GROUPS; ++g) {
+            const float weight = total(wsum[g][r]);
+            if (all > 0.f && fabsf(weight) < LEAST) few |= (weight == 0.f ? 0x10001u : 1u) << (4 * g + r);
+            more[g] = total(csum[g][r]) - 8.f * weight;
+        }
         if (own == 0 && h < w.heads) {
             float* to = lds + (wave * w.room + h) * HD + n;
 #pragma unroll
@@ -636,6 +722,25 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_kv4_decode(WindowDecodeArgs a
                 lds[WAVES * w.room * HD + wave * w.room + h] = ref[r];
                 lds[WAVES * w.room * (HD + 1) + wave * w.room + h] = lost ? NAN : all;
             }
+        }
+    }
+    if (__builtin_expect(__any(few != 0) && !lost, 0)) {
+        const Visible see(ctx, a.window, a.sinks);
+        const int first = (int)((int64_t)see.n_pages * w.split / a.nsplit) + wave * PAGES, to = (int)((int64_t)see.n_pages * (w.split + 1) / a.nsplit);
+        uint32_t scaled = (1u << GROUPS) - 1;      // nothing is right where all scales are 0
+        if (__any(few >> 16 != 0)) scaled = kv4_scaled<HD, PAGES, WAVES>(a, w, see, table, first, to, lane);
+        uint32_t again = 0;                        // a bit a head
+        for (int g = 0; g < GROUPS; ++g)
+            for (int r = 0; r < R; ++r) {
+                const uint64_t low = __ballot(few >> (4 * g + r) & 1 && (scaled >> g & 1 || !(few >> (16 + 4 * g + r) & 1)));
+                for (int x = 0; x < QUADS; ++x) again |= (uint32_t)(low >> 16 * x & 1) << (4 * x + r);
+            }
+        again &= (1u << w.heads) - 1;
+        asm volatile("" : : : "memory");
+        __builtin_amdgcn_wave_barrier();
+        for (; again; again &= again - 1) {
+            const int h = __builtin_ctz(again), slot = wave * w.room + h;
+            kv4_head<T, HD, PAGES, WAVES>(a, w, see, table, first, to, h, lds[WAVES * w.room * HD + slot], lds + slot * HD, lds + WAVES * w.room * (HD + 1) + slot, lane);
         }
     }
     __syncthreads();

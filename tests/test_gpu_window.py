@@ -537,6 +537,51 @@ def test_four_bits_values_of_changing_size(dtype, Hq, Hkv, what):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 1), (6, 1), (12, 1)])
+@pytest.mark.parametrize("what", ["dims", "first", "heads", "none"])
+@pytest.mark.parametrize("apart", [16, 26])
+def test_four_bits_values_far_apart(dtype, Hq, Hkv, what, apart):
+    """Values 2^apart times as large as others, in the other 64 dims, or of tokens whose weight for a head is nothing, which come first, or are all that other heads see;
+    or (none) in a group beside one of equal values.  Every 64 dims of every head are as near as float: 16 times the error of the formula in float32 and 2^-22, beside the
+    roundings of 16-bit calls as random numbers add: of a weight times the scale of its token's values, and of the output."""
+    n, hd, r = 200, 128, np.random.default_rng(12)
+    p = Paged(13, [n, 33], Hq, Hkv, hd, dtype, four=True)
+    k, v, q = r.normal(size=(n, Hkv, hd)), r.normal(size=(n, Hkv, hd)) * 2.0 ** (11 - apart), r.normal(size=(2, Hq, hd))
+    q[..., 0] = 8
+    if what == "dims":
+        v[..., 64:] *= 2.0 ** apart
+    elif what == "first":
+        v[:16] *= 2.0 ** apart
+        k[..., 0], k[:16, :, 0] = 1, -84
+    elif what == "heads":
+        v[:100] *= 2.0 ** apart
+        q[..., 0] *= np.where(np.arange(Hq) % 2, 1, -1)
+        k[:100, :, 0], k[100:, :, 0] = 40, -40
+    else:
+        v[..., 64:] = 3
+    p.q = torch.from_numpy(q.reshape(2, -1)).to(TDT[dtype]).cuda()
+    v = torch.from_numpy(v).to(TDT[dtype])
+    _hold(p, 0, torch.from_numpy(k), v)
+    center = np.repeat(W.kv4_quantize(v.float().numpy())[1][..., 1].astype(np.float64), 64, -1).repeat(Hq // Hkv, 1)
+    q, k, v = _np(p.q)[0].reshape(Hq, hd), p.k[0].repeat(Hq // Hkv, 1), p.v[0].repeat(Hq // Hkv, 1)
+    kf, vf, qf = (torch.from_numpy(np.asarray(t, np.float32)) for t in (k, v, q))
+    square = lambda t: (t.reshape(Hq, 2, 64) ** 2).sum(-1)
+    for window, sinks, nsplit in ((ALL, 0, 1), (150, 20, 1), (ALL, 0, 3)):
+        out = _np(p.run(window, sinks, nsplit=nsplit))[0].reshape(Hq, hd)
+        at = np.flatnonzero(W.visible([n - 1], n, window, sinks)[0])
+        z = (k[at] * q).sum(-1) / np.sqrt(hd)
+        w = np.exp(z - z.max(0))
+        w /= w.sum(0)
+        want = (w[..., None] * v[at]).sum(0)
+        wf = torch.softmax((kf[at] * qf).sum(-1) / np.float32(np.sqrt(hd)), 0)
+        plain = (wf[..., None] * vf[at]).sum(0).double().numpy()
+        rest = ROUNDED[dtype] ** 2 * square(np.sqrt((w[..., None] ** 2 * (v - center)[at] ** 2).sum(0))) + HALF_STEP[dtype] ** 2 * square(want)
+        tiny = (2.0 ** -25 if dtype == "half" else 0.0) * 8                 # half a step of half's smallest values, of 64
+        bound = 16 * np.sqrt(square(plain - want)) + 2.0 ** -22 * np.sqrt(square(want)) + np.sqrt(rest) + tiny
+        assert (np.sqrt(square(out - want)) <= bound).all(), (np.sqrt(square(out - want)) / bound).max()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
 @pytest.mark.parametrize("great,less", [(2.0 ** 15, 2.0 ** 4), (-2.0 ** 15, 2.0 ** 6), (2.0 ** 60, 1.0), (2.0 ** 100, 2.0 ** 10), (-2.0 ** 60, 1.0)])
 @pytest.mark.parametrize("nsplit", [1, 3])
 def test_decode_scores_of_great_size(dtype, great, less, nsplit):
