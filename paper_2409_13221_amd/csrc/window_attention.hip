@@ -318,8 +318,8 @@ template <typename T, int HD> __device__ __forceinline__ void take_alone(const W
 // where these would leave their range, so that most tiles do not rescale the sums.  What a query's outputs are, to the bit, goes by what it sees alone.
 // 32 keys leave registers for three workgroups a compute unit, 64 for two (64 instead: 16384 tokens 1808 -> 1871 us, 16 sequences of 200-800 85 -> 90; heads
 // of 64 gain with long contexts, 4 x 4096 162 -> 150, and lose with short ones, 40 of 1-700 30.5 -> 31.6).
-// 16384 tokens of 64 / 8 heads of 128, window 4096: 1.79 ms, 1.08 PFLOP/s of visible keys, the chip at its power limit (1.6 to 1.9 GHz).
-// 16 sequences of 200-800, window 256: 80 us, 3.3 TB/s where a copy reaches 4.7.  Weights go to the matrix units rounded once to the type, of which an
+// 16384 tokens of 64 / 8 heads of 128, window 4096: 1.79 to 1.87 ms by card, 1.03 to 1.08 PFLOP/s of visible keys, the chip at its power limit (1.6 to 1.9 GHz).
+// 16 sequences of 200-800, window 256: 72 to 82 us by what the caches hold, 3.2 TB/s and more where a copy reaches 4.7.  Weights go to the matrix units rounded once to the type, of which an
 // output is off by up to half a step of the values' spread (two terms would cost as many products again); what it is divided by is the sum of the rounded
 // weights, by the matrix units too, so that equal values come out as they are.
 template <typename T, int HD>
@@ -537,8 +537,8 @@ __device__ __forceinline__ void float_again(const WindowArgs& a, const float* q,
 }
 
 // Float: 128 or 64 queries of a head a workgroup, 16 a wave, against 16 keys at a time, which go to LDS a tile ahead; bound by the float matrix rate (a tenth
-// of the half one).  8192 tokens of 64 / 8 heads of 128, window 1024: 2.11 ms, 123 TFLOP/s with the hidden part of
-// the tiles (waves that read keys from memory for themselves: 3.29); 16 sequences of 200-800, 32 heads, window 256: 288 us (456).
+// of the half one) where tiles are full.  8192 tokens of 64 / 8 heads of 128, window 1024: 2.11 ms, 123 TFLOP/s with the hidden part of
+// the tiles (waves that read keys from memory for themselves: 3.29); 16 sequences of 200-800, 32 heads, window 256: 287 us, 88 TFLOP/s (456).
 // Four waves where tiles are mostly full: twice as many workgroups, nearer to each other in length (2 x 767, 8 heads of 128: 106 us with eight, 71 with
 // four; 2000 tokens of 32 heads 363, 316; 4 x 4096, 12 of 64, window 1024 457, 409; two instead of four: 104, 404, 433); of short sequences the
 // second half would be empty (256 of 20-60, 32 heads of 128 165, 228; 32 of 100, 40 of 64 42.6, 44.7).

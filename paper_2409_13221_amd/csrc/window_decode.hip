@@ -414,9 +414,9 @@ __device__ __forceinline__ uint32_t kv4_scaled(const WindowDecodeArgs& a, const 
 // worked on each for the 16 rows of a matrix product, so it is dealt out: scores are Q K^T with the query heads, up to HEADS = 16 / PAGES of them, repeated in
 // all rows, and of PAGES pages' scores a quad of rows (lanes c) keeps the page that is its own: a lane has one token of PAGES x 16 for R heads.
 // Weights p s_g go to the lanes of the second product through LDS.
-// 64 rows of 512-4096 tokens, 32 heads of 128: 113 us, 6.1 TB/s (68 with all pages in L2; lanes of four tokens for all 16 rows: 142).  PAGES goes by the query
+// 64 rows of 512-4096 tokens, 32 heads of 128: 115 us, 6.0 TB/s (68 with all pages in L2; lanes of four tokens for all 16 rows: 142).  PAGES goes by the query
 // heads of a KV head, 1, up to 4, up to 8, more: with PAGES = 2 for one head 137, 1 for it 182; for two heads 78 with 4, 81 with 2; for
-// eight (170 MB instead of 680) 47 with 2, 65 with 1: bound by the steps of a wave there, two waves a SIMD.  Waves that ask for registers for three a
+// eight (174 MB instead of 690) 47 with 2, 65 with 1 (49.5 now, with what is said below): bound by the steps of a wave there, two waves a SIMD.  Waves that ask for registers for three a
 // SIMD: one head 115, eight 217.
 // A query is scaled to have its greatest magnitude in [2^14, 2^15) and taken as halves, exact from half and bfloat16 down to 2^-35 of that.  Of float calls it
 // comes in two terms, as p s_g does, which leave 2^-24.  The matrix units do not normalize what is below half's normal range before they align a sum:
@@ -785,7 +785,8 @@ static int64_t decode_blocks(int rows, int n_q_heads, int n_kv_heads) { return (
 static int most_waves(int group) { return group > 8 ? 4 : 8; }
 // Eight with 64 pages and more to a row or in parts, four below, and one where eight pages or fewer meet workgroups enough to fill the chip: starting idle
 // waves then costs more than the pages (95 rows of 15-50 tokens, 32 heads of 128: 8 waves 29.4 us, 4 19.8, 1 14.3; 64 rows of 128 tokens 36, 26.4,
-// 25.2; 16 rows of 500 28.3, 26.3, 31.3; 16 rows of 2000, 12 heads of 64 26.1, 26.7, 62).
+// 25.2; 16 rows of 500 28.3, 26.3, 31.3; 16 rows of 2000, 12 heads of 64 26.1, 26.7, 62).  The pages that a row can have are the table's width: on one wider
+// than the contexts need, short rows take the time of eight waves.
 static int decode_waves(const WindowDecodeArgs& a) {
     const int group = a.n_q_heads / a.n_kv_heads;
     const int64_t pages = visible_pages(a.pt_stride, a.window, a.sinks), blocks = decode_blocks(a.rows, a.n_q_heads, a.n_kv_heads);
@@ -802,7 +803,7 @@ static int kv4_waves(const WindowDecodeArgs& a) {
     return pages <= 32 ? 1 : pages <= 96 || blocks >= 4096 ? 2 : 4;
 }
 
-// Into how many parts the visible pages of a row are cut: none below 6 pages a wave, where joining costs more than it gives (two rows of 12 heads of
+// Into how many parts the visible pages of a row are cut, by the waves of the plain cache's kernel for both: none below 6 pages a wave, where joining costs more than it gives (two rows of 12 heads of
 // 64, 700 tokens 7.5 us in one part, 7.8 in four; 1000 tokens 9.2 and 8.2); else a power of two, which leaves the parts of a row's heads on as few XCDs as
 // there are (32 heads of 128, 4000 tokens: 8 parts 16.0 us, 12 18.6, 16 16.2), of a page a wave at least and of 2048 waves in all (8 rows of
 // 8 KV heads, 2000 tokens: 4 parts 15.8 us, 2 21.7, 8 17.2), or 4096 with 32 pages a wave and more (one row of 131072 tokens in 4 bits, 8 KV
