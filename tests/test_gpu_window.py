@@ -446,6 +446,28 @@ def test_decode_pages_without_a_visible_token_are_not_read(four, nsplit):
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "half"])
+@pytest.mark.parametrize("nsplit", [1, 3])
+def test_decode_hidden_tokens_change_nothing(four, dtype, nsplit):
+    """Tokens of pages that are seen in part, before the window, behind the sinks and behind the context: NaN, infinities and numbers of any size in their place leave every bit."""
+    ctx, window, sinks, hd = [203, 90, 37], 40, 18, 64
+    p = Paged(30, ctx, 4, 2, hd, dtype, four)
+    want = p.run(window, sinks, nsplit=nsplit)
+    hidden = []
+    for i, c in enumerate(ctx):
+        last = c + -c % 16
+        hidden += [(int(p.table[p.sample[i], t // 16]), t % 16) for t in range(last) if t >= c or (t < c - window and t >= sinks)]
+    page, token = (torch.tensor(x, device="cuda") for x in zip(*hidden))
+    for bad in (float("nan"), float("inf"), -float("inf"), 60000.0, 0.0):
+        if four:
+            half = p.pool.view(torch.float16).view(p.n_pages, p.layers, 2, 9 * hd)[..., 8 * hd:].view(p.n_pages, p.layers, 2, 2, 16, 2)       # K | V, token, (s, c)
+            half[page, 1, :, :, token] = bad
+        else:
+            p.pool[page, 1, :, :, token] = bad
+        assert torch.equal(p.run(window, sinks, nsplit=nsplit), want), bad
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["paged", "four_bits"])
 @pytest.mark.parametrize("nsplit", [1, 3])
 @pytest.mark.parametrize("dtype", ["fp32", "half"])
 def test_decode_rows_outside_table_or_pool_are_nan(four, nsplit, dtype):
@@ -1060,6 +1082,32 @@ def test_captured_and_replayed(nsplit):
         last = torch.empty(2, 128, device="cuda", dtype=torch.half)
         R.rlhf_op_kv4_read(p.pool, slots, last, torch.empty_like(last), 1, 3, 2, 64)
         np.testing.assert_array_equal(_np(last), _np(torch.from_numpy(W.kv4_round(k.float().cpu().numpy().reshape(2, 2, 64)).reshape(2, 128)).half()))
+
+
+def test_calls_on_two_streams_at_once():
+    """Split decode steps of both caches, whose scratch the binding takes, and packed passes, side by side on two streams: as one after the other."""
+    ps = [Paged(31 + i, [900, 1200, 64], 8, 2, 128, "half", i == 1) for i in range(2)]
+    lens = [700, 33]
+    packed = _packed(33, lens, 4, 2, 64, "bf16")
+    want = [p.run(ALL, 0, nsplit=8) for p in ps] + [_packed_run(*packed, lens, 60, 2, 4, 2, 64)]
+    R = _R()
+    tiles, streams = R.rlhf_attention_tiles(lens), [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for turn in range(6):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                for j in (turn + i) % 3, (turn + i + 1) % 3:
+                    o = torch.full_like(want[j], 7.0)
+                    if j == 2:
+                        R.rlhf_op_window_attention(*packed, tiles, o, 60, 2, 4, 2, 64)
+                    else:
+                        p = ps[j]
+                        call = R.rlhf_op_kv4_decode_attention if p.four else R.rlhf_op_window_decode_attention
+                        call(p.q, p.pool, p.table_d, p.row_d, p.ctx_d, o, p.layer, p.layers, 8, 2, 128, nsplit=8)
+                    outs.append((j, o))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[j]) for j, o in outs)
 
 
 def test_packed_captured_and_replayed():
