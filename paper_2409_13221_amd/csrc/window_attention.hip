@@ -319,9 +319,10 @@ template <typename T, int HD> __device__ __forceinline__ void take_alone(const W
 // 32 keys leave registers for three workgroups a compute unit, 64 for two (64 instead: 16384 tokens 1808 -> 1871 us, 16 sequences of 200-800 85 -> 90; heads
 // of 64 gain with long contexts, 4 x 4096 162 -> 150, and lose with short ones, 40 of 1-700 30.5 -> 31.6).
 // 16384 tokens of 64 / 8 heads of 128, window 4096: 1.79 to 1.87 ms by card, 1.03 to 1.08 PFLOP/s of visible keys, the chip at its power limit (1.6 to 1.9 GHz).
-// 16 sequences of 200-800, window 256: 72 to 82 us by what the caches hold, 3.2 TB/s and more where a copy reaches 4.7.  Weights go to the matrix units rounded once to the type, of which an
-// output is off by up to half a step of the values' spread (two terms would cost as many products again); what it is divided by is the sum of the rounded
-// weights, by the matrix units too, so that equal values come out as they are.
+// 16 sequences of 200-800, window 256: 72 to 82 us by what the caches hold, 3.2 TB/s and more where a copy reaches 4.7.
+// Weights go to the matrix units rounded once to the type, of which an output is off by up to half a step of the values' spread (two terms would cost as
+// many products again); what it is divided by is the sum of the rounded weights, by the matrix units too, so that equal values come out as they are
+// (1 % slower than a sum of the weights as they were; heads of 64 3 to 5 %).
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 3) void k_window_flash(WindowArgs a) {
     using Q = FlashQueries<T, HD, 2>;
